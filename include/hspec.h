@@ -344,6 +344,68 @@ int hspec_debug_gemm_tiles(int32_t M, int32_t n_out, int32_t K, int32_t* tiles4)
 /* h fp16 [M, F] = SiLU(gu[:, :F]) * gu[:, F:], gu fp32 [M, 2F] (App. B.1 "MLP"). */
 int hspec_op_swiglu(const float* gu, void* h_f16, int32_t M, int32_t F, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * The target's side of an iteration: what runs between two draft steps.  The target takes a draft block (or a piece of a
+ * prompt) as a ragged chunk of T rows: request b owns rows cu_q[b] .. cu_q[b+1]-1 (cu_q: device int32 [B+1], ascending, at
+ * most T), and kv_lens[b] (device int32 [B]) counts the tokens of its cache with the chunk's own, so that row i of its n rows
+ * stands at cache position kv_lens[b] - n + i.  The cache is the paged one of the draft step: page_table int32
+ * [B, page_table_stride], pools [num_pages, page_size, Hkv, dh].  Both may be bf16 or fp16 here (`dtype`), Hq a multiple of Hkv,
+ * dh 64 or 128, any page size; q and the pools start on 16-byte boundaries.  Rows behind cu_q[B] (a batch padded to a captured
+ * graph's size) are neither read nor written.  What the device arrays say is held inside T and page_table_stride * page_size; entries
+ * outside, requests with more rows than cached tokens and page ids outside [0, num_pages) are counted (hspec_op_device_status).
+ * The lengths are read on the device: a captured call follows the arrays' contents.
+ * ---------------------------------------------------------------------------------------------- */
+
+/* Norm, rotary positions on one or several axes and the cache write of a chunk.
+ *   qkv        device [T, ld_qkv] fp32, bf16 or fp16 (in_dtype): q | k | v heads of dh values each, from any address
+ *   pos        device int32 [n_axes, T]: position of every row on every axis (1 to 8; time, height and width of a picture's
+ *              rows, say), or NULL with one axis: the row's position in the cache
+ *   pair_axis  HOST uint8 [rot_pairs]: the axis that each pair follows, or NULL: all of them the first
+ *   rot_pairs  pairs (j, j + rot_pairs) of a head that turn, by pos * theta^(-j / rot_pairs); a multiple of 8, at most dh / 2.
+ *              Values behind the first 2 rot_pairs stay as they are.  Angles are formed in 64 bits.
+ *   q_norm_w, k_norm_w  fp32 [dh] or NULL (both): RMSNorm of every query and key head in front of the rotation
+ *   q          out [T, Hq, dh] (out_dtype, also the pools')
+ * Keys and values go to (page_table[b, p / page_size], p % page_size) of their position p; everything else in the pools keeps its
+ * bits.  A row whose position is negative or whose page id is bad has its queries written and no cache entry.  Rows that share a
+ * place in the cache race. */
+int hspec_op_chunk_rope_write(const void* qkv, int32_t in_dtype, int64_t ld_qkv, const int32_t* pos, int32_t n_axes, const uint8_t* pair_axis,
+                              int32_t rot_pairs, const float* q_norm_w, const float* k_norm_w, float eps, float theta, const int32_t* cu_q,
+                              const int32_t* kv_lens, int32_t B, const int32_t* page_table, int32_t page_table_stride, void* q, void* k_pool,
+                              void* v_pool, int32_t out_dtype, int64_t num_pages, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh,
+                              int32_t page_size, void* stream);
+/* Attention of a chunk over the paged cache, which holds the chunk's own keys and values already: row at position p sees keys
+ * max(0, p - window + 1) .. p (window 0: from the first).  Single tokens, draft blocks and pieces of prompts may be mixed.
+ *   q [T, Hq, dh] with row pitch ld_q, o likewise with ld_o (elements, multiples of 8; o of q's type); scale 0: 1 / sqrt(dh)
+ * A row at a negative position sees nothing: its o is zero.  Keys and values at places that a row does not see never reach it, whatever
+ * they hold; page-table entries that no row of the request sees are not read.  A bad page reads as zeros.
+ * workspace: hspec_chunk_attention_workspace_bytes bytes whatever B, T and the lengths are, 256-byte aligned, contents undefined
+ * between calls; calls that may overlap on the GPU need one each. */
+int hspec_op_chunk_attention(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, int64_t num_pages, const int32_t* page_table,
+                             int32_t page_table_stride, const int32_t* cu_q, const int32_t* kv_lens, int32_t B, void* o, int64_t ld_o,
+                             int32_t dtype, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, int32_t page_size, int32_t window, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream);
+size_t hspec_chunk_attention_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t dh);
+/* Verification of a draft block against the target's probabilities, with the caller's uniform numbers (App. A, and the token that follows
+ * the accepted drafts).  With p = softmax(target row / temperature) and q = softmax(draft row / temperature), draft i stands if every earlier one
+ * does, p_i(x_i) > 0 and min(1, p_i(x_i) / q_i(x_i)) >= alpha_i.  Behind the n that stand comes one token of the target's: from max(0, p_n - q_n)
+ * where draft n was refused, from p_n where none was: the lowest token v with sum over w <= v above u times the whole.
+ *   target_logits  device [T, ld_target], fp32, bf16 or fp16 (target_dtype): request b's rows cu_q[b] .. cu_q[b+1]-1 are the logits behind its
+ *                  last token and behind each draft, so it has min(k, rows - 1) drafts.  cu_q NULL: k + 1 rows each
+ *   draft_logits   device [B * k, ld_draft] (draft_dtype): what the drafts were sampled from at the same temperature; NULL: a drafter that takes
+ *                  the arg-max, all of q on the drafted token.  V_draft = V, or with vocab_map (device int32 [V_draft], ascending) a pruned
+ *                  vocabulary's size; q is 0 at tokens outside it
+ *   draft_ids int32 [B, k] target token ids; temperature fp32 [B] or NULL (1); at 0 p is all on the arg-max (lowest on ties), q on the draft
+ *   alpha fp32 [B, k], u fp32 [B] in [0, 1)
+ *   n_accept int32 [B]; tokens int32 [B, k + 1]: the drafts that stand, the token behind them, then -1 (a request without rows: -1 all through)
+ * A NaN logit counts as -infinity, +infinity as the largest finite number; from a row without any weight token 0 is taken.  A draft id outside
+ * [0, V) does not stand (counted).  Decided as in 64-bit arithmetic.  Rows behind a request's first refused draft may stay unread.
+ * workspace: hspec_verify_workspace_bytes(B, k), 256-byte aligned, as above. */
+int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_target, int32_t T, const void* draft_logits, int32_t draft_dtype,
+                    int64_t ld_draft, const int32_t* draft_ids, const int32_t* cu_q, const int32_t* vocab_map, const float* temperature,
+                    const float* alpha, const float* u, int32_t* n_accept, int32_t* tokens, int32_t B, int32_t k, int32_t V, int32_t V_draft,
+                    void* workspace, size_t workspace_bytes, void* stream);
+size_t hspec_verify_workspace_bytes(int32_t B, int32_t k);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,211 @@
+// Norm, rotary positions on several axes and the cache write of a ragged chunk's queries, keys and values.
+//
+// Pair j of a head (elements j and j + rot of its first 2 rot elements) turns by pos[axis(j)][t] * theta^(-j / rot).  The rates come from the
+// host in 64 bits, the product and its reduction modulo 2 pi are 64-bit as well (at position 10^6 a 32-bit product is off by 0.06), and only
+// the remainder, at most pi, goes to sincosf: off by 2^-23 there, which no 16-bit result shows.
+//
+// Bound by memory: every value is read and written once.  A thread takes 16 elements of a head, the 8 lower and the 8 upper partners of its
+// pairs, so that norm, rotation and stores need no exchange but the sum of squares over the head's threads.  A block takes several rows;
+// the loads of its first heads are under way while it looks up the rows' requests, pages and angles (one per row, shared by all heads).
+#include "chunk.cuh"
+
+#include <cmath>
+#include <type_traits>
+
+namespace hspec {
+
+namespace {
+
+constexpr int ROPE_ROWS = 16;      // most rows of a block
+constexpr int ROPE_UNROLL = 4;     // heads in flight per thread
+
+struct RopeArgs {
+  ChunkRopeCall c;
+  double rate[64];
+  uint8_t axis[64];
+  int rows;                        // rows of a block
+  int vec;                         // qkv rows start on 16-byte boundaries
+};
+
+template <typename T> struct Raw16;                       // 16 values as they lie in memory: two groups of 8
+template <> struct Raw16<float> { uint4 v[4]; };
+template <> struct Raw16<__nv_bfloat16> { uint4 v[2]; };
+template <> struct Raw16<__half> { uint4 v[2]; };
+
+__device__ __forceinline__ void widen(const Raw16<float>& r, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[4 * i] = __uint_as_float(r.v[i].x); x[4 * i + 1] = __uint_as_float(r.v[i].y);
+    x[4 * i + 2] = __uint_as_float(r.v[i].z); x[4 * i + 3] = __uint_as_float(r.v[i].w);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void widen(const Raw16<T>& r, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+        x[8 * i + 2 * j] = f.x; x[8 * i + 2 * j + 1] = f.y;
+      } else {
+        x[8 * i + 2 * j] = bf16_bits_to_float(uint16_t(w[j] & 0xffffu)); x[8 * i + 2 * j + 1] = bf16_bits_to_float(uint16_t(w[j] >> 16));
+      }
+    }
+  }
+}
+
+template <typename TI>
+__device__ __forceinline__ void load16(const TI* lo, const TI* hi, bool vec, Raw16<TI>& r) {
+  constexpr int W = sizeof(r.v) / 32;                     // 16-byte words of a group of 8
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      r.v[i] = __ldcs(reinterpret_cast<const uint4*>(lo) + i);
+      r.v[W + i] = __ldcs(reinterpret_cast<const uint4*>(hi) + i);
+    }
+  } else {
+    TI* x = reinterpret_cast<TI*>(r.v);
+    for (int i = 0; i < 8; ++i) { x[i] = lo[i]; x[8 + i] = hi[i]; }
+  }
+}
+
+template <bool F16>
+__device__ __forceinline__ uint4 narrow8(const float* x, uint32_t* status) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = F16 ? pack_f16_sat(x[2 * i], x[2 * i + 1], status) : pack_bf16(x[2 * i], x[2 * i + 1]);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename TI, bool F16>
+__global__ void __launch_bounds__(256) chunk_rope_kernel(const __grid_constant__ RopeArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  const ChunkRopeCall& c = a.c;
+  __shared__ __align__(16) float s_cos[ROPE_ROWS][64], s_sin[ROPE_ROWS][64];
+  __shared__ long long s_slot[ROPE_ROWS];                 // place in the pools in rows of one head; -1: none (the row's queries are still turned)
+  __shared__ int s_at[ROPE_ROWS];
+  __shared__ int s_used[ROPE_ROWS];                       // the row belongs to a request
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t0 = blockIdx.x * a.rows, rows = min(a.rows, c.T - t0);
+  const int lanes = c.dh >> 4, sub = threadIdx.x % lanes, group = threadIdx.x / lanes, groups = 256 / lanes;
+  const int heads = c.Hq + 2 * c.Hkv, rot = c.rot_pairs;
+  // this thread's 16 elements of a head: a pair group of the rotated part, or 16 elements behind it
+  const bool turns = sub * 8 < rot;
+  const int lo = turns ? sub * 8 : 2 * rot + (sub - rot / 8) * 16, hi = turns ? lo + rot : lo + 8;
+  const int items = rows * heads;
+  Raw16<TI> raw[ROPE_UNROLL];
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int u = 0; u < ROPE_UNROLL; ++u) {
+      const int item = first + u * groups + group;
+      if (item < items) {
+        const TI* src = reinterpret_cast<const TI*>(c.qkv) + size_t(t0 + item / heads) * c.ld_qkv + size_t(item % heads) * c.dh;
+        load16<TI>(src + lo, src + hi, a.vec, raw[u]);
+      }
+    }
+  };
+  fetch(0);
+  for (int r = warp; r < rows; r += 8) {
+    const int t = t0 + r, b = chunk_request_of(c.cu_q, c.B, t, lane);
+    if (lane == 0) {
+      long long slot = -1;
+      int at = 0, used = 0;
+      if (b < c.B && t >= c.cu_q[b]) {
+        used = 1;
+        const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
+        const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
+        if (t == q.q0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+        at = q.len - q.n + (t - q.q0);
+        if (at >= 0) {
+          const int page = c.page_table[size_t(b) * c.page_table_stride + at / c.page_size];
+          if (page >= 0 && page < c.num_pages) slot = ((long long)page * c.page_size + at % c.page_size) * c.Hkv;
+          else atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+        }
+      }
+      s_slot[r] = slot; s_at[r] = at; s_used[r] = used;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * rot; i += 256) {
+    const int r = i / rot, j = i % rot;
+    const int p = c.pos ? c.pos[size_t(a.axis[j]) * c.T + t0 + r] : s_at[r];
+    const double ang = double(p) * a.rate[j];
+    // modulo 2 pi, which is taken as the sum of two 64-bit numbers
+    const double n = rint(ang * 0.15915494309189535);
+    const double rem = fma(-n, 2.4492935982947064e-16, fma(-n, 6.283185307179586, ang));
+    sincosf(float(rem), &s_sin[r][j], &s_cos[r][j]);
+  }
+  __syncthreads();
+  for (int first = 0; first < items; first += ROPE_UNROLL * groups) {
+    if (first > 0) fetch(first);
+#pragma unroll
+    for (int u = 0; u < ROPE_UNROLL; ++u) {
+      const int item = first + u * groups + group;
+      const bool on = item < items;
+      const int r = on ? item / heads : 0, h = on ? item % heads : 0;
+      float x[16];
+      if (on) widen(raw[u], x);
+      const float* w = h < c.Hq ? c.q_norm_w : c.k_norm_w;
+      if (c.q_norm_w) {                                   // (uniform: both norms or none)
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ss += on ? x[e] * x[e] : 0.f;
+        for (int off = lanes >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+        if (on && h < c.Hq + c.Hkv) {
+          const float inv = rsqrtf(ss / float(c.dh) + c.eps);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { x[e] *= inv * w[lo + e]; x[8 + e] *= inv * w[hi + e]; }
+        }
+      }
+      if (!on || !s_used[r]) continue;
+      if (turns && h < c.Hq + c.Hkv) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float cs = s_cos[r][lo + e], sn = s_sin[r][lo + e], p = x[e], q = x[8 + e];
+          x[e] = p * cs - q * sn;
+          x[8 + e] = q * cs + p * sn;
+        }
+      }
+      uint16_t* dst;
+      if (h < c.Hq) {
+        dst = reinterpret_cast<uint16_t*>(c.q) + (size_t(t0 + r) * c.Hq + h) * c.dh;
+      } else {
+        if (s_slot[r] < 0) continue;
+        const bool v = h >= c.Hq + c.Hkv;
+        dst = reinterpret_cast<uint16_t*>(v ? c.v_pool : c.k_pool) + (size_t(s_slot[r]) + (h - c.Hq - (v ? c.Hkv : 0))) * c.dh;
+      }
+      *reinterpret_cast<uint4*>(dst + lo) = narrow8<F16>(x, c.status);
+      *reinterpret_cast<uint4*>(dst + hi) = narrow8<F16>(x + 8, c.status);
+    }
+  }
+}
+
+template <typename TI>
+cudaError_t launch_for(const RopeArgs& a, int blocks, cudaStream_t stream) {
+  return launch_pdl(a.c.f16 ? chunk_rope_kernel<TI, true> : chunk_rope_kernel<TI, false>, dim3(blocks), dim3(256), 0, stream, a);
+}
+
+}  // namespace
+
+cudaError_t chunk_rope_launch(const ChunkRopeCall& c, cudaStream_t stream) {
+  RopeArgs a{};
+  a.c = c;
+  for (int j = 0; j < c.rot_pairs; ++j) {
+    a.rate[j] = pow(double(c.theta), -double(j) / double(c.rot_pairs));
+    a.axis[j] = c.pair_axis ? c.pair_axis[j] : 0;
+  }
+  const size_t item = c.in_dtype == CHUNK_F32 ? 4 : 2;
+  a.vec = (reinterpret_cast<uintptr_t>(c.qkv) % 16 == 0 && size_t(c.ld_qkv) * item % 16 == 0) ? 1 : 0;
+  // enough rows that a thread has its four heads to load, as long as four blocks are left for every SM
+  const int want = (ROPE_UNROLL * 256 / (c.dh / 16) + c.Hq + 2 * c.Hkv - 1) / (c.Hq + 2 * c.Hkv), spread = (c.T + 4 * 148 - 1) / (4 * 148);
+  a.rows = want < spread ? want : spread;
+  if (a.rows > ROPE_ROWS) a.rows = ROPE_ROWS;
+  const int blocks = (c.T + a.rows - 1) / a.rows;
+  if (c.in_dtype == CHUNK_F32) return launch_for<float>(a, blocks, stream);
+  return c.in_dtype == CHUNK_F16 ? launch_for<__half>(a, blocks, stream) : launch_for<__nv_bfloat16>(a, blocks, stream);
+}
+
+}  // namespace hspec

@@ -996,4 +996,107 @@ int hspec_op_swiglu(const float* gu, void* h_f16, int32_t M, int32_t F, void* st
   return HSPEC_OK;
 }
 
+// ------------------------------------------------------------------ the target's side of an iteration
+// What the two chunk operators refuse alike; null: nothing.
+static const char* chunk_refusal(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, int32_t page_size, int32_t page_table_stride,
+                                 int64_t num_pages, int32_t dtype, const void* q, const void* k_pool, const void* v_pool) {
+  if (B < 1 || T < 1 || page_size < 1 || page_table_stride < 1 || num_pages < 1 || num_pages > 0x7fffffff) return "bad argument";
+  if (Hkv < 1 || Hq < Hkv || Hq % Hkv) return "the query heads must be a multiple of the KV heads";
+  if (dh != 64 && dh != 128) return "the head dim must be 64 or 128";
+  if (dtype != HSPEC_BF16 && dtype != HSPEC_F16) return "queries and pools must be bf16 or fp16";
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_pool) | reinterpret_cast<uintptr_t>(v_pool)) & 15)
+    return "queries and pools must be 16-byte aligned";
+  return nullptr;
+}
+static int chunk_max_len(int32_t stride, int32_t page_size) {
+  const long long n = (long long)stride * page_size;
+  return n < 0x7fffff00 ? int(n) : 0x7fffff00;
+}
+
+int hspec_op_chunk_rope_write(const void* qkv, int32_t in_dtype, int64_t ld_qkv, const int32_t* pos, int32_t n_axes, const uint8_t* pair_axis,
+                              int32_t rot_pairs, const float* q_norm_w, const float* k_norm_w, float eps, float theta, const int32_t* cu_q,
+                              const int32_t* kv_lens, int32_t B, const int32_t* page_table, int32_t page_table_stride, void* q, void* k_pool,
+                              void* v_pool, int32_t out_dtype, int64_t num_pages, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh,
+                              int32_t page_size, void* stream) {
+  const std::string who = "hspec_op_chunk_rope_write: ";
+  if (T == 0) return HSPEC_OK;                     // (an empty tensor has no address)
+  if (!qkv || !cu_q || !kv_lens || !page_table || !q || !k_pool || !v_pool || !q_norm_w != !k_norm_w || !(theta > 0.f) || !(eps >= 0.f))
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
+  if (in_dtype != HSPEC_BF16 && in_dtype != HSPEC_F16 && in_dtype != HSPEC_F32) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "qkv must be fp32, bf16 or fp16");
+  if (const char* why = chunk_refusal(B, T, Hq, Hkv, dh, page_size, page_table_stride, num_pages, out_dtype, q, k_pool, v_pool))
+    return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + why);
+  if (rot_pairs < 8 || rot_pairs % 8 || rot_pairs > dh / 2) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "the rotated pairs must be a multiple of 8, at most half the head dim");
+  if (n_axes < 1 || n_axes > 8 || (!pos && n_axes != 1)) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "1 to 8 axes, with positions given where there are several");
+  for (int j = 0; pair_axis && j < rot_pairs; ++j)
+    if (pair_axis[j] >= n_axes) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "pair_axis names an axis that is not there");
+  if (ld_qkv < (int64_t(Hq) + 2 * int64_t(Hkv)) * dh) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "row pitch too small");
+  std::string errtxt;
+  ChunkRopeCall c{};
+  c.qkv = qkv; c.in_dtype = in_dtype; c.ld_qkv = ld_qkv; c.pos = pos; c.pair_axis = pair_axis; c.rot_pairs = rot_pairs;
+  c.q_norm_w = q_norm_w; c.k_norm_w = k_norm_w; c.eps = eps; c.theta = theta; c.cu_q = cu_q; c.kv_lens = kv_lens;
+  c.page_table = page_table; c.page_table_stride = page_table_stride; c.max_len = chunk_max_len(page_table_stride, page_size);
+  c.q = q; c.k_pool = k_pool; c.v_pool = v_pool; c.f16 = out_dtype == HSPEC_F16; c.num_pages = num_pages;
+  c.B = B; c.T = T; c.Hq = Hq; c.Hkv = Hkv; c.dh = dh; c.page_size = page_size;
+  c.status = global_status();
+  if (!c.status) return fail(nullptr, HSPEC_ERR_CUDA, who + "cannot allocate the status word");
+  OP_TRY(chunk_rope_launch(c, reinterpret_cast<cudaStream_t>(stream)));
+  return HSPEC_OK;
+}
+
+size_t hspec_chunk_attention_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t dh) { return chunk_attn_workspace_bytes(Hq, Hkv, dh); }
+
+int hspec_op_chunk_attention(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, int64_t num_pages, const int32_t* page_table,
+                             int32_t page_table_stride, const int32_t* cu_q, const int32_t* kv_lens, int32_t B, void* o, int64_t ld_o,
+                             int32_t dtype, int32_t T, int32_t Hq, int32_t Hkv, int32_t dh, int32_t page_size, int32_t window, float scale,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  const std::string who = "hspec_op_chunk_attention: ";
+  if (T == 0) return HSPEC_OK;
+  if (!q || !k_pool || !v_pool || !page_table || !cu_q || !kv_lens || !o || !workspace || window < 0 || !(scale >= 0.f) || scale > 3.0e38f)
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
+  if (const char* why = chunk_refusal(B, T, Hq, Hkv, dh, page_size, page_table_stride, num_pages, dtype, q, k_pool, v_pool))
+    return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + why);
+  if (ld_q < int64_t(Hq) * dh || ld_o < int64_t(Hq) * dh || ld_q % 8 || ld_o % 8 || (reinterpret_cast<uintptr_t>(o) & 15))
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "rows of q and o must start on 16-byte boundaries and hold all heads");
+  if (workspace_bytes < chunk_attn_workspace_bytes(Hq, Hkv, dh)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");
+  std::string errtxt;
+  ChunkAttnCall c{};
+  c.q = q; c.ldq = ld_q; c.k_pool = k_pool; c.v_pool = v_pool; c.num_pages = num_pages; c.cu_q = cu_q; c.kv_lens = kv_lens;
+  c.page_table = page_table; c.page_table_stride = page_table_stride; c.max_len = chunk_max_len(page_table_stride, page_size);
+  c.o = o; c.ldo = ld_o; c.f16 = dtype == HSPEC_F16; c.scale = scale > 0.f ? scale : 1.f / sqrtf(float(dh));
+  c.B = B; c.T = T; c.Hq = Hq; c.Hkv = Hkv; c.dh = dh; c.page_size = page_size; c.window = window; c.ws = workspace;
+  c.status = global_status();
+  if (!c.status) return fail(nullptr, HSPEC_ERR_CUDA, who + "cannot allocate the status word");
+  OP_TRY(chunk_attn_launch(c, reinterpret_cast<cudaStream_t>(stream), &errtxt));
+  return HSPEC_OK;
+}
+
+size_t hspec_verify_workspace_bytes(int32_t B, int32_t k) { return B < 1 || k < 1 ? 0 : verify_workspace_bytes(B, k); }
+
+int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_target, int32_t T, const void* draft_logits, int32_t draft_dtype,
+                    int64_t ld_draft, const int32_t* draft_ids, const int32_t* cu_q, const int32_t* vocab_map, const float* temperature,
+                    const float* alpha, const float* u, int32_t* n_accept, int32_t* tokens, int32_t B, int32_t k, int32_t V, int32_t V_draft,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  const std::string who = "hspec_op_verify: ";
+  if (!target_logits || !draft_ids || !alpha || !u || !n_accept || !tokens || !workspace || B < 1 || k < 1 || V < 1 || T < 1 || ld_target < V)
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
+  auto known = [](int32_t d) { return d == HSPEC_F32 || d == HSPEC_BF16 || d == HSPEC_F16; };
+  if (!known(target_dtype) || (draft_logits && !known(draft_dtype))) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "logits must be fp32, bf16 or fp16");
+  if (!cu_q && int64_t(B) * (k + 1) > T) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "without cu_q every request has k + 1 rows of target logits");
+  if (draft_logits && (V_draft < 1 || V_draft > V || ld_draft < V_draft)) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad drafter vocabulary");
+  if (draft_logits && !vocab_map && V_draft != V) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "a pruned drafter vocabulary needs its map");
+  if (int64_t(B) * k > 0x0fffffff) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "too many drafts");
+  if (workspace_bytes < verify_workspace_bytes(B, k)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");
+  std::string errtxt;
+  VerifyCall c{};
+  c.target = target_logits; c.t_dtype = target_dtype; c.ld_t = ld_target; c.T = T; c.draft = draft_logits; c.d_dtype = draft_dtype; c.ld_d = ld_draft;
+  c.ids = draft_ids; c.cu_q = cu_q; c.vocab_map = draft_logits ? vocab_map : nullptr; c.temperature = temperature; c.alpha = alpha; c.u = u;
+  c.n_accept = n_accept; c.tokens = tokens; c.B = B; c.k = k; c.V = V; c.Vd = draft_logits ? V_draft : V; c.ws = workspace;
+  c.status = global_status();
+  if (!c.status) return fail(nullptr, HSPEC_ERR_CUDA, who + "cannot allocate the status word");
+  OP_TRY(verify_launch(c, reinterpret_cast<cudaStream_t>(stream)));
+  return HSPEC_OK;
+}
+
 }  // extern "C"

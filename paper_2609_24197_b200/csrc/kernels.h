@@ -277,6 +277,56 @@ cudaError_t attention_tc_launch(const AttnCall& c, int max_chunks, cudaStream_t 
 cudaError_t gather_kv_launch(const void* pool, const int32_t* row, int ctx_len, int page_size, int Hkv, int dh,
                              void* dst, cudaStream_t stream);
 
+// ---- the target's side of an iteration: a ragged chunk of new tokens over the paged cache, and the verification of drafts
+constexpr int CHUNK_BF16 = 0, CHUNK_F32 = 1, CHUNK_F16 = 3;      // hspec_dtype
+struct ChunkRopeCall {              // chunk_rope.cu
+  const void* qkv; int in_dtype; long long ld_qkv;
+  const int32_t* pos;               // [axes, T] or null: the position in the cache
+  const uint8_t* pair_axis;         // host: axis of each pair, or null: axis 0
+  int rot_pairs;
+  const float *q_norm_w, *k_norm_w; // both or neither
+  float eps, theta;
+  const int32_t *cu_q, *kv_lens, *page_table;
+  int page_table_stride;
+  int max_len;                      // tokens that a page-table row has room for
+  void *q, *k_pool, *v_pool;
+  bool f16;
+  long long num_pages;
+  uint32_t* status;
+  int B, T, Hq, Hkv, dh, page_size;
+};
+cudaError_t chunk_rope_launch(const ChunkRopeCall& c, cudaStream_t stream);
+struct ChunkAttnCall {              // chunk_attention.cu
+  const void* q; long long ldq;     // [T, Hq, dh], row pitch in elements
+  const void *k_pool, *v_pool;
+  long long num_pages;
+  const int32_t *cu_q, *kv_lens, *page_table;
+  int page_table_stride;
+  int max_len;
+  void* o; long long ldo;
+  bool f16;
+  float scale;
+  uint32_t* status;
+  int B, T, Hq, Hkv, dh, page_size, window;
+  void* ws;
+};
+size_t chunk_attn_workspace_bytes(int Hq, int Hkv, int dh);
+cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string* err);
+struct VerifyCall {                 // verify.cu
+  const void* target; int t_dtype; long long ld_t;      // [T, V]
+  const void* draft; int d_dtype; long long ld_d;       // [B * k, Vd] or null: the arg-max drafter
+  const int32_t* ids;                                   // [B, k]
+  const int32_t *cu_q, *vocab_map;                      // [B + 1] or null: k + 1 rows each; [Vd] or null
+  const float *temperature, *alpha, *u;                 // [B] or null, [B, k], [B]
+  int32_t *n_accept, *tokens;                           // [B], [B, k + 1]
+  int B, k, V, Vd, T;
+  void* ws;
+  uint32_t* status;
+};
+struct VerifyScratch { int* first; float2* mx; int *top, *verdict; };
+size_t verify_workspace_bytes(int B, int k);
+cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream);
+
 // ---- scan (scan.cu)
 struct ScanCall {
   const float* zxbcdt; long long ld_in;

@@ -1,0 +1,191 @@
+"""GPU parity of the verification of drafted tokens against oracle/target_oracle.py: both answers are integers and have to be equal."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import target_oracle as to
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hs():
+    import paper_2609_24197_b200 as m
+    m.load_library()
+    m.hspec_op_device_status(clear=True)
+    return m
+
+
+def _wide(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def _run(hs, target, draft, ids, alpha, u, cu_q=None, vocab_map=None, temperature=None, ws=None):
+    B, k = ids.shape
+    n = torch.full((B,), -9, dtype=torch.int32, device="cuda")
+    tok = torch.full((B, k + 1), -9, dtype=torch.int32, device="cuda")
+    ws = torch.empty(hs.hspec_verify_workspace_bytes(B, k), dtype=torch.uint8, device="cuda") if ws is None else ws
+    hs.hspec_op_verify(target, draft, ids, alpha, u, n, tok, ws, cu_q=cu_q, vocab_map=vocab_map, temperature=temperature)
+    return n, tok
+
+
+def _check(hs, target, draft, ids, alpha, u, cu_q=None, vocab_map=None, temperature=None):
+    target, draft, ids, alpha, u, cu_q, vocab_map, temperature = (None if x is None else x.cuda() for x in
+                                                                    (target, draft, ids, alpha, u, cu_q, vocab_map, temperature))
+    n, tok = _run(hs, target, draft, ids, alpha, u, cu_q, vocab_map, temperature)
+    a = [None if x is None else x.cpu().numpy() for x in (ids, alpha, u, cu_q, vocab_map, temperature)]
+    want_n, want = to.verify(_wide(target), _wide(draft), *a)
+    np.testing.assert_array_equal(n.cpu().numpy(), want_n)
+    np.testing.assert_array_equal(tok.cpu().numpy(), want)
+    return want_n, want
+
+
+def _case(B, k, V, kind, seed, pruned=0, draft=True, right=0.7, spread=3.0):
+    g = torch.Generator().manual_seed(99 + seed)
+    Vd = pruned or V
+    zt, zd = torch.randn((B * (k + 1), V), generator=g) * spread, torch.randn((B, k, Vd), generator=g) * spread
+    vmap = torch.sort(torch.randperm(V, generator=g)[:Vd])[0].to(torch.int32) if pruned else None
+    rows = (torch.arange(B)[:, None] * (k + 1) + torch.arange(k)[None]).flatten()
+    same = rows[torch.rand(B * k, generator=g) < right]
+    b, i = same // (k + 1), same % (k + 1)
+    cols = torch.arange(V) if vmap is None else vmap.long()
+    zt[same[:, None], cols] = zd[b, i] + 0.05 * zt[same[:, None], cols]
+    zd, zt = zd.to(kind), zt.to(kind)
+    q = torch.softmax(zd.float().reshape(B * k, Vd), 1)
+    ids = (torch.multinomial(q, 1, generator=g).squeeze(1) if draft else q.argmax(1)).reshape(B, k)
+    ids = ids if vmap is None else vmap.long()[ids]
+    return dict(target=zt, draft=zd if draft else None, ids=ids.to(torch.int32), alpha=torch.rand((B, k), generator=g), u=torch.rand(B, generator=g),
+                vocab_map=vmap)
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,k,V", [(1, 1, 1), (1, 1, 2), (3, 7, 1000), (1, 16, 32000), (5, 33, 4099), (70, 5, 513), (300, 4, 100), (2, 3, 152064), (9, 2, 128257)])
+def test_sampled_drafts(hs, B, k, V, kind):
+    n, _ = _check(hs, **_case(B, k, V, kind, B + V))
+    if B * k > 100:
+        assert 0 < n.mean() < k
+
+
+@pytest.mark.parametrize("spread", [0.0, 0.3, 12.0])
+@pytest.mark.parametrize("draft", [True, False])
+def test_flat_and_peaked_vocabularies(hs, draft, spread):
+    for seed in range(4):
+        _check(hs, **_case(4, 3, 50000, torch.float32, seed, draft=draft, spread=spread, right=0.5))
+
+
+@pytest.mark.parametrize("B,k,V", [(1, 16, 32000), (40, 8, 2000), (200, 16, 300)])
+def test_argmax_drafts(hs, B, k, V):
+    _check(hs, **_case(B, k, V, torch.float32, V, draft=False, right=0.9, spread=6.0))
+
+
+@pytest.mark.parametrize("V,pruned", [(1000, 1), (1000, 37), (4099, 1000), (152064, 32000), (513, 513)])
+def test_pruned_vocabulary(hs, V, pruned):
+    for B, k in ((3, 5), (64, 2)):
+        _check(hs, **_case(B, k, V, torch.bfloat16, V + B, pruned=pruned, right=0.4))
+
+
+def test_temperatures_and_ragged_rows(hs):
+    B, k, V = 24, 6, 3001
+    for seed, pruned in ((0, 0), (1, 800)):
+        c = _case(B, k, V, torch.float32, seed, pruned=pruned)
+        c["temperature"] = torch.tensor([1.0, 0.0, 0.3, 2.5, 1e-6, 40.0] * 4)
+        rows = torch.tensor([0, 1, 2, 5, 7, 7, 3, 9, 6, 7, 1, 4] * 2)                # none, a token alone, more than k + 1
+        cu = torch.cat([torch.zeros(1, dtype=torch.int64), torch.cumsum(rows, 0)]).to(torch.int32)
+        assert int(cu[-1]) <= c["target"].shape[0]
+        _check(hs, cu_q=cu, **c)
+
+
+def test_greedy_ties_take_the_lowest(hs):
+    V = 777
+    z = torch.zeros((4, V))
+    z[0, [5, 300, 776]] = 3.0
+    z[2, [0, 776]] = 1.0
+    ids = torch.tensor([[5], [0]], dtype=torch.int32)
+    n, tok = _check(hs, z, None, ids, torch.tensor([[0.5], [0.5]]), torch.tensor([0.9, 0.9]), temperature=torch.zeros(2))
+    assert n.tolist() == [1, 1] and tok.tolist() == [[5, 0], [0, 0]]
+
+
+def test_masked_tokens_and_rows_without_weight(hs):
+    V, inf = 500, float("inf")
+    g = torch.Generator().manual_seed(1)
+    z = torch.randn((8, V), generator=g)
+    d = torch.randn((4, 1, V), generator=g)
+    ids = torch.tensor([[3], [4], [5], [6]], dtype=torch.int32)
+    z[0, 3] = -inf                                           # masked: never stands, at alpha 0 either
+    z[2, 10:] = float("nan")
+    z[4] = -inf                                              # nothing to take: token 0
+    z[6, 6] = inf                                            # counts as the largest finite number: all of p
+    d[1, 0, 4] = -inf                                        # q = 0 at a token with p > 0: stands
+    d[2] = -inf
+    for alpha in (0.0, 1e-38, 0.5, 1.0):
+        _check(hs, z, d, ids, torch.full((4, 1), alpha), torch.tensor([0.0, 0.3, 0.7, 0.99999994]))
+    _check(hs, z, d, ids, torch.full((4, 1), 0.5), torch.rand(4, generator=g), temperature=torch.tensor([0.0, 1.0, 0.0, 3.0]))
+
+
+def test_probabilities_next_to_alpha(hs):
+    """alpha at the ratio itself and one step of 32 bits to either side: the 64-bit comparison decides."""
+    B, V = 96, 20011
+    c = _case(B, 1, V, torch.float32, 5, right=0.0, spread=1.5)
+    p, q = (torch.softmax(c[x].double().reshape(B, -1, V)[:, 0], 1) for x in ("target", "draft"))
+    x = c["ids"].long()
+    ratio = (p.gather(1, x) / q.gather(1, x)).float().clamp(max=1.0)
+    step = torch.tensor([0.0, -1.0, 1.0] * 32)[:, None] * ratio * 2.0 ** -23
+    c["alpha"] = (ratio + step).clamp(max=1.0)
+    n, _ = _check(hs, **c)
+    assert 0 < n.sum() < B
+
+
+def test_uniform_numbers_next_to_a_cumulative_sum(hs):
+    """u at the borders between tokens of a flat vocabulary (k / V is exact where V is a power of two, or next to it), and out of range."""
+    V = 4096
+    z = torch.zeros((16, V))
+    u = torch.tensor([0.0, 1 / V, 2 / V, 0.5, 1 - 1 / V, 0.99999994, 1 / V - 2.0 ** -36, 1.0])
+    ids = torch.zeros((8, 1), dtype=torch.int32)
+    n, tok = _run(hs, z.cuda(), None, ids.cuda(), torch.full((8, 1), 0.0, device="cuda"), u.cuda())
+    assert n.tolist() == [1] * 8 and tok[:, 1].tolist() == [0, 1, 2, V // 2, V - 1, V - 1, 0, V - 1]
+
+
+def test_a_draft_outside_the_vocabulary_does_not_stand(hs):
+    c = _case(3, 2, 900, torch.float32, 3)
+    c["ids"][0, 0], c["ids"][1, 1] = -1, 900
+    hs.hspec_op_device_status(clear=True)
+    n, _ = _check(hs, **c)
+    assert n[0] == 0 and n[1] <= 1
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] >= 1
+
+
+def test_row_pitch_and_odd_addresses(hs):
+    c = {k: v.cuda() if v is not None else None for k, v in _case(4, 3, 1001, torch.bfloat16, 8).items()}
+    want = _run(hs, **c)
+    wide = torch.full((16, 1007), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for first in (0, 1, 3, 6):
+        wide[:, first:first + 1001] = c["target"]
+        got = _run(hs, **dict(c, target=wide[:, first:first + 1001]))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_streams_and_graphs(hs):
+    c = {k: v.cuda() if v is not None else None for k, v in _case(130, 12, 1500, torch.float32, 2).items()}
+    want = [x.clone() for x in _run(hs, **c)]
+    side, outs = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for s in side:
+        with torch.cuda.stream(s):
+            outs.append(_run(hs, **c))
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(a, b) for a, b in zip(o, want))
+    ws = torch.randint(0, 255, (hs.hspec_verify_workspace_bytes(130, 12),), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _run(hs, ws=ws, **c)
+    for _ in range(3):
+        ws.random_(0, 255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    c["alpha"].fill_(1.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    again = _run(hs, **c)
+    assert all(torch.equal(a, b) for a, b in zip(got, again)) and not torch.equal(got[0], want[0])
