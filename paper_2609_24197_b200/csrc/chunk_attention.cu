@@ -1,65 +1,897 @@
 // Attention of a ragged chunk of new tokens over the paged cache that holds their keys and values already.
 //   o[t, h] = sum_j p_j v[j, g] / sum_j p_j,  p_j = exp(scale q[t, h] . k[j, g]),  j <= pos(t), j > pos(t) - window,  g = h / (Hq / Hkv)
-// A row that sees no key is zero.  One warp per (row, head), one pass with the running maximum and sum.
+// A row that sees no key is zero.
+//
+// Rows of a request that share a KV head are packed: row r of the head is token r / rep, query head r % rep.  A work item is up to 256 rows
+// of one (request, KV head) and all the 128-key tiles that any of them sees; tiles lie at multiples of 128 keys.  The items' tiles, request by
+// request, are one long line that is cut into equal parts, one per CTA: however ragged the batch, every SM gets the same number of tiles, and
+// an item that a cut goes through leaves partial results (at most two per CTA) which a second kernel joins.
+//
+//   warps 0..3, 4..7   softmax of the two halves, a thread per row: scores from tensor memory, one pass with a reference maximum that moves only
+//                      when the row's outgrows it by 2^8, weights back into tensor memory over the scores they came from.  With more than 128 rows
+//                      a half is 128 rows and both see every tile; with fewer both have the same rows and take turns at the tiles (two tiles are
+//                      then in the softmax at once), and their accumulators meet at the end.
+//   warp 8             producer: K and V tiles through one ring, by TMA boxes of a page's rows (by 16-byte copies where pages are not whole
+//                      groups of 8 rows)
+//   warp 9             issues S = Q K^T and O += P V (P from tensor memory), one half behind the other: while a half's scores are in the
+//                      softmax the tensor core works for the other
+//   warps 10, 11       go over the V tiles that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
+//                      become zero (a zero weight times NaN would not), and so do single values that are not finite.  Those of them that
+//                      some rows see are added to these rows' results at the end, from the cache, on a path that nothing else takes.
+//
+// Every wait is bounded; a role whose wait runs out sets a status word, and the CTA unwinds.
 #include "chunk.cuh"
+
+#include <cstdlib>
 
 namespace hspec {
 
 namespace {
 
+constexpr int KT = 128;              // keys per tile
+constexpr int MAX_CTAS = 148;
+constexpr int ITEM_ROWS = 256;
+constexpr float NEG = -1.0e30f;
+constexpr float LAZY = 8.0f;         // the reference maximum moves when the row's exceeds it by 2^8
+constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 80;
+
+template <int DH> struct Shape {
+  static constexpr int HALF = KT * 128;                      // [128 rows x 64 values]: 16 KiB, rows of 128 swizzled bytes
+  static constexpr int TILE = KT * DH * 2;                   // Q, K or V tile
+  static constexpr int SLOTS = DH == 128 ? 5 : 10;           // 160 KiB of K and V tiles
+};
+
+struct __align__(16) Bars {
+  // a slot's tile has arrived (two arrivals), has been read, and for V tiles that not every row sees in full: has arrived and may be gone
+  // over, after which the warps that do so give the two arrivals of `full`
+  uint64_t full[10], empty[10], raw[10];
+  uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], o_free[2];
+  uint64_t x_write, x_read, drain;
+  uint32_t tmem_base, abort_flag;
+  uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 5 fit into the ring) met a value that is not finite in a tile that not every row sees in full
+  int4 start;                        // where this CTA's part begins: request, KV head, row tile, tile within the item
+  long long left;                    // and how many tiles it has
+  float2 xml[2][128];                // (reference maximum, row sum) of the halves' rows, for the halves that share their rows
+};
+constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
+
+struct Args {
+  ChunkAttnCall c;
+  int rep, box_rows;                 // rows of a TMA box; 0: pages are copied by 16-byte loads
+  float scale_log2;
+  float* ws_o;                       // [slot][DH / 4][256 rows][4]
+  float2* ws_ml;                     // [slot][256 rows]
+  int4* ws_start;                    // [CTA]; how many CTAs have work lies in ws_count
+  int* ws_count;
+};
+
+// ------------------------------------------------------------------ geometry, the same for every role
+struct ItemGeo {
+  int r0, r1;                        // rows of the head
+  int pos0, pos1;                    // positions of the first and the last row's token
+  int key_lo, key_hi;                // keys that any row sees
+  int t0, t1;                        // tiles
+};
+__device__ __forceinline__ bool takes_turns(int rows) { return rows <= 128; }
+__device__ __forceinline__ int row_tiles(int rows) { return takes_turns(rows) ? (rows > 0 ? 1 : 0) : (rows + ITEM_ROWS - 1) / ITEM_ROWS; }
+__device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int window, int rt) {
+  ItemGeo g;
+  const int rows = q.n * rep;
+  g.r0 = rt * ITEM_ROWS;
+  g.r1 = min(rows, g.r0 + ITEM_ROWS);
+  g.pos0 = q.len - q.n + g.r0 / rep;
+  g.pos1 = q.len - q.n + (g.r1 - 1) / rep;
+  g.key_lo = window > 0 ? max(0, g.pos0 - window + 1) : 0;
+  g.key_hi = max(0, g.pos1 + 1);
+  g.t0 = g.key_lo / KT;
+  g.t1 = max(g.t0 + 1, (g.key_hi + KT - 1) / KT);
+  return g;
+}
+
+struct Walk {                        // this CTA's part of the line, item by item
+  int b, kvh, rt, off;
+  long long left;
+  ChunkRequest q, next;
+};
+__device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int b) {
+  if (b >= c.B) return ChunkRequest{0, 0, 0};
+  return chunk_request(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len);
+}
+__device__ __forceinline__ Walk walk_begin(const ChunkAttnCall& c, const Bars* bars) {
+  Walk w;
+  w.b = bars->start.x; w.kvh = bars->start.y; w.rt = bars->start.z; w.off = bars->start.w;
+  w.left = bars->left;
+  w.q = load_request(c, w.b);
+  w.next = load_request(c, w.b + 1);
+  return w;
+}
+struct Segment {
+  ItemGeo g;
+  int ta, tb;                        // tiles of this CTA
+  int nt[2];                         // tiles of each half
+  bool turns, whole;
+};
+__device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
+  Segment s;
+  s.g = item_geo(w.q, a.rep, a.c.window, w.rt);
+  s.ta = s.g.t0 + w.off;
+  s.tb = int(min((long long)s.g.t1, s.ta + w.left));
+  s.whole = w.off == 0 && s.tb == s.g.t1;
+  s.turns = takes_turns(w.q.n * a.rep);
+  const int T = s.tb - s.ta;
+  if (s.turns) {
+    s.nt[0] = (T + 1) / 2; s.nt[1] = T / 2;
+  } else if (s.g.r1 - s.g.r0 > 128) {
+    // the first half's rows end earlier, and with them the tiles that they see
+    const int pos = w.q.len - w.q.n + (s.g.r0 + 127) / a.rep;
+    const int end = max(s.g.t0 + 1, (pos + KT) / KT);
+    s.nt[0] = max(0, min(end - s.ta, T)); s.nt[1] = T;
+  } else {
+    s.nt[0] = T; s.nt[1] = 0;
+  }
+  return s;
+}
+// On to the next item; false at the end of this CTA's part.
+__device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a) {
+  w.left -= s.tb - s.ta;
+  w.off = 0;
+  if (w.left <= 0) return false;
+  if (++w.rt < row_tiles(w.q.n * a.rep)) return true;
+  w.rt = 0;
+  if (++w.kvh < a.c.Hkv) return true;
+  w.kvh = 0;
+  do {
+    ++w.b;
+    w.q = w.next;
+    w.next = load_request(a.c, w.b + 1);
+  } while (w.q.n == 0 && w.b < a.c.B);
+  return w.b < a.c.B;
+}
+// Not every row of the item sees all of the tile's keys.
+__device__ __forceinline__ bool partial_tile(const ItemGeo& g, int window, int t) {
+  return t * KT + KT - 1 > g.pos0 || (window > 0 && t * KT < g.pos1 - window + 1);
+}
+// Place of K and V tile t (0 .. T-1 within the segment) in the segment's sequence of loads: K0, K1, V0, K2, V1, .., V(T-1).
+__device__ __forceinline__ int k_place(int t) { return t == 0 ? 0 : 2 * t - 1; }
+__device__ __forceinline__ int v_place(int t, int T) { return t < T - 1 ? 2 * t + 2 : 2 * T - 1; }
+
+// byte offset of (row, 16-byte chunk) in an operand tile: halves of 64 values, 128-byte swizzle
+__device__ __forceinline__ uint32_t tile_off(int row, int chunk) {
+  return uint32_t((chunk >> 3) * Shape<128>::HALF + (row >> 3) * 1024 + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+}
+// V tile as MN-major B operand: halves HALF bytes apart, groups of 8 keys 1024
+__device__ __forceinline__ uint64_t desc_v(uint32_t addr) {
+  return uint64_t((addr & 0x3FFFF) >> 4) | (uint64_t(Shape<128>::HALF >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+__device__ __forceinline__ uint32_t idesc(bool f16, int n, bool b_mn_major) {
+  const uint32_t fmt = f16 ? 0u : 1u;
+  return (1u << 4) | (fmt << 7) | (fmt << 10) | ((b_mn_major ? 1u : 0u) << 16) | (uint32_t(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
 template <bool F16>
-__device__ __forceinline__ float load16(const void* p, size_t i) {
-  return F16 ? __half2float(reinterpret_cast<const __half*>(p)[i]) : bf16_bits_to_float(reinterpret_cast<const uint16_t*>(p)[i]);
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (F16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return pack_bf16(lo, hi);
+}
+template <bool F16>
+__device__ __forceinline__ bool not_finite16(uint32_t x) {
+  constexpr uint32_t m = F16 ? 0x7c00u : 0x7f80u;
+  return (x & m) == m;
+}
+
+// ------------------------------------------------------------------ the plan
+// Cuts the line: tiles of every request (one warp each), their running sum, the place where this CTA's part begins.  `sums` is shared memory
+// for B + 1 numbers.  Returns false for a CTA without work.
+__device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
+  const ChunkAttnCall& c = a.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  for (int b = warp; b < c.B; b += warps) {
+    const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
+    const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
+    if (blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+    long long n = 0;
+    const int tiles = row_tiles(q.n * a.rep);
+    for (int rt = lane; rt < tiles; rt += 32) { const ItemGeo g = item_geo(q, a.rep, c.window, rt); n += g.t1 - g.t0; }
+    for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(0xffffffffu, n, off);
+    if (lane == 0) sums[b + 1] = n * c.Hkv;
+  }
+  if (threadIdx.x == 0) sums[0] = 0;
+  __syncthreads();
+  if (warp == 0) {
+    long long before = 0;
+    for (int base = 0; base < c.B; base += 32) {
+      long long n = base + lane < c.B ? sums[base + lane + 1] : 0;
+      for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
+      if (base + lane < c.B) sums[base + lane + 1] = before + n;
+      before += __shfl_sync(0xffffffffu, n, 31);
+    }
+    const long long total = before;
+    const int parts = int(min((long long)gridDim.x, total)), me = blockIdx.x;
+    if (me == 0 && lane == 0) *a.ws_count = parts;
+    __syncwarp();
+    if (me < parts) {
+      const long long u0 = total * me / parts, u1 = total * (me + 1) / parts;
+      int lo = 0, hi = c.B;                                   // the request with sums[lo] <= u0 < sums[lo + 1]
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (sums[mid] <= u0) lo = mid; else hi = mid; }
+      const ChunkRequest q = load_request(c, lo);
+      const long long per_head = (sums[lo + 1] - sums[lo]) / c.Hkv;
+      const int kvh = int((u0 - sums[lo]) / per_head);
+      long long rest = (u0 - sums[lo]) - kvh * per_head;
+      const int tiles = row_tiles(q.n * a.rep);
+      int rt = 0;
+      for (int base = 0; base < tiles; base += 32) {
+        int n = 0;
+        if (base + lane < tiles) { const ItemGeo g = item_geo(q, a.rep, c.window, base + lane); n = g.t1 - g.t0; }
+        long long upto = n;
+        for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
+        const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
+        if (in) {
+          const int l = __ffs(in) - 1;
+          rt = base + l;
+          rest -= l > 0 ? __shfl_sync(0xffffffffu, upto, l - 1) : 0;
+          break;
+        }
+        rest -= __shfl_sync(0xffffffffu, upto, 31);
+      }
+      if (lane == 0) {
+        bars->start = make_int4(lo, kvh, rt, int(rest));
+        bars->left = u1 - u0;
+        a.ws_start[me] = bars->start;
+      }
+    } else if (lane == 0) {
+      bars->left = 0;
+    }
+  }
+  __syncthreads();
+  return bars->left > 0;
+}
+
+// ------------------------------------------------------------------ producer
+struct Ring { uint32_t base; };      // tiles loaded in earlier segments
+template <int DH>
+__device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, const CUtensorMap* tmV, uint8_t* ring, Bars* bars, int lane) {
+  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+  const ChunkAttnCall& c = a.c;
+  volatile uint32_t* abort_flag = &bars->abort_flag;
+  Walk w = walk_begin(c, bars);
+  uint32_t at = 0;                                            // tiles issued
+  uint32_t raw_phase = 0, is_raw = 0;                         // a bit per slot: phase of `raw`, and whether the slot's last tile went there
+  bool ok = true;
+  const int boxes = a.box_rows ? KT / a.box_rows : 0;
+  do {
+    const Segment s = segment_of(w, a);
+    const int T = s.tb - s.ta;
+    const int32_t* table = c.page_table + size_t(w.b) * c.page_table_stride;
+    // page of this lane's boxes (up to 16 boxes: one a lane), of the tiles t and t + 1
+    auto page_of = [&](int t) {
+      if (lane >= boxes || t >= s.tb) return -1;
+      const int key = t * KT + lane * a.box_rows;
+      return key < s.g.key_hi && key + a.box_rows > s.g.key_lo ? table[key / c.page_size] : -1;
+    };
+    int page_k = page_of(s.ta), page_next = page_of(s.ta + 1), page_v = page_k;
+    auto load = [&](bool is_v, int t, int page) {
+      const uint32_t slot = at % NS;
+      if (at >= NS && !mbar_wait(smem_u32(&bars->empty[slot]), ((at / NS) - 1) & 1)) ok = false;
+      if (!ok || *abort_flag) { ok = false; return; }
+      const bool raw = is_v && partial_tile(s.g, c.window, t);
+      const uint32_t dst = smem_u32(ring) + slot * TILE, bar = smem_u32(raw ? &bars->raw[slot] : &bars->full[slot]);
+      const int key0 = t * KT;
+      is_raw = raw ? is_raw | (1u << slot) : is_raw & ~(1u << slot);
+      if (raw) raw_phase ^= 1u << slot;
+      if (!raw && lane == 0) mbar_arrive(bar);
+      if (a.box_rows) {
+        const int key = key0 + lane * a.box_rows;
+        const bool on = lane < boxes && key < s.g.key_hi && key + a.box_rows > s.g.key_lo;
+        const unsigned n = __popc(__ballot_sync(0xffffffffu, on));
+        if (lane == 0) {
+          if (n) mbar_expect_tx(bar, n * a.box_rows * DH * 2);
+          else mbar_arrive(bar);
+        }
+        __syncwarp();
+        if (on) {
+          // (a page id outside the pool is outside the tensor map: the copy delivers zeros and touches no memory)
+          if (!is_v && unsigned(page) >= unsigned(c.num_pages)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+#pragma unroll
+          for (int h = 0; h < DH / 64; ++h)
+            tma_load_4d(dst + h * Shape<DH>::HALF + lane * a.box_rows * 128, is_v ? tmV : tmK, h * 64, w.kvh, key % c.page_size, page, bar);
+        }
+      } else {
+        const uint16_t* pool = reinterpret_cast<const uint16_t*>(is_v ? c.v_pool : c.k_pool);
+        for (int i = lane; i < KT * (DH / 8); i += 32) {
+          const int r = i / (DH / 8), chunk = i % (DH / 8), key = key0 + r;
+          bool on = key >= s.g.key_lo && key < s.g.key_hi;
+          size_t from = 0;
+          if (on) {
+            const int id = table[key / c.page_size];
+            if (unsigned(id) >= unsigned(c.num_pages)) {
+              on = false;
+              if (!is_v && chunk == 0 && (key % c.page_size == 0 || key == s.g.key_lo)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+            } else {
+              from = ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + chunk * 8;
+            }
+          }
+          cp_async16(dst + tile_off(r, chunk), pool + from, on);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      }
+      ++at;
+    };
+    load(false, s.ta, page_k);
+    for (int t = s.ta; t < s.tb && ok; ++t) {
+      if (t + 1 < s.tb) {
+        page_k = page_next;
+        page_next = page_of(t + 2);
+        load(false, t + 1, page_k);
+      }
+      if (ok) load(true, t, page_v);
+      page_v = page_k;
+    }
+    if (!ok) break;
+    if (!walk_on(w, s, a)) break;
+  } while (true);
+  if (!ok) {
+    if (lane == 0) {
+      if (!*abort_flag) atomicExch(c.status, STATUS_TIMEOUT_PRODUCER);
+      *abort_flag = 1;
+    }
+    // what has been asked for still arrives in shared memory: it must not outlive the CTA
+    for (uint32_t p = at > NS ? at - NS : 0; p < at; ++p) {
+      const uint32_t slot = p % NS;
+      if ((is_raw >> slot) & 1) mbar_wait(smem_u32(&bars->raw[slot]), ((raw_phase >> slot) & 1) ^ 1);
+      else mbar_wait(smem_u32(&bars->full[slot]), (p / NS) & 1);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ values that not every row sees
+template <int DH, bool F16>
+__device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars* bars, int tid) {
+  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+  volatile uint32_t* abort_flag = &bars->abort_flag;
+  Walk w = walk_begin(a.c, bars);
+  uint32_t base = 0, seg = 0, phase = 0;                      // phase of `raw`, a bit per slot
+  do {
+    const Segment s = segment_of(w, a);
+    const int T = s.tb - s.ta;
+    for (int t = s.ta; t < s.tb; ++t) {
+      if (!partial_tile(s.g, a.c.window, t)) continue;
+      const uint32_t at = base + v_place(t - s.ta, T), slot = at % NS;
+      if (!mbar_wait(smem_u32(&bars->raw[slot]), (phase >> slot) & 1) || *abort_flag) {
+        if (tid == 0 && !*abort_flag) { atomicExch(a.c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
+        return;
+      }
+      phase ^= 1u << slot;
+      uint8_t* tile = ring + slot * TILE;
+      bool bad = false;
+      for (int i = tid; i < KT * (DH / 8); i += 64) {
+        const int r = i / (DH / 8), key = t * KT + r;
+        uint4* p = reinterpret_cast<uint4*>(tile + tile_off(r, i % (DH / 8)));
+        if (key < s.g.key_lo || key >= s.g.key_hi) {
+          *p = make_uint4(0u, 0u, 0u, 0u);
+        } else {
+          uint4 v = *p;
+          uint32_t x[4] = {v.x, v.y, v.z, v.w};
+          bool here = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (not_finite16<F16>(x[e])) { x[e] &= 0xffff0000u; here = true; }
+            if (not_finite16<F16>(x[e] >> 16)) { x[e] &= 0x0000ffffu; here = true; }
+          }
+          if (here) { *p = make_uint4(x[0], x[1], x[2], x[3]); bad = true; }
+        }
+      }
+      if (bad) *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) = seg + 1;
+      fence_proxy_async();
+      __syncwarp();
+      if ((tid & 31) == 0) mbar_arrive(smem_u32(&bars->full[slot]));
+    }
+    base += 2 * T;
+    ++seg;
+    if (!walk_on(w, s, a)) break;
+  } while (true);
+}
+
+// ------------------------------------------------------------------ MMA issuer (one thread)
+template <int DH, bool F16>
+__device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* ring, Bars* bars, uint32_t tmem) {
+  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE, HALF = Shape<DH>::HALF;
+  const uint32_t id_s = idesc(F16, KT, false), id_o = idesc(F16, DH, true);
+  volatile uint32_t* abort_flag = &bars->abort_flag;
+  Walk w = walk_begin(a.c, bars);
+  uint32_t base = 0;
+  uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0};                  // segments and tiles of each half so far
+  bool ok = true;
+  do {
+    const Segment s = segment_of(w, a);
+    const int T = s.tb - s.ta;
+    auto scores = [&](int h, int j) {
+      const int t = s.turns ? 2 * j + h : j;
+      const uint32_t at = base + k_place(t), slot = at % NS;
+      if (!mbar_wait_spin(smem_u32(&bars->full[slot]), (at / NS) & 1)) { ok = false; return; }
+      tc_fence_after();
+      const uint32_t qb = smem_u32(sQ) + h * TILE, kb = smem_u32(ring) + slot * TILE;
+#pragma unroll
+      for (int ks = 0; ks < DH / 16; ++ks)
+        umma_bf16(tmem + h * 128, umma_desc_kmajor_sw128(qb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2),
+                  umma_desc_kmajor_sw128(kb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2), id_s, ks > 0 ? 1u : 0u);
+      umma_commit(smem_u32(&bars->s_ready[h]));
+      if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->empty[slot]));
+    };
+    for (int h = 0; h < 2 && ok; ++h) {
+      if (s.nt[h] == 0) continue;
+      if (!mbar_wait_spin(smem_u32(&bars->q_ready[h]), n_q[h] & 1)) { ok = false; break; }
+      tc_fence_after();
+      scores(h, 0);
+    }
+    const int most = max(s.nt[0], s.nt[1]);
+    for (int j = 0; j < most && ok; ++j) {
+      for (int h = 0; h < 2 && ok; ++h) {
+        if (j >= s.nt[h]) continue;
+        const int t = s.turns ? 2 * j + h : j;
+        const uint32_t at = base + v_place(t, T), slot = at % NS;
+        if (!mbar_wait_spin(smem_u32(&bars->p_ready[h]), n_p[h] & 1)) { ok = false; break; }
+        ++n_p[h];
+        if (!mbar_wait_spin(smem_u32(&bars->full[slot]), (at / NS) & 1)) { ok = false; break; }
+        // the first product of an item overwrites the accumulator: the item before must have been read out
+        if (j == 0 && n_q[h] > 0 && !mbar_wait_spin(smem_u32(&bars->o_free[h]), (n_q[h] - 1) & 1)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t vb = smem_u32(ring) + slot * TILE;
+#pragma unroll
+        for (int ks = 0; ks < KT / 16; ++ks)
+          umma_bf16_ts(tmem + 256 + h * 128, tmem + h * 128 + ks * 8, desc_v(vb + ks * 2048), id_o, (j > 0 || ks > 0) ? 1u : 0u);
+        umma_commit(smem_u32(&bars->pv_done[h]));
+        if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->empty[slot]));
+        if (j + 1 < s.nt[h]) scores(h, j + 1);
+      }
+      if (*abort_flag) ok = false;
+    }
+    if (!ok) break;
+    for (int h = 0; h < 2; ++h) if (s.nt[h] > 0) ++n_q[h];
+    base += 2 * T;
+    if (!walk_on(w, s, a)) break;
+  } while (true);
+  if (!ok) {
+    if (!*abort_flag) atomicExch(a.c.status, STATUS_TIMEOUT_MMA);
+    *abort_flag = 1;
+    umma_commit(smem_u32(&bars->drain));                      // products under way end before the CTA does
+    mbar_wait(smem_u32(&bars->drain), 0);
+  }
+}
+
+// ------------------------------------------------------------------ softmax of one half
+// Adds to 32 columns of a row's accumulator the values that are not finite and that the row sees, from the tiles that were cleaned of them.
+template <int DH, bool F16>
+__device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const Segment& s, int lo, int hi, int col, float* acc) {
+  const ChunkAttnCall& c = a.c;
+  for (int t = s.ta; t < s.tb; ++t) {
+    if (!partial_tile(s.g, c.window, t)) continue;
+    for (int key = max(lo, t * KT); key <= min(hi, t * KT + KT - 1); ++key) {
+      const int id = c.page_table[size_t(w.b) * c.page_table_stride + key / c.page_size];
+      if (unsigned(id) >= unsigned(c.num_pages)) continue;
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(c.v_pool) + ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + col;
+      for (int e = 0; e < 32; ++e) {
+        const uint16_t x = v[e];
+        if (not_finite16<F16>(x)) acc[e] += F16 ? __half2float(__ushort_as_half(x)) : bf16_bits_to_float(x);
+      }
+    }
+  }
 }
 
 template <int DH, bool F16>
-__global__ void __launch_bounds__(256) chunk_attn_kernel(ChunkAttnCall c) {
+__device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* bars, uint32_t tmem, int h, int tid) {
+  constexpr int TILE = Shape<DH>::TILE;
+  const ChunkAttnCall& c = a.c;
+  volatile uint32_t* abort_flag = &bars->abort_flag;
+  const int row = tid & 127, warp = row >> 5, lane = tid & 31;
+  const uint32_t lane_base = uint32_t(warp * 32) << 16;
+  const uint32_t t_s = tmem + h * 128 + lane_base;
+  uint8_t* myQ = sQ + h * TILE;
+  auto first_row = [&](const Segment& s) { return s.g.r0 + (s.turns ? 0 : h * 128); };
+  // this thread's row of Q: 16-byte asynchronous copies into the operand layout, zeros for rows that are not there
+  auto q_issue = [&](const Walk& w, const Segment& s) {
+    const int r = first_row(s) + row;
+    const bool on = r < s.g.r1;
+    const uint16_t* src = reinterpret_cast<const uint16_t*>(c.q);
+    if (on) src += size_t(w.q.q0 + r / a.rep) * c.ldq + size_t(w.kvh * a.rep + r % a.rep) * DH;
+#pragma unroll
+    for (int i = 0; i < DH / 8; ++i) cp_async16(smem_u32(myQ + tile_off(row, i)), src + (on ? i * 8 : 0), on);
+    cp_async_commit();
+  };
+  auto q_finish = [&]() {
+    cp_async_wait<0>();
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&bars->q_ready[h]));
+  };
+  Walk w = walk_begin(c, bars);
+  Segment s = segment_of(w, a);
+  uint32_t tiles[2] = {0, 0}, seg = 0, shared_segs = 0;       // tiles of both halves so far, segments, segments whose rows the halves share
+  if (s.nt[h] > 0) { q_issue(w, s); q_finish(); }
+  bool ok = true, more = true;
+  int slot = 2 * blockIdx.x;                                  // where this CTA's partial results go: its first segment's, then its last one's
+  while (more) {
+    Walk wn = w;
+    more = walk_on(wn, s, a);
+    Segment sn = s;
+    if (more) sn = segment_of(wn, a);
+    const bool q_next = more && sn.nt[h] > 0;
+    const int r = first_row(s) + row;                         // row of the head
+    const bool row_ok = r < s.g.r1;
+    const int hi = row_ok ? w.q.len - w.q.n + r / a.rep : -1;                       // keys lo .. hi are seen
+    const int lo = c.window > 0 ? max(0, hi - c.window + 1) : 0;
+    const bool warp_live = first_row(s) + warp * 32 < s.g.r1;
+    float m_ref = NEG, l_sum = 0.f;
+    if (s.nt[h] == 0 && q_next) { q_issue(wn, sn); q_finish(); }
+    for (int j = 0; j < s.nt[h]; ++j) {
+      const uint32_t n = tiles[h] + j;
+      if (!mbar_wait(smem_u32(&bars->s_ready[h]), n & 1)) { ok = false; break; }
+      // with the last tile's scores all products that read this Q have finished: the next item's goes in
+      const bool q_now = q_next && j == s.nt[h] - 1;
+      if (q_now) q_issue(wn, sn);
+      if (warp_live) {
+        tc_fence_after();
+        float x[128];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + i * 32, reinterpret_cast<uint32_t*>(x + i * 32));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + i * 32));
+        const int key0 = (s.ta + (s.turns ? 2 * j + h : j)) * KT;
+        if (__any_sync(0xffffffffu, hi < key0 + KT - 1 || lo > key0)) {
+          const int jh = hi - key0, jl = lo - key0;
+#pragma unroll
+          for (int i = 0; i < 128; ++i) x[i] = (i <= jh && i >= jl) ? x[i] : -INFINITY;
+        }
+        float m4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int i = 4; i < 128; i += 4) {
+          m4[0] = fmaxf(m4[0], x[i]); m4[1] = fmaxf(m4[1], x[i + 1]); m4[2] = fmaxf(m4[2], x[i + 2]); m4[3] = fmaxf(m4[3], x[i + 3]);
+        }
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
+        const bool grow = mx > m_ref + LAZY;
+        float factor = 1.f;
+        if (grow) { factor = ex2_ftz(m_ref - mx); m_ref = mx; }
+        if (j > 0 && __any_sync(0xffffffffu, grow)) {
+          if (!mbar_wait(smem_u32(&bars->pv_done[h]), (n - 1) & 1)) { ok = false; break; }
+          tc_fence_after();
+          if (lane == 0) atomicAdd(c.status + STATUS_WORD_RESCALES, 1u);
+#pragma unroll 1
+          for (int i = 0; i < DH / 16; ++i) {
+            uint32_t o[16];
+            tmem_ld16(tmem + 256 + h * 128 + lane_base + i * 16, o);
+            tmem_wait_ld16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+            tmem_st16(tmem + 256 + h * 128 + lane_base + i * 16, o);
+          }
+          tmem_st_wait();
+        }
+        l_sum *= factor;
+        const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_m2 = pack_f32x2(-m_ref, -m_ref);
+        uint64_t ls[2] = {0ull, 0ull};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(x[half * 64 + 2 * e], x[half * 64 + 2 * e + 1]), scale2, neg_m2), x0, x1);
+            const float p0 = ex2_ftz(x0), p1 = ex2_ftz(x1);
+            ls[e & 1] = add_f32x2(ls[e & 1], pack_f32x2(p0, p1));
+            p[e] = pack16<F16>(p0, p1);
+          }
+          tmem_st32(t_s + half * 32, p);
+        }
+        float s0, s1, s2, s3;
+        unpack_f32x2(ls[0], s0, s1);
+        unpack_f32x2(ls[1], s2, s3);
+        l_sum += (s0 + s1) + (s2 + s3);
+        tmem_st_wait();
+        tc_fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[h]));
+      if (q_now) q_finish();
+    }
+    tiles[0] += s.nt[0]; tiles[1] += s.nt[1];
+    if (!ok) break;
+    // ---- read-out
+    if (s.nt[h] > 0 && (!mbar_wait(smem_u32(&bars->pv_done[h]), (tiles[h] - 1) & 1) || *abort_flag)) { ok = false; break; }
+    float weight0 = 1.f, weight1 = 0.f;
+    if (s.turns) {
+      // the halves' rows are the same: maxima and sums are exchanged, each half finishes its part of the columns
+      if (shared_segs > 0 && !mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
+      bars->xml[h][row] = make_float2(m_ref, l_sum);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->x_write));
+      if (!mbar_wait(smem_u32(&bars->x_write), shared_segs & 1)) { ok = false; break; }
+      const float2 o = bars->xml[h ^ 1][row];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bars->x_read));
+      ++shared_segs;
+      if (s.nt[h ^ 1] > 0 && !mbar_wait(smem_u32(&bars->pv_done[h ^ 1]), (tiles[h ^ 1] - 1) & 1)) { ok = false; break; }
+      const float m = fmaxf(m_ref, o.x), mine = ex2_ftz(m_ref - m), theirs = ex2_ftz(o.x - m);
+      l_sum = l_sum * mine + o.y * theirs;
+      m_ref = m;
+      weight0 = h == 0 ? mine : theirs; weight1 = h == 0 ? theirs : mine;
+    }
+    tc_fence_after();
+    const bool fix = *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) == seg + 1;
+    const int col0 = s.turns ? h * (DH / 2) : 0, cols = s.turns ? DH / 2 : DH;
+    const float inv = l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum);      // (nothing seen: zero; NaN stays)
+    const bool live = warp_live && (s.turns || s.nt[h] > 0);
+    if (!s.whole && row_ok && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
+    if (live) {
+      uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(w.q.q0 + r / a.rep) * c.ldo + size_t(w.kvh * a.rep + r % a.rep) * DH : 0);
+      float* part = a.ws_o + size_t(slot) * DH * ITEM_ROWS + size_t(r - s.g.r0) * 4;
+#pragma unroll 1
+      for (int col = col0; col < col0 + cols; col += 32) {
+        __syncwarp();
+        float v[32];
+        if (s.turns) {
+          uint32_t o[32];
+          tmem_ld32(tmem + 256 + lane_base + col, o);         // (the first half always has a tile)
+          tmem_wait_ld32(o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * weight0;
+          if (s.nt[1] > 0) {
+            tmem_ld32(tmem + 384 + lane_base + col, o);
+            tmem_wait_ld32(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = fmaf(__uint_as_float(o[e]), weight1, v[e]);
+          }
+        } else {
+          uint32_t o[32];
+          tmem_ld32(tmem + 256 + h * 128 + lane_base + col, o);
+          tmem_wait_ld32(o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]);
+        }
+        if (fix && row_ok) {
+          float copy[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) copy[e] = v[e];
+          add_not_finite<DH, F16>(a, w, s, lo, hi, col, copy);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = copy[e];
+        }
+        if (s.whole && row_ok) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              p[i] = F16 ? pack_f16_sat(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv, c.status) : pack_bf16(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv);
+            *reinterpret_cast<uint4*>(dst + col + e) = make_uint4(p[0], p[1], p[2], p[3]);
+          }
+        } else if (row_ok) {
+          // [column group][row][4]: the lanes of a warp write neighbouring 16 bytes
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        }
+      }
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      if (s.turns) {
+        for (int i = 0; i < 2; ++i) if (s.nt[i] > 0) mbar_arrive(smem_u32(&bars->o_free[i]));
+      } else if (s.nt[h] > 0) {
+        mbar_arrive_n(smem_u32(&bars->o_free[h]), 2);
+      }
+    }
+    slot = 2 * blockIdx.x + 1;
+    ++seg;
+    w = wn;
+    s = sn;
+  }
+  if (!ok) { if (!*abort_flag) atomicExch(c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
+  tc_fence_before();
+}
+
+template <int DH, bool F16>
+__global__ void __launch_bounds__(384, 1)
+chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
+  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint8_t* sQ = smem;
+  uint8_t* ring = smem + 2 * TILE;
+  Bars* bars = reinterpret_cast<Bars*>(ring + NS * TILE);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int t = int(w / c.Hq), h = int(w % c.Hq), g = h / (c.Hq / c.Hkv);
-  if (t >= c.T) return;
-  const int b = chunk_request_of(c.cu_q, c.B, t, lane);
-  if (b >= c.B || t < c.cu_q[b]) return;
-  const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
-  const ChunkRequest r = chunk_request(cu0, cu1, len, c.T, c.max_len);
-  const bool counts = lane == 0 && h == 0 && t == r.q0;       // one row of the request speaks for it
-  if (counts && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-  const int pos = r.len - r.n + (t - r.q0);
-  constexpr int E = DH / 32;
-  float q[E], acc[E], mx = -INFINITY, sum = 0.f;
-  for (int e = 0; e < E; ++e) { q[e] = load16<F16>(c.q, size_t(t) * c.ldq + h * DH + e * 32 + lane) * c.scale; acc[e] = 0.f; }
-  for (int j = c.window > 0 ? max(0, pos - c.window + 1) : 0; j <= pos; ++j) {
-    const int page = c.page_table[size_t(b) * c.page_table_stride + j / c.page_size];
-    const bool ok = page >= 0 && page < c.num_pages;
-    if (!ok && counts) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-    const size_t at = ((size_t(ok ? page : 0) * c.page_size + j % c.page_size) * c.Hkv + g) * DH + lane;
-    float s = 0.f;
-    for (int e = 0; e < E; ++e) s += ok ? q[e] * load16<F16>(c.k_pool, at + e * 32) : 0.f;
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    const float nm = fmaxf(mx, s), f = expf(mx - nm), p = expf(s - nm);
-    mx = nm;
-    sum = sum * f + p;
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + (ok ? p * load16<F16>(c.v_pool, at + e * 32) : 0.f);
+  if (smem_u32(smem) & 1023) {                                // the swizzled tiles need a 1 KiB-aligned base
+    if (tid == 0) atomicExch(a.c.status, STATUS_BAD_SMEM_BASE);
+    return;
   }
-  for (int e = 0; e < E; ++e) {
-    const float v = pos < 0 ? 0.f : acc[e] / sum;
-    const size_t at = size_t(t) * c.ldo + h * DH + e * 32 + lane;
-    if (F16) reinterpret_cast<__half*>(c.o)[at] = f16_sat(v, c.status);
-    else reinterpret_cast<__nv_bfloat16*>(c.o)[at] = __float2bfloat16_rn(v);
+  if (!make_plan(a, bars, reinterpret_cast<long long*>(ring))) return;
+  if (tid == 0) {
+    if (a.box_rows) { tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); }
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(smem_u32(&bars->full[i]), 2);
+      mbar_init(smem_u32(&bars->empty[i]), 1);
+      mbar_init(smem_u32(&bars->raw[i]), 1);
+    }
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(smem_u32(&bars->q_ready[h]), 4);
+      mbar_init(smem_u32(&bars->s_ready[h]), 1);
+      mbar_init(smem_u32(&bars->p_ready[h]), 4);
+      mbar_init(smem_u32(&bars->pv_done[h]), 1);
+      mbar_init(smem_u32(&bars->o_free[h]), 8);
+    }
+    mbar_init(smem_u32(&bars->x_write), 8);
+    mbar_init(smem_u32(&bars->x_read), 8);
+    mbar_init(smem_u32(&bars->drain), 1);
+    bars->abort_flag = 0;
+    for (int i = 0; i < 16; ++i) bars->bad[i] = 0;
+    fence_mbar_init();
   }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    tmem_relinquish();
+  }
+  fence_proxy_async();                                        // (the plan's sums lay where the copies now go)
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;      // scores (and the weights over them) of the halves in columns 0 and 128, accumulators in 256 and 384
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
+    softmax_half<DH, F16>(a, sQ, bars, tmem, warp >> 2, tid);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
+    if (warp == 8) {
+      produce<DH>(a, &tmK, &tmV, ring, bars, lane);
+    } else if (warp == 9) {
+      if (elect_one()) issue_mmas<DH, F16>(a, sQ, ring, bars, tmem);
+      __syncwarp();
+    } else {
+      clean_values<DH, F16>(a, ring, bars, tid - 320);
+    }
+  }
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------ joining items that a cut went through
+// One block per (CTA, 32 rows).  The CTA whose part an item begins in speaks for it: its partial result and those of the CTAs behind, in order.
+// Lane = row, warp = 16 (or 8) columns, so that the loads follow the partials' layout.
+template <int DH, bool F16>
+__global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_constant__ Args a) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int COLS = DH / 8, ROW = DH * 2 + 16;
+  __shared__ __align__(16) uint8_t tile[32 * ROW];
+  const ChunkAttnCall& c = a.c;
+  const int me = blockIdx.x, count = *a.ws_count;
+  if (me + 1 >= count) return;
+  const int4 x = a.ws_start[me + 1], mine = a.ws_start[me];
+  auto same = [&](const int4& y) { return y.x == x.x && y.y == x.y && y.z == x.z; };
+  if (x.w == 0 || (same(mine) && mine.w > 0)) return;         // no cut through an item here, or an earlier CTA speaks for it
+  const int first = 2 * me + (same(mine) ? 0 : 1);
+  int last = me + 1;
+  while (last + 1 < count && same(a.ws_start[last + 1])) ++last;                    // (its place in the item is then behind the item's begin)
+  const ChunkRequest q = load_request(c, x.x);
+  const ItemGeo g = item_geo(q, a.rep, c.window, x.z);
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, r = blockIdx.y * 32 + lane, rows = g.r1 - g.r0;
+  if (blockIdx.y * 32 >= rows) return;
+  if (r < rows) {
+    float m = NEG;
+    for (int i = me; i <= last; ++i) m = fmaxf(m, a.ws_ml[size_t(i == me ? first : 2 * i) * ITEM_ROWS + r].x);
+    float acc[COLS], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+    for (int i = me; i <= last; ++i) {
+      const size_t slot = i == me ? first : 2 * i;
+      const float2 ml = a.ws_ml[slot * ITEM_ROWS + r];
+      if (ml.x == NEG && ml.y == 0.f) continue;               // the row saw nothing there (its half may not even have written)
+      const float f = ex2_ftz(ml.x - m);
+      sum += ml.y * f;
+#pragma unroll
+      for (int e = 0; e < COLS; e += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(a.ws_o + slot * DH * ITEM_ROWS + (size_t(w * COLS + e) / 4 * ITEM_ROWS + r) * 4);
+        acc[e] += v.x * f; acc[e + 1] += v.y * f; acc[e + 2] += v.z * f; acc[e + 3] += v.w * f;
+      }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+#pragma unroll
+    for (int e = 0; e < COLS; e += 8) {
+      uint32_t p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        p[i] = F16 ? pack_f16_sat(acc[e + 2 * i] * inv, acc[e + 2 * i + 1] * inv, c.status) : pack_bf16(acc[e + 2 * i] * inv, acc[e + 2 * i + 1] * inv);
+      *reinterpret_cast<uint4*>(tile + lane * ROW + (w * COLS + e) * 2) = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+  }
+  __syncthreads();
+  constexpr int LANES = DH / 8;                               // lanes that write a row
+  for (int i = threadIdx.x; i < 32 * LANES; i += 256) {
+    const int rl = i / LANES, rr = g.r0 + blockIdx.y * 32 + rl;
+    if (rr < g.r1)
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + size_t(q.q0 + rr / a.rep) * c.ldo + size_t(x.y * a.rep + rr % a.rep) * DH + (i % LANES) * 8) =
+          *reinterpret_cast<const uint4*>(tile + rl * ROW + (i % LANES) * 16);
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// 4-D view of a pool [num_pages, page_size, Hkv, dh]; a box is box_rows rows of one page, one KV head, 64 values.
+bool pool_tmap(CUtensorMap* tm, const void* pool, const ChunkAttnCall& c, int box_rows, std::string* err) {
+  static const EncodeTiledFn enc = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(p);
+  }();
+  if (!enc) { *err = "cuTensorMapEncodeTiled is not available"; return false; }
+  cuuint64_t dims[4] = {cuuint64_t(c.dh), cuuint64_t(c.Hkv), cuuint64_t(c.page_size), cuuint64_t(c.num_pages)};
+  cuuint64_t strides[3] = {cuuint64_t(c.dh) * 2, cuuint64_t(c.Hkv) * c.dh * 2, cuuint64_t(c.page_size) * c.Hkv * c.dh * 2};
+  cuuint32_t box[4] = {64, 1, cuuint32_t(box_rows), 1}, estr[4] = {1, 1, 1, 1};
+  const CUresult r = enc(tm, c.f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) { *err = "cuTensorMapEncodeTiled (KV pool) failed with CUresult " + std::to_string(int(r)); return false; }
+  return true;
+}
+
+template <int DH, bool F16>
+cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tmK, const CUtensorMap& tmV) {
+  constexpr size_t smem = smem_bytes(Shape<DH>::TILE, Shape<DH>::SLOTS);
+  static_assert(smem <= 232448, "shared memory of an SM");
+  static bool done[MAX_DEVICES] = {};
+  static int ctas[MAX_DEVICES] = {};
+  cudaError_t e = once_per_device(done, [&](int dev) {
+    int sms = 0;
+    cudaError_t e1 = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    ctas[dev] = sms < MAX_CTAS ? sms : MAX_CTAS;
+    if (e1 == cudaSuccess) e1 = cudaFuncSetAttribute(chunk_attn_kernel<DH, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    // the warps' shares of the registers must fit into what the block is launched with, or they wait for them for ever
+    cudaFuncAttributes fa{};
+    if (e1 == cudaSuccess) e1 = cudaFuncGetAttributes(&fa, chunk_attn_kernel<DH, F16>);
+    if (e1 == cudaSuccess && fa.numRegs * 384 < 256 * REGS_SOFTMAX + 128 * REGS_OTHER) e1 = cudaErrorLaunchOutOfResources;
+    return e1;
+  });
+  if (e != cudaSuccess) return e;
+  const int n = ctas[current_device()];
+  e = launch_pdl(chunk_attn_kernel<DH, F16>, dim3(n), dim3(384), smem, stream, tmK, tmV, a);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.c.T * a.rep;            // no item has more rows than this
+  return launch_pdl(chunk_attn_join_kernel<DH, F16>, dim3(n, unsigned((rows < ITEM_ROWS ? rows + 31 : ITEM_ROWS) / 32)), dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
-size_t chunk_attn_workspace_bytes(int, int, int) { return 256; }
+size_t chunk_attn_workspace_bytes(int, int, int dh) {
+  return size_t(2 * MAX_CTAS) * ITEM_ROWS * (size_t(dh) * 4 + 8) + MAX_CTAS * sizeof(int4) + 256;
+}
 
-cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string*) {
-  const unsigned blocks = unsigned(((long long)c.T * c.Hq + 7) / 8);
-  auto kernel = c.dh == 64 ? (c.f16 ? chunk_attn_kernel<64, true> : chunk_attn_kernel<64, false>)
-                           : (c.f16 ? chunk_attn_kernel<128, true> : chunk_attn_kernel<128, false>);
-  return launch_pdl(kernel, dim3(blocks), dim3(256), 0, stream, c);
+cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string* err) {
+  Args a{};
+  a.c = c;
+  a.rep = c.Hq / c.Hkv;
+  a.scale_log2 = c.scale * 1.4426950408889634f;
+  a.box_rows = 0;
+  if (c.page_size % 8 == 0)
+    for (a.box_rows = 8; a.box_rows < KT && c.page_size % (2 * a.box_rows) == 0;) a.box_rows *= 2;
+  a.ws_o = reinterpret_cast<float*>(c.ws);
+  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + size_t(2 * MAX_CTAS) * ITEM_ROWS * c.dh);
+  a.ws_start = reinterpret_cast<int4*>(a.ws_ml + size_t(2 * MAX_CTAS) * ITEM_ROWS);
+  a.ws_count = reinterpret_cast<int*>(a.ws_start + MAX_CTAS);
+  CUtensorMap tmK{}, tmV{};
+  if (a.box_rows && (!pool_tmap(&tmK, c.k_pool, c, a.box_rows, err) || !pool_tmap(&tmV, c.v_pool, c, a.box_rows, err))) return cudaErrorInvalidValue;
+  if (c.dh == 64) return c.f16 ? launch_for<64, true>(a, stream, tmK, tmV) : launch_for<64, false>(a, stream, tmK, tmV);
+  return c.f16 ? launch_for<128, true>(a, stream, tmK, tmV) : launch_for<128, false>(a, stream, tmK, tmV);
 }
 
 }  // namespace hspec
