@@ -393,59 +393,65 @@ def hspec_op_swiglu(gu, h):
 
 # ----------------------------------------------------------------------------- the target's side of an iteration
 
-def _arg(name, t, dtypes, shape, inner=None):
-    """Address of an argument: a tensor on the current device, of one of these types and of this shape (None: any size there), contiguous, or
-    with inner given, contiguous from that dimension on and of any row pitch before."""
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+def _arg(name, t, dtypes, shape, dev, rows=False):
+    """Address of an argument: a tensor of one of these types and of this shape on device dev (the current one), contiguous, or with `rows` any
+    pitch between the rows (its first dimension) but none inside them."""
+    if t.dtype in dtypes and t.get_device() == dev and t.shape == shape and (t.is_contiguous() or (rows and _whole_rows(t))):
+        return t.data_ptr()
+    if t.get_device() != dev:
         raise HSpecError(f"{name}: expected a tensor on the current CUDA device")
     if t.dtype not in dtypes:
         raise HSpecError(f"{name}: expected {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if len(shape) != t.dim() or any(want is not None and want != got for want, got in zip(shape, t.shape)):
+    if t.shape != shape:
         raise HSpecError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if inner is None:
-        if not t.is_contiguous():
-            raise HSpecError(f"{name}: expected a contiguous tensor")
-    else:
-        pitch = 1
-        for d in range(t.dim() - 1, inner - 1, -1):
-            if t.shape[d] > 1 and t.stride(d) != pitch:
-                raise HSpecError(f"{name}: expected rows without gaps")
-            pitch *= t.shape[d]
-        if t.shape[0] > 1 and t.stride(0) < pitch:
-            raise HSpecError(f"{name}: rows overlap")
-    return t.data_ptr()
+    raise HSpecError(f"{name}: expected rows without gaps that do not overlap" if rows else f"{name}: expected a contiguous tensor")
 
 
-def _scratch(t):
-    return _arg("workspace", t, (t.dtype,), t.shape)
+def _whole_rows(t):
+    pitch = 1
+    for d in range(t.dim() - 1, 0, -1):
+        if t.shape[d] > 1 and t.stride(d) != pitch:
+            return False
+        pitch *= t.shape[d]
+    return t.shape[0] <= 1 or t.stride(0) >= pitch
 
 
-def _row_pitch(t):
+def _row_pitch(t, width):
     """Elements from one row to the next; a single row has none of its own."""
-    return t.stride(0) if t.shape[0] > 1 else t[0].numel() if t.shape[0] else t.shape[1:].numel()
+    return t.stride(0) if t.shape[0] > 1 else width
 
 
-_HALF, _LOGITS, _I32, _F32 = (torch.bfloat16, torch.float16), (torch.float32, torch.bfloat16, torch.float16), (torch.int32,), (torch.float32,)
+def _device():
+    """The current device's index; -2 where there is none, which no tensor is on."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+
+
+_HALF, _LOGITS = (torch.bfloat16, torch.float16), (torch.float32, torch.bfloat16, torch.float16)
+_I32, _F32, _U8 = (torch.int32,), (torch.float32,), (torch.uint8,)
 
 
 def hspec_op_chunk_rope_write(qkv, pos, pair_axis, cu_q, kv_lens, page_table, q, k_pool, v_pool, theta, q_norm_w=None, k_norm_w=None, eps=1e-6):
     """Norm, rotary positions and cache write of a ragged chunk: qkv [T, (Hq + 2 Hkv) dh] -> q [T, Hq, dh] and the paged pools, in place.
     pos: int32 [axes, T], or None for the position in the cache; pair_axis: the axis of every rotated pair (bytes, or any sequence of small
     numbers; as many as there are pairs), or None for all pairs of the head on the first axis."""
+    dev, half = _device(), (q.dtype,)
     T, Hq, dh = q.shape
-    pages, page, Hkv, _ = k_pool.shape
-    B = kv_lens.shape[0]
-    if pair_axis is not None and not isinstance(pair_axis, bytes):
+    pool = k_pool.shape
+    pages, page, Hkv, _ = pool
+    B, width, entries = kv_lens.shape[0], (Hq + 2 * Hkv) * dh, page_table.shape[1]
+    axes = 1 if pos is None else pos.shape[0]
+    if pool[3] != dh:
+        raise HSpecError(f"k_pool: expected heads of {dh}, got {pool[3]}")
+    if pair_axis is not None and type(pair_axis) is not bytes:
         pair_axis = bytes(pair_axis)
-    pairs = dh // 2 if pair_axis is None else len(pair_axis)
-    pool = (pages, page, Hkv, dh)
     rc = load_library().hspec_op_chunk_rope_write(
-        _arg("qkv", qkv, _LOGITS, (T, (Hq + 2 * Hkv) * dh), inner=1), _DT[qkv.dtype], _row_pitch(qkv),
-        None if pos is None else _arg("pos", pos, _I32, (None, T)), 1 if pos is None else pos.shape[0], pair_axis, pairs,
-        None if q_norm_w is None else _arg("q_norm_w", q_norm_w, _F32, (dh,)), None if k_norm_w is None else _arg("k_norm_w", k_norm_w, _F32, (dh,)),
-        float(eps), float(theta), _arg("cu_q", cu_q, _I32, (B + 1,)), _arg("kv_lens", kv_lens, _I32, (B,)), B,
-        _arg("page_table", page_table, _I32, (B, None)), page_table.shape[1], _arg("q", q, _HALF, (T, Hq, dh)),
-        _arg("k_pool", k_pool, (q.dtype,), pool), _arg("v_pool", v_pool, (q.dtype,), pool), _DT[q.dtype], pages, T, Hq, Hkv, dh, page, _stream())
+        _arg("qkv", qkv, _LOGITS, (T, width), dev, True), _DT[qkv.dtype], _row_pitch(qkv, width),
+        None if pos is None else _arg("pos", pos, _I32, (axes, T), dev), axes, pair_axis, dh // 2 if pair_axis is None else len(pair_axis),
+        None if q_norm_w is None else _arg("q_norm_w", q_norm_w, _F32, (dh,), dev),
+        None if k_norm_w is None else _arg("k_norm_w", k_norm_w, _F32, (dh,), dev), eps, theta, _arg("cu_q", cu_q, _I32, (B + 1,), dev),
+        _arg("kv_lens", kv_lens, _I32, (B,), dev), B, _arg("page_table", page_table, _I32, (B, entries), dev), entries,
+        _arg("q", q, _HALF, (T, Hq, dh), dev), _arg("k_pool", k_pool, half, pool, dev), _arg("v_pool", v_pool, half, pool, dev), _DT[q.dtype],
+        pages, T, Hq, Hkv, dh, page, _stream())
     if rc:
         _check(rc, None, "hspec_op_chunk_rope_write")
 
@@ -456,15 +462,19 @@ def hspec_chunk_attention_workspace_bytes(Hq, Hkv, dh):
 
 def hspec_op_chunk_attention(q, k_pool, v_pool, page_table, cu_q, kv_lens, o, workspace, window=0, scale=0.0):
     """Attention of a ragged chunk q [T, Hq, dh] over the paged cache that holds its own keys and values already -> o [T, Hq, dh]."""
+    dev, half = _device(), (q.dtype,)
     T, Hq, dh = q.shape
-    pages, page, Hkv, _ = k_pool.shape
-    B = kv_lens.shape[0]
-    pool = (pages, page, Hkv, dh)
+    pool = k_pool.shape
+    pages, page, Hkv, _ = pool
+    B, entries, width = kv_lens.shape[0], page_table.shape[1], Hq * dh
+    if pool[3] != dh:
+        raise HSpecError(f"k_pool: expected heads of {dh}, got {pool[3]}")
     rc = load_library().hspec_op_chunk_attention(
-        _arg("q", q, _HALF, (T, Hq, dh), inner=1), _row_pitch(q), _arg("k_pool", k_pool, (q.dtype,), pool), _arg("v_pool", v_pool, (q.dtype,), pool),
-        pages, _arg("page_table", page_table, _I32, (B, None)), page_table.shape[1], _arg("cu_q", cu_q, _I32, (B + 1,)),
-        _arg("kv_lens", kv_lens, _I32, (B,)), B, _arg("o", o, (q.dtype,), (T, Hq, dh), inner=1), _row_pitch(o), _DT[q.dtype], T, Hq, Hkv, dh,
-        page, int(window), float(scale), _scratch(workspace), workspace.nbytes, _stream())
+        _arg("q", q, _HALF, (T, Hq, dh), dev, True), _row_pitch(q, width), _arg("k_pool", k_pool, half, pool, dev),
+        _arg("v_pool", v_pool, half, pool, dev), pages, _arg("page_table", page_table, _I32, (B, entries), dev), entries,
+        _arg("cu_q", cu_q, _I32, (B + 1,), dev), _arg("kv_lens", kv_lens, _I32, (B,), dev), B, _arg("o", o, half, (T, Hq, dh), dev, True),
+        _row_pitch(o, width), _DT[q.dtype], T, Hq, Hkv, dh, page, window, scale, _arg("workspace", workspace, _U8, workspace.shape, dev),
+        workspace.shape[0], _stream())
     if rc:
         _check(rc, None, "hspec_op_chunk_attention")
 
@@ -476,16 +486,18 @@ def hspec_verify_workspace_bytes(B, k):
 def hspec_op_verify(target_logits, draft_logits, draft_ids, alpha, u, n_accept, tokens, workspace, cu_q=None, vocab_map=None, temperature=None):
     """Drafts [B, k] against the target's logits [T, V] -> how many stand [B], and the tokens of the iteration [B, k + 1] (-1 behind the last).
     draft_logits [B, k, V_draft], or None for a drafter that takes the arg-max."""
+    dev = _device()
     B, k = draft_ids.shape
     T, V = target_logits.shape
     Vd = V if draft_logits is None else draft_logits.shape[2]
     rc = load_library().hspec_op_verify(
-        _arg("target_logits", target_logits, _LOGITS, (T, V), inner=1), _DT[target_logits.dtype], _row_pitch(target_logits), T,
-        None if draft_logits is None else _arg("draft_logits", draft_logits, _LOGITS, (B, k, None)),
-        0 if draft_logits is None else _DT[draft_logits.dtype], Vd, _arg("draft_ids", draft_ids, _I32, (B, k)),
-        None if cu_q is None else _arg("cu_q", cu_q, _I32, (B + 1,)), None if vocab_map is None else _arg("vocab_map", vocab_map, _I32, (Vd,)),
-        None if temperature is None else _arg("temperature", temperature, _F32, (B,)), _arg("alpha", alpha, _F32, (B, k)), _arg("u", u, _F32, (B,)),
-        _arg("n_accept", n_accept, _I32, (B,)), _arg("tokens", tokens, _I32, (B, k + 1)), B, k, V, Vd, _scratch(workspace), workspace.nbytes, _stream())
+        _arg("target_logits", target_logits, _LOGITS, (T, V), dev, True), _DT[target_logits.dtype], _row_pitch(target_logits, V), T,
+        None if draft_logits is None else _arg("draft_logits", draft_logits, _LOGITS, (B, k, Vd), dev),
+        0 if draft_logits is None else _DT[draft_logits.dtype], Vd, _arg("draft_ids", draft_ids, _I32, (B, k), dev),
+        None if cu_q is None else _arg("cu_q", cu_q, _I32, (B + 1,), dev), None if vocab_map is None else _arg("vocab_map", vocab_map, _I32, (Vd,), dev),
+        None if temperature is None else _arg("temperature", temperature, _F32, (B,), dev), _arg("alpha", alpha, _F32, (B, k), dev),
+        _arg("u", u, _F32, (B,), dev), _arg("n_accept", n_accept, _I32, (B,), dev), _arg("tokens", tokens, _I32, (B, k + 1), dev), B, k, V, Vd,
+        _arg("workspace", workspace, _U8, workspace.shape, dev), workspace.shape[0], _stream())
     if rc:
         _check(rc, None, "hspec_op_verify")
 

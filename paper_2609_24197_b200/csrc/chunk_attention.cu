@@ -4,8 +4,9 @@
 //
 // Rows of a request that share a KV head are packed: row r of the head is token r / rep, query head r % rep.  A work item is up to 256 rows
 // of one (request, KV head) and all the 128-key tiles that any of them sees; tiles lie at multiples of 128 keys.  The items' tiles, request by
-// request, are one long line that is cut into equal parts, one per CTA: however ragged the batch, every SM gets the same number of tiles, and
-// an item that a cut goes through leaves partial results (at most two per CTA) which a second kernel joins.
+// request, are one long line that is cut into equal parts: however ragged the batch, every SM gets the same number of tiles, and an item that a
+// cut goes through leaves partial results (at most two per CTA) which a second kernel joins.  A part is worked on by as many CTAs as a group
+// has KV heads, one for each: they read neighbouring bytes of the same pages at the same time.
 //
 //   warps 0..3, 4..7   softmax of the two halves, a thread per row: scores from tensor memory, one pass with a reference maximum that moves only
 //                      when the row's outgrows it by 2^8, weights back into tensor memory over the scores they came from.  With more than 128 rows
@@ -49,7 +50,8 @@ struct __align__(16) Bars {
   uint64_t x_write, x_read, drain;
   uint32_t tmem_base, abort_flag;
   uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 5 fit into the ring) met a value that is not finite in a tile that not every row sees in full
-  int4 start;                        // where this CTA's part begins: request, KV head, row tile, tile within the item
+  int4 start;                        // where this CTA's part begins: request, group of KV heads, row tile, tile within the item
+  ChunkRequest req[2];               // that request and the one behind it
   long long left;                    // and how many tiles it has
   float2 xml[2][128];                // (reference maximum, row sum) of the halves' rows, for the halves that share their rows
 };
@@ -58,10 +60,11 @@ constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + sl
 struct Args {
   ChunkAttnCall c;
   int rep, box_rows;                 // rows of a TMA box; 0: pages are copied by 16-byte loads
+  int group;                         // KV heads that are worked on side by side
   float scale_log2;
   float* ws_o;                       // [slot][DH / 4][256 rows][4]
   float2* ws_ml;                     // [slot][256 rows]
-  int4* ws_start;                    // [CTA]; how many CTAs have work lies in ws_count
+  int4* ws_start;                    // [CTA]; how many CTAs (per head of a group) have work lies in ws_count
   int* ws_count;
 };
 
@@ -89,7 +92,7 @@ __device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int 
 }
 
 struct Walk {                        // this CTA's part of the line, item by item
-  int b, kvh, rt, off;
+  int b, g, kvh, rt, off;
   long long left;
   ChunkRequest q, next;
 };
@@ -97,12 +100,13 @@ __device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int
   if (b >= c.B) return ChunkRequest{0, 0, 0};
   return chunk_request(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len);
 }
-__device__ __forceinline__ Walk walk_begin(const ChunkAttnCall& c, const Bars* bars) {
+__device__ __forceinline__ Walk walk_begin(const Args& a, const Bars* bars) {
   Walk w;
-  w.b = bars->start.x; w.kvh = bars->start.y; w.rt = bars->start.z; w.off = bars->start.w;
+  w.b = bars->start.x; w.g = bars->start.y; w.rt = bars->start.z; w.off = bars->start.w;
+  w.kvh = w.g * a.group + blockIdx.x % a.group;
   w.left = bars->left;
-  w.q = load_request(c, w.b);
-  w.next = load_request(c, w.b + 1);
+  w.q = bars->req[0];
+  w.next = bars->req[1];
   return w;
 }
 struct Segment {
@@ -138,8 +142,10 @@ __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a
   if (w.left <= 0) return false;
   if (++w.rt < row_tiles(w.q.n * a.rep)) return true;
   w.rt = 0;
-  if (++w.kvh < a.c.Hkv) return true;
-  w.kvh = 0;
+  w.kvh += a.group;
+  if (w.kvh < a.c.Hkv) { ++w.g; return true; }
+  w.kvh = blockIdx.x % a.group;
+  w.g = 0;
   do {
     ++w.b;
     w.q = w.next;
@@ -189,7 +195,7 @@ __device__ __forceinline__ bool not_finite16(uint32_t x) {
 // for B + 1 numbers.  Returns false for a CTA without work.
 __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
   const ChunkAttnCall& c = a.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group;
   for (int b = warp; b < c.B; b += warps) {
     const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
     const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
@@ -198,7 +204,7 @@ __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* 
     const int tiles = row_tiles(q.n * a.rep);
     for (int rt = lane; rt < tiles; rt += 32) { const ItemGeo g = item_geo(q, a.rep, c.window, rt); n += g.t1 - g.t0; }
     for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(0xffffffffu, n, off);
-    if (lane == 0) sums[b + 1] = n * c.Hkv;
+    if (lane == 0) sums[b + 1] = n * groups;
   }
   if (threadIdx.x == 0) sums[0] = 0;
   __syncthreads();
@@ -211,22 +217,22 @@ __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* 
       before += __shfl_sync(0xffffffffu, n, 31);
     }
     const long long total = before;
-    const int parts = int(min((long long)gridDim.x, total)), me = blockIdx.x;
-    if (me == 0 && lane == 0) *a.ws_count = parts;
+    const int parts = int(min((long long)(gridDim.x / a.group), total)), me = blockIdx.x / a.group;
+    if (blockIdx.x == 0 && lane == 0) *a.ws_count = parts;
     __syncwarp();
     if (me < parts) {
       const long long u0 = total * me / parts, u1 = total * (me + 1) / parts;
       int lo = 0, hi = c.B;                                   // the request with sums[lo] <= u0 < sums[lo + 1]
       while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (sums[mid] <= u0) lo = mid; else hi = mid; }
       const ChunkRequest q = load_request(c, lo);
-      const long long per_head = (sums[lo + 1] - sums[lo]) / c.Hkv;
-      const int kvh = int((u0 - sums[lo]) / per_head);
-      long long rest = (u0 - sums[lo]) - kvh * per_head;
+      const long long per_group = (sums[lo + 1] - sums[lo]) / groups;
+      const int g = int((u0 - sums[lo]) / per_group);
+      long long rest = (u0 - sums[lo]) - g * per_group;
       const int tiles = row_tiles(q.n * a.rep);
       int rt = 0;
       for (int base = 0; base < tiles; base += 32) {
         int n = 0;
-        if (base + lane < tiles) { const ItemGeo g = item_geo(q, a.rep, c.window, base + lane); n = g.t1 - g.t0; }
+        if (base + lane < tiles) { const ItemGeo i = item_geo(q, a.rep, c.window, base + lane); n = i.t1 - i.t0; }
         long long upto = n;
         for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
         const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
@@ -239,9 +245,11 @@ __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* 
         rest -= __shfl_sync(0xffffffffu, upto, 31);
       }
       if (lane == 0) {
-        bars->start = make_int4(lo, kvh, rt, int(rest));
+        bars->start = make_int4(lo, g, rt, int(rest));
         bars->left = u1 - u0;
-        a.ws_start[me] = bars->start;
+        bars->req[0] = q;
+        bars->req[1] = load_request(c, lo + 1);
+        a.ws_start[blockIdx.x] = bars->start;
       }
     } else if (lane == 0) {
       bars->left = 0;
@@ -258,7 +266,7 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, c
   constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
   const ChunkAttnCall& c = a.c;
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  Walk w = walk_begin(c, bars);
+  Walk w = walk_begin(a, bars);
   uint32_t at = 0;                                            // tiles issued
   uint32_t raw_phase = 0, is_raw = 0;                         // a bit per slot: phase of `raw`, and whether the slot's last tile went there
   bool ok = true;
@@ -357,7 +365,7 @@ template <int DH, bool F16>
 __device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars* bars, int tid) {
   constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  Walk w = walk_begin(a.c, bars);
+  Walk w = walk_begin(a, bars);
   uint32_t base = 0, seg = 0, phase = 0;                      // phase of `raw`, a bit per slot
   do {
     const Segment s = segment_of(w, a);
@@ -406,7 +414,7 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
   constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE, HALF = Shape<DH>::HALF;
   const uint32_t id_s = idesc(F16, KT, false), id_o = idesc(F16, DH, true);
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  Walk w = walk_begin(a.c, bars);
+  Walk w = walk_begin(a, bars);
   uint32_t base = 0;
   uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0};                  // segments and tiles of each half so far
   bool ok = true;
@@ -512,7 +520,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&bars->q_ready[h]));
   };
-  Walk w = walk_begin(c, bars);
+  Walk w = walk_begin(a, bars);
   Segment s = segment_of(w, a);
   uint32_t tiles[2] = {0, 0}, seg = 0, shared_segs = 0;       // tiles of both halves so far, segments, segments whose rows the halves share
   if (s.nt[h] > 0) { q_issue(w, s); q_finish(); }
@@ -706,13 +714,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   uint8_t* ring = smem + 2 * TILE;
   Bars* bars = reinterpret_cast<Bars*>(ring + NS * TILE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  pdl_wait();
-  pdl_trigger();
   if (smem_u32(smem) & 1023) {                                // the swizzled tiles need a 1 KiB-aligned base
+    pdl_wait();
     if (tid == 0) atomicExch(a.c.status, STATUS_BAD_SMEM_BASE);
     return;
   }
-  if (!make_plan(a, bars, reinterpret_cast<long long*>(ring))) return;
   if (tid == 0) {
     if (a.box_rows) { tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); }
     for (int i = 0; i < NS; ++i) {
@@ -738,12 +744,17 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tmem_relinquish();
   }
+  pdl_wait();
+  pdl_trigger();
+  const bool work = make_plan(a, bars, reinterpret_cast<long long*>(ring));
   fence_proxy_async();                                        // (the plan's sums lay where the copies now go)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;      // scores (and the weights over them) of the halves in columns 0 and 128, accumulators in 256 and 384
-  if (warp < 8) {
+  if (!work) {
+    // nothing to do here (uniform for the CTA)
+  } else if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
     softmax_half<DH, F16>(a, sQ, bars, tmem, warp >> 2, tid);
   } else {
@@ -765,42 +776,63 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 }
 
 // ------------------------------------------------------------------ joining items that a cut went through
-// One block per (CTA, 32 rows).  The CTA whose part an item begins in speaks for it: its partial result and those of the CTAs behind, in order.
-// Lane = row, warp = 16 (or 8) columns, so that the loads follow the partials' layout.
+// One block per (CTA, 32 rows).  The CTA whose part an item begins in speaks for it: its partial result and those of the parts behind, in order.
+// Lane = row, warp = 16 (or 8) columns, so that the loads follow the partials' layout; the rows' weights come first, through shared memory, and
+// four partials are in flight per thread.
 template <int DH, bool F16>
 __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_constant__ Args a) {
   pdl_wait();
   pdl_trigger();
   constexpr int COLS = DH / 8, ROW = DH * 2 + 16;
   __shared__ __align__(16) uint8_t tile[32 * ROW];
+  __shared__ float2 ml[MAX_CTAS][32];
+  __shared__ int s_last;
   const ChunkAttnCall& c = a.c;
-  const int me = blockIdx.x, count = *a.ws_count;
-  if (me + 1 >= count) return;
-  const int4 x = a.ws_start[me + 1], mine = a.ws_start[me];
+  const int me = blockIdx.x, count = *a.ws_count * a.group, next = me + a.group;
+  if (next >= count) return;
+  const int4 x = a.ws_start[next], mine = a.ws_start[me];
   auto same = [&](const int4& y) { return y.x == x.x && y.y == x.y && y.z == x.z; };
   if (x.w == 0 || (same(mine) && mine.w > 0)) return;         // no cut through an item here, or an earlier CTA speaks for it
   const int first = 2 * me + (same(mine) ? 0 : 1);
-  int last = me + 1;
-  while (last + 1 < count && same(a.ws_start[last + 1])) ++last;                    // (its place in the item is then behind the item's begin)
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (w == 0) {
+    // (a part that begins further on in the same item has its place behind the item's begin)
+    int n = 1;
+    for (int base = next;; base += 32 * a.group) {
+      const int at = base + lane * a.group;
+      const unsigned m = __ballot_sync(0xffffffffu, at < count && same(a.ws_start[at < count ? at : me]));
+      n += m == 0xffffffffu ? 32 : __ffs(~m) - 1;
+      if (m != 0xffffffffu) break;
+    }
+    if (lane == 0) s_last = n;
+  }
+  __syncthreads();
+  const int n = s_last;
   const ChunkRequest q = load_request(c, x.x);
   const ItemGeo g = item_geo(q, a.rep, c.window, x.z);
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, r = blockIdx.y * 32 + lane, rows = g.r1 - g.r0;
-  if (blockIdx.y * 32 >= rows) return;
+  const int kvh = x.y * a.group + me % a.group;
+  const int r = blockIdx.y * 32 + lane, rows = g.r1 - g.r0;
+  if (int(blockIdx.y) * 32 >= rows) return;
+  auto slot = [&](int i) { return size_t(i == 0 ? first : 2 * (me + i * a.group)); };
+  for (int i = w; i < n; i += 8) ml[i][lane] = r < rows ? a.ws_ml[slot(i) * ITEM_ROWS + r] : make_float2(NEG, 0.f);
+  __syncthreads();
   if (r < rows) {
     float m = NEG;
-    for (int i = me; i <= last; ++i) m = fmaxf(m, a.ws_ml[size_t(i == me ? first : 2 * i) * ITEM_ROWS + r].x);
+    for (int i = 0; i < n; ++i) m = fmaxf(m, ml[i][lane].x);
     float acc[COLS], sum = 0.f;
 #pragma unroll
     for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
-    for (int i = me; i <= last; ++i) {
-      const size_t slot = i == me ? first : 2 * i;
-      const float2 ml = a.ws_ml[slot * ITEM_ROWS + r];
-      if (ml.x == NEG && ml.y == 0.f) continue;               // the row saw nothing there (its half may not even have written)
-      const float f = ex2_ftz(ml.x - m);
-      sum += ml.y * f;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float2 part = ml[i][lane];
+      // a half whose rows saw nothing in that part may not even have written its accumulator
+      const bool none = part.x == NEG && part.y == 0.f;
+      const float f = none ? 0.f : ex2_ftz(part.x - m);
+      sum += part.y * f;
+      const float* src = a.ws_o + slot(i) * DH * ITEM_ROWS + (size_t(w * COLS) / 4 * ITEM_ROWS + r) * 4;
 #pragma unroll
       for (int e = 0; e < COLS; e += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(a.ws_o + slot * DH * ITEM_ROWS + (size_t(w * COLS + e) / 4 * ITEM_ROWS + r) * 4);
+        const float4 v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(src + size_t(e) * ITEM_ROWS);
         acc[e] += v.x * f; acc[e + 1] += v.y * f; acc[e + 2] += v.z * f; acc[e + 3] += v.w * f;
       }
     }
@@ -819,7 +851,7 @@ __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_const
   for (int i = threadIdx.x; i < 32 * LANES; i += 256) {
     const int rl = i / LANES, rr = g.r0 + blockIdx.y * 32 + rl;
     if (rr < g.r1)
-      *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + size_t(q.q0 + rr / a.rep) * c.ldo + size_t(x.y * a.rep + rr % a.rep) * DH + (i % LANES) * 8) =
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + size_t(q.q0 + rr / a.rep) * c.ldo + size_t(kvh * a.rep + rr % a.rep) * DH + (i % LANES) * 8) =
           *reinterpret_cast<const uint4*>(tile + rl * ROW + (i % LANES) * 16);
   }
 }
@@ -881,6 +913,8 @@ cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::
   a.c = c;
   a.rep = c.Hq / c.Hkv;
   a.scale_log2 = c.scale * 1.4426950408889634f;
+  // the largest group of heads that leaves at most four SMs without work
+  for (a.group = c.Hkv < 16 ? c.Hkv : 16; a.group > 1 && (c.Hkv % a.group || MAX_CTAS % a.group > 4); --a.group) {}
   a.box_rows = 0;
   if (c.page_size % 8 == 0)
     for (a.box_rows = 8; a.box_rows < KT && c.page_size % (2 * a.box_rows) == 0;) a.box_rows *= 2;

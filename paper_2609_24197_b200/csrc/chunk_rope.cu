@@ -193,8 +193,16 @@ cudaError_t launch_for(const RopeArgs& a, int blocks, cudaStream_t stream) {
 cudaError_t chunk_rope_launch(const ChunkRopeCall& c, cudaStream_t stream) {
   RopeArgs a{};
   a.c = c;
+  // (64 powers cost the host 3 us: a thread keeps the last base's)
+  thread_local float theta = 0.f;
+  thread_local int pairs = 0;
+  thread_local double rate[64];
+  if (theta != c.theta || pairs != c.rot_pairs) {
+    for (int j = 0; j < c.rot_pairs; ++j) rate[j] = pow(double(c.theta), -double(j) / double(c.rot_pairs));
+    theta = c.theta; pairs = c.rot_pairs;
+  }
   for (int j = 0; j < c.rot_pairs; ++j) {
-    a.rate[j] = pow(double(c.theta), -double(j) / double(c.rot_pairs));
+    a.rate[j] = rate[j];
     a.axis[j] = c.pair_axis ? c.pair_axis[j] : 0;
   }
   const size_t item = c.in_dtype == CHUNK_F32 ? 4 : 2;

@@ -88,7 +88,7 @@ def test_the_binding_refuses_before_the_library(lib):
     q = torch.zeros((3, 4, 64), dtype=torch.bfloat16)
     pool, ints = torch.zeros((5, 16, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
     with pytest.raises(hs.HSpecError, match="current CUDA device"):
-        hs.hspec_op_chunk_attention(q, pool, pool, ints[None], ints, ints[:1], q.clone(), torch.zeros(8))
+        hs.hspec_op_chunk_attention(q, pool, pool, ints[None], ints, ints[:1], q.clone(), torch.zeros(8, dtype=torch.uint8))
     with pytest.raises(hs.HSpecError, match="current CUDA device"):
         hs.hspec_op_verify(torch.zeros((4, 9)), None, torch.zeros((1, 3), dtype=torch.int32), torch.zeros((1, 3)), torch.zeros(1), ints[:1],
-                           torch.zeros((1, 4), dtype=torch.int32), torch.zeros(8))
+                           torch.zeros((1, 4), dtype=torch.int32), torch.zeros(8, dtype=torch.uint8))
