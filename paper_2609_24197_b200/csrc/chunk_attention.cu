@@ -8,15 +8,15 @@
 // cut goes through leaves partial results (at most two per CTA) which a second kernel joins.  A part is worked on by as many CTAs as a group
 // has KV heads, one for each: they read neighbouring bytes of the same pages at the same time.
 //
-//   warps 0..3, 4..7   softmax of the two halves, a thread per row: scores from tensor memory, one pass with a reference maximum that moves only
-//                      when the row's outgrows it by 2^8, weights back into tensor memory over the scores they came from.  With more than 128 rows
-//                      a half is 128 rows and both see every tile; with fewer both have the same rows and take turns at the tiles (two tiles are
-//                      then in the softmax at once), and their accumulators meet at the end.
-//   warp 8             producer: K and V tiles through one ring, by TMA boxes of a page's rows (by 16-byte copies where pages are not whole
-//                      groups of 8 rows)
-//   warp 9             issues S = Q K^T and O += P V (P from tensor memory), one half behind the other: while a half's scores are in the
+//   warps 0..7, 8..15  softmax of the two halves, two threads per row with half of a tile's keys each: scores from tensor memory, one pass with a
+//                      reference maximum that moves only when the row's outgrows it by 2^8, weights back into tensor memory over the scores they
+//                      came from.  With more than 128 rows a half is 128 rows and both see every tile; with fewer both have the same rows and take
+//                      turns at the tiles (two tiles are then in the softmax at once), and their accumulators meet at the end.
+//   warps 16, 18       producers of the K and of the V tiles, a ring each, by TMA boxes of a page's rows (by 16-byte copies where pages are not
+//                      whole groups of 8 rows).  One warp for both could not issue the boxes of 16-token pages fast enough.
+//   warp 17            issues S = Q K^T and O += P V (P from tensor memory), one half behind the other: while a half's scores are in the
 //                      softmax the tensor core works for the other
-//   warps 10, 11       go over the V tiles that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
+//   warp 19            goes over the V tiles that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
 //                      become zero (a zero weight times NaN would not), and so do single values that are not finite.  Those of them that
 //                      some rows see are added to these rows' results at the end, from the cache, on a path that nothing else takes.
 //
@@ -34,26 +34,29 @@ constexpr int MAX_CTAS = 148;
 constexpr int ITEM_ROWS = 256;
 constexpr float NEG = -1.0e30f;
 constexpr float LAZY = 8.0f;         // the reference maximum moves when the row's exceeds it by 2^8
-constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 80;
+constexpr int THREADS = 640, SOFTMAX_THREADS = 512;
+constexpr int REGS_SOFTMAX = 104, REGS_OTHER = 64;
 
 template <int DH> struct Shape {
   static constexpr int HALF = KT * 128;                      // [128 rows x 64 values]: 16 KiB, rows of 128 swizzled bytes
   static constexpr int TILE = KT * DH * 2;                   // Q, K or V tile
-  static constexpr int SLOTS = DH == 128 ? 5 : 10;           // 160 KiB of K and V tiles
+  static constexpr int NK = DH == 128 ? 2 : 4, NV = DH == 128 ? 3 : 6;      // slots of the rings: 160 KiB of K and V tiles
 };
 
 struct __align__(16) Bars {
-  // a slot's tile has arrived (two arrivals), has been read, and for V tiles that not every row sees in full: has arrived and may be gone
-  // over, after which the warps that do so give the two arrivals of `full`
-  uint64_t full[10], empty[10], raw[10];
+  // a slot's tile has arrived, has been read, and for V tiles that not every row sees in full: has arrived and is to be gone over, after which
+  // the warp that does so gives the arrival of `full`
+  uint64_t k_full[4], k_empty[4], v_full[6], v_empty[6], v_raw[6];
   uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], o_free[2];
+  uint64_t pair[8];                  // the two warps that share 32 rows
   uint64_t x_write, x_read, drain;
   uint32_t tmem_base, abort_flag;
-  uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 5 fit into the ring) met a value that is not finite in a tile that not every row sees in full
+  uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 6 fit into the ring) met a value that is not finite in a tile
+                                     // that not every row sees in full
   int4 start;                        // where this CTA's part begins: request, group of KV heads, row tile, tile within the item
   ChunkRequest req[2];               // that request and the one behind it
   long long left;                    // and how many tiles it has
-  float2 xml[2][128];                // (reference maximum, row sum) of the halves' rows, for the halves that share their rows
+  float xch[2][2][128];              // [half][half of the columns][row]: what the threads of a row tell each other
 };
 constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
 
@@ -157,10 +160,6 @@ __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a
 __device__ __forceinline__ bool partial_tile(const ItemGeo& g, int window, int t) {
   return t * KT + KT - 1 > g.pos0 || (window > 0 && t * KT < g.pos1 - window + 1);
 }
-// Place of K and V tile t (0 .. T-1 within the segment) in the segment's sequence of loads: K0, K1, V0, K2, V1, .., V(T-1).
-__device__ __forceinline__ int k_place(int t) { return t == 0 ? 0 : 2 * t - 1; }
-__device__ __forceinline__ int v_place(int t, int T) { return t < T - 1 ? 2 * t + 2 : 2 * T - 1; }
-
 // byte offset of (row, 16-byte chunk) in an operand tile: halves of 64 values, 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_off(int row, int chunk) {
   return uint32_t((chunk >> 3) * Shape<128>::HALF + (row >> 3) * 1024 + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4));
@@ -259,39 +258,40 @@ __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* 
   return bars->left > 0;
 }
 
-// ------------------------------------------------------------------ producer
-struct Ring { uint32_t base; };      // tiles loaded in earlier segments
-template <int DH>
-__device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, const CUtensorMap* tmV, uint8_t* ring, Bars* bars, int lane) {
-  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+// ------------------------------------------------------------------ producers (one warp each)
+template <int DH, bool IS_V>
+__device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, uint8_t* ring, Bars* bars, int lane) {
+  constexpr int NS = IS_V ? Shape<DH>::NV : Shape<DH>::NK, TILE = Shape<DH>::TILE;
   const ChunkAttnCall& c = a.c;
+  uint64_t* full = IS_V ? bars->v_full : bars->k_full;
+  uint64_t* empty = IS_V ? bars->v_empty : bars->k_empty;
   volatile uint32_t* abort_flag = &bars->abort_flag;
   Walk w = walk_begin(a, bars);
   uint32_t at = 0;                                            // tiles issued
-  uint32_t raw_phase = 0, is_raw = 0;                         // a bit per slot: phase of `raw`, and whether the slot's last tile went there
+  uint32_t raw_phase = 0, is_raw = 0;                         // a bit per slot: phase of `v_raw`, and whether the slot's last tile went there
   bool ok = true;
   const int boxes = a.box_rows ? KT / a.box_rows : 0;
   do {
     const Segment s = segment_of(w, a);
-    const int T = s.tb - s.ta;
     const int32_t* table = c.page_table + size_t(w.b) * c.page_table_stride;
-    // page of this lane's boxes (up to 16 boxes: one a lane), of the tiles t and t + 1
+    // page of this lane's box (up to 16 of them), fetched a tile ahead
     auto page_of = [&](int t) {
       if (lane >= boxes || t >= s.tb) return -1;
       const int key = t * KT + lane * a.box_rows;
       return key < s.g.key_hi && key + a.box_rows > s.g.key_lo ? table[key / c.page_size] : -1;
     };
-    int page_k = page_of(s.ta), page_next = page_of(s.ta + 1), page_v = page_k;
-    auto load = [&](bool is_v, int t, int page) {
+    int page_next = page_of(s.ta);
+    for (int t = s.ta; t < s.tb; ++t, ++at) {
+      const int page = page_next;
+      page_next = page_of(t + 1);
       const uint32_t slot = at % NS;
-      if (at >= NS && !mbar_wait(smem_u32(&bars->empty[slot]), ((at / NS) - 1) & 1)) ok = false;
-      if (!ok || *abort_flag) { ok = false; return; }
-      const bool raw = is_v && partial_tile(s.g, c.window, t);
-      const uint32_t dst = smem_u32(ring) + slot * TILE, bar = smem_u32(raw ? &bars->raw[slot] : &bars->full[slot]);
+      if (at >= NS && !mbar_wait(smem_u32(&empty[slot]), ((at / NS) - 1) & 1)) ok = false;
+      if (!ok || *abort_flag) { ok = false; break; }
+      const bool raw = IS_V && partial_tile(s.g, c.window, t);
+      const uint32_t dst = smem_u32(ring) + slot * TILE, bar = smem_u32(raw ? &bars->v_raw[slot] : &full[slot]);
       const int key0 = t * KT;
       is_raw = raw ? is_raw | (1u << slot) : is_raw & ~(1u << slot);
       if (raw) raw_phase ^= 1u << slot;
-      if (!raw && lane == 0) mbar_arrive(bar);
       if (a.box_rows) {
         const int key = key0 + lane * a.box_rows;
         const bool on = lane < boxes && key < s.g.key_hi && key + a.box_rows > s.g.key_lo;
@@ -303,13 +303,13 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, c
         __syncwarp();
         if (on) {
           // (a page id outside the pool is outside the tensor map: the copy delivers zeros and touches no memory)
-          if (!is_v && unsigned(page) >= unsigned(c.num_pages)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+          if (!IS_V && unsigned(page) >= unsigned(c.num_pages)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
 #pragma unroll
           for (int h = 0; h < DH / 64; ++h)
-            tma_load_4d(dst + h * Shape<DH>::HALF + lane * a.box_rows * 128, is_v ? tmV : tmK, h * 64, w.kvh, key % c.page_size, page, bar);
+            tma_load_4d(dst + h * Shape<DH>::HALF + lane * a.box_rows * 128, tm, h * 64, w.kvh, key % c.page_size, page, bar);
         }
       } else {
-        const uint16_t* pool = reinterpret_cast<const uint16_t*>(is_v ? c.v_pool : c.k_pool);
+        const uint16_t* pool = reinterpret_cast<const uint16_t*>(IS_V ? c.v_pool : c.k_pool);
         for (int i = lane; i < KT * (DH / 8); i += 32) {
           const int r = i / (DH / 8), chunk = i % (DH / 8), key = key0 + r;
           bool on = key >= s.g.key_lo && key < s.g.key_hi;
@@ -318,7 +318,7 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, c
             const int id = table[key / c.page_size];
             if (unsigned(id) >= unsigned(c.num_pages)) {
               on = false;
-              if (!is_v && chunk == 0 && (key % c.page_size == 0 || key == s.g.key_lo)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+              if (!IS_V && chunk == 0 && (key % c.page_size == 0 || key == s.g.key_lo)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
             } else {
               from = ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + chunk * 8;
             }
@@ -331,20 +331,8 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, c
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
       }
-      ++at;
-    };
-    load(false, s.ta, page_k);
-    for (int t = s.ta; t < s.tb && ok; ++t) {
-      if (t + 1 < s.tb) {
-        page_k = page_next;
-        page_next = page_of(t + 2);
-        load(false, t + 1, page_k);
-      }
-      if (ok) load(true, t, page_v);
-      page_v = page_k;
     }
-    if (!ok) break;
-    if (!walk_on(w, s, a)) break;
+    if (!ok || !walk_on(w, s, a)) break;
   } while (true);
   if (!ok) {
     if (lane == 0) {
@@ -354,33 +342,32 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tmK, c
     // what has been asked for still arrives in shared memory: it must not outlive the CTA
     for (uint32_t p = at > NS ? at - NS : 0; p < at; ++p) {
       const uint32_t slot = p % NS;
-      if ((is_raw >> slot) & 1) mbar_wait(smem_u32(&bars->raw[slot]), ((raw_phase >> slot) & 1) ^ 1);
-      else mbar_wait(smem_u32(&bars->full[slot]), (p / NS) & 1);
+      if ((is_raw >> slot) & 1) mbar_wait(smem_u32(&bars->v_raw[slot]), ((raw_phase >> slot) & 1) ^ 1);
+      else mbar_wait(smem_u32(&full[slot]), (p / NS) & 1);
     }
   }
 }
 
 // ------------------------------------------------------------------ values that not every row sees
 template <int DH, bool F16>
-__device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars* bars, int tid) {
-  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+__device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars* bars, int lane) {
+  constexpr int NS = Shape<DH>::NV, TILE = Shape<DH>::TILE;
   volatile uint32_t* abort_flag = &bars->abort_flag;
   Walk w = walk_begin(a, bars);
-  uint32_t base = 0, seg = 0, phase = 0;                      // phase of `raw`, a bit per slot
+  uint32_t base = 0, seg = 0, phase = 0;                      // phase of `v_raw`, a bit per slot
   do {
     const Segment s = segment_of(w, a);
-    const int T = s.tb - s.ta;
     for (int t = s.ta; t < s.tb; ++t) {
       if (!partial_tile(s.g, a.c.window, t)) continue;
-      const uint32_t at = base + v_place(t - s.ta, T), slot = at % NS;
-      if (!mbar_wait(smem_u32(&bars->raw[slot]), (phase >> slot) & 1) || *abort_flag) {
-        if (tid == 0 && !*abort_flag) { atomicExch(a.c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
+      const uint32_t slot = (base + (t - s.ta)) % NS;
+      if (!mbar_wait(smem_u32(&bars->v_raw[slot]), (phase >> slot) & 1) || *abort_flag) {
+        if (lane == 0 && !*abort_flag) { atomicExch(a.c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
         return;
       }
       phase ^= 1u << slot;
       uint8_t* tile = ring + slot * TILE;
       bool bad = false;
-      for (int i = tid; i < KT * (DH / 8); i += 64) {
+      for (int i = lane; i < KT * (DH / 8); i += 32) {
         const int r = i / (DH / 8), key = t * KT + r;
         uint4* p = reinterpret_cast<uint4*>(tile + tile_off(r, i % (DH / 8)));
         if (key < s.g.key_lo || key >= s.g.key_hi) {
@@ -400,9 +387,9 @@ __device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars*
       if (bad) *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) = seg + 1;
       fence_proxy_async();
       __syncwarp();
-      if ((tid & 31) == 0) mbar_arrive(smem_u32(&bars->full[slot]));
+      if (lane == 0) mbar_arrive(smem_u32(&bars->v_full[slot]));
     }
-    base += 2 * T;
+    base += s.tb - s.ta;
     ++seg;
     if (!walk_on(w, s, a)) break;
   } while (true);
@@ -410,8 +397,8 @@ __device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars*
 
 // ------------------------------------------------------------------ MMA issuer (one thread)
 template <int DH, bool F16>
-__device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* ring, Bars* bars, uint32_t tmem) {
-  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE, HALF = Shape<DH>::HALF;
+__device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* ring_k, uint8_t* ring_v, Bars* bars, uint32_t tmem) {
+  constexpr int NK = Shape<DH>::NK, NV = Shape<DH>::NV, TILE = Shape<DH>::TILE, HALF = Shape<DH>::HALF;
   const uint32_t id_s = idesc(F16, KT, false), id_o = idesc(F16, DH, true);
   volatile uint32_t* abort_flag = &bars->abort_flag;
   Walk w = walk_begin(a, bars);
@@ -420,19 +407,18 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
   bool ok = true;
   do {
     const Segment s = segment_of(w, a);
-    const int T = s.tb - s.ta;
     auto scores = [&](int h, int j) {
       const int t = s.turns ? 2 * j + h : j;
-      const uint32_t at = base + k_place(t), slot = at % NS;
-      if (!mbar_wait_spin(smem_u32(&bars->full[slot]), (at / NS) & 1)) { ok = false; return; }
+      const uint32_t at = base + t, slot = at % NK;
+      if (!mbar_wait_spin(smem_u32(&bars->k_full[slot]), (at / NK) & 1)) { ok = false; return; }
       tc_fence_after();
-      const uint32_t qb = smem_u32(sQ) + h * TILE, kb = smem_u32(ring) + slot * TILE;
+      const uint32_t qb = smem_u32(sQ) + h * TILE, kb = smem_u32(ring_k) + slot * TILE;
 #pragma unroll
       for (int ks = 0; ks < DH / 16; ++ks)
         umma_bf16(tmem + h * 128, umma_desc_kmajor_sw128(qb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2),
                   umma_desc_kmajor_sw128(kb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2), id_s, ks > 0 ? 1u : 0u);
       umma_commit(smem_u32(&bars->s_ready[h]));
-      if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->empty[slot]));
+      if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->k_empty[slot]));
     };
     for (int h = 0; h < 2 && ok; ++h) {
       if (s.nt[h] == 0) continue;
@@ -445,26 +431,26 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
       for (int h = 0; h < 2 && ok; ++h) {
         if (j >= s.nt[h]) continue;
         const int t = s.turns ? 2 * j + h : j;
-        const uint32_t at = base + v_place(t, T), slot = at % NS;
+        const uint32_t at = base + t, slot = at % NV;
         if (!mbar_wait_spin(smem_u32(&bars->p_ready[h]), n_p[h] & 1)) { ok = false; break; }
         ++n_p[h];
-        if (!mbar_wait_spin(smem_u32(&bars->full[slot]), (at / NS) & 1)) { ok = false; break; }
+        if (!mbar_wait_spin(smem_u32(&bars->v_full[slot]), (at / NV) & 1)) { ok = false; break; }
         // the first product of an item overwrites the accumulator: the item before must have been read out
         if (j == 0 && n_q[h] > 0 && !mbar_wait_spin(smem_u32(&bars->o_free[h]), (n_q[h] - 1) & 1)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t vb = smem_u32(ring) + slot * TILE;
+        const uint32_t vb = smem_u32(ring_v) + slot * TILE;
 #pragma unroll
         for (int ks = 0; ks < KT / 16; ++ks)
           umma_bf16_ts(tmem + 256 + h * 128, tmem + h * 128 + ks * 8, desc_v(vb + ks * 2048), id_o, (j > 0 || ks > 0) ? 1u : 0u);
         umma_commit(smem_u32(&bars->pv_done[h]));
-        if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->empty[slot]));
+        if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->v_empty[slot]));
         if (j + 1 < s.nt[h]) scores(h, j + 1);
       }
       if (*abort_flag) ok = false;
     }
     if (!ok) break;
     for (int h = 0; h < 2; ++h) if (s.nt[h] > 0) ++n_q[h];
-    base += 2 * T;
+    base += s.tb - s.ta;
     if (!walk_on(w, s, a)) break;
   } while (true);
   if (!ok) {
@@ -476,7 +462,7 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
 }
 
 // ------------------------------------------------------------------ softmax of one half
-// Adds to 32 columns of a row's accumulator the values that are not finite and that the row sees, from the tiles that were cleaned of them.
+// Adds to 16 columns of a row's accumulator the values that are not finite and that the row sees, from the tiles that were cleaned of them.
 template <int DH, bool F16>
 __device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const Segment& s, int lo, int hi, int col, float* acc) {
   const ChunkAttnCall& c = a.c;
@@ -486,7 +472,7 @@ __device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const 
       const int id = c.page_table[size_t(w.b) * c.page_table_stride + key / c.page_size];
       if (unsigned(id) >= unsigned(c.num_pages)) continue;
       const uint16_t* v = reinterpret_cast<const uint16_t*>(c.v_pool) + ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + col;
-      for (int e = 0; e < 32; ++e) {
+      for (int e = 0; e < 16; ++e) {
         const uint16_t x = v[e];
         if (not_finite16<F16>(x)) acc[e] += F16 ? __half2float(__ushort_as_half(x)) : bf16_bits_to_float(x);
       }
@@ -494,91 +480,133 @@ __device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const 
   }
 }
 
+// Where a role stands.  The softmax warps keep theirs in local memory (functions that are not inlined take its address): 64 scores leave no room
+// for it in registers, and the compiler would put something of the inner loop there instead.
+struct Stand { Walk w; Segment s; };
+__device__ __noinline__ bool next_segment(const Args& a, Stand& at) {
+  if (!walk_on(at.w, at.s, a)) return false;
+  at.s = segment_of(at.w, a);
+  return true;
+}
+// Half of a row of Q: 16-byte asynchronous copies into the operand layout, zeros for rows that are not there.
+template <int DH>
+__device__ __forceinline__ void copy_q(const Args& a, const Walk& w, const Segment& s, uint32_t q_tile, int h, int row, int ch) {
+  const int r = s.g.r0 + (s.turns ? 0 : h * 128) + row;
+  const bool on = r < s.g.r1;
+  const uint16_t* src = reinterpret_cast<const uint16_t*>(a.c.q);
+  if (on) src += size_t(w.q.q0 + r / a.rep) * a.c.ldq + size_t(w.kvh * a.rep + r % a.rep) * DH + ch * (DH / 2);
+#pragma unroll
+  for (int i = 0; i < DH / 16; ++i) cp_async16(q_tile + tile_off(row, ch * (DH / 16) + i), src + (on ? i * 8 : 0), on);
+  cp_async_commit();
+}
+// The same for the segment behind this one; false where it has nothing for this half, or is not there.
+template <int DH>
+__device__ __noinline__ bool copy_next_q(const Args& a, const Stand& at, uint32_t q_tile, int h, int row, int ch) {
+  Walk w = at.w;
+  if (!walk_on(w, at.s, a)) return false;
+  const Segment s = segment_of(w, a);
+  if (s.nt[h] == 0) return false;
+  copy_q<DH>(a, w, s, q_tile, h, row, ch);
+  return true;
+}
+
+// Warp w of the half's eight: rows 32 (w % 4) .. + 31, key columns 64 (w / 4) .. + 63 of every tile.
 template <int DH, bool F16>
 __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* bars, uint32_t tmem, int h, int tid) {
   constexpr int TILE = Shape<DH>::TILE;
   const ChunkAttnCall& c = a.c;
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  const int row = tid & 127, warp = row >> 5, lane = tid & 31;
-  const uint32_t lane_base = uint32_t(warp * 32) << 16;
-  const uint32_t t_s = tmem + h * 128 + lane_base;
-  uint8_t* myQ = sQ + h * TILE;
-  auto first_row = [&](const Segment& s) { return s.g.r0 + (s.turns ? 0 : h * 128); };
-  // this thread's row of Q: 16-byte asynchronous copies into the operand layout, zeros for rows that are not there
-  auto q_issue = [&](const Walk& w, const Segment& s) {
-    const int r = first_row(s) + row;
-    const bool on = r < s.g.r1;
-    const uint16_t* src = reinterpret_cast<const uint16_t*>(c.q);
-    if (on) src += size_t(w.q.q0 + r / a.rep) * c.ldq + size_t(w.kvh * a.rep + r % a.rep) * DH;
-#pragma unroll
-    for (int i = 0; i < DH / 8; ++i) cp_async16(smem_u32(myQ + tile_off(row, i)), src + (on ? i * 8 : 0), on);
-    cp_async_commit();
-  };
+  const int row = tid & 127, ch = (tid >> 7) & 1, quarter = row >> 5, lane = tid & 31;
+  const uint32_t lane_base = uint32_t(quarter * 32) << 16;
+  const uint32_t t_s = tmem + h * 128 + lane_base, t_o = tmem + 256 + h * 128 + lane_base;
+  const uint32_t pair = smem_u32(&bars->pair[h * 4 + quarter]);
+  float* mine = &bars->xch[h][ch][row];
+  const float* theirs = &bars->xch[h][ch ^ 1][row];
+  const uint32_t my_q = smem_u32(sQ) + h * TILE;
   auto q_finish = [&]() {
     cp_async_wait<0>();
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&bars->q_ready[h]));
   };
-  Walk w = walk_begin(a, bars);
-  Segment s = segment_of(w, a);
-  uint32_t tiles[2] = {0, 0}, seg = 0, shared_segs = 0;       // tiles of both halves so far, segments, segments whose rows the halves share
-  if (s.nt[h] > 0) { q_issue(w, s); q_finish(); }
-  bool ok = true, more = true;
+  uint32_t pair_phase = 0;
+  // both warps of a row have come here, and see what the other has written before
+  auto pair_sync = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(pair);
+    const bool ok = mbar_wait_spin(pair, pair_phase);
+    pair_phase ^= 1;
+    return ok;
+  };
+  Stand at;
+  at.w = walk_begin(a, bars);
+  at.s = segment_of(at.w, a);
+  const Walk& w = at.w;
+  const Segment& s = at.s;
+  uint32_t done0 = 0, done1 = 0, seg = 0, shared_segs = 0;    // tiles of the halves so far, segments, segments whose rows the halves share
+  if ((h == 0 ? s.nt[0] : s.nt[1]) > 0) { copy_q<DH>(a, w, s, my_q, h, row, ch); q_finish(); }
+  bool ok = true, x_pending = false;
   int slot = 2 * blockIdx.x;                                  // where this CTA's partial results go: its first segment's, then its last one's
-  while (more) {
-    Walk wn = w;
-    more = walk_on(wn, s, a);
-    Segment sn = s;
-    if (more) sn = segment_of(wn, a);
-    const bool q_next = more && sn.nt[h] > 0;
-    const int r = first_row(s) + row;                         // row of the head
+  do {
+    const bool turns = s.turns;
+    const int nt = h == 0 ? s.nt[0] : s.nt[1], nt_other = h == 0 ? s.nt[1] : s.nt[0];
+    const int r = s.g.r0 + (turns ? 0 : h * 128) + row;       // row of the head
     const bool row_ok = r < s.g.r1;
     const int hi = row_ok ? w.q.len - w.q.n + r / a.rep : -1;                       // keys lo .. hi are seen
     const int lo = c.window > 0 ? max(0, hi - c.window + 1) : 0;
-    const bool warp_live = first_row(s) + warp * 32 < s.g.r1;
+    const bool live = r - row + quarter * 32 < s.g.r1;        // (the same for both warps of a row)
+    int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys
+    const int key_step = turns ? 2 * KT : KT;
     float m_ref = NEG, l_sum = 0.f;
-    if (s.nt[h] == 0 && q_next) { q_issue(wn, sn); q_finish(); }
-    for (int j = 0; j < s.nt[h]; ++j) {
-      const uint32_t n = tiles[h] + j;
+    if (nt == 0 && copy_next_q<DH>(a, at, my_q, h, row, ch)) q_finish();
+    const uint32_t done = h == 0 ? done0 : done1;
+    for (int j = 0; j < nt; ++j, key0 += key_step) {
+      const uint32_t n = done + j;
       if (!mbar_wait(smem_u32(&bars->s_ready[h]), n & 1)) { ok = false; break; }
       // with the last tile's scores all products that read this Q have finished: the next item's goes in
-      const bool q_now = q_next && j == s.nt[h] - 1;
-      if (q_now) q_issue(wn, sn);
-      if (warp_live) {
+      const bool q_now = j == nt - 1 && copy_next_q<DH>(a, at, my_q, h, row, ch);
+      if (live) {
         tc_fence_after();
-        float x[128];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + i * 32, reinterpret_cast<uint32_t*>(x + i * 32));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + i * 32));
-        const int key0 = (s.ta + (s.turns ? 2 * j + h : j)) * KT;
-        if (__any_sync(0xffffffffu, hi < key0 + KT - 1 || lo > key0)) {
+        float x[64];
+        tmem_ld32(t_s + ch * 64, reinterpret_cast<uint32_t*>(x));
+        tmem_ld32(t_s + ch * 64 + 32, reinterpret_cast<uint32_t*>(x + 32));
+        tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
+        tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + 32));
+        if (__any_sync(0xffffffffu, hi < key0 + 63 || lo > key0)) {
           const int jh = hi - key0, jl = lo - key0;
 #pragma unroll
-          for (int i = 0; i < 128; ++i) x[i] = (i <= jh && i >= jl) ? x[i] : -INFINITY;
+          for (int i = 0; i < 64; ++i) x[i] = (i <= jh && i >= jl) ? x[i] : -INFINITY;
         }
         float m4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-        for (int i = 4; i < 128; i += 4) {
+        for (int i = 4; i < 64; i += 4) {
           m4[0] = fmaxf(m4[0], x[i]); m4[1] = fmaxf(m4[1], x[i + 1]); m4[2] = fmaxf(m4[2], x[i + 2]); m4[3] = fmaxf(m4[3], x[i + 3]);
         }
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale_log2;
+        const float mx_own = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        if (j == 0 && x_pending) {
+          if (!mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
+          x_pending = false;
+        }
+        // the threads of a row tell each other their maxima.  (What was written here a tile ago has been read: the scores of this tile were issued
+        // behind the weights of all eight warps.)  Past the exchange both have their scores in registers, and the weights may go over them.
+        *mine = mx_own;
+        if (!pair_sync()) { ok = false; break; }
+        const float mx = fmaxf(mx_own, *theirs) * a.scale_log2;
         const bool grow = mx > m_ref + LAZY;
         float factor = 1.f;
         if (grow) { factor = ex2_ftz(m_ref - mx); m_ref = mx; }
         if (j > 0 && __any_sync(0xffffffffu, grow)) {
           if (!mbar_wait(smem_u32(&bars->pv_done[h]), (n - 1) & 1)) { ok = false; break; }
           tc_fence_after();
-          if (lane == 0) atomicAdd(c.status + STATUS_WORD_RESCALES, 1u);
+          if (lane == 0 && ch == 0) atomicAdd(c.status + STATUS_WORD_RESCALES, 1u);
 #pragma unroll 1
-          for (int i = 0; i < DH / 16; ++i) {
+          for (int col = ch * (DH / 2); col < (ch + 1) * (DH / 2); col += 16) {
             uint32_t o[16];
-            tmem_ld16(tmem + 256 + h * 128 + lane_base + i * 16, o);
+            tmem_ld16(t_o + col, o);
             tmem_wait_ld16(o);
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-            tmem_st16(tmem + 256 + h * 128 + lane_base + i * 16, o);
+            tmem_st16(t_o + col, o);
           }
           tmem_st_wait();
         }
@@ -586,17 +614,17 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
         const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_m2 = pack_f32x2(-m_ref, -m_ref);
         uint64_t ls[2] = {0ull, 0ull};
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t p[32];
+        for (int part = 0; part < 2; ++part) {
+          uint32_t p[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
             float x0, x1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(x[half * 64 + 2 * e], x[half * 64 + 2 * e + 1]), scale2, neg_m2), x0, x1);
+            unpack_f32x2(fma_f32x2(pack_f32x2(x[part * 32 + 2 * e], x[part * 32 + 2 * e + 1]), scale2, neg_m2), x0, x1);
             const float p0 = ex2_ftz(x0), p1 = ex2_ftz(x1);
             ls[e & 1] = add_f32x2(ls[e & 1], pack_f32x2(p0, p1));
             p[e] = pack16<F16>(p0, p1);
           }
-          tmem_st32(t_s + half * 32, p);
+          tmem_st16(t_s + ch * 32 + part * 16, p);
         }
         float s0, s1, s2, s3;
         unpack_f32x2(ls[0], s0, s1);
@@ -609,71 +637,81 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
       if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[h]));
       if (q_now) q_finish();
     }
-    tiles[0] += s.nt[0]; tiles[1] += s.nt[1];
+    done0 += s.nt[0]; done1 += s.nt[1];
     if (!ok) break;
     // ---- read-out
-    if (s.nt[h] > 0 && (!mbar_wait(smem_u32(&bars->pv_done[h]), (tiles[h] - 1) & 1) || *abort_flag)) { ok = false; break; }
+    if (nt > 0 && (!mbar_wait(smem_u32(&bars->pv_done[h]), ((h == 0 ? done0 : done1) - 1) & 1) || *abort_flag)) { ok = false; break; }
+    if (x_pending) {
+      if (!mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
+      x_pending = false;
+    }
+    if (live) {                                               // the row's sum from its two threads
+      *mine = l_sum;
+      if (!pair_sync()) { ok = false; break; }
+      l_sum = ch == 0 ? l_sum + *theirs : *theirs + l_sum;    // (in one order: the same bits in both)
+      if (!pair_sync()) { ok = false; break; }
+    }
     float weight0 = 1.f, weight1 = 0.f;
     if (s.turns) {
-      // the halves' rows are the same: maxima and sums are exchanged, each half finishes its part of the columns
-      if (shared_segs > 0 && !mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
-      bars->xml[h][row] = make_float2(m_ref, l_sum);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->x_write));
+      // the halves' rows are the same: maxima and sums are exchanged, and each of a row's four threads finishes a quarter of the columns
+      if (ch == 0) {
+        bars->xch[h][0][row] = m_ref;
+        bars->xch[h][1][row] = l_sum;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->x_write));
+      }
       if (!mbar_wait(smem_u32(&bars->x_write), shared_segs & 1)) { ok = false; break; }
-      const float2 o = bars->xml[h ^ 1][row];
+      const float m0 = bars->xch[0][0][row], l0 = bars->xch[0][1][row], m1 = bars->xch[1][0][row], l1 = bars->xch[1][1][row];
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars->x_read));
       ++shared_segs;
-      if (s.nt[h ^ 1] > 0 && !mbar_wait(smem_u32(&bars->pv_done[h ^ 1]), (tiles[h ^ 1] - 1) & 1)) { ok = false; break; }
-      const float m = fmaxf(m_ref, o.x), mine = ex2_ftz(m_ref - m), theirs = ex2_ftz(o.x - m);
-      l_sum = l_sum * mine + o.y * theirs;
-      m_ref = m;
-      weight0 = h == 0 ? mine : theirs; weight1 = h == 0 ? theirs : mine;
+      x_pending = true;
+      if (nt_other > 0 && !mbar_wait(smem_u32(&bars->pv_done[h ^ 1]), ((h == 0 ? done1 : done0) - 1) & 1)) { ok = false; break; }
+      m_ref = fmaxf(m0, m1);
+      weight0 = ex2_ftz(m0 - m_ref); weight1 = ex2_ftz(m1 - m_ref);
+      l_sum = l0 * weight0 + l1 * weight1;
     }
     tc_fence_after();
     const bool fix = *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) == seg + 1;
-    const int col0 = s.turns ? h * (DH / 2) : 0, cols = s.turns ? DH / 2 : DH;
+    const int cols = s.turns ? DH / 4 : DH / 2, col0 = (s.turns ? h * 2 + ch : ch) * cols;
     const float inv = l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum);      // (nothing seen: zero; NaN stays)
-    const bool live = warp_live && (s.turns || s.nt[h] > 0);
-    if (!s.whole && row_ok && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
-    if (live) {
+    if (!s.whole && row_ok && ch == 0 && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
+    if (live && (s.turns || nt > 0)) {
       uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(w.q.q0 + r / a.rep) * c.ldo + size_t(w.kvh * a.rep + r % a.rep) * DH : 0);
       float* part = a.ws_o + size_t(slot) * DH * ITEM_ROWS + size_t(r - s.g.r0) * 4;
 #pragma unroll 1
-      for (int col = col0; col < col0 + cols; col += 32) {
+      for (int col = col0; col < col0 + cols; col += 16) {
         __syncwarp();
-        float v[32];
+        float v[16];
+        uint32_t o[16];
         if (s.turns) {
-          uint32_t o[32];
-          tmem_ld32(tmem + 256 + lane_base + col, o);         // (the first half always has a tile)
-          tmem_wait_ld32(o);
+          tmem_ld16(tmem + 256 + lane_base + col, o);         // (the first half always has a tile)
+          tmem_wait_ld16(o);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]) * weight0;
+          for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(o[e]) * weight0;
           if (s.nt[1] > 0) {
-            tmem_ld32(tmem + 384 + lane_base + col, o);
-            tmem_wait_ld32(o);
+            tmem_ld16(tmem + 384 + lane_base + col, o);
+            tmem_wait_ld16(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = fmaf(__uint_as_float(o[e]), weight1, v[e]);
+            for (int e = 0; e < 16; ++e) v[e] = fmaf(__uint_as_float(o[e]), weight1, v[e]);
           }
         } else {
-          uint32_t o[32];
-          tmem_ld32(tmem + 256 + h * 128 + lane_base + col, o);
-          tmem_wait_ld32(o);
+          tmem_ld16(t_o + col, o);
+          tmem_wait_ld16(o);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(o[e]);
+          for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(o[e]);
         }
         if (fix && row_ok) {
-          float copy[32];
+          float copy[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) copy[e] = v[e];
+          for (int e = 0; e < 16; ++e) copy[e] = v[e];
           add_not_finite<DH, F16>(a, w, s, lo, hi, col, copy);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = copy[e];
+          for (int e = 0; e < 16; ++e) v[e] = copy[e];
         }
         if (s.whole && row_ok) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 16; e += 8) {
             uint32_t p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -683,7 +721,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
         } else if (row_ok) {
           // [column group][row][4]: the lanes of a warp write neighbouring 16 bytes
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
       }
     }
@@ -691,28 +729,28 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     __syncwarp();
     if (lane == 0) {
       if (s.turns) {
-        for (int i = 0; i < 2; ++i) if (s.nt[i] > 0) mbar_arrive(smem_u32(&bars->o_free[i]));
-      } else if (s.nt[h] > 0) {
+        if (s.nt[0] > 0) mbar_arrive(smem_u32(&bars->o_free[0]));
+        if (s.nt[1] > 0) mbar_arrive(smem_u32(&bars->o_free[1]));
+      } else if (nt > 0) {
         mbar_arrive_n(smem_u32(&bars->o_free[h]), 2);
       }
     }
     slot = 2 * blockIdx.x + 1;
     ++seg;
-    w = wn;
-    s = sn;
-  }
+  } while (next_segment(a, at));
   if (!ok) { if (!*abort_flag) atomicExch(c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
   tc_fence_before();
 }
 
 template <int DH, bool F16>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(THREADS, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Args a) {
-  constexpr int NS = Shape<DH>::SLOTS, TILE = Shape<DH>::TILE;
+  constexpr int NK = Shape<DH>::NK, NV = Shape<DH>::NV, TILE = Shape<DH>::TILE;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;
-  uint8_t* ring = smem + 2 * TILE;
-  Bars* bars = reinterpret_cast<Bars*>(ring + NS * TILE);
+  uint8_t* ring_k = smem + 2 * TILE;
+  uint8_t* ring_v = ring_k + NK * TILE;
+  Bars* bars = reinterpret_cast<Bars*>(ring_v + NV * TILE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (smem_u32(smem) & 1023) {                                // the swizzled tiles need a 1 KiB-aligned base
     pdl_wait();
@@ -721,32 +759,37 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
   if (tid == 0) {
     if (a.box_rows) { tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV); }
-    for (int i = 0; i < NS; ++i) {
-      mbar_init(smem_u32(&bars->full[i]), 2);
-      mbar_init(smem_u32(&bars->empty[i]), 1);
-      mbar_init(smem_u32(&bars->raw[i]), 1);
+    for (int i = 0; i < NK; ++i) {
+      mbar_init(smem_u32(&bars->k_full[i]), 1);
+      mbar_init(smem_u32(&bars->k_empty[i]), 1);
+    }
+    for (int i = 0; i < NV; ++i) {
+      mbar_init(smem_u32(&bars->v_full[i]), 1);
+      mbar_init(smem_u32(&bars->v_empty[i]), 1);
+      mbar_init(smem_u32(&bars->v_raw[i]), 1);
     }
     for (int h = 0; h < 2; ++h) {
-      mbar_init(smem_u32(&bars->q_ready[h]), 4);
+      mbar_init(smem_u32(&bars->q_ready[h]), 8);
       mbar_init(smem_u32(&bars->s_ready[h]), 1);
-      mbar_init(smem_u32(&bars->p_ready[h]), 4);
+      mbar_init(smem_u32(&bars->p_ready[h]), 8);
       mbar_init(smem_u32(&bars->pv_done[h]), 1);
-      mbar_init(smem_u32(&bars->o_free[h]), 8);
+      mbar_init(smem_u32(&bars->o_free[h]), 16);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&bars->pair[i]), 2);
     mbar_init(smem_u32(&bars->x_write), 8);
-    mbar_init(smem_u32(&bars->x_read), 8);
+    mbar_init(smem_u32(&bars->x_read), 16);
     mbar_init(smem_u32(&bars->drain), 1);
     bars->abort_flag = 0;
     for (int i = 0; i < 16; ++i) bars->bad[i] = 0;
     fence_mbar_init();
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tmem_relinquish();
   }
   pdl_wait();
   pdl_trigger();
-  const bool work = make_plan(a, bars, reinterpret_cast<long long*>(ring));
+  const bool work = make_plan(a, bars, reinterpret_cast<long long*>(ring_k));
   fence_proxy_async();                                        // (the plan's sums lay where the copies now go)
   tc_fence_before();
   __syncthreads();
@@ -754,22 +797,24 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const uint32_t tmem = bars->tmem_base;      // scores (and the weights over them) of the halves in columns 0 and 128, accumulators in 256 and 384
   if (!work) {
     // nothing to do here (uniform for the CTA)
-  } else if (warp < 8) {
+  } else if (warp < 16) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
-    softmax_half<DH, F16>(a, sQ, bars, tmem, warp >> 2, tid);
+    softmax_half<DH, F16>(a, sQ, bars, tmem, warp >> 3, tid);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
-    if (warp == 8) {
-      produce<DH>(a, &tmK, &tmV, ring, bars, lane);
-    } else if (warp == 9) {
-      if (elect_one()) issue_mmas<DH, F16>(a, sQ, ring, bars, tmem);
+    if (warp == 16) {
+      produce<DH, false>(a, &tmK, ring_k, bars, lane);
+    } else if (warp == 18) {
+      produce<DH, true>(a, &tmV, ring_v, bars, lane);
+    } else if (warp == 17) {
+      if (elect_one()) issue_mmas<DH, F16>(a, sQ, ring_k, ring_v, bars, tmem);
       __syncwarp();
     } else {
-      clean_values<DH, F16>(a, ring, bars, tid - 320);
+      clean_values<DH, F16>(a, ring_v, bars, lane);
     }
   }
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 17) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -879,7 +924,7 @@ bool pool_tmap(CUtensorMap* tm, const void* pool, const ChunkAttnCall& c, int bo
 
 template <int DH, bool F16>
 cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tmK, const CUtensorMap& tmV) {
-  constexpr size_t smem = smem_bytes(Shape<DH>::TILE, Shape<DH>::SLOTS);
+  constexpr size_t smem = smem_bytes(Shape<DH>::TILE, Shape<DH>::NK + Shape<DH>::NV);
   static_assert(smem <= 232448, "shared memory of an SM");
   static bool done[MAX_DEVICES] = {};
   static int ctas[MAX_DEVICES] = {};
@@ -891,12 +936,12 @@ cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tm
     // the warps' shares of the registers must fit into what the block is launched with, or they wait for them for ever
     cudaFuncAttributes fa{};
     if (e1 == cudaSuccess) e1 = cudaFuncGetAttributes(&fa, chunk_attn_kernel<DH, F16>);
-    if (e1 == cudaSuccess && fa.numRegs * 384 < 256 * REGS_SOFTMAX + 128 * REGS_OTHER) e1 = cudaErrorLaunchOutOfResources;
+    if (e1 == cudaSuccess && fa.numRegs * THREADS < SOFTMAX_THREADS * REGS_SOFTMAX + (THREADS - SOFTMAX_THREADS) * REGS_OTHER) e1 = cudaErrorLaunchOutOfResources;
     return e1;
   });
   if (e != cudaSuccess) return e;
   const int n = ctas[current_device()];
-  e = launch_pdl(chunk_attn_kernel<DH, F16>, dim3(n), dim3(384), smem, stream, tmK, tmV, a);
+  e = launch_pdl(chunk_attn_kernel<DH, F16>, dim3(n), dim3(THREADS), smem, stream, tmK, tmV, a);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.c.T * a.rep;            // no item has more rows than this
   return launch_pdl(chunk_attn_join_kernel<DH, F16>, dim3(n, unsigned((rows < ITEM_ROWS ? rows + 31 : ITEM_ROWS) / 32)), dim3(256), 0, stream, a);
