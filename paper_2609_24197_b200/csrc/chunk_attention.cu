@@ -23,7 +23,9 @@
 // Every wait is bounded; a role whose wait runs out sets a status word, and the CTA unwinds.
 #include "chunk.cuh"
 
+#include <cstddef>
 #include <cstdlib>
+#include <type_traits>
 
 namespace hspec {
 
@@ -33,9 +35,12 @@ constexpr int KT = 128;              // keys per tile
 constexpr int MAX_CTAS = 148;
 constexpr int ITEM_ROWS = 256;
 constexpr float NEG = -1.0e30f;
-constexpr float LAZY = 8.0f;         // the reference maximum moves when the row's exceeds it by 2^8
-constexpr int THREADS = 640, SOFTMAX_THREADS = 512;
-constexpr int REGS_SOFTMAX = 104, REGS_OTHER = 64;
+// What an item costs where every CTA has many tiles, in units of 900 clocks: a tile whose halves take turns 2650 (its 64 KB at a CTA's share of
+// the memory's rate), a tile that both halves see 3550, the way from an item's last tile to the next one's first 4500.
+constexpr int COST_TURNS = 3, COST_BOTH = 4, COST_ITEM = 5;
+constexpr float LAZY = 8.0f;         // the reference maximum moves, for the next tile, when the row's exceeds it by 2^8
+constexpr float LIMIT_BF16 = 60.0f, LIMIT_F16 = 15.0f;      // and at once when it exceeds it by more than the weights' type can hold
+constexpr int THREADS = 640;
 
 template <int DH> struct Shape {
   static constexpr int HALF = KT * 128;                      // [128 rows x 64 values]: 16 KiB, rows of 128 swizzled bytes
@@ -47,15 +52,13 @@ struct __align__(16) Bars {
   // a slot's tile has arrived, has been read, and for V tiles that not every row sees in full: has arrived and is to be gone over, after which
   // the warp that does so gives the arrival of `full`
   uint64_t k_full[4], k_empty[4], v_full[6], v_empty[6], v_raw[6];
-  uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], o_free[2];
-  uint64_t pair[8];                  // the two warps that share 32 rows
+  uint64_t q_ready[2], s_ready[2], p_half[2], p_ready[2], pv_done[2], o_free[2];
   uint64_t x_write, x_read, drain;
   uint32_t tmem_base, abort_flag;
   uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 6 fit into the ring) met a value that is not finite in a tile
                                      // that not every row sees in full
-  int4 start;                        // where this CTA's part begins: request, group of KV heads, row tile, tile within the item
-  ChunkRequest req[2];               // that request and the one behind it
-  long long left;                    // and how many tiles it has
+  int4 start, stop;                  // where this CTA's part begins and where the next one's does: request, group of KV heads, row tile, tile of the item
+  ChunkRequest req[2];               // the request that it begins in and the one behind it
   float xch[2][2][128];              // [half][half of the columns][row]: what the threads of a row tell each other
 };
 constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
@@ -96,7 +99,7 @@ __device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int 
 
 struct Walk {                        // this CTA's part of the line, item by item
   int b, g, kvh, rt, off;
-  long long left;
+  int4 stop;
   ChunkRequest q, next;
 };
 __device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int b) {
@@ -107,7 +110,7 @@ __device__ __forceinline__ Walk walk_begin(const Args& a, const Bars* bars) {
   Walk w;
   w.b = bars->start.x; w.g = bars->start.y; w.rt = bars->start.z; w.off = bars->start.w;
   w.kvh = w.g * a.group + blockIdx.x % a.group;
-  w.left = bars->left;
+  w.stop = bars->stop;
   w.q = bars->req[0];
   w.next = bars->req[1];
   return w;
@@ -122,7 +125,7 @@ __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
   Segment s;
   s.g = item_geo(w.q, a.rep, a.c.window, w.rt);
   s.ta = s.g.t0 + w.off;
-  s.tb = int(min((long long)s.g.t1, s.ta + w.left));
+  s.tb = w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z ? s.g.t0 + w.stop.w : s.g.t1;
   s.whole = w.off == 0 && s.tb == s.g.t1;
   s.turns = takes_turns(w.q.n * a.rep);
   const int T = s.tb - s.ta;
@@ -140,21 +143,22 @@ __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
 }
 // On to the next item; false at the end of this CTA's part.
 __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a) {
-  w.left -= s.tb - s.ta;
   w.off = 0;
-  if (w.left <= 0) return false;
-  if (++w.rt < row_tiles(w.q.n * a.rep)) return true;
-  w.rt = 0;
-  w.kvh += a.group;
-  if (w.kvh < a.c.Hkv) { ++w.g; return true; }
-  w.kvh = blockIdx.x % a.group;
-  w.g = 0;
-  do {
-    ++w.b;
-    w.q = w.next;
-    w.next = load_request(a.c, w.b + 1);
-  } while (w.q.n == 0 && w.b < a.c.B);
-  return w.b < a.c.B;
+  if (s.tb < s.g.t1) return false;
+  if (++w.rt == row_tiles(w.q.n * a.rep)) {
+    w.rt = 0;
+    w.kvh += a.group;
+    if (++w.g == a.c.Hkv / a.group) {
+      w.kvh -= w.g * a.group;
+      w.g = 0;
+      do {
+        ++w.b;
+        w.q = w.next;
+        w.next = load_request(a.c, w.b + 1);
+      } while (w.q.n == 0 && w.b < a.c.B);
+    }
+  }
+  return w.b < a.c.B && !(w.stop.w == 0 && w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z);
 }
 // Not every row of the item sees all of the tile's keys.
 __device__ __forceinline__ bool partial_tile(const ItemGeo& g, int window, int t) {
@@ -163,10 +167,6 @@ __device__ __forceinline__ bool partial_tile(const ItemGeo& g, int window, int t
 // byte offset of (row, 16-byte chunk) in an operand tile: halves of 64 values, 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_off(int row, int chunk) {
   return uint32_t((chunk >> 3) * Shape<128>::HALF + (row >> 3) * 1024 + (row & 7) * 128 + (((chunk & 7) ^ (row & 7)) << 4));
-}
-// V tile as MN-major B operand: halves HALF bytes apart, groups of 8 keys 1024
-__device__ __forceinline__ uint64_t desc_v(uint32_t addr) {
-  return uint64_t((addr & 0x3FFFF) >> 4) | (uint64_t(Shape<128>::HALF >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
 }
 __device__ __forceinline__ uint32_t idesc(bool f16, int n, bool b_mn_major) {
   const uint32_t fmt = f16 ? 0u : 1u;
@@ -190,72 +190,97 @@ __device__ __forceinline__ bool not_finite16(uint32_t x) {
 }
 
 // ------------------------------------------------------------------ the plan
-// Cuts the line: tiles of every request (one warp each), their running sum, the place where this CTA's part begins.  `sums` is shared memory
-// for B + 1 numbers.  Returns false for a CTA without work.
+// The line is measured in costs: an item has `item` in front of its first tile and `turns` or `both` for every tile.  A tile belongs to the part in
+// which its beginning lies.  Where the parts would be so short that one might hold no beginning, every tile counts one and nothing else does.
+struct Costs { int item, turns, both; };
+__device__ __forceinline__ int item_cost(const Costs& k, const ChunkRequest& q, const Args& a, int rt, int* tiles = nullptr) {
+  const ItemGeo g = item_geo(q, a.rep, a.c.window, rt);
+  if (tiles) *tiles = g.t1 - g.t0;
+  return k.item + (takes_turns(q.n * a.rep) ? k.turns : k.both) * (g.t1 - g.t0);
+}
+// The first tile that begins at u or behind (one warp): request, group of heads, row tile, tile of the item; request B at the end of the line.
+__device__ __forceinline__ int4 place_of(const Args& a, const Costs& k, const long long* sums, long long u, int lane) {
+  const ChunkAttnCall& c = a.c;
+  const int groups = c.Hkv / a.group;
+  if (u >= sums[c.B]) return make_int4(c.B, 0, 0, 0);
+  int lo = 0, hi = c.B;                                       // the request with sums[lo] <= u < sums[lo + 1]
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (sums[mid] <= u) lo = mid; else hi = mid; }
+  const ChunkRequest q = load_request(c, lo);
+  const long long per_group = (sums[lo + 1] - sums[lo]) / groups;
+  int g = int((u - sums[lo]) / per_group), rt = 0;
+  long long rest = (u - sums[lo]) - g * per_group;
+  const int count = row_tiles(q.n * a.rep);
+  for (int base = 0; base < count; base += 32) {
+    long long upto = base + lane < count ? item_cost(k, q, a, base + lane) : 0;
+    for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
+    const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
+    if (in) {
+      const int l = __ffs(in) - 1;
+      const long long before = __shfl_sync(0xffffffffu, upto, l > 0 ? l - 1 : 0);
+      rt = base + l;
+      rest -= l > 0 ? before : 0;
+      break;
+    }
+    rest -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  int tiles, off = 0;
+  item_cost(k, q, a, rt, &tiles);
+  const int each = takes_turns(q.n * a.rep) ? k.turns : k.both;
+  if (rest > 0) off = max(1, int((rest - k.item + each - 1) / each));
+  if (off < tiles) return make_int4(lo, g, rt, off);
+  if (rt + 1 < count) return make_int4(lo, g, rt + 1, 0);
+  if (g + 1 < groups) return make_int4(lo, g + 1, 0, 0);
+  do ++lo; while (lo < c.B && sums[lo + 1] == sums[lo]);
+  return make_int4(lo, 0, 0, 0);
+}
+// Cuts the line: costs of every request (one warp each), their running sum, the places where this CTA's part begins and ends.  `sums` is shared
+// memory for B + 1 numbers.  Returns false for a CTA without work.
 __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
   const ChunkAttnCall& c = a.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group;
-  for (int b = warp; b < c.B; b += warps) {
-    const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
-    const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
-    if (blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-    long long n = 0;
-    const int tiles = row_tiles(q.n * a.rep);
-    for (int rt = lane; rt < tiles; rt += 32) { const ItemGeo g = item_geo(q, a.rep, c.window, rt); n += g.t1 - g.t0; }
-    for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(0xffffffffu, n, off);
-    if (lane == 0) sums[b + 1] = n * groups;
-  }
-  if (threadIdx.x == 0) sums[0] = 0;
-  __syncthreads();
-  if (warp == 0) {
-    long long before = 0;
-    for (int base = 0; base < c.B; base += 32) {
-      long long n = base + lane < c.B ? sums[base + lane + 1] : 0;
-      for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
-      if (base + lane < c.B) sums[base + lane + 1] = before + n;
-      before += __shfl_sync(0xffffffffu, n, 31);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group, most = gridDim.x / a.group;
+  Costs k{COST_ITEM, COST_TURNS, COST_BOTH};
+  for (int turn = 0;; ++turn) {
+    for (int b = warp; b < c.B; b += warps) {
+      const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
+      const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
+      if (turn == 0 && blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+      long long n = 0;
+      const int count = row_tiles(q.n * a.rep);
+      for (int rt = lane; rt < count; rt += 32) n += item_cost(k, q, a, rt);
+      for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(0xffffffffu, n, off);
+      if (lane == 0) sums[b + 1] = n * groups;
     }
-    const long long total = before;
-    const int parts = int(min((long long)(gridDim.x / a.group), total)), me = blockIdx.x / a.group;
-    if (blockIdx.x == 0 && lane == 0) *a.ws_count = parts;
-    __syncwarp();
-    if (me < parts) {
-      const long long u0 = total * me / parts, u1 = total * (me + 1) / parts;
-      int lo = 0, hi = c.B;                                   // the request with sums[lo] <= u0 < sums[lo + 1]
-      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (sums[mid] <= u0) lo = mid; else hi = mid; }
-      const ChunkRequest q = load_request(c, lo);
-      const long long per_group = (sums[lo + 1] - sums[lo]) / groups;
-      const int g = int((u0 - sums[lo]) / per_group);
-      long long rest = (u0 - sums[lo]) - g * per_group;
-      const int tiles = row_tiles(q.n * a.rep);
-      int rt = 0;
-      for (int base = 0; base < tiles; base += 32) {
-        int n = 0;
-        if (base + lane < tiles) { const ItemGeo i = item_geo(q, a.rep, c.window, base + lane); n = i.t1 - i.t0; }
-        long long upto = n;
-        for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
-        const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
-        if (in) {
-          const int l = __ffs(in) - 1;
-          rt = base + l;
-          rest -= l > 0 ? __shfl_sync(0xffffffffu, upto, l - 1) : 0;
-          break;
-        }
-        rest -= __shfl_sync(0xffffffffu, upto, 31);
+    if (threadIdx.x == 0) sums[0] = 0;
+    __syncthreads();
+    if (warp == 0) {
+      long long before = 0;
+      for (int base = 0; base < c.B; base += 32) {
+        long long n = base + lane < c.B ? sums[base + lane + 1] : 0;
+        for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
+        if (base + lane < c.B) sums[base + lane + 1] = before + n;
+        before += __shfl_sync(0xffffffffu, n, 31);
       }
-      if (lane == 0) {
-        bars->start = make_int4(lo, g, rt, int(rest));
-        bars->left = u1 - u0;
-        bars->req[0] = q;
-        bars->req[1] = load_request(c, lo + 1);
-        a.ws_start[blockIdx.x] = bars->start;
-      }
-    } else if (lane == 0) {
-      bars->left = 0;
     }
+    __syncthreads();
+    if (turn > 0 || sums[c.B] >= (long long)most * (COST_ITEM + COST_BOTH)) break;
+    k = Costs{0, 1, 1};
+    __syncthreads();                                          // (everyone has read the sum)
   }
-  __syncthreads();
-  return bars->left > 0;
+  const long long total = sums[c.B];
+  const int parts = int(min((long long)most, total)), me = blockIdx.x / a.group;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.ws_count = parts;
+  if (me >= parts) return false;
+  if (warp < 2) {
+    const int4 at = place_of(a, k, sums, total * (me + warp) / parts, lane);
+    if (warp == 0 && lane == 0) {
+      bars->start = at;
+      bars->req[0] = load_request(c, at.x);
+      bars->req[1] = load_request(c, at.x + 1);
+      a.ws_start[blockIdx.x] = at;
+    }
+    if (warp == 1 && lane == 0) bars->stop = at;
+  }
+  return true;                                                // (read behind the next barrier)
 }
 
 // ------------------------------------------------------------------ producers (one warp each)
@@ -396,69 +421,132 @@ __device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars*
 }
 
 // ------------------------------------------------------------------ MMA issuer (one thread)
+// Everything this thread does between two products is time in which the tensor core may run dry: descriptors are a constant upper word and a lower
+// word that is added to, places in the rings are counted along and not divided out, tiles are asked for before the weights that they wait for.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);          // groups of 8 rows 1024 bytes apart, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_lo_kmajor(uint32_t addr) { return (addr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mnmajor(uint32_t addr) { return (addr >> 4) | (uint32_t(Shape<128>::HALF >> 4) << 16); }
+template <bool ACC>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t id) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 p, %5, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(id), "r"(DESC_HI), "r"(ACC ? 1u : 0u)
+               : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t id, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tmov.b64 b, {%2, %4};\n\tsetp.ne.b32 p, %5, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(id), "r"(DESC_HI), "r"(acc)
+               : "memory");
+}
+template <int N> struct RingPos {    // a place in a ring of N slots, and the parity of its use
+  uint32_t slot = 0, phase = 0;
+  __device__ __forceinline__ void step(uint32_t n) {          // n <= N
+    slot += n;
+    if (slot >= N) { slot -= N; phase ^= 1u; }
+  }
+};
+
 template <int DH, bool F16>
 __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* ring_k, uint8_t* ring_v, Bars* bars, uint32_t tmem) {
   constexpr int NK = Shape<DH>::NK, NV = Shape<DH>::NV, TILE = Shape<DH>::TILE, HALF = Shape<DH>::HALF;
   const uint32_t id_s = idesc(F16, KT, false), id_o = idesc(F16, DH, true);
+  const uint32_t q_lo = desc_lo_kmajor(smem_u32(sQ)), k_lo = desc_lo_kmajor(smem_u32(ring_k)), v_lo = desc_lo_mnmajor(smem_u32(ring_v));
+  const uint32_t bar0 = smem_u32(bars);
+#define BAR(field, i) (bar0 + uint32_t(offsetof(Bars, field)) + uint32_t(i) * 8u)
   volatile uint32_t* abort_flag = &bars->abort_flag;
   Walk w = walk_begin(a, bars);
-  uint32_t base = 0;
-  uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0};                  // segments and tiles of each half so far
+  RingPos<NK> k_at[2];                                        // next K and V tile of each half
+  RingPos<NV> v_at[2];
+  uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
   bool ok = true;
   do {
     const Segment s = segment_of(w, a);
-    auto scores = [&](int h, int j) {
-      const int t = s.turns ? 2 * j + h : j;
-      const uint32_t at = base + t, slot = at % NK;
-      if (!mbar_wait_spin(smem_u32(&bars->k_full[slot]), (at / NK) & 1)) { ok = false; return; }
-      tc_fence_after();
-      const uint32_t qb = smem_u32(sQ) + h * TILE, kb = smem_u32(ring_k) + slot * TILE;
+    const bool turns = s.turns;
+    const int T = s.tb - s.ta, nt0 = s.nt[0], nt1 = s.nt[1];
+    const uint32_t step = turns ? 2 : 1;
+    if (turns) { k_at[1].step(1); v_at[1].step(1); }
+    auto scores = [&](auto H, bool there, bool last_reader) {
+      constexpr int h = decltype(H)::value;
+      if (!there && !mbar_wait_spin(BAR(k_full, k_at[h].slot), k_at[h].phase)) { ok = false; return; }
+      const uint32_t kb = k_lo + k_at[h].slot * (TILE >> 4), qb = q_lo + h * (TILE >> 4);
 #pragma unroll
-      for (int ks = 0; ks < DH / 16; ++ks)
-        umma_bf16(tmem + h * 128, umma_desc_kmajor_sw128(qb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2),
-                  umma_desc_kmajor_sw128(kb + (ks >> 2) * HALF) + uint64_t((ks & 3) * 2), id_s, ks > 0 ? 1u : 0u);
-      umma_commit(smem_u32(&bars->s_ready[h]));
-      if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->k_empty[slot]));
-    };
-    for (int h = 0; h < 2 && ok; ++h) {
-      if (s.nt[h] == 0) continue;
-      if (!mbar_wait_spin(smem_u32(&bars->q_ready[h]), n_q[h] & 1)) { ok = false; break; }
-      tc_fence_after();
-      scores(h, 0);
-    }
-    const int most = max(s.nt[0], s.nt[1]);
-    for (int j = 0; j < most && ok; ++j) {
-      for (int h = 0; h < 2 && ok; ++h) {
-        if (j >= s.nt[h]) continue;
-        const int t = s.turns ? 2 * j + h : j;
-        const uint32_t at = base + t, slot = at % NV;
-        if (!mbar_wait_spin(smem_u32(&bars->p_ready[h]), n_p[h] & 1)) { ok = false; break; }
-        ++n_p[h];
-        if (!mbar_wait_spin(smem_u32(&bars->v_full[slot]), (at / NV) & 1)) { ok = false; break; }
-        // the first product of an item overwrites the accumulator: the item before must have been read out
-        if (j == 0 && n_q[h] > 0 && !mbar_wait_spin(smem_u32(&bars->o_free[h]), (n_q[h] - 1) & 1)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t vb = smem_u32(ring_v) + slot * TILE;
-#pragma unroll
-        for (int ks = 0; ks < KT / 16; ++ks)
-          umma_bf16_ts(tmem + 256 + h * 128, tmem + h * 128 + ks * 8, desc_v(vb + ks * 2048), id_o, (j > 0 || ks > 0) ? 1u : 0u);
-        umma_commit(smem_u32(&bars->pv_done[h]));
-        if (s.turns || h == (j < s.nt[1] ? 1 : 0)) umma_commit(smem_u32(&bars->v_empty[slot]));
-        if (j + 1 < s.nt[h]) scores(h, j + 1);
+      for (int ks = 0; ks < DH / 16; ++ks) {
+        constexpr uint32_t H4 = HALF >> 4;
+        const uint32_t off = (ks >> 2) * H4 + (ks & 3) * 2;
+        if (ks == 0) mma_ss<false>(tmem + h * 128, qb + off, kb + off, id_s);
+        else mma_ss<true>(tmem + h * 128, qb + off, kb + off, id_s);
       }
-      if (*abort_flag) ok = false;
+      umma_commit(BAR(s_ready, h));
+      if (last_reader) umma_commit(BAR(k_empty, k_at[h].slot));
+      k_at[h].step(step);
+    };
+    auto first = [&](auto H, int nt, bool last_reader) {
+      constexpr int h = decltype(H)::value;
+      if (nt == 0 || !ok) return;
+      if (!mbar_wait_spin(BAR(q_ready, h), q_phase[h])) { ok = false; return; }
+      q_phase[h] ^= 1u;
+      tc_fence_after();
+      scores(H, false, last_reader);
+    };
+    // tile j of one half: the product of its weights, and the scores of the half's next tile behind it.  A tile's last reader frees its slot.
+    auto step_of = [&](auto H, int j, int nt, bool last_reader, bool last_reader_next) {
+      constexpr int h = decltype(H)::value;
+      if (j >= nt || !ok) return;
+      if (j == 0) {                                           // the accumulator is written over: the item before must have been read out
+        if (!mbar_wait_spin(BAR(o_free, h), o_phase[h])) { ok = false; return; }
+        o_phase[h] ^= 1u;
+      }
+      const bool more = j + 1 < nt;
+      if (!mbar_wait_spin(BAR(v_full, v_at[h].slot), v_at[h].phase)) { ok = false; return; }
+      const bool there = more && mbar_test(BAR(k_full, k_at[h].slot), k_at[h].phase);
+      const uint32_t vb = v_lo + v_at[h].slot * (TILE >> 4), o = tmem + 256 + h * 128, p = tmem + h * 128;
+      if (!mbar_wait_spin(BAR(p_half, h), p_phase[h])) { ok = false; return; }
+      tc_fence_after();
+      // the first half of every thread's weights: keys 0 .. 31 and 64 .. 95 (16 keys: 8 columns of weights, 2048 bytes of values)
+      mma_ts(o, p, vb, id_o, j > 0);
+      mma_ts(o, p + 8, vb + 128, id_o, 1);
+      mma_ts(o, p + 64, vb + 512, id_o, 1);
+      mma_ts(o, p + 72, vb + 640, id_o, 1);
+      if (!mbar_wait_spin(BAR(p_ready, h), p_phase[h])) { ok = false; return; }
+      p_phase[h] ^= 1u;
+      tc_fence_after();
+      mma_ts(o, p + 16, vb + 256, id_o, 1);
+      mma_ts(o, p + 24, vb + 384, id_o, 1);
+      mma_ts(o, p + 80, vb + 768, id_o, 1);
+      mma_ts(o, p + 88, vb + 896, id_o, 1);
+      if (last_reader) umma_commit(BAR(v_empty, v_at[h].slot));
+      v_at[h].step(step);
+      if (more) scores(H, there, last_reader_next);
+      umma_commit(BAR(pv_done, h));
+    };
+    using H0 = std::integral_constant<int, 0>;
+    using H1 = std::integral_constant<int, 1>;
+    first(H0{}, nt0, turns || nt1 == 0);
+    first(H1{}, nt1, true);
+    const int most = nt0 > nt1 ? nt0 : nt1;
+    for (int j = 0; j < most && ok; ++j) {
+      step_of(H0{}, j, nt0, turns || j >= nt1, turns || j + 1 >= nt1);
+      step_of(H1{}, j, nt1, true, true);
     }
     if (!ok) break;
-    for (int h = 0; h < 2; ++h) if (s.nt[h] > 0) ++n_q[h];
-    base += s.tb - s.ta;
+    // both halves' places go on behind the segment's last tile
+    if (turns) {
+      const int ahead = T & 1 ? 0 : 1;                        // the half that stands one tile further on than the segment's end
+      if (ahead) { k_at[1] = k_at[0]; v_at[1] = v_at[0]; }
+      else { k_at[0] = k_at[1]; v_at[0] = v_at[1]; }
+    } else if (nt0 >= nt1) {
+      k_at[1] = k_at[0]; v_at[1] = v_at[0];
+    } else {
+      k_at[0] = k_at[1]; v_at[0] = v_at[1];
+    }
     if (!walk_on(w, s, a)) break;
   } while (true);
   if (!ok) {
     if (!*abort_flag) atomicExch(a.c.status, STATUS_TIMEOUT_MMA);
     *abort_flag = 1;
-    umma_commit(smem_u32(&bars->drain));                      // products under way end before the CTA does
-    mbar_wait(smem_u32(&bars->drain), 0);
+    umma_commit(BAR(drain, 0));                               // products under way end before the CTA does
+    mbar_wait(BAR(drain, 0), 0);
   }
+#undef BAR
 }
 
 // ------------------------------------------------------------------ softmax of one half
@@ -478,6 +566,13 @@ __device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const 
       }
     }
   }
+}
+
+// The largest of three; NaN where one of them is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // Where a role stands.  The softmax warps keep theirs in local memory (functions that are not inlined take its address): 64 scores leave no room
@@ -519,7 +614,6 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
   const int row = tid & 127, ch = (tid >> 7) & 1, quarter = row >> 5, lane = tid & 31;
   const uint32_t lane_base = uint32_t(quarter * 32) << 16;
   const uint32_t t_s = tmem + h * 128 + lane_base, t_o = tmem + 256 + h * 128 + lane_base;
-  const uint32_t pair = smem_u32(&bars->pair[h * 4 + quarter]);
   float* mine = &bars->xch[h][ch][row];
   const float* theirs = &bars->xch[h][ch ^ 1][row];
   const uint32_t my_q = smem_u32(sQ) + h * TILE;
@@ -529,15 +623,11 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&bars->q_ready[h]));
   };
-  uint32_t pair_phase = 0;
-  // both warps of a row have come here, and see what the other has written before
-  auto pair_sync = [&]() {
-    __syncwarp();
-    if (lane == 0) mbar_arrive(pair);
-    const bool ok = mbar_wait_spin(pair, pair_phase);
-    pair_phase ^= 1;
-    return ok;
-  };
+  // Both warps of a row have come here, and see what the other has written before.  This wait has no limit of its own: the two warps come here
+  // equally often, also after one of the bounded waits has run out, because nothing below leaves a loop early.
+  auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + h * 4 + quarter) : "memory"); };
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) { if (ok) ok = mbar_wait(smem_u32(bar), parity); };
   Stand at;
   at.w = walk_begin(a, bars);
   at.s = segment_of(at.w, a);
@@ -545,7 +635,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
   const Segment& s = at.s;
   uint32_t done0 = 0, done1 = 0, seg = 0, shared_segs = 0;    // tiles of the halves so far, segments, segments whose rows the halves share
   if ((h == 0 ? s.nt[0] : s.nt[1]) > 0) { copy_q<DH>(a, w, s, my_q, h, row, ch); q_finish(); }
-  bool ok = true, x_pending = false;
+  bool x_pending = false;
   int slot = 2 * blockIdx.x;                                  // where this CTA's partial results go: its first segment's, then its last one's
   do {
     const bool turns = s.turns;
@@ -557,46 +647,47 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     const bool live = r - row + quarter * 32 < s.g.r1;        // (the same for both warps of a row)
     int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys
     const int key_step = turns ? 2 * KT : KT;
-    float m_ref = NEG, l_sum = 0.f;
+    float m_ref = NEG, m_next = NEG, l_sum = 0.f;
     if (nt == 0 && copy_next_q<DH>(a, at, my_q, h, row, ch)) q_finish();
     const uint32_t done = h == 0 ? done0 : done1;
     for (int j = 0; j < nt; ++j, key0 += key_step) {
       const uint32_t n = done + j;
-      if (!mbar_wait(smem_u32(&bars->s_ready[h]), n & 1)) { ok = false; break; }
+      wait(&bars->s_ready[h], n & 1);
       // with the last tile's scores all products that read this Q have finished: the next item's goes in
       const bool q_now = j == nt - 1 && copy_next_q<DH>(a, at, my_q, h, row, ch);
       if (live) {
         tc_fence_after();
-        float x[64];
-        tmem_ld32(t_s + ch * 64, reinterpret_cast<uint32_t*>(x));
-        tmem_ld32(t_s + ch * 64 + 32, reinterpret_cast<uint32_t*>(x + 32));
-        tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
-        tmem_wait_ld32(reinterpret_cast<uint32_t*>(x + 32));
-        if (__any_sync(0xffffffffu, hi < key0 + 63 || lo > key0)) {
-          const int jh = hi - key0, jl = lo - key0;
+        const bool masked = __any_sync(0xffffffffu, hi < key0 + 63 || lo > key0);
+        // 32 scores of the row at a time: more would not fit into the registers, and local memory is out of reach here (its lines miss an L1 that
+        // shared memory has taken nearly all of)
+        float x[32];
+        auto fetch = [&](int part) {
+          tmem_ld32(t_s + ch * 64 + part * 32, reinterpret_cast<uint32_t*>(x));
+          tmem_wait_ld32(reinterpret_cast<uint32_t*>(x));
+          if (masked) {
+            const int jh = hi - key0 - part * 32, jl = lo - key0 - part * 32;
 #pragma unroll
-          for (int i = 0; i < 64; ++i) x[i] = (i <= jh && i >= jl) ? x[i] : -INFINITY;
-        }
-        float m4[4] = {x[0], x[1], x[2], x[3]};
+            for (int i = 0; i < 32; ++i) x[i] = (i <= jh && i >= jl) ? x[i] : -INFINITY;
+          }
+        };
+        auto largest = [&]() {
+          float m0 = x[0], m1 = x[1];
 #pragma unroll
-        for (int i = 4; i < 64; i += 4) {
-          m4[0] = fmaxf(m4[0], x[i]); m4[1] = fmaxf(m4[1], x[i + 1]); m4[2] = fmaxf(m4[2], x[i + 2]); m4[3] = fmaxf(m4[3], x[i + 3]);
-        }
-        const float mx_own = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        if (j == 0 && x_pending) {
-          if (!mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
-          x_pending = false;
-        }
-        // the threads of a row tell each other their maxima.  (What was written here a tile ago has been read: the scores of this tile were issued
-        // behind the weights of all eight warps.)  Past the exchange both have their scores in registers, and the weights may go over them.
-        *mine = mx_own;
-        if (!pair_sync()) { ok = false; break; }
-        const float mx = fmaxf(mx_own, *theirs) * a.scale_log2;
-        const bool grow = mx > m_ref + LAZY;
-        float factor = 1.f;
-        if (grow) { factor = ex2_ftz(m_ref - mx); m_ref = mx; }
-        if (j > 0 && __any_sync(0xffffffffu, grow)) {
-          if (!mbar_wait(smem_u32(&bars->pv_done[h]), (n - 1) & 1)) { ok = false; break; }
+          for (int i = 2; i < 30; i += 4) { m0 = max3(m0, x[i], x[i + 1]); m1 = max3(m1, x[i + 2], x[i + 3]); }
+          return max3(max3(m0, m1, x[30]), x[31], x[31]);
+        };
+        // The threads of a row tell each other their maxima.  (What was written here a tile ago has been read: the scores of this tile were issued
+        // behind the weights of all eight warps.)
+        auto exchange = [&](float own) {
+          *mine = own;
+          pair_sync();
+          return max3(own, *theirs, *theirs) * a.scale_log2;
+        };
+        // The accumulated values and the sum follow the reference maximum.
+        auto rescale = [&](float factor) {
+          l_sum *= factor;
+          if (j == 0) return;
+          wait(&bars->pv_done[h], (n - 1) & 1);
           tc_fence_after();
           if (lane == 0 && ch == 0) atomicAdd(c.status + STATUS_WORD_RESCALES, 1u);
 #pragma unroll 1
@@ -609,47 +700,100 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
             tmem_st16(t_o + col, o);
           }
           tmem_st_wait();
-        }
-        l_sum *= factor;
-        const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_m2 = pack_f32x2(-m_ref, -m_ref);
+        };
         uint64_t ls[2] = {0ull, 0ull};
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
+        // Weights of the 32 keys, over scores of this thread that have been fetched.
+        auto weights_of = [&](int part, float ref) {
+          const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_m2 = pack_f32x2(-ref, -ref);
           uint32_t p[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float x0, x1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(x[part * 32 + 2 * e], x[part * 32 + 2 * e + 1]), scale2, neg_m2), x0, x1);
+            unpack_f32x2(fma_f32x2(pack_f32x2(x[2 * e], x[2 * e + 1]), scale2, neg_m2), x0, x1);
             const float p0 = ex2_ftz(x0), p1 = ex2_ftz(x1);
             ls[e & 1] = add_f32x2(ls[e & 1], pack_f32x2(p0, p1));
             p[e] = pack16<F16>(p0, p1);
           }
-          tmem_st16(t_s + ch * 32 + part * 16, p);
+          tmem_st16(t_s + ch * 64 + part * 16, p);
+        };
+        constexpr float LIMIT = F16 ? LIMIT_F16 : LIMIT_BF16;
+        float mx;
+        if (j == 0) {
+          fetch(1);
+          mx = largest();
+          fetch(0);
+          mx = max3(mx, largest(), largest());
+          if (x_pending) wait(&bars->x_read, (shared_segs - 1) & 1);                // (an item ago the halves talked here)
+          x_pending = false;
+          mx = exchange(mx);
+          m_ref = max3(mx, NEG, NEG);
+          weights_of(0, m_ref);
+          fetch(1);
+        } else {
+          // The weights do not wait for the row's maximum: the reference is that of the tiles before.  Only where this tile is above it by more than
+          // the weights' type can hold do they follow at once: the first 32 from their own maximum, then, when the row's is known, scaled to it.
+          if (__any_sync(0xffffffffu, m_next != m_ref)) {
+            const float factor = m_next != m_ref ? ex2_ftz(m_ref - m_next) : 1.f;
+            m_ref = m_next;
+            rescale(factor);
+          }
+          fetch(0);
+          mx = largest();
+          const float own = mx * a.scale_log2;
+          const float ref0 = !(own <= m_ref + LIMIT) ? own : m_ref;                 // (NaN: it becomes the reference, and all of the row)
+          weights_of(0, ref0);
+          fetch(1);
+          mx = exchange(max3(mx, largest(), largest()));
+          const bool over = !(mx <= m_ref + LIMIT);
+          if (__any_sync(0xffffffffu, over)) {
+            const float m_new = over ? mx : m_ref;
+            const float factor = over ? ex2_ftz(m_ref - m_new) : 1.f, f0 = over ? ex2_ftz(ref0 - m_new) : 1.f;
+            m_ref = m_new;
+            rescale(factor);
+            tmem_st_wait();
+            uint32_t p[16];
+            tmem_ld16(t_s + ch * 64, p);
+            tmem_wait_ld16(p);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float p0 = F16 ? __half2float(__ushort_as_half(uint16_t(p[e] & 0xffffu))) : bf16_bits_to_float(uint16_t(p[e] & 0xffffu));
+              const float p1 = F16 ? __half2float(__ushort_as_half(uint16_t(p[e] >> 16))) : bf16_bits_to_float(uint16_t(p[e] >> 16));
+              p[e] = pack16<F16>(p0 * f0, p1 * f0);
+            }
+            tmem_st16(t_s + ch * 64, p);
+            const uint64_t f2 = pack_f32x2(f0, f0);
+            ls[0] = fma_f32x2(ls[0], f2, 0ull); ls[1] = fma_f32x2(ls[1], f2, 0ull);
+          }
         }
+        m_next = mx > m_ref + LAZY ? mx : m_ref;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->p_half[h]));
+        weights_of(1, m_ref);
+        tmem_st_wait();
+        tc_fence_before();
         float s0, s1, s2, s3;
         unpack_f32x2(ls[0], s0, s1);
         unpack_f32x2(ls[1], s2, s3);
         l_sum += (s0 + s1) + (s2 + s3);
-        tmem_st_wait();
-        tc_fence_before();
+      } else if (lane == 0) {
+        mbar_arrive(smem_u32(&bars->p_half[h]));
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[h]));
       if (q_now) q_finish();
     }
     done0 += s.nt[0]; done1 += s.nt[1];
-    if (!ok) break;
     // ---- read-out
-    if (nt > 0 && (!mbar_wait(smem_u32(&bars->pv_done[h]), ((h == 0 ? done0 : done1) - 1) & 1) || *abort_flag)) { ok = false; break; }
-    if (x_pending) {
-      if (!mbar_wait(smem_u32(&bars->x_read), (shared_segs - 1) & 1)) { ok = false; break; }
-      x_pending = false;
-    }
+    if (nt > 0) wait(&bars->pv_done[h], ((h == 0 ? done0 : done1) - 1) & 1);
+    if (x_pending) wait(&bars->x_read, (shared_segs - 1) & 1);
+    x_pending = false;
     if (live) {                                               // the row's sum from its two threads
       *mine = l_sum;
-      if (!pair_sync()) { ok = false; break; }
+      pair_sync();
       l_sum = ch == 0 ? l_sum + *theirs : *theirs + l_sum;    // (in one order: the same bits in both)
-      if (!pair_sync()) { ok = false; break; }
+      pair_sync();
     }
     float weight0 = 1.f, weight1 = 0.f;
     if (s.turns) {
@@ -660,13 +804,13 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->x_write));
       }
-      if (!mbar_wait(smem_u32(&bars->x_write), shared_segs & 1)) { ok = false; break; }
+      wait(&bars->x_write, shared_segs & 1);
       const float m0 = bars->xch[0][0][row], l0 = bars->xch[0][1][row], m1 = bars->xch[1][0][row], l1 = bars->xch[1][1][row];
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars->x_read));
       ++shared_segs;
       x_pending = true;
-      if (nt_other > 0 && !mbar_wait(smem_u32(&bars->pv_done[h ^ 1]), ((h == 0 ? done1 : done0) - 1) & 1)) { ok = false; break; }
+      if (nt_other > 0) wait(&bars->pv_done[h ^ 1], ((h == 0 ? done1 : done0) - 1) & 1);
       m_ref = fmaxf(m0, m1);
       weight0 = ex2_ftz(m0 - m_ref); weight1 = ex2_ftz(m1 - m_ref);
       l_sum = l0 * weight0 + l1 * weight1;
@@ -675,6 +819,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     const bool fix = *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) == seg + 1;
     const int cols = s.turns ? DH / 4 : DH / 2, col0 = (s.turns ? h * 2 + ch : ch) * cols;
     const float inv = l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum);      // (nothing seen: zero; NaN stays)
+    if (*abort_flag) ok = false;
     if (!s.whole && row_ok && ch == 0 && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
     if (live && (s.turns || nt > 0)) {
       uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(w.q.q0 + r / a.rep) * c.ldo + size_t(w.kvh * a.rep + r % a.rep) * DH : 0);
@@ -709,7 +854,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[e] = copy[e];
         }
-        if (s.whole && row_ok) {
+        if (s.whole && row_ok && ok) {
 #pragma unroll
           for (int e = 0; e < 16; e += 8) {
             uint32_t p[4];
@@ -718,7 +863,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
               p[i] = F16 ? pack_f16_sat(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv, c.status) : pack_bf16(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv);
             *reinterpret_cast<uint4*>(dst + col + e) = make_uint4(p[0], p[1], p[2], p[3]);
           }
-        } else if (row_ok) {
+        } else if (row_ok && ok) {
           // [column group][row][4]: the lanes of a warp write neighbouring 16 bytes
 #pragma unroll
           for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
@@ -771,11 +916,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     for (int h = 0; h < 2; ++h) {
       mbar_init(smem_u32(&bars->q_ready[h]), 8);
       mbar_init(smem_u32(&bars->s_ready[h]), 1);
+      mbar_init(smem_u32(&bars->p_half[h]), 8);
       mbar_init(smem_u32(&bars->p_ready[h]), 8);
       mbar_init(smem_u32(&bars->pv_done[h]), 1);
       mbar_init(smem_u32(&bars->o_free[h]), 16);
     }
-    for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&bars->pair[i]), 2);
     mbar_init(smem_u32(&bars->x_write), 8);
     mbar_init(smem_u32(&bars->x_read), 16);
     mbar_init(smem_u32(&bars->drain), 1);
@@ -798,10 +943,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if (!work) {
     // nothing to do here (uniform for the CTA)
   } else if (warp < 16) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
     softmax_half<DH, F16>(a, sQ, bars, tmem, warp >> 3, tid);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
     if (warp == 16) {
       produce<DH, false>(a, &tmK, ring_k, bars, lane);
     } else if (warp == 18) {
@@ -933,10 +1076,6 @@ cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tm
     cudaError_t e1 = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     ctas[dev] = sms < MAX_CTAS ? sms : MAX_CTAS;
     if (e1 == cudaSuccess) e1 = cudaFuncSetAttribute(chunk_attn_kernel<DH, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-    // the warps' shares of the registers must fit into what the block is launched with, or they wait for them for ever
-    cudaFuncAttributes fa{};
-    if (e1 == cudaSuccess) e1 = cudaFuncGetAttributes(&fa, chunk_attn_kernel<DH, F16>);
-    if (e1 == cudaSuccess && fa.numRegs * THREADS < SOFTMAX_THREADS * REGS_SOFTMAX + (THREADS - SOFTMAX_THREADS) * REGS_OTHER) e1 = cudaErrorLaunchOutOfResources;
     return e1;
   });
   if (e != cudaSuccess) return e;
