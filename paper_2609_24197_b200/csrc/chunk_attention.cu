@@ -16,7 +16,9 @@
 //                      whole groups of 8 rows).  One warp for both could not issue the boxes of 16-token pages fast enough.
 //   warp 17            issues S = Q K^T and O += P V (P from tensor memory), one half behind the other: while a half's scores are in the
 //                      softmax the tensor core works for the other
-//   warp 19            goes over the V tiles that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
+//   warp 19            finds the CTA's share of the items, one after the other, and hands it to the others through shared memory (a place in the
+//                      walk that every thread kept for itself went to local memory, and cost 20 000 clocks an item); and goes over the V tiles
+//                      that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
 //                      become zero (a zero weight times NaN would not), and so do single values that are not finite.  Those of them that
 //                      some rows see are added to these rows' results at the end, from the cache, on a path that nothing else takes.
 //
@@ -48,20 +50,7 @@ template <int DH> struct Shape {
   static constexpr int NK = DH == 128 ? 2 : 4, NV = DH == 128 ? 3 : 6;      // slots of the rings: 160 KiB of K and V tiles
 };
 
-struct __align__(16) Bars {
-  // a slot's tile has arrived, has been read, and for V tiles that not every row sees in full: has arrived and is to be gone over, after which
-  // the warp that does so gives the arrival of `full`
-  uint64_t k_full[4], k_empty[4], v_full[6], v_empty[6], v_raw[6];
-  uint64_t q_ready[2], s_ready[2], p_half[2], p_ready[2], pv_done[2], o_free[2];
-  uint64_t x_write, x_read, drain;
-  uint32_t tmem_base, abort_flag;
-  uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 6 fit into the ring) met a value that is not finite in a tile
-                                     // that not every row sees in full
-  int4 start, stop;                  // where this CTA's part begins and where the next one's does: request, group of KV heads, row tile, tile of the item
-  ChunkRequest req[2];               // the request that it begins in and the one behind it
-  float xch[2][2][128];              // [half][half of the columns][row]: what the threads of a row tell each other
-};
-constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
+
 
 struct Args {
   ChunkAttnCall c;
@@ -97,15 +86,42 @@ __device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int 
   return g;
 }
 
+__device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int b) {
+  if (b >= c.B) return ChunkRequest{0, 0, 0};
+  return chunk_request(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len);
+}
+// A CTA's share of an item, as every role needs it.
+struct Segment {
+  ItemGeo g;
+  int b, kvh, q0, pos;               // request, KV head, the request's first row and its position
+  int ta, tb;                        // tiles
+  int nt[2];                         // tiles of each half
+  int turns, whole, end;             // end: there is none any more
+};
+constexpr int SEGS = 4;
+
+struct __align__(16) Bars {
+  // a slot's tile has arrived, has been read, and for V tiles that not every row sees in full: has arrived and is to be gone over, after which
+  // the warp that does so gives the arrival of `full`
+  uint64_t k_full[4], k_empty[4], v_full[6], v_empty[6], v_raw[6];
+  uint64_t q_ready[2], s_ready[2], p_half[2], p_ready[2], pv_done[2], o_free[2];
+  uint64_t x_write, x_read, drain;
+  uint64_t seg_full[SEGS], seg_empty[SEGS];
+  Segment seg[SEGS];                 // what the roles work on, in order
+  uint32_t tmem_base, abort_flag;
+  uint32_t bad[16];                  // n + 1 where segment n (modulo 16; at most 6 fit into the ring) met a value that is not finite in a tile
+                                     // that not every row sees in full
+  int4 start, stop;                  // where this CTA's part begins and where the next one's does: request, group of KV heads, row tile, tile of the item
+  ChunkRequest req[2];               // the request that it begins in and the one behind it
+  float xch[2][2][128];              // [half][half of the columns][row]: what the threads of a row tell each other
+};
+constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
+
 struct Walk {                        // this CTA's part of the line, item by item
   int b, g, kvh, rt, off;
   int4 stop;
   ChunkRequest q, next;
 };
-__device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int b) {
-  if (b >= c.B) return ChunkRequest{0, 0, 0};
-  return chunk_request(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len);
-}
 __device__ __forceinline__ Walk walk_begin(const Args& a, const Bars* bars) {
   Walk w;
   w.b = bars->start.x; w.g = bars->start.y; w.rt = bars->start.z; w.off = bars->start.w;
@@ -115,26 +131,21 @@ __device__ __forceinline__ Walk walk_begin(const Args& a, const Bars* bars) {
   w.next = bars->req[1];
   return w;
 }
-struct Segment {
-  ItemGeo g;
-  int ta, tb;                        // tiles of this CTA
-  int nt[2];                         // tiles of each half
-  bool turns, whole;
-};
 __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
   Segment s;
   s.g = item_geo(w.q, a.rep, a.c.window, w.rt);
+  s.b = w.b; s.kvh = w.kvh; s.q0 = w.q.q0; s.pos = w.q.len - w.q.n;
   s.ta = s.g.t0 + w.off;
   s.tb = w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z ? s.g.t0 + w.stop.w : s.g.t1;
   s.whole = w.off == 0 && s.tb == s.g.t1;
   s.turns = takes_turns(w.q.n * a.rep);
+  s.end = 0;
   const int T = s.tb - s.ta;
   if (s.turns) {
     s.nt[0] = (T + 1) / 2; s.nt[1] = T / 2;
   } else if (s.g.r1 - s.g.r0 > 128) {
     // the first half's rows end earlier, and with them the tiles that they see
-    const int pos = w.q.len - w.q.n + (s.g.r0 + 127) / a.rep;
-    const int end = max(s.g.t0 + 1, (pos + KT) / KT);
+    const int end = max(s.g.t0 + 1, (s.pos + (s.g.r0 + 127) / a.rep + KT) / KT);
     s.nt[0] = max(0, min(end - s.ta, T)); s.nt[1] = T;
   } else {
     s.nt[0] = T; s.nt[1] = 0;
@@ -160,6 +171,9 @@ __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a
   }
   return w.b < a.c.B && !(w.stop.w == 0 && w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z);
 }
+// Segment n is there (bounded), and has been read.
+__device__ __forceinline__ bool segment_wait(Bars* bars, uint32_t n) { return mbar_wait(smem_u32(&bars->seg_full[n % SEGS]), (n / SEGS) & 1); }
+__device__ __forceinline__ void segment_read(Bars* bars, uint32_t n) { mbar_arrive(smem_u32(&bars->seg_empty[n % SEGS])); }
 // Not every row of the item sees all of the tile's keys.
 __device__ __forceinline__ bool partial_tile(const ItemGeo& g, int window, int t) {
   return t * KT + KT - 1 > g.pos0 || (window > 0 && t * KT < g.pos1 - window + 1);
@@ -291,14 +305,17 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
   uint64_t* full = IS_V ? bars->v_full : bars->k_full;
   uint64_t* empty = IS_V ? bars->v_empty : bars->k_empty;
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  Walk w = walk_begin(a, bars);
   uint32_t at = 0;                                            // tiles issued
   uint32_t raw_phase = 0, is_raw = 0;                         // a bit per slot: phase of `v_raw`, and whether the slot's last tile went there
   bool ok = true;
   const int boxes = a.box_rows ? KT / a.box_rows : 0;
-  do {
-    const Segment s = segment_of(w, a);
-    const int32_t* table = c.page_table + size_t(w.b) * c.page_table_stride;
+  for (uint32_t n = 0; ok; ++n) {
+    if (!segment_wait(bars, n)) { ok = false; break; }
+    const Segment s = bars->seg[n % SEGS];
+    __syncwarp();
+    if (lane == 0) segment_read(bars, n);
+    if (s.end) break;
+    const int32_t* table = c.page_table + size_t(s.b) * c.page_table_stride;
     // page of this lane's box (up to 16 of them), fetched a tile ahead
     auto page_of = [&](int t) {
       if (lane >= boxes || t >= s.tb) return -1;
@@ -320,9 +337,9 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
       if (a.box_rows) {
         const int key = key0 + lane * a.box_rows;
         const bool on = lane < boxes && key < s.g.key_hi && key + a.box_rows > s.g.key_lo;
-        const unsigned n = __popc(__ballot_sync(0xffffffffu, on));
+        const unsigned count = __popc(__ballot_sync(0xffffffffu, on));
         if (lane == 0) {
-          if (n) mbar_expect_tx(bar, n * a.box_rows * DH * 2);
+          if (count) mbar_expect_tx(bar, count * a.box_rows * DH * 2);
           else mbar_arrive(bar);
         }
         __syncwarp();
@@ -331,7 +348,7 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
           if (!IS_V && unsigned(page) >= unsigned(c.num_pages)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
 #pragma unroll
           for (int h = 0; h < DH / 64; ++h)
-            tma_load_4d(dst + h * Shape<DH>::HALF + lane * a.box_rows * 128, tm, h * 64, w.kvh, key % c.page_size, page, bar);
+            tma_load_4d(dst + h * Shape<DH>::HALF + lane * a.box_rows * 128, tm, h * 64, s.kvh, key % c.page_size, page, bar);
         }
       } else {
         const uint16_t* pool = reinterpret_cast<const uint16_t*>(IS_V ? c.v_pool : c.k_pool);
@@ -345,7 +362,7 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
               on = false;
               if (!IS_V && chunk == 0 && (key % c.page_size == 0 || key == s.g.key_lo)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
             } else {
-              from = ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + chunk * 8;
+              from = ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + s.kvh) * DH + chunk * 8;
             }
           }
           cp_async16(dst + tile_off(r, chunk), pool + from, on);
@@ -357,8 +374,7 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
         if (lane == 0) mbar_arrive(bar);
       }
     }
-    if (!ok || !walk_on(w, s, a)) break;
-  } while (true);
+  }
   if (!ok) {
     if (lane == 0) {
       if (!*abort_flag) atomicExch(c.status, STATUS_TIMEOUT_PRODUCER);
@@ -373,15 +389,41 @@ __device__ __forceinline__ void produce(const Args& a, const CUtensorMap* tm, ui
   }
 }
 
-// ------------------------------------------------------------------ values that not every row sees
+// ------------------------------------------------------------------ the segments, and values that not every row sees
+// This warp also tells the others what they work on, two segments ahead of its own.
 template <int DH, bool F16>
-__device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars* bars, int lane) {
+__device__ __forceinline__ void lead_and_clean(const Args& a, uint8_t* ring, Bars* bars, int lane) {
   constexpr int NS = Shape<DH>::NV, TILE = Shape<DH>::TILE;
   volatile uint32_t* abort_flag = &bars->abort_flag;
   Walk w = walk_begin(a, bars);
-  uint32_t base = 0, seg = 0, phase = 0;                      // phase of `v_raw`, a bit per slot
-  do {
-    const Segment s = segment_of(w, a);
+  Segment ahead = segment_of(w, a);
+  uint32_t told = 0;                                          // segments that the others know of
+  bool more = true;
+  auto tell = [&]() {
+    if (told >= SEGS && !mbar_wait(smem_u32(&bars->seg_empty[told % SEGS]), ((told / SEGS) - 1) & 1)) return false;
+    if (!more) ahead.end = 1;
+    if (lane == 0) {
+      bars->seg[told % SEGS] = ahead;
+      mbar_arrive(smem_u32(&bars->seg_full[told % SEGS]));
+    }
+    __syncwarp();
+    ++told;
+    if (more) {
+      more = walk_on(w, ahead, a);
+      if (more) ahead = segment_of(w, a);
+    }
+    return true;
+  };
+  uint32_t base = 0, phase = 0;                               // phase of `v_raw`, a bit per slot
+  for (uint32_t seg = 0;; ++seg) {
+    while (told <= seg + 2 && !ahead.end) {
+      if (!tell()) {
+        if (lane == 0 && !*abort_flag) { atomicExch(a.c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
+        return;
+      }
+    }
+    const Segment s = bars->seg[seg % SEGS];
+    if (s.end) return;
     for (int t = s.ta; t < s.tb; ++t) {
       if (!partial_tile(s.g, a.c.window, t)) continue;
       const uint32_t slot = (base + (t - s.ta)) % NS;
@@ -415,9 +457,7 @@ __device__ __forceinline__ void clean_values(const Args& a, uint8_t* ring, Bars*
       if (lane == 0) mbar_arrive(smem_u32(&bars->v_full[slot]));
     }
     base += s.tb - s.ta;
-    ++seg;
-    if (!walk_on(w, s, a)) break;
-  } while (true);
+  }
 }
 
 // ------------------------------------------------------------------ MMA issuer (one thread)
@@ -453,15 +493,17 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
   const uint32_t bar0 = smem_u32(bars);
 #define BAR(field, i) (bar0 + uint32_t(offsetof(Bars, field)) + uint32_t(i) * 8u)
   volatile uint32_t* abort_flag = &bars->abort_flag;
-  Walk w = walk_begin(a, bars);
   RingPos<NK> k_at[2];                                        // next K and V tile of each half
   RingPos<NV> v_at[2];
   uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
   bool ok = true;
-  do {
-    const Segment s = segment_of(w, a);
-    const bool turns = s.turns;
-    const int T = s.tb - s.ta, nt0 = s.nt[0], nt1 = s.nt[1];
+  for (uint32_t n = 0; ok; ++n) {
+    if (!segment_wait(bars, n)) { ok = false; break; }
+    const Segment* s = &bars->seg[n % SEGS];
+    const bool turns = s->turns, end = s->end;
+    const int T = s->tb - s->ta, nt0 = s->nt[0], nt1 = s->nt[1];
+    segment_read(bars, n);
+    if (end) break;
     const uint32_t step = turns ? 2 : 1;
     if (turns) { k_at[1].step(1); v_at[1].step(1); }
     auto scores = [&](auto H, bool there, bool last_reader) {
@@ -538,8 +580,7 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
     } else {
       k_at[0] = k_at[1]; v_at[0] = v_at[1];
     }
-    if (!walk_on(w, s, a)) break;
-  } while (true);
+  }
   if (!ok) {
     if (!*abort_flag) atomicExch(a.c.status, STATUS_TIMEOUT_MMA);
     *abort_flag = 1;
@@ -552,14 +593,14 @@ __device__ __forceinline__ void issue_mmas(const Args& a, uint8_t* sQ, uint8_t* 
 // ------------------------------------------------------------------ softmax of one half
 // Adds to 16 columns of a row's accumulator the values that are not finite and that the row sees, from the tiles that were cleaned of them.
 template <int DH, bool F16>
-__device__ __noinline__ void add_not_finite(const Args& a, const Walk& w, const Segment& s, int lo, int hi, int col, float* acc) {
+__device__ __noinline__ void add_not_finite(const Args& a, const Segment& s, int lo, int hi, int col, float* acc) {
   const ChunkAttnCall& c = a.c;
   for (int t = s.ta; t < s.tb; ++t) {
     if (!partial_tile(s.g, c.window, t)) continue;
     for (int key = max(lo, t * KT); key <= min(hi, t * KT + KT - 1); ++key) {
-      const int id = c.page_table[size_t(w.b) * c.page_table_stride + key / c.page_size];
+      const int id = c.page_table[size_t(s.b) * c.page_table_stride + key / c.page_size];
       if (unsigned(id) >= unsigned(c.num_pages)) continue;
-      const uint16_t* v = reinterpret_cast<const uint16_t*>(c.v_pool) + ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + w.kvh) * DH + col;
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(c.v_pool) + ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + s.kvh) * DH + col;
       for (int e = 0; e < 16; ++e) {
         const uint16_t x = v[e];
         if (not_finite16<F16>(x)) acc[e] += F16 ? __half2float(__ushort_as_half(x)) : bf16_bits_to_float(x);
@@ -575,36 +616,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// Where a role stands.  The softmax warps keep theirs in local memory (functions that are not inlined take its address): 64 scores leave no room
-// for it in registers, and the compiler would put something of the inner loop there instead.
-struct Stand { Walk w; Segment s; };
-__device__ __noinline__ bool next_segment(const Args& a, Stand& at) {
-  if (!walk_on(at.w, at.s, a)) return false;
-  at.s = segment_of(at.w, a);
-  return true;
-}
 // Half of a row of Q: 16-byte asynchronous copies into the operand layout, zeros for rows that are not there.
 template <int DH>
-__device__ __forceinline__ void copy_q(const Args& a, const Walk& w, const Segment& s, uint32_t q_tile, int h, int row, int ch) {
+__device__ __forceinline__ void copy_q(const Args& a, const Segment& s, uint32_t q_tile, int h, int row, int ch) {
   const int r = s.g.r0 + (s.turns ? 0 : h * 128) + row;
   const bool on = r < s.g.r1;
   const uint16_t* src = reinterpret_cast<const uint16_t*>(a.c.q);
-  if (on) src += size_t(w.q.q0 + r / a.rep) * a.c.ldq + size_t(w.kvh * a.rep + r % a.rep) * DH + ch * (DH / 2);
+  if (on) src += size_t(s.q0 + r / a.rep) * a.c.ldq + size_t(s.kvh * a.rep + r % a.rep) * DH + ch * (DH / 2);
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) cp_async16(q_tile + tile_off(row, ch * (DH / 16) + i), src + (on ? i * 8 : 0), on);
   cp_async_commit();
 }
-// The same for the segment behind this one; false where it has nothing for this half, or is not there.
-template <int DH>
-__device__ __noinline__ bool copy_next_q(const Args& a, const Stand& at, uint32_t q_tile, int h, int row, int ch) {
-  Walk w = at.w;
-  if (!walk_on(w, at.s, a)) return false;
-  const Segment s = segment_of(w, a);
-  if (s.nt[h] == 0) return false;
-  copy_q<DH>(a, w, s, q_tile, h, row, ch);
-  return true;
-}
-
 // Warp w of the half's eight: rows 32 (w % 4) .. + 31, key columns 64 (w / 4) .. + 63 of every tile.
 template <int DH, bool F16>
 __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* bars, uint32_t tmem, int h, int tid) {
@@ -628,33 +650,47 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
   auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + h * 4 + quarter) : "memory"); };
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) { if (ok) ok = mbar_wait(smem_u32(bar), parity); };
-  Stand at;
-  at.w = walk_begin(a, bars);
-  at.s = segment_of(at.w, a);
-  const Walk& w = at.w;
-  const Segment& s = at.s;
-  uint32_t done0 = 0, done1 = 0, seg = 0, shared_segs = 0;    // tiles of the halves so far, segments, segments whose rows the halves share
-  if ((h == 0 ? s.nt[0] : s.nt[1]) > 0) { copy_q<DH>(a, w, s, my_q, h, row, ch); q_finish(); }
+  // True in both warps of a row, or in neither.
+  auto pair_and = [&](bool x) {
+    int r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 64, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(int(x)), "r"(1 + h * 4 + quarter) : "memory");
+    return r != 0;
+  };
+  uint32_t done0 = 0, done1 = 0, shared_segs = 0;             // tiles of the halves so far, segments whose rows the halves share
   bool x_pending = false;
   int slot = 2 * blockIdx.x;                                  // where this CTA's partial results go: its first segment's, then its last one's
-  do {
+  // Q of segment n, if this half has tiles there
+  auto q_of = [&](uint32_t n) {
+    if (ok) ok = segment_wait(bars, n);
+    const Segment& s = bars->seg[n % SEGS];
+    if (!ok || s.end || s.nt[h] == 0) return false;
+    copy_q<DH>(a, s, my_q, h, row, ch);
+    return true;
+  };
+  if (q_of(0)) q_finish();
+  for (uint32_t seg = 0;; ++seg) {
+    if (ok) ok = segment_wait(bars, seg);
+    if (!pair_and(ok)) { ok = false; break; }                 // (without a segment there is nothing to go through)
+    const Segment& s = bars->seg[seg % SEGS];
+    if (s.end) break;
     const bool turns = s.turns;
-    const int nt = h == 0 ? s.nt[0] : s.nt[1], nt_other = h == 0 ? s.nt[1] : s.nt[0];
+    const int nt = s.nt[h], nt_other = s.nt[h ^ 1];
     const int r = s.g.r0 + (turns ? 0 : h * 128) + row;       // row of the head
     const bool row_ok = r < s.g.r1;
-    const int hi = row_ok ? w.q.len - w.q.n + r / a.rep : -1;                       // keys lo .. hi are seen
+    const int hi = row_ok ? s.pos + r / a.rep : -1;           // keys lo .. hi are seen
     const int lo = c.window > 0 ? max(0, hi - c.window + 1) : 0;
     const bool live = r - row + quarter * 32 < s.g.r1;        // (the same for both warps of a row)
     int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys
     const int key_step = turns ? 2 * KT : KT;
     float m_ref = NEG, m_next = NEG, l_sum = 0.f;
-    if (nt == 0 && copy_next_q<DH>(a, at, my_q, h, row, ch)) q_finish();
+    if (nt == 0 && q_of(seg + 1)) q_finish();
     const uint32_t done = h == 0 ? done0 : done1;
     for (int j = 0; j < nt; ++j, key0 += key_step) {
       const uint32_t n = done + j;
       wait(&bars->s_ready[h], n & 1);
       // with the last tile's scores all products that read this Q have finished: the next item's goes in
-      const bool q_now = j == nt - 1 && copy_next_q<DH>(a, at, my_q, h, row, ch);
+      const bool q_now = j == nt - 1 && q_of(seg + 1);
       if (live) {
         tc_fence_after();
         const bool masked = __any_sync(0xffffffffu, hi < key0 + 63 || lo > key0);
@@ -822,7 +858,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     if (*abort_flag) ok = false;
     if (!s.whole && row_ok && ch == 0 && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
     if (live && (s.turns || nt > 0)) {
-      uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(w.q.q0 + r / a.rep) * c.ldo + size_t(w.kvh * a.rep + r % a.rep) * DH : 0);
+      uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(s.q0 + r / a.rep) * c.ldo + size_t(s.kvh * a.rep + r % a.rep) * DH : 0);
       float* part = a.ws_o + size_t(slot) * DH * ITEM_ROWS + size_t(r - s.g.r0) * 4;
 #pragma unroll 1
       for (int col = col0; col < col0 + cols; col += 16) {
@@ -850,7 +886,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
           float copy[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) copy[e] = v[e];
-          add_not_finite<DH, F16>(a, w, s, lo, hi, col, copy);
+          add_not_finite<DH, F16>(a, s, lo, hi, col, copy);
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[e] = copy[e];
         }
@@ -873,16 +909,16 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     tc_fence_before();
     __syncwarp();
     if (lane == 0) {
-      if (s.turns) {
+      if (turns) {
         if (s.nt[0] > 0) mbar_arrive(smem_u32(&bars->o_free[0]));
         if (s.nt[1] > 0) mbar_arrive(smem_u32(&bars->o_free[1]));
       } else if (nt > 0) {
         mbar_arrive_n(smem_u32(&bars->o_free[h]), 2);
       }
     }
+    if (lane == 0) segment_read(bars, seg);
     slot = 2 * blockIdx.x + 1;
-    ++seg;
-  } while (next_segment(a, at));
+  }
   if (!ok) { if (!*abort_flag) atomicExch(c.status, STATUS_TIMEOUT_EPILOGUE); *abort_flag = 1; }
   tc_fence_before();
 }
@@ -924,6 +960,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     mbar_init(smem_u32(&bars->x_write), 8);
     mbar_init(smem_u32(&bars->x_read), 16);
     mbar_init(smem_u32(&bars->drain), 1);
+    for (int i = 0; i < SEGS; ++i) {
+      mbar_init(smem_u32(&bars->seg_full[i]), 1);
+      mbar_init(smem_u32(&bars->seg_empty[i]), 19);           // sixteen softmax warps, two producers, the MMA thread
+    }
     bars->abort_flag = 0;
     for (int i = 0; i < 16; ++i) bars->bad[i] = 0;
     fence_mbar_init();
@@ -953,7 +993,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (elect_one()) issue_mmas<DH, F16>(a, sQ, ring_k, ring_v, bars, tmem);
       __syncwarp();
     } else {
-      clean_values<DH, F16>(a, ring_v, bars, lane);
+      lead_and_clean<DH, F16>(a, ring_v, bars, lane);
     }
   }
   __syncthreads();
