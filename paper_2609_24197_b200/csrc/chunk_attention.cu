@@ -19,8 +19,8 @@
 //   warp 19            finds the CTA's share of the items, one after the other, and hands it to the others through shared memory (a place in the
 //                      walk that every thread kept for itself went to local memory, and cost 20 000 clocks an item); and goes over the V tiles
 //                      that not every row sees in full: values that no row sees, whatever was in the cache or in shared memory,
-//                      become zero (a zero weight times NaN would not), and so do single values that are not finite.  Those of them that
-//                      some rows see are added to these rows' results at the end, from the cache, on a path that nothing else takes.
+//                      become zero (a zero weight times NaN would not), and so do single values that are not finite and that some rows do not see.
+//                      They are added to these rows' results at the end, from the cache, on a path that nothing else takes.
 //
 // Every wait is bounded; a role whose wait runs out sets a status word, and the CTA unwinds.
 #include "chunk.cuh"
@@ -55,6 +55,7 @@ template <int DH> struct Shape {
 struct Args {
   ChunkAttnCall c;
   int rep, box_rows;                 // rows of a TMA box; 0: pages are copied by 16-byte loads
+  uint32_t inv_rep;                  // 2^20 / rep, rounded up
   int group;                         // KV heads that are worked on side by side
   float scale_log2;
   float* ws_o;                       // [slot][DH / 4][256 rows][4]
@@ -94,6 +95,7 @@ __device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int
 struct Segment {
   ItemGeo g;
   int b, kvh, q0, pos;               // request, KV head, the request's first row and its position
+  int tok0, rem0;                    // the item's first row is query head rem0 (of the KV head's) of the request's token tok0
   int ta, tb;                        // tiles
   int nt[2];                         // tiles of each half
   int turns, whole, end;             // end: there is none any more
@@ -135,6 +137,7 @@ __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
   Segment s;
   s.g = item_geo(w.q, a.rep, a.c.window, w.rt);
   s.b = w.b; s.kvh = w.kvh; s.q0 = w.q.q0; s.pos = w.q.len - w.q.n;
+  s.tok0 = s.g.r0 / a.rep; s.rem0 = s.g.r0 - s.tok0 * a.rep;
   s.ta = s.g.t0 + w.off;
   s.tb = w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z ? s.g.t0 + w.stop.w : s.g.t1;
   s.whole = w.off == 0 && s.tb == s.g.t1;
@@ -170,6 +173,13 @@ __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a
     }
   }
   return w.b < a.c.B && !(w.stop.w == 0 && w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z);
+}
+// Row r of the item (below 256): its token, and its query head among the KV head's.  (x inv_rep >> 20 is x / rep for x (inv_rep rep - 2^20) < 2^20, which
+// x < 256 + rep and rep <= 512 hold to; a division took 100 clocks several times an item.)
+__device__ __forceinline__ void token_of(const Segment& s, const Args& a, int r, int& token, int& head) {
+  const uint32_t x = uint32_t(s.rem0 + r), t = (x * a.inv_rep) >> 20;
+  token = s.tok0 + int(t);
+  head = int(x - t * uint32_t(a.rep));
 }
 // Segment n is there (bounded), and has been read.
 __device__ __forceinline__ bool segment_wait(Bars* bars, uint32_t n) { return mbar_wait(smem_u32(&bars->seg_full[n % SEGS]), (n / SEGS) & 1); }
@@ -432,23 +442,33 @@ __device__ __forceinline__ void lead_and_clean(const Args& a, uint8_t* ring, Bar
         return;
       }
       phase ^= 1u << slot;
+      // rows [seen0, seen1) of the tile are seen by some rows of the item, [all0, all1) of them by every one
+      const int key = t * KT, seen0 = max(0, s.g.key_lo - key), seen1 = min(KT, s.g.key_hi - key);
+      const int all0 = a.c.window > 0 ? max(seen0, s.g.pos1 - a.c.window + 1 - key) : seen0, all1 = min(seen1, s.g.pos0 + 1 - key);
       uint8_t* tile = ring + slot * TILE;
+      constexpr uint32_t EXP = F16 ? 0x7c007c00u : 0x7f807f80u, ONE = F16 ? 0x04000400u : 0x00800080u;
       bool bad = false;
-      for (int i = lane; i < KT * (DH / 8); i += 32) {
-        const int r = i / (DH / 8), key = t * KT + r;
-        uint4* p = reinterpret_cast<uint4*>(tile + tile_off(r, i % (DH / 8)));
-        if (key < s.g.key_lo || key >= s.g.key_hi) {
-          *p = make_uint4(0u, 0u, 0u, 0u);
-        } else {
-          uint4 v = *p;
-          uint32_t x[4] = {v.x, v.y, v.z, v.w};
-          bool here = false;
+      // a row is 128 bytes in each half of the tile; 4 rows a step of the warp
+      for (int half = 0; half < DH / 64; ++half) {
+        uint4* p = reinterpret_cast<uint4*>(tile + half * Shape<DH>::HALF) + lane;
+        const int r0 = lane >> 3;
+#pragma unroll 8
+        for (int i = 0; i < KT / 4; ++i) {
+          const int r = i * 4 + r0;
+          if (r >= all0 && r < all1) continue;
+          if (r < seen0 || r >= seen1) { p[i * 32] = make_uint4(0u, 0u, 0u, 0u); continue; }
+          const uint4 v = p[i * 32];
+          // (an exponent of ones is the only one that carries into its sign's place)
+          if (((((v.x & EXP) + ONE) | ((v.y & EXP) + ONE) | ((v.z & EXP) + ONE) | ((v.w & EXP) + ONE)) & 0x80008000u) != 0u) {
+            uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (not_finite16<F16>(x[e])) { x[e] &= 0xffff0000u; here = true; }
-            if (not_finite16<F16>(x[e] >> 16)) { x[e] &= 0x0000ffffu; here = true; }
+            for (int e = 0; e < 4; ++e) {
+              if (not_finite16<F16>(x[e])) x[e] &= 0xffff0000u;
+              if (not_finite16<F16>(x[e] >> 16)) x[e] &= 0x0000ffffu;
+            }
+            p[i * 32] = make_uint4(x[0], x[1], x[2], x[3]);
+            bad = true;
           }
-          if (here) { *p = make_uint4(x[0], x[1], x[2], x[3]); bad = true; }
         }
       }
       if (bad) *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) = seg + 1;
@@ -598,6 +618,7 @@ __device__ __noinline__ void add_not_finite(const Args& a, const Segment& s, int
   for (int t = s.ta; t < s.tb; ++t) {
     if (!partial_tile(s.g, c.window, t)) continue;
     for (int key = max(lo, t * KT); key <= min(hi, t * KT + KT - 1); ++key) {
+      if (key <= s.g.pos0 && (c.window <= 0 || key > s.g.pos1 - c.window)) continue;         // (seen by every row: left as it was)
       const int id = c.page_table[size_t(s.b) * c.page_table_stride + key / c.page_size];
       if (unsigned(id) >= unsigned(c.num_pages)) continue;
       const uint16_t* v = reinterpret_cast<const uint16_t*>(c.v_pool) + ((size_t(id) * c.page_size + key % c.page_size) * c.Hkv + s.kvh) * DH + col;
@@ -619,10 +640,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // Half of a row of Q: 16-byte asynchronous copies into the operand layout, zeros for rows that are not there.
 template <int DH>
 __device__ __forceinline__ void copy_q(const Args& a, const Segment& s, uint32_t q_tile, int h, int row, int ch) {
-  const int r = s.g.r0 + (s.turns ? 0 : h * 128) + row;
-  const bool on = r < s.g.r1;
+  const int r = (s.turns ? 0 : h * 128) + row;
+  const bool on = s.g.r0 + r < s.g.r1;
+  int token, head;
+  token_of(s, a, r, token, head);
   const uint16_t* src = reinterpret_cast<const uint16_t*>(a.c.q);
-  if (on) src += size_t(s.q0 + r / a.rep) * a.c.ldq + size_t(s.kvh * a.rep + r % a.rep) * DH + ch * (DH / 2);
+  if (on) src += size_t(s.q0 + token) * a.c.ldq + size_t(s.kvh * a.rep + head) * DH + ch * (DH / 2);
 #pragma unroll
   for (int i = 0; i < DH / 16; ++i) cp_async16(q_tile + tile_off(row, ch * (DH / 16) + i), src + (on ? i * 8 : 0), on);
   cp_async_commit();
@@ -676,11 +699,13 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     if (s.end) break;
     const bool turns = s.turns;
     const int nt = s.nt[h], nt_other = s.nt[h ^ 1];
-    const int r = s.g.r0 + (turns ? 0 : h * 128) + row;       // row of the head
-    const bool row_ok = r < s.g.r1;
-    const int hi = row_ok ? s.pos + r / a.rep : -1;           // keys lo .. hi are seen
+    const int r = (turns ? 0 : h * 128) + row, rows = s.g.r1 - s.g.r0;              // row of the item
+    const bool row_ok = r < rows;
+    int token, head;
+    token_of(s, a, r, token, head);
+    const int hi = row_ok ? s.pos + token : -1;               // keys lo .. hi are seen
     const int lo = c.window > 0 ? max(0, hi - c.window + 1) : 0;
-    const bool live = r - row + quarter * 32 < s.g.r1;        // (the same for both warps of a row)
+    const bool live = r - row + quarter * 32 < rows;          // (the same for both warps of a row)
     int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys
     const int key_step = turns ? 2 * KT : KT;
     float m_ref = NEG, m_next = NEG, l_sum = 0.f;
@@ -856,16 +881,15 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     const int cols = s.turns ? DH / 4 : DH / 2, col0 = (s.turns ? h * 2 + ch : ch) * cols;
     const float inv = l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum);      // (nothing seen: zero; NaN stays)
     if (*abort_flag) ok = false;
-    if (!s.whole && row_ok && ch == 0 && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + (r - s.g.r0)] = make_float2(m_ref, l_sum);
+    if (!s.whole && row_ok && ch == 0 && (!s.turns || h == 0)) a.ws_ml[size_t(slot) * ITEM_ROWS + r] = make_float2(m_ref, l_sum);
     if (live && (s.turns || nt > 0)) {
-      uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + (row_ok ? size_t(s.q0 + r / a.rep) * c.ldo + size_t(s.kvh * a.rep + r % a.rep) * DH : 0);
-      float* part = a.ws_o + size_t(slot) * DH * ITEM_ROWS + size_t(r - s.g.r0) * 4;
-#pragma unroll 1
-      for (int col = col0; col < col0 + cols; col += 16) {
-        __syncwarp();
-        float v[16];
+      token_of(s, a, r, token, head);
+      const long long dst = row_ok && ok ? (long long)(s.q0 + token) * c.ldo + (s.kvh * a.rep + head) * DH : -1;
+      float* part = a.ws_o + size_t(slot) * DH * ITEM_ROWS + size_t(r) * 4;
+      // 16 columns of the row, of both halves where they share it
+      auto read16 = [&](int col, float (&v)[16]) {
         uint32_t o[16];
-        if (s.turns) {
+        if (turns) {
           tmem_ld16(tmem + 256 + lane_base + col, o);         // (the first half always has a tile)
           tmem_wait_ld16(o);
 #pragma unroll
@@ -890,19 +914,61 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[e] = copy[e];
         }
-        if (s.whole && row_ok && ok) {
+        __syncwarp();
+      };
+      if (s.whole) {
+        // Four lanes exchange 16-byte pieces until each holds the same piece of four rows: a store of the warp then touches 16 half lines and not 32
+        // pieces of as many lines (which took the load/store unit 4000 clocks an item).  32 columns at a time, or 16 of a quarter of heads of 64.
+        const int q = lane & 3;
+        long long to[4];
 #pragma unroll
-          for (int e = 0; e < 16; e += 8) {
-            uint32_t p[4];
+        for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, dst, (lane & ~3) + i);
+#pragma unroll 1
+        for (int col = col0; col < col0 + cols; col += 32) {
+          const bool wide = col + 32 <= col0 + cols;
+          uint32_t p[4][4];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float v[16];
+            if (k == 0 || wide) read16(col + k * 16, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              p[2 * k + e / 4][e % 4] = F16 ? pack_f16_sat(v[2 * e] * inv, v[2 * e + 1] * inv, row_ok && (k == 0 || wide) ? c.status : nullptr)
+                                            : pack_bf16(v[2 * e] * inv, v[2 * e + 1] * inv);
+          }
+#pragma unroll
+          for (int m = 1; m < 4; m <<= 1) {
+            const bool up = (q & m) != 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (k & m) continue;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? p[k][e] : p[k + m][e], m);
+                if (up) p[k][e] = got;
+                else p[k + m][e] = got;
+              }
+            }
+          }
+          if (wide || q < 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              p[i] = F16 ? pack_f16_sat(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv, c.status) : pack_bf16(v[e + 2 * i] * inv, v[e + 2 * i + 1] * inv);
-            *reinterpret_cast<uint4*>(dst + col + e) = make_uint4(p[0], p[1], p[2], p[3]);
+              if (to[i] >= 0)
+                *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + to[i] + col + q * 8) = make_uint4(p[i][0], p[i][1], p[i][2], p[i][3]);
           }
-        } else if (row_ok && ok) {
+          __syncwarp();
+        }
+      } else {
+#pragma unroll 1
+        for (int col = col0; col < col0 + cols; col += 16) {
+          float v[16];
+          read16(col, v);
           // [column group][row][4]: the lanes of a warp write neighbouring 16 bytes
+          if (row_ok && ok) {
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + size_t((col + e) / 4) * ITEM_ROWS * 4) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          }
+          __syncwarp();
         }
       }
     }
@@ -1136,6 +1202,7 @@ cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::
   Args a{};
   a.c = c;
   a.rep = c.Hq / c.Hkv;
+  a.inv_rep = ((1u << 20) + a.rep - 1) / a.rep;
   a.scale_log2 = c.scale * 1.4426950408889634f;
   // the largest group of heads that leaves at most four SMs without work
   for (a.group = c.Hkv < 16 ? c.Hkv : 16; a.group > 1 && (c.Hkv % a.group || MAX_CTAS % a.group > 4); --a.group) {}
