@@ -38,8 +38,9 @@ constexpr int MAX_CTAS = 148;
 constexpr int ITEM_ROWS = 256;
 constexpr float NEG = -1.0e30f;
 // What an item costs where every CTA has many tiles, in units of 900 clocks: a tile whose halves take turns 2650 (its 64 KB at a CTA's share of
-// the memory's rate), a tile that both halves see 3550, the way from an item's last tile to the next one's first 4500.
-constexpr int COST_TURNS = 3, COST_BOTH = 4, COST_ITEM = 5;
+// the memory's rate), a tile that both halves see 3550, the way from an item's last tile to the next one's first 12 600 (with 5 in
+// place of 14 a prompt of 8192 tokens takes 638 us, not 548).
+constexpr int COST_TURNS = 3, COST_BOTH = 4, COST_ITEM = 14;
 constexpr float LAZY = 8.0f;         // the reference maximum moves, for the next tile, when the row's exceeds it by 2^8
 constexpr float LIMIT_BF16 = 60.0f, LIMIT_F16 = 15.0f;      // and at once when it exceeds it by more than the weights' type can hold
 constexpr int THREADS = 640;

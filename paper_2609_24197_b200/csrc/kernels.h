@@ -323,7 +323,7 @@ struct VerifyCall {                 // verify.cu
   void* ws;
   uint32_t* status;
 };
-struct VerifyScratch { int* first; float2* mx; int *top, *verdict; };
+struct VerifyScratch { int *first, *open; float2* mx; int *top, *verdict; };
 size_t verify_workspace_bytes(int B, int k);
 cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream);
 

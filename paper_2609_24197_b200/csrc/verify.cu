@@ -5,13 +5,14 @@
 //   behind the n drafts that stand one token more: from max(0, p_n - q_n) where draft n was refused, from p_n where none was; the lowest v whose
 //   cumulative sum exceeds u times the whole
 //
-// Both answers are integers that hang on a comparison of real numbers, so they are decided as if in 64 bits: the ratio is taken from 32-bit sums,
-// and once more from 64-bit sums where it comes so near to alpha that the 32-bit ones could be on the wrong side; the cumulative sum is 64-bit
-// throughout (a vocabulary has 10^5 steps, and a 32-bit sum would land on the wrong one in one of a hundred draws).
+// Both answers are integers that hang on a comparison of real numbers, and they are decided as if in 64 bits: each comparison is made with 32-bit
+// exponentials first and made again with 64-bit ones where the numbers come so near to one another that the first could be wrong.
 //
-// Two launches.  The first takes one (request, position) per cluster of blocks, reads the target's and the drafter's row once and decides whether
-// the position would be refused.  Items go out position by position, and one whose request is known to have been refused before is not read.
-// The second takes one request per cluster and samples.  The first is bound by memory, the second by the 64-bit exponentials of its row.
+// Three launches.  The first takes one (request, position) per cluster of blocks, reads the target's and the drafter's row once and decides whether
+// the position would be refused; items are started position by position, and one whose request is known to have been refused before is not read.
+// The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for the requests whose uniform
+// number came within 2^-15 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by memory,
+// the third by the 64-bit pipe (128 requests of 152 064 tokens in 64 bits alone: 238 us; XX with the 32-bit pass in front).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -24,6 +25,9 @@ namespace {
 
 constexpr int VT = 512;              // threads of a block
 constexpr int VW = VT / 32;
+#ifndef ROWS_S
+#define ROWS_S 2
+#endif
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A logit as it counts: NaN as -infinity (as in every arg-max of this library), +infinity as the largest finite number.
@@ -42,36 +46,65 @@ __device__ __forceinline__ float load_logit(const Row& r, int i) {
   return logit(value_of(reinterpret_cast<const __nv_bfloat16*>(r.z)[i]));
 }
 
-// Calls f(first index, values of N neighbours) for this thread's share of [begin, end): 16-byte loads, four of them in flight, scalar loads in
-// front of the first 16-byte boundary and behind the last.
-template <typename T, typename F>
+// 16 bytes of a row as logits.
+__device__ __forceinline__ void unpack16(const uint4& w, float (&v)[4], float) {
+  v[0] = logit(__uint_as_float(w.x)); v[1] = logit(__uint_as_float(w.y)); v[2] = logit(__uint_as_float(w.z)); v[3] = logit(__uint_as_float(w.w));
+}
+__device__ __forceinline__ void unpack16(const uint4& w, float (&v)[8], __half) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = logit(__half2float(__ushort_as_half(uint16_t(x[j] & 0xffffu))));
+    v[2 * j + 1] = logit(__half2float(__ushort_as_half(uint16_t(x[j] >> 16))));
+  }
+}
+__device__ __forceinline__ void unpack16(const uint4& w, float (&v)[8], __nv_bfloat16) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = logit(__uint_as_float(x[j] << 16));
+    v[2 * j + 1] = logit(__uint_as_float(x[j] & 0xffff0000u));
+  }
+}
+// A word of logits that are all -infinity.
+__device__ __forceinline__ uint32_t nothing(float) { return 0xff800000u; }
+__device__ __forceinline__ uint32_t nothing(__half) { return 0xfc00fc00u; }
+__device__ __forceinline__ uint32_t nothing(__nv_bfloat16) { return 0xff80ff80u; }
+// Calls f(first index, values of N neighbours) for this thread's share of [begin, end): 16-byte loads, U of them in flight (behind the last: values
+// of -infinity), scalar loads in front of the first 16-byte boundary and behind the last.
+template <int U, typename T, typename F>
 __device__ __forceinline__ void walk(const T* z, int begin, int end, F f) {
-  constexpr int N = 16 / sizeof(T), U = 4;
+  constexpr int N = 16 / sizeof(T);
   const int off = int((reinterpret_cast<uintptr_t>(z + begin) & 15) / sizeof(T));
   const int head = min(end, begin + (off ? N - off : 0)), n16 = (end - head) / N;
   for (int i = begin + int(threadIdx.x); i < head; i += VT) { float v[1] = {logit(value_of(z[i]))}; f(i, v); }
   const uint4* p = reinterpret_cast<const uint4*>(z + head);
+  const uint32_t none = nothing(T());
+  uint4 next[U];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = i0 + u * VT < n16 ? __ldg(p + i0 + u * VT) : make_uint4(none, none, none, none);
+  };
+  fetch(threadIdx.x);
   for (int i0 = threadIdx.x; i0 < n16; i0 += U * VT) {
     uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) if (i0 + u * VT < n16) w[u] = __ldg(p + i0 + u * VT);
+    for (int u = 0; u < U; ++u) w[u] = next[u];
+    fetch(i0 + U * VT);                           // (under way while these are dealt with)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u * VT >= n16) break;
       float v[N];
-      const T* e = reinterpret_cast<const T*>(&w[u]);
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = logit(value_of(e[j]));
+      unpack16(w[u], v, T());
       f(head + (i0 + u * VT) * N, v);
     }
   }
   for (int i = head + n16 * N + int(threadIdx.x); i < end; i += VT) { float v[1] = {logit(value_of(z[i]))}; f(i, v); }
 }
-template <typename F>
+template <int U, typename F>
 __device__ __forceinline__ void walk(const Row& r, int begin, int end, F f) {
-  if (r.dtype == CHUNK_F32) walk(reinterpret_cast<const float*>(r.z), begin, end, f);
-  else if (r.dtype == CHUNK_F16) walk(reinterpret_cast<const __half*>(r.z), begin, end, f);
-  else walk(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, f);
+  if (r.dtype == CHUNK_F32) walk<U>(reinterpret_cast<const float*>(r.z), begin, end, f);
+  else if (r.dtype == CHUNK_F16) walk<U>(reinterpret_cast<const __half*>(r.z), begin, end, f);
+  else walk<U>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, f);
 }
 
 struct MaxSum { float mx, sum; };
@@ -80,27 +113,29 @@ __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c) {
   if (m == -INFINITY) return a;
   return MaxSum{m, (a.mx > -INFINITY ? a.sum * ex2_ftz((a.mx - m) * c) : 0.f) + (b.mx > -INFINITY ? b.sum * ex2_ftz((b.mx - m) * c) : 0.f)};
 }
-// One pass: the running maximum and the sum of 2^((z - max) c) over this thread's share.
-__device__ __forceinline__ MaxSum sum_row(const Row& r, int begin, int end, float c) {
+// One pass: the running maximum and the sum of 2^((z - max) c) over this thread's share.  (Functions of their own, so that the three types' loops do
+// not share the registers of the kernel around them.)
+__device__ __noinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
   float mx = -INFINITY, sum = 0.f;
-  walk(r, begin, end, [&](int, auto& v) {
+  walk<4>(r, begin, end, [&](int, auto& v) {
     constexpr int N = sizeof(v) / sizeof(float);
     float mu = v[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) mu = fmaxf(mu, v[j]);
     if (mu > mx) { sum *= ex2_ftz((mx - mu) * c); mx = mu; }
-    if (mx > -INFINITY) {
+    // (nothing but -infinity so far: the differences are not numbers, and the sum stays nothing)
+    float part = 0.f;
 #pragma unroll
-      for (int j = 0; j < N; ++j) sum += ex2_ftz((v[j] - mx) * c);
-    }
+    for (int j = 0; j < N; ++j) part += ex2_ftz((v[j] - mx) * c);
+    sum += mx > -INFINITY ? part : 0.f;
   });
   return MaxSum{mx, sum};
 }
 // The largest value and its lowest index over this thread's share, as one number (argmax_key).
-__device__ __forceinline__ unsigned long long key_row(const Row& r, int begin, int end) {
+__device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
   unsigned long long best = 0;
   float mx = -INFINITY;
-  walk(r, begin, end, [&](int i, auto& v) {
+  walk<4>(r, begin, end, [&](int i, auto& v) {
     constexpr int N = sizeof(v) / sizeof(float);
 #pragma unroll
     for (int j = 0; j < N; ++j) if (v[j] > mx || best == 0) { mx = v[j]; best = argmax_key(v[j], i + j); }
@@ -112,15 +147,16 @@ __device__ __forceinline__ unsigned long long key_row(const Row& r, int begin, i
 __device__ __forceinline__ double weight64(float z, float m, double inv_t) {
   return z > -INFINITY ? exp((double(z) - double(m)) * inv_t) : 0.0;
 }
-__device__ __forceinline__ double sum_row64(const Row& r, int begin, int end, float m, double inv_t) {
-  double s = 0.0;
+template <typename W>
+__device__ __forceinline__ double sum_row64(const Row& r, int begin, int end, float m, W weigh) {
+  double s0 = 0.0, s1 = 0.0;
   if (m > -INFINITY)
-    walk(r, begin, end, [&](int, auto& v) {
+    walk<2>(r, begin, end, [&](int, auto& v) {
       constexpr int N = sizeof(v) / sizeof(float);
 #pragma unroll
-      for (int j = 0; j < N; ++j) s += weight64(v[j], m, inv_t);
+      for (int j = 0; j < N; ++j) (j & 1 ? s1 : s0) += weigh(v[j]);
     });
-  return s;
+  return s0 + s1;
 }
 
 __device__ __forceinline__ double shfl_xor64(double v, int off) { return __shfl_xor_sync(0xffffffffu, v, off); }
@@ -213,34 +249,33 @@ __global__ void verify_init_kernel(int* first, int B) {
   for (int i = threadIdx.x; i < B; i += blockDim.x) first[i] = 0x7fffffff;
 }
 
-// One (position, request) per cluster.  verdict[b * k + i] = 1 if the draft would stand; the row maxima (and for greedy requests the arg-max) are
-// left for the kernel behind.  skip: first[b] holds the lowest position refused so far.
-__global__ void __launch_bounds__(VT)
-verify_rows_kernel(VerifyCall c, VerifyScratch s, int S, int skip) {
-  pdl_wait();
-  pdl_trigger();
-  const int item = blockIdx.x / S, rank = blockIdx.x % S, i = item / c.B, b = item % c.B;
+// One item whose ratio is so near to alpha that the 32-bit sums do not decide: the same in 64 bits.  (Rare, and kept out of the registers of the rest.)
+__device__ __noinline__ void verify_row64(const VerifyCall& c, const VerifyScratch& s, int S, int rank, int skip, int i, int b, Reduce64& sh_sum, float mt,
+                                          float md) {
   const Request r = request(c, b);
-  __shared__ MaxSum sh_warp[2][VW];
-  __shared__ unsigned long long sh_block[2][8];
-  __shared__ Reduce64 sh_sum;
-  __shared__ ReduceKey sh_key;
-  __shared__ float sh_max[2];
-  __shared__ int sh_go, sh_near;
-  if (i >= r.drafts) return;                      // (uniform for the cluster)
-  if (threadIdx.x == 0) {
-    sh_near = 0;
-    sh_go = skip ? *reinterpret_cast<volatile int*>(s.first + b) >= i : 1;
+  const int at = b * c.k + i, id = c.ids[at];
+  const bool both = c.draft != nullptr;
+  const Row zt = row_at(c.target, c.t_dtype, c.ld_t, r.row0 + i), zd = both ? row_at(c.draft, c.d_dtype, c.ld_d, at) : zt;
+  int begin, end, dbegin, dend;
+  share_of(c.V, S, rank, begin, end);
+  share_of(c.Vd, S, rank, dbegin, dend);
+  const double inv_t = 1.0 / double(r.t);
+  double st = sum_row64(zt, begin, end, mt, [&](float z) { return weight64(z, mt, inv_t); });
+  double sd = both ? sum_row64(zd, dbegin, dend, md, [&](float z) { return weight64(z, md, inv_t); }) : 0.0;
+  cluster_sum2(sh_sum, S, rank, st, sd);
+  if (rank == 0 && threadIdx.x == 0) {
+    const double p = weight64(load_logit(zt, id), mt, inv_t) / st;
+    const int di = both ? draft_index(c, id) : -1;
+    const double q = !both ? 1.0 : di >= 0 ? weight64(load_logit(zd, di), md, inv_t) / sd : 0.0;
+    const int verdict = p > 0.0 && (q > 0.0 ? p / q : INFINITY) >= double(c.alpha[at]);
+    s.verdict[at] = verdict;
+    if (skip && !verdict) atomicMin(s.first + b, i);
   }
-  cluster_or_block_sync(S);                       // from here every block of the cluster runs, and its shared memory may be written to
-  if (skip) {
-    // all blocks of the cluster go by what the leader read
-    const bool go = ld_cluster_u32(mapa_rank(smem_u32(&sh_go), 0)) != 0;
-    if (!go) {
-      cluster_or_block_sync(S);
-      return;
-    }
-  }
+}
+
+__device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScratch& s, int S, int rank, int skip, int i, int b, MaxSum (&sh_warp)[2][VW],
+                                           unsigned long long (&sh_block)[2][8], Reduce64& sh_sum, ReduceKey& sh_key, float (&sh_max)[2], int& sh_near) {
+  const Request r = request(c, b);
   const int at = b * c.k + i, id = c.ids[at];
   const Row zt = row_at(c.target, c.t_dtype, c.ld_t, r.row0 + i);
   int begin, end;
@@ -317,37 +352,222 @@ verify_rows_kernel(VerifyCall c, VerifyScratch s, int S, int skip) {
   }
   cluster_or_block_sync(S);
   if (!sh_near) return;
-  // so near to alpha that the 32-bit sums do not decide: the same in 64 bits
-  const double inv_t = 1.0 / double(r.t);
-  double st = sum_row64(zt, begin, end, sh_max[0], inv_t), sd = both ? sum_row64(zd, dbegin, dend, sh_max[1], inv_t) : 0.0;
-  cluster_sum2(sh_sum, S, rank, st, sd);
-  if (rank == 0 && threadIdx.x == 0) {
-    const double p = weight64(load_logit(zt, id), sh_max[0], inv_t) / st;
-    const int di = both ? draft_index(c, id) : -1;
-    const double q = !both ? 1.0 : di >= 0 ? weight64(load_logit(zd, di), sh_max[1], inv_t) / sd : 0.0;
-    const int verdict = p > 0.0 && (q > 0.0 ? p / q : INFINITY) >= double(c.alpha[at]);
-    s.verdict[at] = verdict;
-    if (skip && !verdict) atomicMin(s.first + b, i);
+  verify_row64(c, s, S, rank, skip, i, b, sh_sum, sh_max[0], sh_max[1]);
+}
+
+// One (position, request) per cluster, position by position.  verdict[b * k + i] = 1 if the draft would stand; the row maxima (and for greedy requests
+// the arg-max) are left for the kernel behind.  skip: first[b] holds the lowest position refused so far, and items behind it are passed over.
+__global__ void __launch_bounds__(VT, 2)
+verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S, int skip) {
+  pdl_wait();
+  pdl_trigger();
+  const int item = blockIdx.x / S, rank = blockIdx.x % S, i = item / c.B, b = item % c.B;
+  __shared__ MaxSum sh_warp[2][VW];
+  __shared__ unsigned long long sh_block[2][8];
+  __shared__ Reduce64 sh_sum;
+  __shared__ ReduceKey sh_key;
+  __shared__ float sh_max[2];
+  __shared__ int sh_go, sh_near;
+  if (i >= request(c, b).drafts) return;          // (uniform for the cluster)
+  if (threadIdx.x == 0) {
+    sh_near = 0;
+    sh_go = skip ? *reinterpret_cast<volatile int*>(s.first + b) >= i : 1;
   }
+  cluster_or_block_sync(S);                       // every block of the cluster runs, and its shared memory may be written to
+  if (skip) {
+    // all blocks of the cluster go by what the leader read
+    const bool go = ld_cluster_u32(mapa_rank(smem_u32(&sh_go), 0)) != 0;
+    if (!go) {
+      cluster_or_block_sync(S);
+      return;
+    }
+  }
+  verify_row(c, s, S, rank, skip, i, b, sh_warp, sh_block, sh_sum, sh_key, sh_max, sh_near);
+}
+
+// ------------------------------------------------------------------ the token behind the drafts that stand
+// A row is full of 64-bit exponentials here: e^x = 2^n 2^(i / 256) e^f with |f| <= ln 2 / 512, 2^(i / 256) from a table in shared memory (times the
+// factor that the row's weights need anyway) and e^f by its series up to f^4 / 24 (the next term is 4e-17): 10 operations in 64 bits, where the
+// library's function takes three times as many.  Nothing below e^-700, which no sum of weights with a 1 among them shows.
+struct Weights {
+  double table[256];
+};
+template <bool EXACT>
+struct RowWeights {                    // the weights of one row's logits, from its maximum, temperature and factor
+  const Weights* w;
+  const void* z;
+  float m, inv_tf;
+  double md, inv_t;
+  float log2_t, factor;                // of the 32-bit ones: log2(e) / temperature
+  bool bf16;
+  __device__ __forceinline__ double operator()(float v) const {
+    if (!EXACT) return double(quick(v));
+    const double magic = 6755399441055744.0;                  // 1.5 2^52: whole numbers end up in the low bits
+    const double x = (double(v) - md) * inv_t, t = fma(x, 369.32993046757655, magic);      // 256 / ln 2
+    const int k = __double2loint(t);
+    const double f = fma(t - magic, -0.0027076061740622863, x);                              // ln 2 / 256
+    const double p = f * fma(f, fma(f, fma(f, 1.0 / 24.0, 1.0 / 6.0), 0.5), 1.0), y = w->table[k & 255];
+    const double r = fma(y, p, y);
+    return (v - m) * inv_tf > -700.f ? __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r)) : 0.0;
+  }
+  __device__ __forceinline__ float quick(float v) const { return ex2_ftz((v - m) * log2_t) * factor; }
+  // A logit as it lies in memory, and what it says.  (Two steps, so that many loads go out before the first is looked at; no branch on the type.)
+  template <bool F32>
+  __device__ __forceinline__ uint32_t raw(int i) const {
+    return F32 ? reinterpret_cast<const uint32_t*>(z)[i] : reinterpret_cast<const uint16_t*>(z)[i];
+  }
+  template <bool F32>
+  __device__ __forceinline__ float value(uint32_t x) const {
+    if (F32) return logit(__uint_as_float(x));
+    return logit(bf16 ? __uint_as_float(x << 16) : __half2float(__ushort_as_half(uint16_t(x))));
+  }
+  // (a word that says -infinity)
+  template <bool F32>
+  __device__ __forceinline__ uint32_t none() const { return F32 ? 0xff800000u : bf16 ? 0xff80u : 0xfc00u; }
+};
+// The table times a factor; e^700 has room above it.
+__device__ __forceinline__ void weights_init(Weights& w, double factor) {
+  for (int i = threadIdx.x; i < 256; i += VT) w.table[i] = exp2(double(i) / 256.0) * factor;
 }
 
 struct SampleShared {
+  Weights p, q;
   Reduce64 sum;
   ReduceKey key;
   double warp[VW];
   double block[8];
-  float q[VW][32];
-  int n;
+  float map[VW][128];
+  int n, found, last;
 };
 
-// One request per cluster: counts the drafts that stand and takes the token behind them.
-__global__ void __launch_bounds__(VT)
-verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
+// Sum of a row's weights over this thread's share of [begin, end).  (The weights come by value: through a reference every use is a load from local memory.)
+template <bool EXACT>
+__device__ __noinline__ double row_sum(RowWeights<EXACT> w, Row r, int begin, int end) {
+  double s0 = 0.0, s1 = 0.0;
+  walk<EXACT ? 2 : 4>(r, begin, end, [&](int, auto& v) {
+    constexpr int N = sizeof(v) / sizeof(float);
+    if (EXACT) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) (j & 1 ? s1 : s0) += w(v[j]);
+    } else {
+      float part = 0.f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) part += w.quick(v[j]);
+      s0 += double(part);
+    }
+  });
+  return s0 + s1;
+}
+
+// The first place in an ascending map whose token is v or above (one warp).
+__device__ __forceinline__ int map_place(const int* map, int n, int v, int lane) {
+  int lo = 0, hi = n;                                          // it is in [lo, hi]
+  while (hi > lo) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && map[at] < v));
+    if (below == 0) return lo;
+    lo += (below - 1) * step + 1;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
+}
+
+// One warp's sum of max(0, p - q) over tokens [begin, end); MINUS: 0 p alone, 1 q has 16 bits, 2 it has 32.  gone: a token that counts nothing.
+template <bool EXACT, bool F32, int MINUS>
+__device__ __noinline__ double rest_sum(RowWeights<EXACT> p, RowWeights<EXACT> q, int begin, int end, int gone, const int* map, int n_map, float* q_of) {
+  const int lane = threadIdx.x & 31;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  auto add = [&](float (&t)[4], const float (&d)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (EXACT) s[u] += MINUS ? fmax(0.0, p(t[u]) - q(d[u])) : p(t[u]);
+      else t[u] = MINUS ? fmaxf(0.f, p.quick(t[u]) - q.quick(d[u])) : p.quick(t[u]);
+    }
+    if (!EXACT) s[0] += double((t[0] + t[1]) + (t[2] + t[3]));
+  };
+  auto target = [&](int base, uint32_t (&t)[4]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int v = base + u * 32 + lane;
+      t[u] = v < end && v != gone ? p.template raw<F32>(v) : p.template none<F32>();
+    }
+  };
+  if (MINUS && map) {
+    int at = begin < end ? map_place(map, n_map, begin, lane) : 0;
+    uint32_t t_next[4];
+    target(begin, t_next);
+    for (int base = begin; base < end; base += 128) {
+      float t[4], d[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) t[u] = p.template value<F32>(t_next[u]);
+      target(base + 128, t_next);
+      // 128 neighbours hold at most as many entries of the map, which lie together
+#pragma unroll
+      for (int u = 0; u < 4; ++u) q_of[u * 32 + lane] = -INFINITY;
+      __syncwarp();
+      int count = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = at + u * 32 + lane, v = i < n_map ? map[i] : 0x7fffffff;
+        const bool in = v >= base && v < base + 128;
+        if (in) q_of[v - base] = q.template value<MINUS == 2>(q.template raw<MINUS == 2>(i));
+        count += __popc(__ballot_sync(0xffffffffu, in));
+      }
+      at += count;
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) d[u] = q_of[u * 32 + lane];
+      __syncwarp();
+      add(t, d);
+    }
+  } else {
+    // two steps of 128 tokens under way in front of the one that is added
+    constexpr int AHEAD = 2;
+    uint32_t t[AHEAD][4], d[AHEAD][4];
+    auto fetch = [&](int base, int at) {
+      target(base, t[at]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int v = base + u * 32 + lane;
+        d[at][u] = MINUS && v < end ? q.template raw<MINUS == 2>(v) : q.template none<MINUS == 2>();
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) fetch(begin + i * 128, i);
+    for (int base = begin; base < end; base += AHEAD * 128) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        float ti[4], di[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { ti[u] = p.template value<F32>(t[i][u]); di[u] = MINUS ? q.template value<MINUS == 2>(d[i][u]) : -INFINITY; }
+        fetch(base + (AHEAD + i) * 128, i);
+        add(ti, di);
+      }
+    }
+  }
+  double all = (s[0] + s[1]) + (s[2] + s[3]);
+  for (int off = 16; off > 0; off >>= 1) all += shfl_xor64(all, off);
+  return all;
+}
+
+// One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by less
+// than 2^-19 of itself on average over a row (its exponent, of size x, by 2^-23 x; the special function by 2^-22; sums of four), and from there on
+// sums are 64-bit ones: 2^-17 of the rows' whole weight leaves room.  A goal that is not that far inside its token's share is left to the kernel with EXACT.
+template <bool EXACT>
+__global__ void __launch_bounds__(VT, 2)
+verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S) {
   pdl_wait();
   pdl_trigger();
   __shared__ SampleShared sh;
   const int b = blockIdx.x / S, rank = blockIdx.x % S, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (EXACT && s.open[b] == 0) return;            // (uniform for the cluster)
   const Request r = request(c, b);
+  if (EXACT) {
+    weights_init(sh.p, 1.0);
+    weights_init(sh.q, 1.0);
+  }
+  if (!EXACT && rank == 0 && threadIdx.x == 0) s.open[b] = 0;
+  if (threadIdx.x == 0) { sh.found = 0x7fffffff; sh.last = -1; }
   if (r.drafts >= 0 && S > 1) cluster_sync_all();  // from here every block of the cluster runs, and its shared memory may be written to
   if (warp == 0) {
     int n = max(r.drafts, 0);
@@ -357,7 +577,7 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
       if (m) { n = base + __ffs(m) - 1; break; }
     }
     if (lane == 0) sh.n = n;
-    if (rank == 0) {
+    if (!EXACT && rank == 0) {
       if (lane == 0) c.n_accept[b] = n;
       for (int i = lane; i <= c.k; i += 32)
         if (i != n || r.drafts < 0) c.tokens[size_t(b) * (c.k + 1) + i] = i < n ? c.ids[b * c.k + i] : -1;
@@ -371,7 +591,7 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
   int* out = c.tokens + size_t(b) * (c.k + 1) + n;
   int begin, end;
   share_of(c.V, S, rank, begin, end);
-  float mt, md = 0.f;
+  float mt, md = -INFINITY;
   if (refused && r.greedy) {
     if (rank == 0 && threadIdx.x == 0) *out = s.top[at];
     return;
@@ -387,63 +607,52 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
       return;
     }
   }
-  const double inv_t = 1.0 / double(r.t), u = double(c.u[b]);
-  const bool both = refused && c.draft != nullptr;
-  const int gone = refused && !both ? c.ids[at] : -1;       // the arg-max drafter's token, which takes all of its q
+  if (!(mt > -INFINITY)) {                        // a row without any weight: as an arg-max of nothing (uniform for the cluster)
+    if (rank == 0 && threadIdx.x == 0) *out = 0;
+    return;
+  }
+  const bool both = refused && c.draft != nullptr && md > -INFINITY;
   const Row zd = both ? row_at(c.draft, c.d_dtype, c.ld_d, at) : zt;
-  double wt = 1.0, wd = 0.0;                                  // weights are p * wt and q * wd, up to a common factor
+  const double inv_t = 1.0 / double(r.t);
+  const float inv_tf = fminf(float(inv_t), 3.0e38f);
+  const bool t32 = c.t_dtype == CHUNK_F32, d32 = c.d_dtype == CHUNK_F32;
+  const float log2_t = fminf(fmaxf(LOG2E / r.t, 1e-30f), 1e30f);
+  RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, double(mt), inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
+  RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, double(md), inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
+  const int gone_token = refused && !c.draft ? c.ids[at] : -1;        // the arg-max drafter's, which takes all of its q
   if (both) {
     int dbegin, dend;
     share_of(c.Vd, S, rank, dbegin, dend);
-    double st = sum_row64(zt, begin, end, mt, inv_t), sd = sum_row64(zd, dbegin, dend, md, inv_t);
-    cluster_sum2(sh.sum, S, rank, st, sd);
-    wt = 1.0 / st;
-    wd = sd > 0.0 ? 1.0 / sd : 0.0;
+    double st = row_sum(p, zt, begin, end), sd = row_sum(q, zd, dbegin, dend);
+    cluster_sum2(sh.sum, S, rank, st, sd);        // (its barriers lie between the tables' last use and the next lines)
+    if (EXACT) {
+      weights_init(sh.p, 1.0 / st);
+      weights_init(sh.q, 1.0 / sd);
+      __syncthreads();
+    } else {
+      p.factor = float(1.0 / st);
+      q.factor = float(1.0 / sd);
+    }
   }
-  // a warp's part of the block's share, walked 32 neighbours at a time
-  const int per = ((end - begin + VW - 1) / VW + 31) & ~31;
-  const int wb = min(end, begin + warp * per), we = min(end, wb + per);
-  for (int less = 1; less >= 0; --less) {                     // once more without q where max(0, p - q) is nothing anywhere
-    auto each = [&](auto take) {
-      int mapped = 0;
-      if (both && less && c.vocab_map) {                      // map entries below the part's first token
-        int hi = c.Vd;
-        while (mapped < hi) { const int mid = (mapped + hi) >> 1; if (c.vocab_map[mid] < wb) mapped = mid + 1; else hi = mid; }
-      }
-      for (int base = wb; base < we; base += 32) {
-        const int v = base + lane;
-        const bool on = v < we;
-        float d = -INFINITY;
-        if (both && less) {
-          if (!c.vocab_map) {
-            if (on && v < c.Vd) d = load_logit(zd, v);
-          } else {
-            // (32 neighbours hold at most 32 entries of an ascending map)
-            sh.q[warp][lane] = -INFINITY;
-            __syncwarp();
-            const int m = mapped + lane < c.Vd ? c.vocab_map[mapped + lane] : 0x7fffffff;
-            const bool in = m >= base && m < base + 32;
-            if (in) sh.q[warp][m - base] = load_logit(zd, mapped + lane);
-            mapped += __popc(__ballot_sync(0xffffffffu, in));
-            __syncwarp();
-            d = sh.q[warp][lane];
-            __syncwarp();
-          }
-        }
-        double w = 0.0;
-        if (on && mt > -INFINITY && !(less && v == gone)) {
-          w = weight64(load_logit(zt, v), mt, inv_t) * wt;
-          if (both && less && d > -INFINITY) w = fmax(0.0, w - weight64(d, md, inv_t) * wd);
-        }
-        if (take(v, w)) return;
-      }
+  const double u = double(c.u[b]);
+  for (int less = 1; less >= 0; --less) {         // once more without q where max(0, p - q) is nothing anywhere
+    const int gone = less ? gone_token : -1, minus = both && less ? (d32 ? 2 : 1) : 0;
+    auto sum_of = [&](int from, int to) {
+      float* q_of = sh.map[warp];
+      if (minus == 0) return t32 ? rest_sum<EXACT, true, 0>(p, q, from, to, gone, nullptr, 0, q_of) : rest_sum<EXACT, false, 0>(p, q, from, to, gone, nullptr, 0, q_of);
+      if (minus == 1) return t32 ? rest_sum<EXACT, true, 1>(p, q, from, to, gone, c.vocab_map, c.Vd, q_of) : rest_sum<EXACT, false, 1>(p, q, from, to, gone, c.vocab_map, c.Vd, q_of);
+      return t32 ? rest_sum<EXACT, true, 2>(p, q, from, to, gone, c.vocab_map, c.Vd, q_of) : rest_sum<EXACT, false, 2>(p, q, from, to, gone, c.vocab_map, c.Vd, q_of);
     };
-    double mine = 0.0;
-    each([&](int, double w) { mine += w; return false; });
-    for (int off = 16; off > 0; off >>= 1) mine += shfl_xor64(mine, off);
-    __syncthreads();
-    if (lane == 0) sh.warp[warp] = mine;
-    __syncthreads();
+    // sums of the warps' parts of [from, to) into sh.warp; the width of a part
+    auto parts_of = [&](int from, int to) {
+      const int per = ((to - from + VW - 1) / VW + 31) & ~31, wb = min(to, from + warp * per);
+      const double mine = sum_of(wb, min(to, wb + per));
+      __syncthreads();                            // (the sums in front have been read)
+      if (lane == 0) sh.warp[warp] = mine;
+      __syncthreads();
+      return per;
+    };
+    const int per = parts_of(begin, end);
     if (threadIdx.x < unsigned(S)) {
       double x = 0.0;
       for (int w = 0; w < VW; ++w) x += sh.warp[w];
@@ -452,14 +661,21 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
     cluster_or_block_sync(S);
     double whole = 0.0;
     for (int j = 0; j < S; ++j) whole += sh.block[j];
-    if (!(whole > 0.0)) {
-      if (less) { cluster_or_block_sync(S); continue; }       // (the others may still be reading)
-      if (rank == 0 && threadIdx.x == 0) *out = 0;            // a row without any weight: as an arg-max of nothing
+    // (how far the 32-bit sums may be off: p and q weigh 1 each where both count, else p is all there is)
+    const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * (1.0 / 131072.0);
+    if (!EXACT && both && less && !(whole > 64.0 * tol)) {    // nearly nothing left of p - q: left to the other kernel
+      if (rank == 0 && threadIdx.x == 0) s.open[b] = 1;
       break;
     }
-    // the block, then the warp, in which the sum passes u * whole; where rounding hides the place, the last with any weight
+    if (!(whole > 0.0) && less) {
+      cluster_or_block_sync(S);                   // (the others may still be reading)
+      continue;
+    }
+    // The block, the warp's part, the part of that part in which the sum passes u * whole, and in there the token; where rounding hides the place,
+    // the last with any weight.
     const double goal = u * whole;
-    auto find = [&](const double* part, int count, double& before) {
+    double before = 0.0;
+    auto find = [&](const double* part, int count) {
       int last = 0;
       double x = before, x_last = before;
       for (int j = 0; j < count; ++j) {
@@ -470,20 +686,49 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
       before = x_last;
       return last;
     };
-    double before = 0.0;
-    if (find(sh.block, S, before) == rank && find(sh.warp, VW, before) == warp) {
-      int found = -1, last = wb;
+    if (find(sh.block, S) != rank) break;
+    const int from = begin + find(sh.warp, VW) * per, to = min(end, from + per);
+    const int fine = parts_of(from, to);
+    int v0 = from + find(sh.warp, VW) * fine;
+    const int v1 = min(to, v0 + fine);
+    for (; v0 < v1; v0 += VT) {
+      // a token for every thread
+      const int v = v0 + int(threadIdx.x);
+      float* q_of = &sh.map[0][0];
+      const bool on = v < v1 && v != gone;
+      double w = 0.0;
+      if (minus && c.vocab_map) {
+        q_of[threadIdx.x] = -INFINITY;
+        __syncthreads();
+        const int i = map_place(c.vocab_map, c.Vd, v0, lane) + int(threadIdx.x), m = i < c.Vd ? c.vocab_map[i] : 0x7fffffff;
+        if (m >= v0 && m < v0 + VT) q_of[m - v0] = load_logit(zd, i);
+        __syncthreads();
+        if (on) w = fmax(0.0, p(load_logit(zt, v)) - q(q_of[threadIdx.x]));
+      } else if (on) {
+        w = p(load_logit(zt, v));
+        if (minus) w = fmax(0.0, w - q(load_logit(zd, v)));
+      }
+      double run = w;
+      for (int off = 1; off < 32; off <<= 1) { const double o = shfl_up64(run, off); if (lane >= off) run += o; }
+      __syncthreads();
+      if (lane == 31) sh.warp[warp] = run;
+      __syncthreads();
       double x = before;
-      each([&](int v, double w) {
-        double run = w;
-        for (int off = 1; off < 32; off <<= 1) { const double o = shfl_up64(run, off); if (lane >= off) run += o; }
-        const unsigned hit = __ballot_sync(0xffffffffu, w > 0.0 && x + run > goal), any = __ballot_sync(0xffffffffu, w > 0.0);
-        if (any) last = v - lane + 31 - __clz(any);
-        if (hit) { found = v - lane + __ffs(hit) - 1; return true; }
-        x += __shfl_sync(0xffffffffu, run, 31);
-        return false;
-      });
-      if (lane == 0) *out = found >= 0 ? found : last;
+      for (int j = 0; j < warp; ++j) x += sh.warp[j];
+      if (w > 0.0) {
+        if (x + run > goal) atomicMin(&sh.found, v);
+        atomicMax(&sh.last, v);
+      }
+      __syncthreads();
+      // (the goal's own error is the whole's)
+      if (!EXACT && v == sh.found && !(goal - (x + run - w) > 2.0 * tol && x + run - goal > 2.0 * tol)) s.open[b] = 1;
+      for (int j = 0; j < VW; ++j) before += sh.warp[j];
+      __syncthreads();
+      if (sh.found != 0x7fffffff) break;          // (uniform for the block)
+    }
+    if (threadIdx.x == 0) {
+      *out = sh.found != 0x7fffffff ? sh.found : max(sh.last, 0);
+      if (!EXACT && sh.found == 0x7fffffff) s.open[b] = 1;
     }
     break;
   }
@@ -493,25 +738,27 @@ verify_sample_kernel(VerifyCall c, VerifyScratch s, int S) {
 }  // namespace
 
 size_t verify_workspace_bytes(int B, int k) {
-  return ((size_t(B) * 4 + 255) & ~size_t(255)) + size_t(B) * k * (sizeof(float2) + 8) + 256;
+  return ((size_t(B) * 8 + 255) & ~size_t(255)) + size_t(B) * k * (sizeof(float2) + 8) + 256;
 }
 
 cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
   VerifyScratch s;
   uint8_t* ws = reinterpret_cast<uint8_t*>(c.ws);
   s.first = reinterpret_cast<int*>(ws);
-  s.mx = reinterpret_cast<float2*>(ws + ((size_t(c.B) * 4 + 255) & ~size_t(255)));
+  s.open = s.first + c.B;
+  s.mx = reinterpret_cast<float2*>(ws + ((size_t(c.B) * 8 + 255) & ~size_t(255)));
   s.top = reinterpret_cast<int*>(s.mx + size_t(c.B) * c.k);
   s.verdict = s.top + size_t(c.B) * c.k;
   cudaError_t e = cudaSuccess;
   const long long items = (long long)c.B * c.k;
-  auto blocks_for = [&](long long n, int least) {              // blocks of a cluster: two for every SM, as long as each has a few KB to read
+  // blocks of a cluster: two for every SM where there are few items, as long as each has a few KB to read
+  auto blocks_for = [&](long long n, int least) {
     int S = least;
-    while (S < 8 && n * S < 2 * 148 && c.V / (2 * S) >= 2048) S *= 2;
+    while (S < 8 && n * 2 * S <= 2 * 148 && c.V / (2 * S) >= 2048) S *= 2;
     return S;
   };
   if (items > 0) {
-    const int S = blocks_for(items, 1), skip = items * S > 4 * 148;
+    const int S = blocks_for(items, c.V >= 16384 ? ROWS_S : 1), skip = items * S > 2 * 148;
     if (skip) {
       e = launch_pdl(verify_init_kernel, dim3(1), dim3(256), 0, stream, s.first, c.B);
       if (e != cudaSuccess) return e;
@@ -519,8 +766,10 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip);
     if (e != cudaSuccess) return e;
   }
-  const int S = blocks_for(c.B, 1);
-  return launch_pdl_cluster(verify_sample_kernel, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
+  const int S = blocks_for(c.B, 1), S64 = blocks_for(1, 1);   // (few requests are left for the third)
+  e = launch_pdl_cluster(verify_sample_kernel<false>, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
+  if (e != cudaSuccess) return e;
+  return launch_pdl_cluster(verify_sample_kernel<true>, dim3(unsigned(c.B) * S64), dim3(VT), dim3(S64), 0, stream, c, s, S64);
 }
 
 }  // namespace hspec
