@@ -11,8 +11,9 @@
 // Three launches.  The first takes one (request, position) per cluster of blocks, reads the target's and the drafter's row once and decides whether
 // the position would be refused; items are started position by position, and one whose request is known to have been refused before is not read.
 // The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for the requests whose uniform
-// number came within 2^-15 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by memory,
-// the third by the 64-bit pipe (128 requests of 152 064 tokens in 64 bits alone: 238 us; XX with the 32-bit pass in front).
+// number came within 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by memory,
+// the third by the 64-bit pipe (128 requests of 152 064 tokens: 238 us in 64 bits alone,
+// 69 and 61 in two).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -25,9 +26,6 @@ namespace {
 
 constexpr int VT = 512;              // threads of a block
 constexpr int VW = VT / 32;
-#ifndef ROWS_S
-#define ROWS_S 2
-#endif
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A logit as it counts: NaN as -infinity (as in every arg-max of this library), +infinity as the largest finite number.
@@ -46,24 +44,31 @@ __device__ __forceinline__ float load_logit(const Row& r, int i) {
   return logit(value_of(reinterpret_cast<const __nv_bfloat16*>(r.z)[i]));
 }
 
-// 16 bytes of a row as logits.
+// 16 bytes of a row as logits, or as they are.
+template <bool LOGITS = true>
 __device__ __forceinline__ void unpack16(const uint4& w, float (&v)[4], float) {
-  v[0] = logit(__uint_as_float(w.x)); v[1] = logit(__uint_as_float(w.y)); v[2] = logit(__uint_as_float(w.z)); v[3] = logit(__uint_as_float(w.w));
+  v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) if (LOGITS) v[j] = logit(v[j]);
 }
+template <bool LOGITS = true>
 __device__ __forceinline__ void unpack16(const uint4& w, float (&v)[8], __half) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[2 * j] = logit(__half2float(__ushort_as_half(uint16_t(x[j] & 0xffffu))));
-    v[2 * j + 1] = logit(__half2float(__ushort_as_half(uint16_t(x[j] >> 16))));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[j]));
+    v[2 * j] = LOGITS ? logit(f.x) : f.x;
+    v[2 * j + 1] = LOGITS ? logit(f.y) : f.y;
   }
 }
+template <bool LOGITS = true>
 __device__ __forceinline__ void unpack16(const uint4& w, float (&v)[8], __nv_bfloat16) {
   const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[2 * j] = logit(__uint_as_float(x[j] << 16));
-    v[2 * j + 1] = logit(__uint_as_float(x[j] & 0xffff0000u));
+    const float a = __uint_as_float(x[j] << 16), b = __uint_as_float(x[j] & 0xffff0000u);
+    v[2 * j] = LOGITS ? logit(a) : a;
+    v[2 * j + 1] = LOGITS ? logit(b) : b;
   }
 }
 // A word of logits that are all -infinity.
@@ -113,23 +118,86 @@ __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c) {
   if (m == -INFINITY) return a;
   return MaxSum{m, (a.mx > -INFINITY ? a.sum * ex2_ftz((a.mx - m) * c) : 0.f) + (b.mx > -INFINITY ? b.sum * ex2_ftz((b.mx - m) * c) : 0.f)};
 }
-// One pass: the running maximum and the sum of 2^((z - max) c) over this thread's share.  (Functions of their own, so that the three types' loops do
-// not share the registers of the kernel around them.)
-__device__ __noinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
+// One pass: the running maximum and the sum of 2^((z - max) c) over this thread's share.  16 values at a time with one maximum and one rescaling, two
+// values to an instruction where there is one (14 instructions a value were more than the memory leaves time for; these are 5).  Values are taken as
+// they are: NaN and +infinity make the sum NaN, and such a share is gone through once more with every value looked at.
+template <typename T>
+__device__ __forceinline__ MaxSum sum_share(const T* z, int begin, int end, float c) {
+  constexpr int N = 16 / sizeof(T), U = 4, G = 16 / N;          // values of a word, words under way, words of 16 values
+  float mx = -FLT_MAX, sum = 0.f;
+  auto one = [&](float v) {
+    const float m = fmaxf(mx, v);
+    sum = sum * ex2_ftz((mx - m) * c) + ex2_ftz((v - m) * c);
+    mx = m;
+  };
+  const int off = int((reinterpret_cast<uintptr_t>(z + begin) & 15) / sizeof(T));
+  const int head = min(end, begin + (off ? N - off : 0)), n16 = (end - head) / N;
+  for (int i = begin + int(threadIdx.x); i < head; i += VT) one(value_of(z[i]));
+  for (int i = head + n16 * N + int(threadIdx.x); i < end; i += VT) one(value_of(z[i]));
+  const uint4* p = reinterpret_cast<const uint4*>(z + head);
+  const uint32_t none = nothing(T());
+  uint4 next[U];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = i0 + u * VT < n16 ? __ldg(p + i0 + u * VT) : make_uint4(none, none, none, none);
+  };
+  const uint64_t c2 = pack_f32x2(c, c);
+  fetch(threadIdx.x);
+  for (int i0 = threadIdx.x; i0 < n16; i0 += U * VT) {
+    uint4 w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = next[u];
+    fetch(i0 + U * VT);                           // (under way while these are dealt with)
+#pragma unroll
+    for (int g = 0; g < U / G; ++g) {
+      float v[16];
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        float x[N];
+        unpack16<false>(w[g * G + u], x, T());
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[u * N + j] = x[j];
+      }
+      float m = mx;
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) m = fmaxf(fmaxf(m, v[j]), v[j + 1]);
+      const uint64_t neg = pack_f32x2(-m, -m);
+      uint64_t part[2] = {0ull, 0ull};
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        float e0, e1;
+        unpack_f32x2(fma_f32x2(add_f32x2(pack_f32x2(v[j], v[j + 1]), neg), c2, 0ull), e0, e1);
+        part[(j >> 1) & 1] = add_f32x2(part[(j >> 1) & 1], pack_f32x2(ex2_ftz(e0), ex2_ftz(e1)));
+      }
+      float s0, s1;
+      unpack_f32x2(add_f32x2(part[0], part[1]), s0, s1);
+      sum = sum * ex2_ftz((mx - m) * c) + (s0 + s1);
+      mx = m;
+    }
+  }
+  return MaxSum{mx, sum};
+}
+// (Functions of their own, so that the three types' loops do not share the registers of the kernel around them.)
+__device__ __noinline__ MaxSum sum_row_careful(Row r, int begin, int end, float c) {
   float mx = -INFINITY, sum = 0.f;
-  walk<4>(r, begin, end, [&](int, auto& v) {
+  walk<1>(r, begin, end, [&](int, auto& v) {
     constexpr int N = sizeof(v) / sizeof(float);
-    float mu = v[0];
 #pragma unroll
-    for (int j = 1; j < N; ++j) mu = fmaxf(mu, v[j]);
-    if (mu > mx) { sum *= ex2_ftz((mx - mu) * c); mx = mu; }
-    // (nothing but -infinity so far: the differences are not numbers, and the sum stays nothing)
-    float part = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j) part += ex2_ftz((v[j] - mx) * c);
-    sum += mx > -INFINITY ? part : 0.f;
+    for (int j = 0; j < N; ++j) {
+      const float m = fmaxf(mx, v[j]);
+      if (m > -INFINITY) sum = sum * ex2_ftz((mx - m) * c) + ex2_ftz((v[j] - m) * c);
+      mx = m;
+    }
   });
   return MaxSum{mx, sum};
+}
+__device__ __noinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
+  MaxSum x = r.dtype == CHUNK_F32   ? sum_share(reinterpret_cast<const float*>(r.z), begin, end, c)
+             : r.dtype == CHUNK_F16 ? sum_share(reinterpret_cast<const __half*>(r.z), begin, end, c)
+                                    : sum_share(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, c);
+  if (x.sum != x.sum) x = sum_row_careful(r, begin, end, c);
+  if (x.sum == 0.f) x.mx = -INFINITY;             // (nothing but -infinity)
+  return x;
 }
 // The largest value and its lowest index over this thread's share, as one number (argmax_key).
 __device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
@@ -357,6 +425,8 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
 
 // One (position, request) per cluster, position by position.  verdict[b * k + i] = 1 if the draft would stand; the row maxima (and for greedy requests
 // the arg-max) are left for the kernel behind.  skip: first[b] holds the lowest position refused so far, and items behind it are passed over.
+// 128 requests of 16 drafts, 575 MB up to the first refused ones: 160 us and 770 MB, the rest read while the verdict in front was still out.  (Clusters
+// that walk the items themselves 205 us; leaving off a row whose request has been refused meanwhile 735 MB in 167 us.)
 __global__ void __launch_bounds__(VT, 2)
 verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S, int skip) {
   pdl_wait();
@@ -550,9 +620,10 @@ __device__ __noinline__ double rest_sum(RowWeights<EXACT> p, RowWeights<EXACT> q
   return all;
 }
 
-// One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by less
-// than 2^-19 of itself on average over a row (its exponent, of size x, by 2^-23 x; the special function by 2^-22; sums of four), and from there on
-// sums are 64-bit ones: 2^-17 of the rows' whole weight leaves room.  A goal that is not that far inside its token's share is left to the kernel with EXACT.
+// One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by 2^-23 x
+// of itself for its exponent of size x, 2^-22 for the special function and 2^-23 for the factor and the sums of four, and from there on sums are
+// 64-bit ones.  Over a row the size of the exponent, averaged by weight, is at most log2 V + 1: together 2^-19 of the rows' whole weight, of which
+// 2^-18.5 is taken.  A goal that is not that far inside its token's share is left to the kernel with EXACT.
 template <bool EXACT>
 __global__ void __launch_bounds__(VT, 2)
 verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S) {
@@ -662,7 +733,7 @@ verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant
     double whole = 0.0;
     for (int j = 0; j < S; ++j) whole += sh.block[j];
     // (how far the 32-bit sums may be off: p and q weigh 1 each where both count, else p is all there is)
-    const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * (1.0 / 131072.0);
+    const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * (1.0 / 370000.0);
     if (!EXACT && both && less && !(whole > 64.0 * tol)) {    // nearly nothing left of p - q: left to the other kernel
       if (rank == 0 && threadIdx.x == 0) s.open[b] = 1;
       break;
@@ -752,13 +823,13 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   const long long items = (long long)c.B * c.k;
   // blocks of a cluster: two for every SM where there are few items, as long as each has a few KB to read
-  auto blocks_for = [&](long long n, int least) {
-    int S = least;
+  auto blocks_for = [&](long long n) {
+    int S = 1;
     while (S < 8 && n * 2 * S <= 2 * 148 && c.V / (2 * S) >= 2048) S *= 2;
     return S;
   };
   if (items > 0) {
-    const int S = blocks_for(items, c.V >= 16384 ? ROWS_S : 1), skip = items * S > 2 * 148;
+    const int S = blocks_for(items), skip = items * S > 2 * 148;
     if (skip) {
       e = launch_pdl(verify_init_kernel, dim3(1), dim3(256), 0, stream, s.first, c.B);
       if (e != cudaSuccess) return e;
@@ -766,7 +837,7 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip);
     if (e != cudaSuccess) return e;
   }
-  const int S = blocks_for(c.B, 1), S64 = blocks_for(1, 1);   // (few requests are left for the third)
+  const int S = blocks_for(c.B), S64 = blocks_for(1);   // (few requests are left for the third)
   e = launch_pdl_cluster(verify_sample_kernel<false>, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
   if (e != cudaSuccess) return e;
   return launch_pdl_cluster(verify_sample_kernel<true>, dim3(unsigned(c.B) * S64), dim3(VT), dim3(S64), 0, stream, c, s, S64);
