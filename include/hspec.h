@@ -376,7 +376,7 @@ int hspec_op_chunk_rope_write(const void* qkv, int32_t in_dtype, int64_t ld_qkv,
 /* Attention of a chunk over the paged cache, which holds the chunk's own keys and values already: row at position p sees keys
  * max(0, p - window + 1) .. p (window 0: from the first).  Single tokens, draft blocks and pieces of prompts may be mixed.
  *   q [T, Hq, dh] with row pitch ld_q, o likewise with ld_o (elements, multiples of 8; o of q's type); scale 0: 1 / sqrt(dh)
- * At most 16384 requests, and 512 query heads for a KV head.  A row at a negative position sees nothing: its o is zero.  Keys and values at places that a row does not see never reach it, whatever
+ * At most 8192 requests, and 512 query heads for a KV head.  A row at a negative position sees nothing: its o is zero.  Keys and values at places that a row does not see never reach it, whatever
  * they hold; page-table entries that no row of the request sees are not read.  A bad page reads as zeros.
  * workspace: hspec_chunk_attention_workspace_bytes bytes whatever B, T and the lengths are, 256-byte aligned, contents undefined
  * between calls; calls that may overlap on the GPU need one each. */

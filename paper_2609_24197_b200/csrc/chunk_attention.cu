@@ -218,9 +218,9 @@ __device__ __forceinline__ bool not_finite16(uint32_t x) {
 // The line is measured in costs: an item has `item` in front of its first tile and `turns` or `both` for every tile.  A tile belongs to the part in
 // which its beginning lies.  Where the parts would be so short that one might hold no beginning, every tile counts one and nothing else does.
 struct Costs { int item, turns, both; };
-__device__ __forceinline__ int item_cost(const Costs& k, const ChunkRequest& q, const Args& a, int rt, int* tiles = nullptr) {
+__device__ __forceinline__ int item_cost(const Costs& k, const ChunkRequest& q, const Args& a, int rt, int* tiles) {
   const ItemGeo g = item_geo(q, a.rep, a.c.window, rt);
-  if (tiles) *tiles = g.t1 - g.t0;
+  *tiles = g.t1 - g.t0;
   return k.item + (takes_turns(q.n * a.rep) ? k.turns : k.both) * (g.t1 - g.t0);
 }
 // The first tile that begins at u or behind (one warp): request, group of heads, row tile, tile of the item; request B at the end of the line.
@@ -236,7 +236,8 @@ __device__ __forceinline__ int4 place_of(const Args& a, const Costs& k, const lo
   long long rest = (u - sums[lo]) - g * per_group;
   const int count = row_tiles(q.n * a.rep);
   for (int base = 0; base < count; base += 32) {
-    long long upto = base + lane < count ? item_cost(k, q, a, base + lane) : 0;
+    int tiles;
+    long long upto = base + lane < count ? item_cost(k, q, a, base + lane, &tiles) : 0;
     for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
     const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
     if (in) {
@@ -258,38 +259,43 @@ __device__ __forceinline__ int4 place_of(const Args& a, const Costs& k, const lo
   do ++lo; while (lo < c.B && sums[lo + 1] == sums[lo]);
   return make_int4(lo, 0, 0, 0);
 }
-// Cuts the line: costs of every request (one warp each), their running sum, the places where this CTA's part begins and ends.  `sums` is shared
-// memory for B + 1 numbers.  Returns false for a CTA without work.
+// Cuts the line: costs and tiles of every request (one warp each), their running sums, the places where this CTA's part begins and ends.  `sums` is
+// shared memory for twice B + 1 numbers.  Returns false for a CTA without work.
 __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
   const ChunkAttnCall& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group, most = gridDim.x / a.group;
+  long long* tile_sums = sums + c.B + 1;
   Costs k{COST_ITEM, COST_TURNS, COST_BOTH};
-  for (int turn = 0;; ++turn) {
-    for (int b = warp; b < c.B; b += warps) {
-      const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
-      const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
-      if (turn == 0 && blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-      long long n = 0;
-      const int count = row_tiles(q.n * a.rep);
-      for (int rt = lane; rt < count; rt += 32) n += item_cost(k, q, a, rt);
-      for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(0xffffffffu, n, off);
-      if (lane == 0) sums[b + 1] = n * groups;
+  for (int b = warp; b < c.B; b += warps) {
+    const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
+    const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
+    if (blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+    long long n = 0, m = 0;
+    const int count = row_tiles(q.n * a.rep);
+    for (int rt = lane; rt < count; rt += 32) {
+      int tiles;
+      n += item_cost(k, q, a, rt, &tiles);
+      m += tiles;
     }
-    if (threadIdx.x == 0) sums[0] = 0;
-    __syncthreads();
-    if (warp == 0) {
-      long long before = 0;
-      for (int base = 0; base < c.B; base += 32) {
-        long long n = base + lane < c.B ? sums[base + lane + 1] : 0;
-        for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
-        if (base + lane < c.B) sums[base + lane + 1] = before + n;
-        before += __shfl_sync(0xffffffffu, n, 31);
-      }
+    if (count > 1) for (int off = 16; off > 0; off >>= 1) { n += __shfl_xor_sync(0xffffffffu, n, off); m += __shfl_xor_sync(0xffffffffu, m, off); }
+    if (lane == 0) { sums[b + 1] = n * groups; tile_sums[b + 1] = m * groups; }
+  }
+  if (threadIdx.x == 0) sums[0] = tile_sums[0] = 0;
+  __syncthreads();
+  if (warp < 2) {
+    long long* s = warp == 0 ? sums : tile_sums;
+    long long before = 0;
+    for (int base = 0; base < c.B; base += 32) {
+      long long n = base + lane < c.B ? s[base + lane + 1] : 0;
+      for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
+      if (base + lane < c.B) s[base + lane + 1] = before + n;
+      before += __shfl_sync(0xffffffffu, n, 31);
     }
-    __syncthreads();
-    if (turn > 0 || sums[c.B] >= (long long)most * (COST_ITEM + COST_BOTH)) break;
+  }
+  __syncthreads();
+  if (sums[c.B] < (long long)most * (COST_ITEM + COST_BOTH)) {
     k = Costs{0, 1, 1};
-    __syncthreads();                                          // (everyone has read the sum)
+    sums = tile_sums;
   }
   const long long total = sums[c.B];
   const int parts = int(min((long long)most, total)), me = blockIdx.x / a.group;
@@ -449,28 +455,36 @@ __device__ __forceinline__ void lead_and_clean(const Args& a, uint8_t* ring, Bar
       uint8_t* tile = ring + slot * TILE;
       constexpr uint32_t EXP = F16 ? 0x7c007c00u : 0x7f807f80u, ONE = F16 ? 0x04000400u : 0x00800080u;
       bool bad = false;
-      // a row is 128 bytes in each half of the tile; 4 rows a step of the warp
-      for (int half = 0; half < DH / 64; ++half) {
-        uint4* p = reinterpret_cast<uint4*>(tile + half * Shape<DH>::HALF) + lane;
-        const int r0 = lane >> 3;
-#pragma unroll 8
-        for (int i = 0; i < KT / 4; ++i) {
-          const int r = i * 4 + r0;
-          if (r >= all0 && r < all1) continue;
-          if (r < seen0 || r >= seen1) { p[i * 32] = make_uint4(0u, 0u, 0u, 0u); continue; }
-          const uint4 v = p[i * 32];
-          // (an exponent of ones is the only one that carries into its sign's place)
-          if (((((v.x & EXP) + ONE) | ((v.y & EXP) + ONE) | ((v.z & EXP) + ONE) | ((v.w & EXP) + ONE)) & 0x80008000u) != 0u) {
-            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+      // a row is 128 bytes in each half of the tile; 4 rows a step of the warp, from the first step that has rows to look at
+      auto go_over = [&](int from, int to) {
+#pragma unroll 4
+        for (int i = from; i < to; ++i) {
+          const int r = i * 4 + (lane >> 3);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (not_finite16<F16>(x[e])) x[e] &= 0xffff0000u;
-              if (not_finite16<F16>(x[e] >> 16)) x[e] &= 0x0000ffffu;
+          for (int half = 0; half < DH / 64; ++half) {
+            uint4* p = reinterpret_cast<uint4*>(tile + half * Shape<DH>::HALF) + i * 32 + lane;
+            if (r >= all0 && r < all1) continue;
+            if (r < seen0 || r >= seen1) { *p = make_uint4(0u, 0u, 0u, 0u); continue; }
+            const uint4 v = *p;
+            // (an exponent of ones is the only one that carries into its sign's place)
+            if (((((v.x & EXP) + ONE) | ((v.y & EXP) + ONE) | ((v.z & EXP) + ONE) | ((v.w & EXP) + ONE)) & 0x80008000u) != 0u) {
+              uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (not_finite16<F16>(x[e])) x[e] &= 0xffff0000u;
+                if (not_finite16<F16>(x[e] >> 16)) x[e] &= 0x0000ffffu;
+              }
+              *p = make_uint4(x[0], x[1], x[2], x[3]);
+              bad = true;
             }
-            p[i * 32] = make_uint4(x[0], x[1], x[2], x[3]);
-            bad = true;
           }
         }
+      };
+      if (all0 < all1) {
+        go_over(0, min((all0 + 3) / 4, all1 / 4));
+        go_over(all1 / 4, KT / 4);
+      } else {
+        go_over(0, KT / 4);
       }
       if (bad) *reinterpret_cast<volatile uint32_t*>(&bars->bad[seg & 15]) = seg + 1;
       fence_proxy_async();

@@ -16,14 +16,15 @@ namespace hspec {
 
 namespace {
 
-constexpr int ROPE_ROWS = 16;      // most rows of a block
-constexpr int ROPE_UNROLL = 4;     // heads in flight per thread
+constexpr int ROPE_ROWS = 4;       // most rows of a block
+constexpr int ROPE_UNROLL = 2;     // heads of a thread that are loaded together, one such load ahead of their use
 
 struct RopeArgs {
   ChunkRopeCall c;
   double rate[64];
   uint8_t axis[64];
   int rows;                        // rows of a block
+  int step_rows, step_heads;       // the groups of threads of a block, in rows and heads
   int vec;                         // qkv rows start on 16-byte boundaries
 };
 
@@ -80,7 +81,7 @@ __device__ __forceinline__ uint4 narrow8(const float* x, uint32_t* status) {
 }
 
 template <typename TI, bool F16>
-__global__ void __launch_bounds__(256) chunk_rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(256, 3) chunk_rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_wait();
   pdl_trigger();
   const ChunkRopeCall& c = a.c;
@@ -95,19 +96,27 @@ __global__ void __launch_bounds__(256) chunk_rope_kernel(const __grid_constant__
   // this thread's 16 elements of a head: a pair group of the rotated part, or 16 elements behind it
   const bool turns = sub * 8 < rot;
   const int lo = turns ? sub * 8 : 2 * rot + (sub - rot / 8) * 16, hi = turns ? lo + rot : lo + 8;
-  const int items = rows * heads;
+  // This thread's heads: every groups-th of the block's, row by row.  (The place is counted along: a division for every head, twice, was a third of
+  // all instructions.)
+  struct Place { int r, h; };
+  auto next_of = [&](Place& x) {
+    x.r += a.step_rows;
+    x.h += a.step_heads;
+    if (x.h >= heads) { x.h -= heads; ++x.r; }
+  };
   Raw16<TI> raw[ROPE_UNROLL];
-  auto fetch = [&](int first) {
+  Place to_fetch{group / heads, group % heads}, at = to_fetch;
+  auto fetch = [&]() {
 #pragma unroll
     for (int u = 0; u < ROPE_UNROLL; ++u) {
-      const int item = first + u * groups + group;
-      if (item < items) {
-        const TI* src = reinterpret_cast<const TI*>(c.qkv) + size_t(t0 + item / heads) * c.ld_qkv + size_t(item % heads) * c.dh;
+      if (to_fetch.r < rows) {
+        const TI* src = reinterpret_cast<const TI*>(c.qkv) + size_t(t0 + to_fetch.r) * c.ld_qkv + to_fetch.h * c.dh;
         load16<TI>(src + lo, src + hi, a.vec, raw[u]);
       }
+      next_of(to_fetch);
     }
   };
-  fetch(0);
+  fetch();                                                // (under way while the rows are looked up)
   for (int r = warp; r < rows; r += 8) {
     const int t = t0 + r, b = chunk_request_of(c.cu_q, c.B, t, lane);
     if (lane == 0) {
@@ -139,15 +148,19 @@ __global__ void __launch_bounds__(256) chunk_rope_kernel(const __grid_constant__
     sincosf(float(rem), &s_sin[r][j], &s_cos[r][j]);
   }
   __syncthreads();
+  const int items = rows * heads;
   for (int first = 0; first < items; first += ROPE_UNROLL * groups) {
-    if (first > 0) fetch(first);
+    Raw16<TI> now[ROPE_UNROLL];
+#pragma unroll
+    for (int u = 0; u < ROPE_UNROLL; ++u) now[u] = raw[u];
+    if (first + ROPE_UNROLL * groups < items) fetch();
 #pragma unroll
     for (int u = 0; u < ROPE_UNROLL; ++u) {
-      const int item = first + u * groups + group;
-      const bool on = item < items;
-      const int r = on ? item / heads : 0, h = on ? item % heads : 0;
+      const int r = at.r, h = at.h;
+      const bool on = r < rows;
+      next_of(at);
       float x[16];
-      if (on) widen(raw[u], x);
+      if (on) widen(now[u], x);
       const float* w = h < c.Hq ? c.q_norm_w : c.k_norm_w;
       if (c.q_norm_w) {                                   // (uniform: both norms or none)
         float ss = 0.f;
@@ -163,10 +176,15 @@ __global__ void __launch_bounds__(256) chunk_rope_kernel(const __grid_constant__
       if (!on || !s_used[r]) continue;
       if (turns && h < c.Hq + c.Hkv) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float cs = s_cos[r][lo + e], sn = s_sin[r][lo + e], p = x[e], q = x[8 + e];
-          x[e] = p * cs - q * sn;
-          x[8 + e] = q * cs + p * sn;
+        for (int v = 0; v < 2; ++v) {
+          const float4 c4 = *reinterpret_cast<const float4*>(&s_cos[r][sub * 8 + v * 4]), s4 = *reinterpret_cast<const float4*>(&s_sin[r][sub * 8 + v * 4]);
+          const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = x[v * 4 + e], q = x[8 + v * 4 + e];
+            x[v * 4 + e] = p * cs[e] - q * sn[e];
+            x[8 + v * 4 + e] = q * cs[e] + p * sn[e];
+          }
         }
       }
       uint16_t* dst;
@@ -207,10 +225,13 @@ cudaError_t chunk_rope_launch(const ChunkRopeCall& c, cudaStream_t stream) {
   }
   const size_t item = c.in_dtype == CHUNK_F32 ? 4 : 2;
   a.vec = (reinterpret_cast<uintptr_t>(c.qkv) % 16 == 0 && size_t(c.ld_qkv) * item % 16 == 0) ? 1 : 0;
-  // enough rows that a thread has its four heads to load, as long as four blocks are left for every SM
-  const int want = (ROPE_UNROLL * 256 / (c.dh / 16) + c.Hq + 2 * c.Hkv - 1) / (c.Hq + 2 * c.Hkv), spread = (c.T + 4 * 148 - 1) / (4 * 148);
-  a.rows = want < spread ? want : spread;
-  if (a.rows > ROPE_ROWS) a.rows = ROPE_ROWS;
+  // The look-up of a row (three loads that wait for one another, then its angles) takes longer than the row itself: a block has up to ROPE_ROWS of
+  // them, as long as four blocks are left for every SM.  8200 rows of 80 heads, bf16, three axes, 333 MB: 61 us (5.4 TB/s); 63 with 3, 65 with 5 and
+  // 82 with 16 of them, 79 without a load ahead.
+  const int spread = (c.T + 4 * 148 - 1) / (4 * 148);
+  a.rows = spread < ROPE_ROWS ? spread : ROPE_ROWS;
+  a.step_rows = 256 / (c.dh / 16) / (c.Hq + 2 * c.Hkv);
+  a.step_heads = 256 / (c.dh / 16) % (c.Hq + 2 * c.Hkv);
   const int blocks = (c.T + a.rows - 1) / a.rows;
   if (c.in_dtype == CHUNK_F32) return launch_for<float>(a, blocks, stream);
   return c.in_dtype == CHUNK_F16 ? launch_for<__half>(a, blocks, stream) : launch_for<__nv_bfloat16>(a, blocks, stream);

@@ -1057,7 +1057,7 @@ int hspec_op_chunk_attention(const void* q, int64_t ld_q, const void* k_pool, co
     return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + why);
   if (ld_q < int64_t(Hq) * dh || ld_o < int64_t(Hq) * dh || ld_q % 8 || ld_o % 8 || (reinterpret_cast<uintptr_t>(o) & 15))
     return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "rows of q and o must start on 16-byte boundaries and hold all heads");
-  if (B > 16384) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 16384 requests");
+  if (B > 8192) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 8192 requests");
   if (Hq / Hkv > 512) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 512 query heads for a KV head");
   if (workspace_bytes < chunk_attn_workspace_bytes(Hq, Hkv, dh)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");

@@ -51,7 +51,7 @@ def _attn(lib, **over):
     (dict(dtype=F32), -2, "bf16 or fp16"), (dict(dh=256), -2, "head dim"), (dict(Hq=33), -2, "multiple"), (dict(k=A + 4), -2, "16-byte"),
     (dict(ldq=32 * 128 - 8), -1, "rows of q and o"), (dict(ldo=32 * 128 + 4), -1, "rows of q and o"), (dict(o=A + 8), -1, "rows of q and o"),
     (dict(ws_bytes=0), -4, "workspace too small"), (dict(ws=A + 16), -1, "256-byte"), (dict(B=0), -2, "bad argument"),
-    (dict(B=16385), -2, "16384 requests"), (dict(Hq=513, Hkv=1, ldq=513 * 128, ldo=513 * 128), -2, "512 query heads")])
+    (dict(B=8193), -2, "8192 requests"), (dict(Hq=513, Hkv=1, ldq=513 * 128, ldo=513 * 128), -2, "512 query heads")])
 def test_chunk_attention_refuses(lib, over, code, text):
     rc, msg = _attn(lib, **over)
     assert rc == code and "hspec_op_chunk_attention" in msg and text in msg
