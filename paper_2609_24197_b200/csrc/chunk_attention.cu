@@ -61,7 +61,8 @@ struct Args {
   float scale_log2;
   float* ws_o;                       // [slot][DH / 4][256 rows][4]
   float2* ws_ml;                     // [slot][256 rows]
-  int4* ws_start;                    // [CTA]; how many CTAs (per head of a group) have work lies in ws_count
+  int4* ws_start;                    // [CTA]: where its part begins; [MAX_CTAS + CTA]: of the item there, first row, token and query head of the first
+                                     // row, rows.  How many CTAs (per head of a group) have work lies in ws_count
   int* ws_count;
 };
 
@@ -308,6 +309,9 @@ __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* 
       bars->req[0] = load_request(c, at.x);
       bars->req[1] = load_request(c, at.x + 1);
       a.ws_start[blockIdx.x] = at;
+      const ChunkRequest q = bars->req[0];
+      const int r0 = at.z * ITEM_ROWS, tok0 = r0 / a.rep;
+      a.ws_start[MAX_CTAS + blockIdx.x] = make_int4(q.q0, tok0, r0 - tok0 * a.rep, min(q.n * a.rep - r0, ITEM_ROWS));
     }
     if (warp == 1 && lane == 0) bars->stop = at;
   }
@@ -1086,8 +1090,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 
 // ------------------------------------------------------------------ joining items that a cut went through
 // One block per (CTA, 32 rows).  The CTA whose part an item begins in speaks for it: its partial result and those of the parts behind, in order.
-// Lane = row, warp = 16 (or 8) columns, so that the loads follow the partials' layout; the rows' weights come first, through shared memory, and
-// four partials are in flight per thread.
+// Lane = row, warp = 16 (or 8) columns, so that the loads follow the partials' layout.  All that the kernel waits for in turn is the places, then the
+// rows' maxima and sums, then the partials, four under way per thread (with the places one after the other and the request's lengths behind them a
+// single token's call took 1.4 us more).
 template <int DH, bool F16>
 __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_constant__ Args a) {
   pdl_wait();
@@ -1095,32 +1100,25 @@ __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_const
   constexpr int COLS = DH / 8, ROW = DH * 2 + 16;
   __shared__ __align__(16) uint8_t tile[32 * ROW];
   __shared__ float2 ml[MAX_CTAS][32];
-  __shared__ int s_last;
   const ChunkAttnCall& c = a.c;
-  const int me = blockIdx.x, count = *a.ws_count * a.group, next = me + a.group;
+  const int me = blockIdx.x, next = me + a.group, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (next >= MAX_CTAS) return;
+  const int count = *a.ws_count * a.group, behind = next + lane * a.group;
+  const int4 mine = a.ws_start[me], x = a.ws_start[next], item = a.ws_start[MAX_CTAS + next];
+  const int4 y = behind < MAX_CTAS ? a.ws_start[behind] : make_int4(-1, 0, 0, 0);     // (of parts without work: anything)
   if (next >= count) return;
-  const int4 x = a.ws_start[next], mine = a.ws_start[me];
-  auto same = [&](const int4& y) { return y.x == x.x && y.y == x.y && y.z == x.z; };
+  auto same = [&](const int4& p) { return p.x == x.x && p.y == x.y && p.z == x.z; };
   if (x.w == 0 || (same(mine) && mine.w > 0)) return;         // no cut through an item here, or an earlier CTA speaks for it
   const int first = 2 * me + (same(mine) ? 0 : 1);
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (w == 0) {
-    // (a part that begins further on in the same item has its place behind the item's begin)
-    int n = 1;
-    for (int base = next;; base += 32 * a.group) {
-      const int at = base + lane * a.group;
-      const unsigned m = __ballot_sync(0xffffffffu, at < count && same(a.ws_start[at < count ? at : me]));
-      n += m == 0xffffffffu ? 32 : __ffs(~m) - 1;
-      if (m != 0xffffffffu) break;
-    }
-    if (lane == 0) s_last = n;
+  // (a part that begins further on in the same item has its place behind the item's begin)
+  unsigned run = __ballot_sync(0xffffffffu, behind < count && same(y));
+  int n = 1 + (run == 0xffffffffu ? 32 : __ffs(~run) - 1);
+  for (int base = next + 32 * a.group; run == 0xffffffffu; base += 32 * a.group) {
+    const int at = base + lane * a.group;
+    run = __ballot_sync(0xffffffffu, at < count && same(a.ws_start[at < count ? at : me]));
+    n += run == 0xffffffffu ? 32 : __ffs(~run) - 1;
   }
-  __syncthreads();
-  const int n = s_last;
-  const ChunkRequest q = load_request(c, x.x);
-  const ItemGeo g = item_geo(q, a.rep, c.window, x.z);
-  const int kvh = x.y * a.group + me % a.group;
-  const int r = blockIdx.y * 32 + lane, rows = g.r1 - g.r0;
+  const int kvh = x.y * a.group + me % a.group, r = blockIdx.y * 32 + lane, rows = item.w;
   if (int(blockIdx.y) * 32 >= rows) return;
   auto slot = [&](int i) { return size_t(i == 0 ? first : 2 * (me + i * a.group)); };
   for (int i = w; i < n; i += 8) ml[i][lane] = r < rows ? a.ws_ml[slot(i) * ITEM_ROWS + r] : make_float2(NEG, 0.f);
@@ -1158,9 +1156,10 @@ __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_const
   __syncthreads();
   constexpr int LANES = DH / 8;                               // lanes that write a row
   for (int i = threadIdx.x; i < 32 * LANES; i += 256) {
-    const int rl = i / LANES, rr = g.r0 + blockIdx.y * 32 + rl;
-    if (rr < g.r1)
-      *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + size_t(q.q0 + rr / a.rep) * c.ldo + size_t(kvh * a.rep + rr % a.rep) * DH + (i % LANES) * 8) =
+    const int rl = i / LANES, row = int(blockIdx.y) * 32 + rl;
+    const uint32_t at = uint32_t(item.z + row), t = (at * a.inv_rep) >> 20;          // (token_of)
+    if (row < rows)
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.o) + size_t(item.x + item.y + int(t)) * c.ldo + size_t(kvh * a.rep + int(at - t * a.rep)) * DH + (i % LANES) * 8) =
           *reinterpret_cast<const uint4*>(tile + rl * ROW + (i % LANES) * 16);
   }
 }
@@ -1210,7 +1209,7 @@ cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tm
 }  // namespace
 
 size_t chunk_attn_workspace_bytes(int, int, int dh) {
-  return size_t(2 * MAX_CTAS) * ITEM_ROWS * (size_t(dh) * 4 + 8) + MAX_CTAS * sizeof(int4) + 256;
+  return size_t(2 * MAX_CTAS) * ITEM_ROWS * (size_t(dh) * 4 + 8) + 2 * MAX_CTAS * sizeof(int4) + 256;
 }
 
 cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string* err) {
@@ -1227,7 +1226,7 @@ cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::
   a.ws_o = reinterpret_cast<float*>(c.ws);
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + size_t(2 * MAX_CTAS) * ITEM_ROWS * c.dh);
   a.ws_start = reinterpret_cast<int4*>(a.ws_ml + size_t(2 * MAX_CTAS) * ITEM_ROWS);
-  a.ws_count = reinterpret_cast<int*>(a.ws_start + MAX_CTAS);
+  a.ws_count = reinterpret_cast<int*>(a.ws_start + 2 * MAX_CTAS);
   CUtensorMap tmK{}, tmV{};
   if (a.box_rows && (!pool_tmap(&tmK, c.k_pool, c, a.box_rows, err) || !pool_tmap(&tmV, c.v_pool, c, a.box_rows, err))) return cudaErrorInvalidValue;
   if (c.dh == 64) return c.f16 ? launch_for<64, true>(a, stream, tmK, tmV) : launch_for<64, false>(a, stream, tmK, tmV);
