@@ -122,13 +122,13 @@ __global__ void __launch_bounds__(256, 3) chunk_rope_kernel(const __grid_constan
     if (lane == 0) {
       long long slot = -1;
       int at = 0, used = 0;
-      if (b < c.B && t >= c.cu_q[b]) {
-        used = 1;
+      if (b < c.B) {
         const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
         const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
         if (t == q.q0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+        used = t >= q.q0 && t < q.q0 + q.n;               // (a cu_q that does not ascend may have counted t to a request that does not own it)
         at = q.len - q.n + (t - q.q0);
-        if (at >= 0) {
+        if (used && at >= 0) {
           const int page = c.page_table[size_t(b) * c.page_table_stride + at / c.page_size];
           if (page >= 0 && page < c.num_pages) slot = ((long long)page * c.page_size + at % c.page_size) * c.Hkv;
           else atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);

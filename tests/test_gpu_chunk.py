@@ -356,6 +356,22 @@ def test_rope_rows_without_a_place(hs):
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 1 + 4
 
 
+def test_rope_rows_of_offsets_that_do_not_ascend(hs):
+    """A row that the offsets give to no request has nothing written, least of all through the next request's page-table entries."""
+    Hq, Hkv, dh = HEADS["three"]
+    table = torch.arange(8, dtype=torch.int32, device="cuda")[:, None]              # one page per request, and entries behind the last request's
+    cu = torch.tensor([0, 20, 3, 3, 1, 30], dtype=torch.int32, device="cuda")       # rows 3 .. 19 are counted to request 3, which has none
+    kv = torch.full((5,), 16, dtype=torch.int32, device="cuda")
+    k, v = (torch.full((8, 16, Hkv, dh), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.full((30, Hq, dh), 7.0, dtype=torch.bfloat16, device="cuda")
+    hs.hspec_op_chunk_rope_write(torch.randn((30, (Hq + 2 * Hkv) * dh), device="cuda"), None, None, cu, kv, table[:5], q, k, v, 1.0e4)
+    torch.cuda.synchronize()
+    assert (q[3:20] == 7.0).all()
+    for pool in (k, v):                                      # (request 4's own rows, 20 .. 29, go to places 6 .. 15 of its page)
+        assert (pool[4, :6] == 5.0).all() and (pool[5:] == 5.0).all() and (pool[4, 6:] != 5.0).any(-1).all()
+    hs.hspec_op_device_status(clear=True)
+
+
 def test_rope_fp16_range(hs):
     c = Chunk(HEADS["three"], torch.float16, [1], [0], seed=2, poison=False)
     qkv = torch.full((1, 10 * 128), 1.0e6, device="cuda")
