@@ -80,8 +80,8 @@ __device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int 
   const int rows = q.n * rep;
   g.r0 = rt * ITEM_ROWS;
   g.r1 = min(rows, g.r0 + ITEM_ROWS);
-  g.pos0 = q.len - q.n + g.r0 / rep;
-  g.pos1 = q.len - q.n + (g.r1 - 1) / rep;
+  g.pos0 = max(-1, q.len - q.n + g.r0 / rep);                 // (a place in front of the cache sees nothing, whichever it is: no window wraps round)
+  g.pos1 = max(-1, q.len - q.n + (g.r1 - 1) / rep);
   g.key_lo = window > 0 ? max(0, g.pos0 - window + 1) : 0;
   g.key_hi = max(0, g.pos1 + 1);
   g.t0 = g.key_lo / KT;
@@ -722,7 +722,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     const bool row_ok = r < rows;
     int token, head;
     token_of(s, a, r, token, head);
-    const int hi = row_ok ? s.pos + token : -1;               // keys lo .. hi are seen
+    const int hi = row_ok ? max(-1, s.pos + token) : -1;      // keys lo .. hi are seen
     const int lo = c.window > 0 ? max(0, hi - c.window + 1) : 0;
     const bool live = r - row + quarter * 32 < rows;          // (the same for both warps of a row)
     int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys

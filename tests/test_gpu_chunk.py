@@ -174,6 +174,14 @@ def test_rows_with_no_place_see_nothing(hs):
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3
 
 
+@pytest.mark.parametrize("window", [1, 100, 2 ** 31 - 1])
+def test_windows_of_rows_with_no_place(hs, window):
+    """The largest window reaches back from a negative position past 32 bits."""
+    c = Chunk(HEADS["8b"], torch.bfloat16, [10, 200, 4, 70], [-9, -150, -4, 300], seed=6)
+    c.check(c.run(hs, window=window), window=window, what="no place")
+    hs.hspec_op_device_status(clear=True)
+
+
 @pytest.mark.parametrize("what", ["value", "key"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_what_a_row_does_not_see_never_reaches_it(hs, what, bad):
