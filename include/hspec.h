@@ -351,7 +351,7 @@ int hspec_op_swiglu(const float* gu, void* h_f16, int32_t M, int32_t F, void* st
  * stands at cache position kv_lens[b] - n + i.  The cache is the paged one of the draft step: page_table int32
  * [B, page_table_stride], pools [num_pages, page_size, Hkv, dh].  Both may be bf16 or fp16 here (`dtype`), Hq a multiple of Hkv,
  * dh 64 or 128, any page size; q and the pools start on 16-byte boundaries.  Rows behind cu_q[B] (a batch padded to a captured
- * graph's size) are neither read nor written.  What the device arrays say is held inside T and page_table_stride * page_size; entries
+ * graph's size) are not written, and nothing depends on what they hold.  Outputs share no memory with inputs.  What the device arrays say is held inside T and page_table_stride * page_size; entries
  * outside, requests with more rows than cached tokens and page ids outside [0, num_pages) are counted (hspec_op_device_status).
  * The lengths are read on the device: a captured call follows the arrays' contents.
  * ---------------------------------------------------------------------------------------------- */
@@ -376,8 +376,9 @@ int hspec_op_chunk_rope_write(const void* qkv, int32_t in_dtype, int64_t ld_qkv,
 /* Attention of a chunk over the paged cache, which holds the chunk's own keys and values already: row at position p sees keys
  * max(0, p - window + 1) .. p (window 0: from the first).  Single tokens, draft blocks and pieces of prompts may be mixed.
  *   q [T, Hq, dh] with row pitch ld_q, o likewise with ld_o (elements, multiples of 8; o of q's type); scale 0: 1 / sqrt(dh)
- * At most 8192 requests, and 512 query heads for a KV head.  A row at a negative position sees nothing: its o is zero.  Keys and values at places that a row does not see never reach it, whatever
- * they hold; page-table entries that no row of the request sees are not read.  A bad page reads as zeros.
+ * At most 8192 requests, and 512 query heads for a KV head.  A row at a negative position sees nothing: its o is zero.  Keys
+ * and values at places that a row does not see never reach it, whatever they hold; page-table entries that no row of the request
+ * sees are not read.  A bad page reads as zeros.
  * workspace: hspec_chunk_attention_workspace_bytes bytes whatever B, T and the lengths are, 256-byte aligned, contents undefined
  * between calls; calls that may overlap on the GPU need one each. */
 int hspec_op_chunk_attention(const void* q, int64_t ld_q, const void* k_pool, const void* v_pool, int64_t num_pages, const int32_t* page_table,
@@ -388,7 +389,8 @@ size_t hspec_chunk_attention_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t dh
 /* Verification of a draft block against the target's probabilities, with the caller's uniform numbers (App. A, and the token that follows
  * the accepted drafts).  With p = softmax(target row / temperature) and q = softmax(draft row / temperature), draft i stands if every earlier one
  * does, p_i(x_i) > 0 and min(1, p_i(x_i) / q_i(x_i)) >= alpha_i.  Behind the n that stand comes one token of the target's: from max(0, p_n - q_n)
- * where draft n was refused, from p_n where none was: the lowest token v with sum over w <= v above u times the whole.
+ * where draft n was refused (from p_n where that is nothing anywhere), from p_n where none was: the lowest token v with sum over w <= v above u
+ * times the whole.
  *   target_logits  device [T, ld_target], fp32, bf16 or fp16 (target_dtype): request b's rows cu_q[b] .. cu_q[b+1]-1 are the logits behind its
  *                  last token and behind each draft, so it has min(k, rows - 1) drafts.  cu_q NULL: k + 1 rows each
  *   draft_logits   device [B * k, ld_draft] (draft_dtype): what the drafts were sampled from at the same temperature; NULL: a drafter that takes

@@ -1003,6 +1003,7 @@ static const char* chunk_refusal(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, 
   if (B < 1 || T < 1 || page_size < 1 || page_table_stride < 1 || num_pages < 1 || num_pages > 0x7fffffff) return "bad argument";
   if (Hkv < 1 || Hq < Hkv || Hq % Hkv) return "the query heads must be a multiple of the KV heads";
   if (dh != 64 && dh != 128) return "the head dim must be 64 or 128";
+  if (int64_t(T) * Hq > 0x7fffff00) return "too many rows";
   if (dtype != HSPEC_BF16 && dtype != HSPEC_F16) return "queries and pools must be bf16 or fp16";
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_pool) | reinterpret_cast<uintptr_t>(v_pool)) & 15)
     return "queries and pools must be 16-byte aligned";
@@ -1088,6 +1089,7 @@ int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_
   if (draft_logits && (V_draft < 1 || V_draft > V || ld_draft < V_draft)) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad drafter vocabulary");
   if (draft_logits && !vocab_map && V_draft != V) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "a pruned drafter vocabulary needs its map");
   if (int64_t(B) * k > 0x0fffffff) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "too many drafts");
+  if (V > 1 << 30) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 2^30 tokens");
   if (workspace_bytes < verify_workspace_bytes(B, k)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");
   std::string errtxt;

@@ -11,9 +11,8 @@
 // Three launches.  The first takes one (request, position) per cluster of blocks, reads the target's and the drafter's row once and decides whether
 // the position would be refused; items are started position by position, and one whose request is known to have been refused before is not read.
 // The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for the requests whose uniform
-// number came within 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by memory,
-// the third by the 64-bit pipe (128 requests of 152 064 tokens: 238 us in 64 bits alone,
-// 69 and 61 in two).
+// number came within some 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by
+// memory, the third by the 64-bit pipe (128 requests of 152 064 tokens: 238 us in 64 bits alone, 69 and 61 in two).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -622,8 +621,9 @@ __device__ __noinline__ double rest_sum(RowWeights<EXACT> p, RowWeights<EXACT> q
 
 // One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by 2^-23 x
 // of itself for its exponent of size x, 2^-22 for the special function and 2^-23 for the factor and the sums of four, and from there on sums are
-// 64-bit ones.  Over a row the size of the exponent, averaged by weight, is at most log2 V + 1: together 2^-19 of the rows' whole weight, of which
-// 2^-18.5 is taken.  A goal that is not that far inside its token's share is left to the kernel with EXACT.
+// 64-bit ones.  Averaged by weight, the exponents' size is the entropy of the weights less log2 of their sum W, so at most log2 (V / W): V weights are off by
+// 2^-23 (log2 V - log2 W + 3) of their sum together (W is 1 or more, but where an arg-max drafter's token is left out).  A goal that is not that far
+// inside its token's share is left to the kernel with EXACT.
 template <bool EXACT>
 __global__ void __launch_bounds__(VT, 2)
 verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S) {
@@ -733,7 +733,7 @@ verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant
     double whole = 0.0;
     for (int j = 0; j < S; ++j) whole += sh.block[j];
     // (how far the 32-bit sums may be off: p and q weigh 1 each where both count, else p is all there is)
-    const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * (1.0 / 370000.0);
+    const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * double(log2f(float(c.V)) + fmaxf(0.f, -log2f(float(whole))) + 4.f) * 0x1p-23;
     if (!EXACT && both && less && !(whole > 64.0 * tol)) {    // nearly nothing left of p - q: left to the other kernel
       if (rank == 0 && threadIdx.x == 0) s.open[b] = 1;
       break;

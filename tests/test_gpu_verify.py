@@ -145,6 +145,20 @@ def test_uniform_numbers_next_to_a_cumulative_sum(hs):
     assert n.tolist() == [1] * 8 and tok[:, 1].tolist() == [0, 1, 2, V // 2, V - 1, V - 1, 0, V - 1]
 
 
+def test_what_an_argmax_drafter_leaves_over(hs):
+    """The refused token holds nearly all of p: the rest is as small as 2^-39 of it, and its tokens are alike or far apart."""
+    B, V = 240, 5003
+    g = torch.Generator().manual_seed(77)
+    z = torch.randn((B, 2, V), generator=g)
+    z[0::3] = 0.0
+    z[1::3, :, 40:] = -float("inf")
+    ids = torch.randint(0, 40, (B, 1), generator=g, dtype=torch.int32)
+    gap = torch.linspace(4.0, 30.0, B)
+    z[torch.arange(B), 0, ids[:, 0].long()] = gap + 1.0
+    n, _ = _check(hs, z.reshape(2 * B, V), None, ids, torch.ones((B, 1)), torch.rand(B, generator=g))
+    assert n.sum() == 0
+
+
 def test_a_draft_outside_the_vocabulary_does_not_stand(hs):
     c = _case(3, 2, 900, torch.float32, 3)
     c["ids"][0, 0], c["ids"][1, 1] = -1, 900

@@ -51,7 +51,7 @@ def _attn(lib, **over):
     (dict(dtype=F32), -2, "bf16 or fp16"), (dict(dh=256), -2, "head dim"), (dict(Hq=33), -2, "multiple"), (dict(k=A + 4), -2, "16-byte"),
     (dict(ldq=32 * 128 - 8), -1, "rows of q and o"), (dict(ldo=32 * 128 + 4), -1, "rows of q and o"), (dict(o=A + 8), -1, "rows of q and o"),
     (dict(ws_bytes=0), -4, "workspace too small"), (dict(ws=A + 16), -1, "256-byte"), (dict(B=0), -2, "bad argument"),
-    (dict(B=8193), -2, "8192 requests"), (dict(Hq=513, Hkv=1, ldq=513 * 128, ldo=513 * 128), -2, "512 query heads")])
+    (dict(B=8193), -2, "8192 requests"), (dict(T=2 ** 27), -2, "too many rows"), (dict(Hq=513, Hkv=1, ldq=513 * 128, ldo=513 * 128), -2, "512 query heads")])
 def test_chunk_attention_refuses(lib, over, code, text):
     rc, msg = _attn(lib, **over)
     assert rc == code and "hspec_op_chunk_attention" in msg and text in msg
@@ -68,7 +68,8 @@ def _verify(lib, **over):
     (dict(target=None), -1, "bad argument"), (dict(u=None), -1, "bad argument"), (dict(k=0), -1, "bad argument"), (dict(ld_t=999), -1, "bad argument"),
     (dict(t_dtype=I32), -1, "logits must be"), (dict(d_dtype=9), -1, "logits must be"), (dict(T=67), -1, "k + 1 rows"), (dict(Vd=900), -1, "needs its map"),
     (dict(Vd=0, vmap=A), -1, "drafter vocabulary"), (dict(Vd=1001, vmap=A), -1, "drafter vocabulary"), (dict(ld_d=999), -1, "drafter vocabulary"),
-    (dict(B=1 << 24, k=1 << 5, cu=A), -2, "too many drafts"), (dict(ws_bytes=100), -4, "workspace too small"), (dict(ws=A + 4), -1, "256-byte")])
+    (dict(B=1 << 24, k=1 << 5, cu=A), -2, "too many drafts"), (dict(V=2 ** 31 - 1, Vd=2 ** 31 - 1, ld_t=2 ** 31, ld_d=2 ** 31), -2, "2^30 tokens"),
+    (dict(ws_bytes=100), -4, "workspace too small"), (dict(ws=A + 4), -1, "256-byte")])
 def test_verify_refuses(lib, over, code, text):
     rc, msg = _verify(lib, **over)
     assert rc == code and "hspec_op_verify" in msg and text in msg
