@@ -150,6 +150,50 @@ def test_attention_long_and_wide(hs, heads, new, past):
     c.check(c.run(hs), what=f"{heads} {len(new)}")
 
 
+@pytest.mark.parametrize("heads", [(5, 5, 64), (14, 7, 128), (32, 16, 64), (32, 32, 128), (37, 37, 64), (64, 64, 64), (512, 1, 64), (1024, 2, 128), (129, 1, 64)])
+def test_attention_head_counts(hs, heads):
+    # groups of KV heads of every kind (one head, all of them, a part), and up to 512 rows of a single token
+    c = Chunk(heads, torch.bfloat16, [3, 1, 0, 40], [500, 131, 7, 90], seed=heads[0])
+    c.check(c.run(hs), what=str(heads))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attention_of_thousands_of_requests(hs, dtype):
+    # the most requests, two thirds of them without a row: every CTA goes through many short items
+    new = [(0, 1, 0, 2, 0, 0)[b % 6] for b in range(8192)]
+    past = [(b * 37) % 150 for b in range(8192)]
+    c = Chunk(HEADS["tiny"], dtype, new, past, seed=21)
+    c.check(c.run(hs), what="many")
+
+
+def test_attention_past_32_bit_offsets(hs):
+    """Pools of more than 2^32 bytes with the request's pages at their ends, and rows of q and o that lie 2^27 values apart."""
+    small = Chunk(HEADS["8b"], torch.bfloat16, [17, 1], [300, 900], seed=22, poison=False)
+    want = small.run(hs)
+    pages = 2 ** 32 // (16 * 8 * 128 * 2) + 500
+    k, v = (torch.empty((pages, 16, 8, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    n = small.k.shape[0]
+    order = torch.randperm(n, generator=_gen(1))
+    to_page = torch.where(order % 2 == 0, pages - 1 - order, order).cuda()
+    k[to_page], v[to_page] = small.k, small.v
+    table = torch.where(small.table >= 0, to_page[small.table.clamp(min=0).long()].to(torch.int32), -1).to(torch.int32)
+    q, o = (torch.empty((17, 2 ** 27), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cut = small.cu.clone()
+    cut[2] = 17                                              # (the second request's row does not fit: it has none)
+    q[:, :4096], o[:, 4096] = small.q[:17].reshape(17, -1), 7.0
+    small.run(hs, q=q[:, :4096].unflatten(1, (32, 128)), o=o[:, :4096].unflatten(1, (32, 128)), k=k, v=v, table=table, cu=cut)
+    torch.cuda.synchronize()
+    assert torch.equal(o[:, :4096].reshape(17, 32, 128), want[:17]) and (o[:, 4096] == 7.0).all()
+
+
+def test_requests_that_share_pages(hs):
+    """Two requests over the same prefix, and one whose cache names one page twice: read only, so they may."""
+    c = Chunk(HEADS["three"], torch.bfloat16, [4, 9, 1], [60, 60, 63], seed=23)
+    c.table[1, :3] = c.table[0, :3]
+    c.table[2, 1] = c.table[2, 0]
+    c.check(c.run(hs), what="shared")
+
+
 @pytest.mark.parametrize("spread", [0.0, 8.0, 40.0])
 def test_attention_of_flat_and_peaked_rows(hs, spread):
     # (scores up to some hundreds: the running maximum moves)
@@ -343,6 +387,24 @@ def test_rope_far_positions(hs):
 def test_rope_rows_off_the_vector_boundaries(hs, gap):
     for source in (torch.float32, torch.bfloat16):
         _rope_case(hs, "three", source, torch.bfloat16, [9, 2], [0, 4], axes=3, gap=gap, seed=gap)
+
+
+def test_rope_past_32_bit_offsets(hs):
+    """Rows of qkv 2^27 values apart, and a page past 2^32 bytes of the pools."""
+    pages = 2 ** 32 // (16 * 2 * 128 * 2) + 3
+    qkv = torch.empty((33, 2 ** 27), dtype=torch.bfloat16, device="cuda")
+    row = torch.randn((33, 10 * 128), device="cuda").to(torch.bfloat16)
+    qkv[:, :1280] = row
+    k, v, few_k, few_v = (torch.zeros((n, 16, 2, 128), dtype=torch.bfloat16, device="cuda") for n in (pages, pages, 4, 4))
+    cu, kv = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 33], [40]))
+    q, few_q = (torch.empty((33, 6, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    hs.hspec_op_chunk_rope_write(row, None, None, cu, kv, torch.tensor([[1, 0, 2]], dtype=torch.int32, device="cuda"), few_q, few_k, few_v, 1.0e4)
+    far = torch.tensor([[pages - 2, 0, pages - 1]], dtype=torch.int32, device="cuda")
+    hs.hspec_op_chunk_rope_write(qkv[:, :1280], None, None, cu, kv, far, q, k, v, 1.0e4)
+    torch.cuda.synchronize()
+    assert torch.equal(q, few_q)
+    for a, b in ((k, few_k), (v, few_v)):
+        assert torch.equal(a[far[0].long()], b[[1, 0, 2]]) and not a[1:pages - 2].any() and b[[0, 1, 2]].any()
 
 
 def test_rope_rows_without_a_place(hs):

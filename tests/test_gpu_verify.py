@@ -178,6 +178,20 @@ def test_row_pitch_and_odd_addresses(hs):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_rows_past_32_bit_offsets(hs):
+    c = {k: v.cuda() if v is not None else None for k, v in _case(4, 4, 5001, torch.bfloat16, 12).items()}
+    want = _run(hs, **c)
+    far = torch.empty((20, 2 ** 27), dtype=torch.bfloat16, device="cuda")
+    far[:, :5001] = c["target"]
+    got = _run(hs, **{**c, "target": far[:, :5001]})
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_thousands_of_requests(hs):
+    _check(hs, **_case(9000, 2, 33, torch.float16, 13))
+
+
 def test_streams_and_graphs(hs):
     c = {k: v.cuda() if v is not None else None for k, v in _case(130, 12, 1500, torch.float32, 2).items()}
     want = [x.clone() for x in _run(hs, **c)]
