@@ -260,26 +260,40 @@ __device__ __forceinline__ int4 place_of(const Args& a, const Costs& k, const lo
   do ++lo; while (lo < c.B && sums[lo + 1] == sums[lo]);
   return make_int4(lo, 0, 0, 0);
 }
-// Cuts the line: costs and tiles of every request (one warp each), their running sums, the places where this CTA's part begins and ends.  `sums` is
+// Cuts the line: costs and tiles of every request, their running sums, the places where this CTA's part begins and ends.  `sums` is
 // shared memory for twice B + 1 numbers.  Returns false for a CTA without work.
 __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
   const ChunkAttnCall& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group, most = gridDim.x / a.group;
   long long* tile_sums = sums + c.B + 1;
   Costs k{COST_ITEM, COST_TURNS, COST_BOTH};
-  for (int b = warp; b < c.B; b += warps) {
-    const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
-    const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
-    if (blockIdx.x == 0 && lane == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+  // a request per lane; those with more than one row tile by the whole warp
+  for (int base = warp * 32; base < c.B; base += warps * 32) {
+    const int b = base + lane;
+    const bool on = b < c.B;
+    const int cu0 = on ? c.cu_q[b] : 0, cu1 = on ? c.cu_q[b + 1] : 0, len = on ? c.kv_lens[b] : 0;
+    const ChunkRequest mine = chunk_request(cu0, cu1, len, c.T, c.max_len);
+    if (blockIdx.x == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+    const int count = row_tiles(mine.n * a.rep);
     long long n = 0, m = 0;
-    const int count = row_tiles(q.n * a.rep);
-    for (int rt = lane; rt < count; rt += 32) {
+    if (count == 1) {
       int tiles;
-      n += item_cost(k, q, a, rt, &tiles);
-      m += tiles;
+      n = item_cost(k, mine, a, 0, &tiles);
+      m = tiles;
     }
-    if (count > 1) for (int off = 16; off > 0; off >>= 1) { n += __shfl_xor_sync(0xffffffffu, n, off); m += __shfl_xor_sync(0xffffffffu, m, off); }
-    if (lane == 0) { sums[b + 1] = n * groups; tile_sums[b + 1] = m * groups; }
+    for (unsigned many = __ballot_sync(0xffffffffu, count > 1); many; many &= many - 1) {
+      const int l = __ffs(many) - 1;
+      const ChunkRequest q{0, __shfl_sync(0xffffffffu, mine.n, l), __shfl_sync(0xffffffffu, mine.len, l)};
+      long long ni = 0, mi = 0;
+      for (int rt = lane; rt < row_tiles(q.n * a.rep); rt += 32) {
+        int tiles;
+        ni += item_cost(k, q, a, rt, &tiles);
+        mi += tiles;
+      }
+      for (int off = 16; off > 0; off >>= 1) { ni += __shfl_xor_sync(0xffffffffu, ni, off); mi += __shfl_xor_sync(0xffffffffu, mi, off); }
+      if (lane == l) { n = ni; m = mi; }
+    }
+    if (on) { sums[b + 1] = n * groups; tile_sums[b + 1] = m * groups; }
   }
   if (threadIdx.x == 0) sums[0] = tile_sums[0] = 0;
   __syncthreads();
