@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libhspec.so")
 SOURCES = ["hspec.cu", "gemm.cu", "gemm_2sm.cu", "attention.cu", "attention_tc.cu", "scan.cu", "elementwise.cu",
-           "noalloc.cu", "next_ops.cu", "markov_chain.cu", "chunk_rope.cu", "chunk_attention.cu", "verify.cu"]
+           "noalloc.cu", "next_ops.cu", "markov_chain.cu", "chunk_rope.cu", "chunk_attention.cu", "chunk_few.cu", "verify.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 
 

@@ -23,7 +23,7 @@
 //                      They are added to these rows' results at the end, from the cache, on a path that nothing else takes.
 //
 // Every wait is bounded; a role whose wait runs out sets a status word, and the CTA unwinds.
-#include "chunk.cuh"
+#include "chunk_plan.cuh"
 
 #include <cstddef>
 #include <cstdlib>
@@ -35,8 +35,6 @@ namespace {
 
 constexpr int KT = 128;              // keys per tile
 constexpr int MAX_CTAS = 148;
-constexpr int ITEM_ROWS = 256;
-constexpr float NEG = -1.0e30f;
 // What an item costs where every CTA has many tiles, in units of 900 clocks: a tile whose halves take turns 2650 (its 64 KB at a CTA's share of
 // the memory's rate), a tile that both halves see 3550, the way from an item's last tile to the next one's first 12 600 (with 5 in
 // place of 14 a prompt of 8192 tokens takes 638 us, not 548).
@@ -53,46 +51,6 @@ template <int DH> struct Shape {
 
 
 
-struct Args {
-  ChunkAttnCall c;
-  int rep, box_rows;                 // rows of a TMA box; 0: pages are copied by 16-byte loads
-  uint32_t inv_rep;                  // 2^20 / rep, rounded up
-  int group;                         // KV heads that are worked on side by side
-  float scale_log2;
-  float* ws_o;                       // [slot][DH / 4][256 rows][4]
-  float2* ws_ml;                     // [slot][256 rows]
-  int4* ws_start;                    // [CTA]: where its part begins; [MAX_CTAS + CTA]: of the item there, first row, token and query head of the first
-                                     // row, rows.  How many CTAs (per head of a group) have work lies in ws_count
-  int* ws_count;
-};
-
-// ------------------------------------------------------------------ geometry, the same for every role
-struct ItemGeo {
-  int r0, r1;                        // rows of the head
-  int pos0, pos1;                    // positions of the first and the last row's token
-  int key_lo, key_hi;                // keys that any row sees
-  int t0, t1;                        // tiles
-};
-__device__ __forceinline__ bool takes_turns(int rows) { return rows <= 128; }
-__device__ __forceinline__ int row_tiles(int rows) { return takes_turns(rows) ? (rows > 0 ? 1 : 0) : (rows + ITEM_ROWS - 1) / ITEM_ROWS; }
-__device__ __forceinline__ ItemGeo item_geo(const ChunkRequest& q, int rep, int window, int rt) {
-  ItemGeo g;
-  const int rows = q.n * rep;
-  g.r0 = rt * ITEM_ROWS;
-  g.r1 = min(rows, g.r0 + ITEM_ROWS);
-  g.pos0 = max(-1, q.len - q.n + g.r0 / rep);                 // (a place in front of the cache sees nothing, whichever it is: no window wraps round)
-  g.pos1 = max(-1, q.len - q.n + (g.r1 - 1) / rep);
-  g.key_lo = window > 0 ? max(0, g.pos0 - window + 1) : 0;
-  g.key_hi = max(0, g.pos1 + 1);
-  g.t0 = g.key_lo / KT;
-  g.t1 = max(g.t0 + 1, (g.key_hi + KT - 1) / KT);
-  return g;
-}
-
-__device__ __forceinline__ ChunkRequest load_request(const ChunkAttnCall& c, int b) {
-  if (b >= c.B) return ChunkRequest{0, 0, 0};
-  return chunk_request(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len);
-}
 // A CTA's share of an item, as every role needs it.
 struct Segment {
   ItemGeo g;
@@ -121,7 +79,7 @@ struct __align__(16) Bars {
 };
 constexpr size_t smem_bytes(int tile, int slots) { return size_t(tile) * (2 + slots) + sizeof(Bars); }
 
-struct Walk {                        // this CTA's part of the line, item by item
+struct Walk {                        // this CTA's part of the line, item by item; `next` is request b + 1
   int b, g, kvh, rt, off;
   int4 stop;
   ChunkRequest q, next;
@@ -137,7 +95,7 @@ __device__ __forceinline__ Walk walk_begin(const Args& a, const Bars* bars) {
 }
 __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
   Segment s;
-  s.g = item_geo(w.q, a.rep, a.c.window, w.rt);
+  s.g = item_geo<KT>(w.q, a.rep, a.c.window, w.rt);
   s.b = w.b; s.kvh = w.kvh; s.q0 = w.q.q0; s.pos = w.q.len - w.q.n;
   s.tok0 = s.g.r0 / a.rep; s.rem0 = s.g.r0 - s.tok0 * a.rep;
   s.ta = s.g.t0 + w.off;
@@ -157,7 +115,7 @@ __device__ __forceinline__ Segment segment_of(const Walk& w, const Args& a) {
   }
   return s;
 }
-// On to the next item; false at the end of this CTA's part.
+// On to the next item; false at the end of this CTA's part.  (The whole warp.)
 __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a) {
   w.off = 0;
   if (s.tb < s.g.t1) return false;
@@ -167,11 +125,10 @@ __device__ __forceinline__ bool walk_on(Walk& w, const Segment& s, const Args& a
     if (++w.g == a.c.Hkv / a.group) {
       w.kvh -= w.g * a.group;
       w.g = 0;
-      do {
-        ++w.b;
-        w.q = w.next;
-        w.next = load_request(a.c, w.b + 1);
-      } while (w.q.n == 0 && w.b < a.c.B);
+      ++w.b;
+      w.q = w.next;
+      if (w.q.n == 0) w.q = request_from(a, w.b);
+      w.next = load_request(a, w.b + 1);
     }
   }
   return w.b < a.c.B && !(w.stop.w == 0 && w.b == w.stop.x && w.g == w.stop.y && w.rt == w.stop.z);
@@ -216,116 +173,19 @@ __device__ __forceinline__ bool not_finite16(uint32_t x) {
 }
 
 // ------------------------------------------------------------------ the plan
-// The line is measured in costs: an item has `item` in front of its first tile and `turns` or `both` for every tile.  A tile belongs to the part in
-// which its beginning lies.  Where the parts would be so short that one might hold no beginning, every tile counts one and nothing else does.
-struct Costs { int item, turns, both; };
-__device__ __forceinline__ int item_cost(const Costs& k, const ChunkRequest& q, const Args& a, int rt, int* tiles) {
-  const ItemGeo g = item_geo(q, a.rep, a.c.window, rt);
-  *tiles = g.t1 - g.t0;
-  return k.item + (takes_turns(q.n * a.rep) ? k.turns : k.both) * (g.t1 - g.t0);
-}
-// The first tile that begins at u or behind (one warp): request, group of heads, row tile, tile of the item; request B at the end of the line.
-__device__ __forceinline__ int4 place_of(const Args& a, const Costs& k, const long long* sums, long long u, int lane) {
-  const ChunkAttnCall& c = a.c;
-  const int groups = c.Hkv / a.group;
-  if (u >= sums[c.B]) return make_int4(c.B, 0, 0, 0);
-  int lo = 0, hi = c.B;                                       // the request with sums[lo] <= u < sums[lo + 1]
-  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (sums[mid] <= u) lo = mid; else hi = mid; }
-  const ChunkRequest q = load_request(c, lo);
-  const long long per_group = (sums[lo + 1] - sums[lo]) / groups;
-  int g = int((u - sums[lo]) / per_group), rt = 0;
-  long long rest = (u - sums[lo]) - g * per_group;
-  const int count = row_tiles(q.n * a.rep);
-  for (int base = 0; base < count; base += 32) {
-    int tiles;
-    long long upto = base + lane < count ? item_cost(k, q, a, base + lane, &tiles) : 0;
-    for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, upto, off); if (lane >= off) upto += o; }
-    const unsigned in = __ballot_sync(0xffffffffu, upto > rest);
-    if (in) {
-      const int l = __ffs(in) - 1;
-      const long long before = __shfl_sync(0xffffffffu, upto, l > 0 ? l - 1 : 0);
-      rt = base + l;
-      rest -= l > 0 ? before : 0;
-      break;
-    }
-    rest -= __shfl_sync(0xffffffffu, upto, 31);
-  }
-  int tiles, off = 0;
-  item_cost(k, q, a, rt, &tiles);
-  const int each = takes_turns(q.n * a.rep) ? k.turns : k.both;
-  if (rest > 0) off = max(1, int((rest - k.item + each - 1) / each));
-  if (off < tiles) return make_int4(lo, g, rt, off);
-  if (rt + 1 < count) return make_int4(lo, g, rt + 1, 0);
-  if (g + 1 < groups) return make_int4(lo, g + 1, 0, 0);
-  do ++lo; while (lo < c.B && sums[lo + 1] == sums[lo]);
-  return make_int4(lo, 0, 0, 0);
-}
-// Cuts the line: costs and tiles of every request, their running sums, the places where this CTA's part begins and ends.  `sums` is
-// shared memory for twice B + 1 numbers.  Returns false for a CTA without work.
+// Cuts the line: `sums` is shared memory for twice B + 1 numbers.  Returns false for a CTA without work.
 __device__ __forceinline__ bool make_plan(const Args& a, Bars* bars, long long* sums) {
-  const ChunkAttnCall& c = a.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, groups = c.Hkv / a.group, most = gridDim.x / a.group;
-  long long* tile_sums = sums + c.B + 1;
-  Costs k{COST_ITEM, COST_TURNS, COST_BOTH};
-  // a request per lane; those with more than one row tile by the whole warp
-  for (int base = warp * 32; base < c.B; base += warps * 32) {
-    const int b = base + lane;
-    const bool on = b < c.B;
-    const int cu0 = on ? c.cu_q[b] : 0, cu1 = on ? c.cu_q[b + 1] : 0, len = on ? c.kv_lens[b] : 0;
-    const ChunkRequest mine = chunk_request(cu0, cu1, len, c.T, c.max_len);
-    if (blockIdx.x == 0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-    const int count = row_tiles(mine.n * a.rep);
-    long long n = 0, m = 0;
-    if (count == 1) {
-      int tiles;
-      n = item_cost(k, mine, a, 0, &tiles);
-      m = tiles;
-    }
-    for (unsigned many = __ballot_sync(0xffffffffu, count > 1); many; many &= many - 1) {
-      const int l = __ffs(many) - 1;
-      const ChunkRequest q{0, __shfl_sync(0xffffffffu, mine.n, l), __shfl_sync(0xffffffffu, mine.len, l)};
-      long long ni = 0, mi = 0;
-      for (int rt = lane; rt < row_tiles(q.n * a.rep); rt += 32) {
-        int tiles;
-        ni += item_cost(k, q, a, rt, &tiles);
-        mi += tiles;
-      }
-      for (int off = 16; off > 0; off >>= 1) { ni += __shfl_xor_sync(0xffffffffu, ni, off); mi += __shfl_xor_sync(0xffffffffu, mi, off); }
-      if (lane == l) { n = ni; m = mi; }
-    }
-    if (on) { sums[b + 1] = n * groups; tile_sums[b + 1] = m * groups; }
-  }
-  if (threadIdx.x == 0) sums[0] = tile_sums[0] = 0;
-  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, most = gridDim.x / a.group, me = blockIdx.x / a.group;
+  const Line l = make_line<KT>(a, sums, Costs{COST_ITEM, COST_TURNS, COST_BOTH}, most);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.ws_count = l.parts;
+  if (me >= l.parts) return false;
   if (warp < 2) {
-    long long* s = warp == 0 ? sums : tile_sums;
-    long long before = 0;
-    for (int base = 0; base < c.B; base += 32) {
-      long long n = base + lane < c.B ? s[base + lane + 1] : 0;
-      for (int off = 1; off < 32; off <<= 1) { const long long o = __shfl_up_sync(0xffffffffu, n, off); if (lane >= off) n += o; }
-      if (base + lane < c.B) s[base + lane + 1] = before + n;
-      before += __shfl_sync(0xffffffffu, n, 31);
-    }
-  }
-  __syncthreads();
-  if (sums[c.B] < (long long)most * (COST_ITEM + COST_BOTH)) {
-    k = Costs{0, 1, 1};
-    sums = tile_sums;
-  }
-  const long long total = sums[c.B];
-  const int parts = int(min((long long)most, total)), me = blockIdx.x / a.group;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.ws_count = parts;
-  if (me >= parts) return false;
-  if (warp < 2) {
-    const int4 at = place_of(a, k, sums, total * (me + warp) / parts, lane);
+    const int4 at = place_of<KT>(a, l, me + warp, lane);
     if (warp == 0 && lane == 0) {
       bars->start = at;
-      bars->req[0] = load_request(c, at.x);
-      bars->req[1] = load_request(c, at.x + 1);
-      a.ws_start[blockIdx.x] = at;
-      const ChunkRequest q = bars->req[0];
-      const int r0 = at.z * ITEM_ROWS, tok0 = r0 / a.rep;
-      a.ws_start[MAX_CTAS + blockIdx.x] = make_int4(q.q0, tok0, r0 - tok0 * a.rep, min(q.n * a.rep - r0, ITEM_ROWS));
+      bars->req[0] = load_request(a, at.x);
+      bars->req[1] = load_request(a, at.x + 1);
+      put_start(a, blockIdx.x, at, bars->req[0]);
     }
     if (warp == 1 && lane == 0) bars->stop = at;
   }
@@ -1118,7 +978,7 @@ __global__ void __launch_bounds__(256) chunk_attn_join_kernel(const __grid_const
   const int me = blockIdx.x, next = me + a.group, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   if (next >= MAX_CTAS) return;
   const int count = *a.ws_count * a.group, behind = next + lane * a.group;
-  const int4 mine = a.ws_start[me], x = a.ws_start[next], item = a.ws_start[MAX_CTAS + next];
+  const int4 mine = a.ws_start[me], x = a.ws_start[next], item = a.ws_start[a.units + next];
   const int4 y = behind < MAX_CTAS ? a.ws_start[behind] : make_int4(-1, 0, 0, 0);     // (of parts without work: anything)
   if (next >= count) return;
   auto same = [&](const int4& p) { return p.x == x.x && p.y == x.y && p.z == x.z; };
@@ -1222,13 +1082,17 @@ cudaError_t launch_for(const Args& a, cudaStream_t stream, const CUtensorMap& tm
 
 }  // namespace
 
-size_t chunk_attn_workspace_bytes(int, int, int dh) {
-  return size_t(2 * MAX_CTAS) * ITEM_ROWS * (size_t(dh) * 4 + 8) + 2 * MAX_CTAS * sizeof(int4) + 256;
-}
+static size_t own_workspace_bytes(int dh) { return size_t(2 * MAX_CTAS) * ITEM_ROWS * (size_t(dh) * 4 + 8) + 2 * MAX_CTAS * sizeof(int4) + 256; }
+size_t chunk_attn_workspace_bytes(int, int, int dh) { return own_workspace_bytes(dh) + chunk_few_workspace_bytes(dh); }
 
 cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string* err) {
   Args a{};
   a.c = c;
+  if (chunk_few_takes(c)) {
+    const cudaError_t e = chunk_few_launch(c, reinterpret_cast<uint8_t*>(c.ws) + own_workspace_bytes(c.dh), stream);
+    if (e != cudaSuccess || chunk_few_takes_all(c)) return e;
+    a.kind = KIND_MANY;
+  }
   a.rep = c.Hq / c.Hkv;
   a.inv_rep = ((1u << 20) + a.rep - 1) / a.rep;
   a.scale_log2 = c.scale * 1.4426950408889634f;
@@ -1241,6 +1105,7 @@ cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + size_t(2 * MAX_CTAS) * ITEM_ROWS * c.dh);
   a.ws_start = reinterpret_cast<int4*>(a.ws_ml + size_t(2 * MAX_CTAS) * ITEM_ROWS);
   a.ws_count = reinterpret_cast<int*>(a.ws_start + 2 * MAX_CTAS);
+  a.units = MAX_CTAS;
   CUtensorMap tmK{}, tmV{};
   if (a.box_rows && (!pool_tmap(&tmK, c.k_pool, c, a.box_rows, err) || !pool_tmap(&tmV, c.v_pool, c, a.box_rows, err))) return cudaErrorInvalidValue;
   if (c.dh == 64) return c.f16 ? launch_for<64, true>(a, stream, tmK, tmV) : launch_for<64, false>(a, stream, tmK, tmV);

@@ -312,6 +312,11 @@ struct ChunkAttnCall {              // chunk_attention.cu
 };
 size_t chunk_attn_workspace_bytes(int Hq, int Hkv, int dh);
 cudaError_t chunk_attn_launch(const ChunkAttnCall& c, cudaStream_t stream, std::string* err);
+// Requests with few rows (chunk_few.cu): whether a call's are handed to it (all of them, or those behind it are done by the other kernel).
+bool chunk_few_takes(const ChunkAttnCall& c);
+bool chunk_few_takes_all(const ChunkAttnCall& c);
+size_t chunk_few_workspace_bytes(int dh);
+cudaError_t chunk_few_launch(const ChunkAttnCall& c, void* ws, cudaStream_t stream);
 struct VerifyCall {                 // verify.cu
   const void* target; int t_dtype; long long ld_t;      // [T, V]
   const void* draft; int d_dtype; long long ld_d;       // [B * k, Vd] or null: the arg-max drafter

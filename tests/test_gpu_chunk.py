@@ -157,6 +157,93 @@ def test_attention_head_counts(hs, heads):
     c.check(c.run(hs), what=str(heads))
 
 
+FEW = {"8b": (32, 8, 128), "32b": (64, 8, 128), "mha64": (3, 3, 64), "tiny": (4, 2, 64), "seven": (35, 5, 128), "wide64": (128, 16, 64)}
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads", sorted(FEW))
+def test_attention_of_few_rows(hs, heads, dtype):
+    # single tokens, some twos and threes, empty requests and one without an earlier token; lengths around the tiles and steps; one longer block
+    rep = FEW[heads][0] // FEW[heads][1]
+    most = max(1, 8 // rep)
+    new = [1, 1, 0, min(2, most), 1, 1, most, 1, 0, 1, 1, 1, min(3, most), 1, 1]
+    past = [0, 15, 3, 16, 62, 63, 64, 65, 9, 127, 128, 1000, 700, 5, 4095]
+    for extra in ([], [8 // rep + 1]):
+        c = Chunk(FEW[heads], dtype, new + extra, past + [333] * len(extra), seed=len(heads))
+        c.check(c.run(hs), what=heads)
+
+
+@pytest.mark.parametrize("page", [1, 3, 16, 24, 128])
+@pytest.mark.parametrize("window", [0, 1, 17, 100, 2 ** 31 - 1])
+def test_windows_and_pages_of_few_rows(hs, page, window):
+    c = Chunk((4, 4, 128) if page % 2 else (16, 4, 64), torch.bfloat16, [1, 2, 1, 1, 2, 1], [500, 99, 0, 77, 1, 2000], page=page, seed=page)
+    c.check(c.run(hs, window=window), window=window, what=f"page {page} window {window}")
+
+
+def test_few_rows_without_a_place(hs):
+    c = Chunk((4, 4, 64), torch.bfloat16, [6, 2, 1, 0], [-2, -2, 40, 5], seed=5)
+    hs.hspec_op_device_status(clear=True)
+    o = c.run(hs)
+    c.check(o, what="no place")
+    assert (o[:2] == 0).all() and (o[6:8] == 0).all() and (o[2] != 0).any()
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 2
+
+
+@pytest.mark.parametrize("what", ["value", "key"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_what_few_rows_do_not_see_never_reaches_them(hs, what, bad):
+    """Four tokens of a request whose third has a bad key or value, and a window that leaves a bad place to the first row alone."""
+    c = Chunk((4, 2, 128), torch.bfloat16, [4, 1], [150, 3], page=16, seed=9)
+    good = c.run(hs, window=100).clone()
+    pool = c.v if what == "value" else c.k
+    for key in (152, 51):                                    # row i stands at 150 + i and sees 51 + i .. 150 + i
+        pool[c.table[0, key // 16].long(), key % 16, 1, 7] = bad
+    o = c.run(hs, window=100)
+    assert torch.equal(o[1], good[1]) and torch.equal(o[4], good[4]) and torch.equal(o[:, :2], good[:, :2])
+    for row in (0, 2, 3):
+        if what == "value":
+            x = o[row, 2:, 7]
+            assert torch.isnan(x).all() if bad != bad else (x == bad).all()
+            assert torch.equal(o[row, 2:, 8:], good[row, 2:, 8:])
+        else:                                                # (an infinite key is a score of +-infinity, of either sign for a query)
+            assert torch.isnan(o[row, 2:]).any() or bad == bad
+    hs.hspec_op_device_status(clear=True)
+
+
+@pytest.mark.parametrize("spread", [0.0, 8.0, 40.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_few_flat_and_peaked_rows(hs, spread, dtype):
+    c = Chunk(HEADS["8b"], dtype, [1] * 9, [3000, 64, 17, 900, 1, 0, 5000, 128, 2], seed=3, spread=spread)
+    c.check(c.run(hs), what=f"spread {spread}")
+
+
+def test_few_rows_same_bits_on_streams_and_in_graphs(hs):
+    c = Chunk(HEADS["8b"], torch.bfloat16, [1, 2, 1], [3000, 700, 60], seed=13)
+    first = c.run(hs).clone()
+    side, outs = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for s in side:
+        with torch.cuda.stream(s):
+            outs.append(c.run(hs, o=torch.full_like(c.q, 7.0), ws=c.workspace(hs)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, first) for o in outs)
+    graph, o, ws = torch.cuda.CUDAGraph(), torch.full_like(c.q, 7.0), c.workspace(hs)
+    with torch.cuda.graph(graph):
+        c.run(hs, o=o, ws=ws)
+    for _ in range(2):
+        o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, first)
+    c.kv_lens -= 1
+    c.cu[3] = c.cu[2]
+    o.fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    c.rows, c.kv = 3, [x - 1 for x in c.kv]
+    c.check(o, what="replay")
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_attention_of_thousands_of_requests(hs, dtype):
     # the most requests, two thirds of them without a row: every CTA goes through many short items
