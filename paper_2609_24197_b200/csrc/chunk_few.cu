@@ -2,8 +2,9 @@
 //   o[t, h] = sum_j p_j v[j, g] / sum_j p_j,  p_j = exp(scale q[t, h] . k[j, g]),  the keys as in chunk_attention.cu
 //
 // With 4 or 8 rows there is next to nothing to compute, and what counts is how many bytes are under way and how long the way from an item's first byte to
-// its result is.  The tcgen05 kernel has one item at a time on an SM, and that way takes 13 000 clocks (8192 single tokens over 100 others: 3080 us).  Here
-// every warp has an item of its own, twelve to an SM, and needs no shared memory and no barrier for it.
+// its result is.  The tcgen05 kernel has one item at a time on an SM, and that way takes 13 000 clocks.  Here every warp has an item of its own, twelve to
+// an SM, and needs no shared memory and no barrier for it.  32 query heads on 8 of 128, bf16: 2000 single tokens over 300 others 412 us (6.0 TB/s; the
+// other kernel 1324), 8192 over 100 others 677 us (5.5 TB/s; 3080), one over 2047 others 14.0 us (20.5; latency alone).
 //
 // A warp takes 16 keys a step, on mma.sync with the keys in the rows of the product: S^T = K Q^T and O^T += V^T P^T, so that 8 columns hold all rows of
 // the head and nothing is padded.  Loads go straight to registers, 16 bytes of a key (value) for a thread, and are under way a step ahead.
@@ -19,8 +20,10 @@ namespace hspec {
 
 namespace {
 
-constexpr int TILE = 64;             // keys that are not shared between warps
-constexpr int WARPS = 12;            // of an SM: as many as 168 registers leave room for
+// Keys that are not shared between warps: one token over 2047 others takes 14.0 us, 15.4 with 64 and 15.1 with 16 (more parts to join), and long lines
+// do not care.
+constexpr int TILE = 32;
+constexpr int WARPS = 12;            // of an SM: as many as 168 registers leave room for (10 are 3 to 6 % slower on long lines)
 constexpr int UNITS = 148 * WARPS;
 constexpr int COST_ITEM = 1, COST_TILE = 1;
 constexpr float LAZY = 8.0f;
@@ -55,6 +58,29 @@ template <bool F16> __device__ __forceinline__ bool not_finite16(uint32_t x) {
 }
 template <bool F16> __device__ __forceinline__ float widen16(uint16_t x) { return F16 ? __half2float(__ushort_as_half(x)) : bf16_bits_to_float(x); }
 
+__device__ __forceinline__ long long quotient(long long a, int b) {      // (a >= 0, b > 0; a 64-bit division is some hundred instructions)
+  return (a >> 32) == 0 ? (long long)(uint32_t(a) / uint32_t(b)) : a / b;
+}
+// place_of, for items of one row tile and costs of one a tile: every lane may ask for another part.
+__device__ __forceinline__ int4 place_of_few(const Args& a, const Line& line, int i) {
+  const long long* sums = line.sums;
+  const int B = a.c.B, groups = a.c.Hkv / a.group;
+  const long long u = quotient(sums[B] * i, line.parts);
+  auto request_at = [&](long long v) {                        // the request with sums[r] <= v < sums[r + 1], or B
+    int lo = 0, hi = B;
+    while (lo < hi) { const int mid = (lo + hi) >> 1; if (sums[mid + 1] <= v) lo = mid + 1; else hi = mid; }
+    return lo;
+  };
+  const int r = request_at(u);
+  if (r >= B) return make_int4(B, 0, 0, 0);
+  const long long each = quotient(sums[r + 1] - sums[r], groups);
+  const int item = int(each), rest0 = int(u - sums[r] - quotient(u - sums[r], item) * item), g = int(quotient(u - sums[r], item));
+  const int off = rest0 > 0 ? max(1, rest0 - line.k.item) : 0;
+  if (off < item - line.k.item) return make_int4(r, g, 0, off);
+  if (g + 1 < groups) return make_int4(r, g + 1, 0, 0);
+  return make_int4(request_at(sums[r + 1]), 0, 0, 0);
+}
+
 template <int DH, bool F16>
 __global__ void __launch_bounds__(WARPS * 32, 1) chunk_few_kernel(const __grid_constant__ Args a) {
   constexpr int KP = DH / 32, VB = DH / 64;                   // 16-byte pieces of a key for a thread, blocks of 64 columns
@@ -67,7 +93,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) chunk_few_kernel(const __grid_c
   const Line line = make_line<TILE>(a, sums, Costs{COST_ITEM, COST_TILE, COST_TILE}, int(gridDim.x) * WARPS / a.group);
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.ws_count = line.parts;
   if (part >= line.parts) return;
-  const int4 start = place_of<TILE>(a, line, part, lane), stop = place_of<TILE>(a, line, part + 1, lane);
+  int4 start = place_of_few(a, line, part + (lane & 1)), stop;
+  stop.x = __shfl_sync(0xffffffffu, start.x, 1); stop.y = __shfl_sync(0xffffffffu, start.y, 1); stop.w = __shfl_sync(0xffffffffu, start.w, 1);
+  start.x = __shfl_sync(0xffffffffu, start.x, 0); start.y = __shfl_sync(0xffffffffu, start.y, 0); start.w = __shfl_sync(0xffffffffu, start.w, 0);
   int b = start.x, group = start.y, tile = start.w, slot = 2 * unit;
   ChunkRequest q = load_request(a, b), q_next = load_request(a, b + 1);
   if (lane == 0) put_start(a, unit, start, q);
@@ -264,62 +292,114 @@ __global__ void __launch_bounds__(WARPS * 32, 1) chunk_few_kernel(const __grid_c
   }
 }
 
-// Joins the items that a cut went through: a block per part, a warp per row.  The part that an item begins in speaks for it.
+// Joins the items that a cut went through; the part that an item begins in speaks for it.  A block looks at a part for every SM (a warp each), then
+// joins what there is to join, 16 warps to an item: a warp per row and share of the parts.  What it waits for in turn is the places, the rows' maxima
+// and sums, and the partial results.
+constexpr int JOIN_WARPS = 16;
 template <int DH, bool F16>
-__global__ void __launch_bounds__(FEW_ROWS * 32) chunk_few_join_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_few_join_kernel(const __grid_constant__ Args a) {
   pdl_wait();
   pdl_trigger();
   constexpr int COLS = DH / 32;                               // of a lane
+  static_assert(WARPS <= JOIN_WARPS, "a warp for every part");
+  struct Job { int4 at, item; int unit, first, n; };
+  __shared__ Job jobs[WARPS];
+  __shared__ float part[JOIN_WARPS][DH];
+  __shared__ float2 part_ml[JOIN_WARPS];
   const ChunkAttnCall& c = a.c;
-  const int me = blockIdx.x, next = me + a.group, lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-  if (next >= a.units) return;
-  const int count = *a.ws_count * a.group, behind = next + lane * a.group;
-  const int4 mine = a.ws_start[me], x = a.ws_start[next], item = a.ws_start[a.units + next];
-  const int4 y = behind < a.units ? a.ws_start[behind] : make_int4(-1, 0, 0, 0);      // (of parts without work: anything)
-  if (next >= count) return;
-  auto same = [&](const int4& p) { return p.x == x.x && p.y == x.y && p.z == x.z; };
-  if (x.w == 0 || (same(mine) && mine.w > 0) || r >= item.w) return;     // no cut through an item here, or an earlier part speaks for it
-  unsigned run = __ballot_sync(0xffffffffu, behind < count && same(y));
-  int n = 1 + (run == 0xffffffffu ? 32 : __ffs(~run) - 1);
-  for (int base = next + 32 * a.group; run == 0xffffffffu; base += 32 * a.group) {
-    const int at = base + lane * a.group;
-    run = __ballot_sync(0xffffffffu, at < count && same(a.ws_start[at < count ? at : me]));
-    n += run == 0xffffffffu ? 32 : __ffs(~run) - 1;
-  }
-  const int first = 2 * me + (same(mine) ? 0 : 1);
-  auto row_of = [&](int i) { return size_t(i == 0 ? first : 2 * (me + i * a.group)) * FEW_ROWS + r; };
-  float m = NEG, sum = 0.f, acc[COLS];
-#pragma unroll
-  for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
-  for (int base = 0; base < n; base += 32) {
-    const float2 ml = base + lane < n ? a.ws_ml[row_of(base + lane)] : make_float2(NEG, 0.f);
-    float mm = fmaxf(ml.x, m);
-    for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-    const float f = ex2_ftz(m - mm), w = ml.x == NEG && ml.y == 0.f ? 0.f : ex2_ftz(ml.x - mm);
-    float s = ml.y * w;
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    m = mm;
-    sum = sum * f + s;
-#pragma unroll
-    for (int e = 0; e < COLS; ++e) acc[e] *= f;
-#pragma unroll 8
-    for (int i = 0; i < min(32, n - base); ++i) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float* src = a.ws_o + row_of(base + i) * DH + lane * COLS;
-#pragma unroll
-      for (int e = 0; e < COLS; e += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(src + e);
-        acc[e] = fmaf(wi, v.x, acc[e]);
-        acc[e + 1] = fmaf(wi, v.y, acc[e + 1]);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (warp < WARPS) {
+    const int me = blockIdx.x + gridDim.x * warp, next = me + a.group, behind = next + lane * a.group;
+    int n = 0;
+    if (next < a.units) {
+      const int count = *a.ws_count * a.group;
+      const int4 mine = a.ws_start[me], x = a.ws_start[next], item = a.ws_start[a.units + next];
+      const int4 y = behind < a.units ? a.ws_start[behind] : make_int4(-1, 0, 0, 0);  // (of parts without work: anything)
+      auto same = [&](const int4& p) { return p.x == x.x && p.y == x.y && p.z == x.z; };
+      // a cut through an item here, and no earlier part that speaks for it
+      if (next < count && x.w > 0 && !(same(mine) && mine.w > 0)) {
+        unsigned run = __ballot_sync(0xffffffffu, behind < count && same(y));
+        n = 1 + (run == 0xffffffffu ? 32 : __ffs(~run) - 1);
+        for (int base = next + 32 * a.group; run == 0xffffffffu; base += 32 * a.group) {
+          const int at = base + lane * a.group;
+          run = __ballot_sync(0xffffffffu, at < count && same(a.ws_start[at < count ? at : me]));
+          n += run == 0xffffffffu ? 32 : __ffs(~run) - 1;
+        }
+        if (lane == 0) jobs[warp] = Job{x, item, me, 2 * me + (same(mine) ? 0 : 1), n};
       }
     }
+    if (n == 0 && lane == 0) jobs[warp].n = 0;
   }
-  const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
-  const int at = item.z + r, token = item.y + at / a.rep, kvh = x.y * a.group + me % a.group;
-  uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + size_t(item.x + token) * c.ldo + size_t(kvh * a.rep + at % a.rep) * DH + lane * COLS;
+  __syncthreads();
+  for (int j = 0; j < WARPS; ++j) {
+    const int n = jobs[j].n;
+    if (n == 0) continue;
+    const int rows = jobs[j].item.w, me = jobs[j].unit, first = jobs[j].first;
+    const int wide = rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = JOIN_WARPS / wide, r = warp % wide, share = warp / wide;
+    auto row_of = [&](int i) { return size_t(i == 0 ? first : 2 * (me + i * a.group)) * FEW_ROWS + r; };
+    float m = NEG, sum = 0.f, acc[COLS];
 #pragma unroll
-  for (int e = 0; e < COLS; e += 2)
-    *reinterpret_cast<uint32_t*>(dst + e) = F16 ? pack_f16_sat(acc[e] * inv, acc[e + 1] * inv, c.status) : pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+    for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+    // this warp's parts: share, share + shares, ..
+    for (int base = share; base < n && r < rows; base += 32 * shares) {
+      const int mine = base + lane * shares, count = min(32, (n - base + shares - 1) / shares);
+      const float2 ml = mine < n ? a.ws_ml[row_of(mine)] : make_float2(NEG, 0.f);
+      float v[8][COLS];
+      auto load = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+          for (int e = 0; e < COLS; e += 2) {
+            const float2 x = i + u < count ? *reinterpret_cast<const float2*>(a.ws_o + row_of(base + (i + u) * shares) * DH + lane * COLS + e) : make_float2(0.f, 0.f);
+            v[u][e] = x.x; v[u][e + 1] = x.y;
+          }
+      };
+      load(0);                                                // (under way with the maxima)
+      float mm = fmaxf(ml.x, m);
+      for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+      const float f = ex2_ftz(m - mm), w = ml.x == NEG && ml.y == 0.f ? 0.f : ex2_ftz(ml.x - mm);
+      float s = ml.y * w;
+      for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+      m = mm;
+      sum = sum * f + s;
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] *= f;
+      for (int i = 0; i < count; i += 8) {
+        if (i > 0) load(i);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float wi = __shfl_sync(0xffffffffu, w, (i + u) & 31);
+#pragma unroll
+          for (int e = 0; e < COLS; ++e) acc[e] = i + u < count ? fmaf(wi, v[u][e], acc[e]) : acc[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) part[warp][lane * COLS + e] = acc[e];
+    if (lane == 0) part_ml[warp] = make_float2(m, sum);
+    __syncthreads();
+    if (share == 0 && r < rows) {
+      for (int i = 1; i < shares; ++i) m = fmaxf(m, part_ml[i * wide + r].x);
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+      for (int i = 0; i < shares; ++i) {
+        const float2 ml = part_ml[i * wide + r];
+        const float f = ml.x == NEG && ml.y == 0.f ? 0.f : ex2_ftz(ml.x - m);
+        sum += ml.y * f;
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) acc[e] = fmaf(part[i * wide + r][lane * COLS + e], f, acc[e]);
+      }
+      const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+      const int4 item = jobs[j].item;
+      const int at = item.z + r, token = item.y + at / a.rep, kvh = jobs[j].at.y * a.group + me % a.group;
+      uint16_t* dst = reinterpret_cast<uint16_t*>(c.o) + size_t(item.x + token) * c.ldo + size_t(kvh * a.rep + at % a.rep) * DH + lane * COLS;
+#pragma unroll
+      for (int e = 0; e < COLS; e += 2)
+        *reinterpret_cast<uint32_t*>(dst + e) = F16 ? pack_f16_sat(acc[e] * inv, acc[e + 1] * inv, c.status) : pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+    }
+    __syncthreads();                                          // (the arrays are free again)
+  }
 }
 
 template <int DH, bool F16>
@@ -335,7 +415,7 @@ cudaError_t launch_for(const Args& a, cudaStream_t stream) {
   const int n = min(sms[current_device()], UNITS / WARPS);
   e = launch_pdl(chunk_few_kernel<DH, F16>, dim3(n), dim3(WARPS * 32), 2 * (size_t(a.c.B) + 1) * 8, stream, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(chunk_few_join_kernel<DH, F16>, dim3(n * WARPS), dim3(FEW_ROWS * 32), 0, stream, a);
+  return launch_pdl(chunk_few_join_kernel<DH, F16>, dim3(UNITS / WARPS), dim3(JOIN_WARPS * 32), 0, stream, a);
 }
 
 }  // namespace
