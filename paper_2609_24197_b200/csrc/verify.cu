@@ -25,6 +25,7 @@ namespace {
 
 constexpr int VT = 512;              // threads of a block
 constexpr int VW = VT / 32;
+constexpr int MAX_S = 16;            // most blocks of a cluster
 constexpr float LOG2E = 1.4426950408889634f;
 
 // A logit as it counts: NaN as -infinity (as in every arg-max of this library), +infinity as the largest finite number.
@@ -248,7 +249,7 @@ __device__ __forceinline__ void cluster_or_block_sync(int S) {
 // Sum over the cluster's threads, the same bits in every one of them: lanes, warps and blocks are added in a fixed order.
 struct Reduce64 {
   double warp[2][VW];
-  double block[2][8];
+  double block[2][MAX_S];
 };
 __device__ __forceinline__ void cluster_sum2(Reduce64& sh, int S, int rank, double& a, double& b) {
   for (int off = 16; off > 0; off >>= 1) { a += shfl_xor64(a, off); b += shfl_xor64(b, off); }
@@ -267,7 +268,7 @@ __device__ __forceinline__ void cluster_sum2(Reduce64& sh, int S, int rank, doub
 }
 
 struct ReduceKey {
-  unsigned long long warp[VW], block[8];
+  unsigned long long warp[VW], block[MAX_S];
 };
 __device__ __forceinline__ unsigned long long cluster_max_key(ReduceKey& sh, int S, int rank, unsigned long long k) {
   for (int off = 16; off > 0; off >>= 1) { const unsigned long long o = __shfl_xor_sync(0xffffffffu, k, off); k = o > k ? o : k; }
@@ -504,7 +505,7 @@ struct SampleShared {
   Reduce64 sum;
   ReduceKey key;
   double warp[VW];
-  double block[8];
+  double block[MAX_S];
   float map[VW][128];
   int n, found, last;
 };
@@ -823,13 +824,13 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   const long long items = (long long)c.B * c.k;
   // blocks of a cluster: two for every SM where there are few items, as long as each has a few KB to read
-  auto blocks_for = [&](long long n) {
+  auto blocks_for = [&](long long n, int most) {
     int S = 1;
-    while (S < 8 && n * 2 * S <= 2 * 148 && c.V / (2 * S) >= 2048) S *= 2;
+    while (S < most && n * 2 * S <= 2 * 148 && c.V / (2 * S) >= 2048) S *= 2;
     return S;
   };
   if (items > 0) {
-    const int S = blocks_for(items), skip = items * S > 2 * 148;
+    const int S = blocks_for(items, 8), skip = items * S > 2 * 148;
     if (skip) {
       e = launch_pdl(verify_init_kernel, dim3(1), dim3(256), 0, stream, s.first, c.B);
       if (e != cudaSuccess) return e;
@@ -837,7 +838,15 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip);
     if (e != cudaSuccess) return e;
   }
-  const int S = blocks_for(c.B), S64 = blocks_for(1);   // (few requests are left for the third)
+  // About one request in ten is left for the third kernel, and what it waits for is the 64-bit pipes of its SMs: 16 blocks each as long as there are SMs
+  // for them (37 requests of 151 937 tokens: 45 us, 58 with 8; 128 of 152 064: 77, 60 with 8).
+  const int S = blocks_for(c.B, MAX_S), S64 = blocks_for(1, c.B <= 64 ? MAX_S : 8);
+  static bool done[MAX_DEVICES] = {};
+  e = once_per_device(done, [](int) {
+    const cudaError_t e1 = cudaFuncSetAttribute(verify_sample_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e1 != cudaSuccess ? e1 : cudaFuncSetAttribute(verify_sample_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  });
+  if (e != cudaSuccess) return e;
   e = launch_pdl_cluster(verify_sample_kernel<false>, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
   if (e != cudaSuccess) return e;
   return launch_pdl_cluster(verify_sample_kernel<true>, dim3(unsigned(c.B) * S64), dim3(VT), dim3(S64), 0, stream, c, s, S64);
