@@ -76,8 +76,8 @@ __device__ __forceinline__ uint32_t nothing(float) { return 0xff800000u; }
 __device__ __forceinline__ uint32_t nothing(__half) { return 0xfc00fc00u; }
 __device__ __forceinline__ uint32_t nothing(__nv_bfloat16) { return 0xff80ff80u; }
 // Calls f(first index, values of N neighbours) for this thread's share of [begin, end): 16-byte loads, U of them in flight (behind the last: values
-// of -infinity), scalar loads in front of the first 16-byte boundary and behind the last.
-template <int U, typename T, typename F>
+// of -infinity), scalar loads in front of the first 16-byte boundary and behind the last.  LOGITS: values as they count, else words as they are.
+template <int U, bool LOGITS = true, typename T, typename F>
 __device__ __forceinline__ void walk(const T* z, int begin, int end, F f) {
   constexpr int N = 16 / sizeof(T);
   const int off = int((reinterpret_cast<uintptr_t>(z + begin) & 15) / sizeof(T));
@@ -99,17 +99,17 @@ __device__ __forceinline__ void walk(const T* z, int begin, int end, F f) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float v[N];
-      unpack16(w[u], v, T());
+      unpack16<LOGITS>(w[u], v, T());
       f(head + (i0 + u * VT) * N, v);
     }
   }
   for (int i = head + n16 * N + int(threadIdx.x); i < end; i += VT) { float v[1] = {logit(value_of(z[i]))}; f(i, v); }
 }
-template <int U, typename F>
+template <int U, bool LOGITS = true, typename F>
 __device__ __forceinline__ void walk(const Row& r, int begin, int end, F f) {
-  if (r.dtype == CHUNK_F32) walk<U>(reinterpret_cast<const float*>(r.z), begin, end, f);
-  else if (r.dtype == CHUNK_F16) walk<U>(reinterpret_cast<const __half*>(r.z), begin, end, f);
-  else walk<U>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, f);
+  if (r.dtype == CHUNK_F32) walk<U, LOGITS>(reinterpret_cast<const float*>(r.z), begin, end, f);
+  else if (r.dtype == CHUNK_F16) walk<U, LOGITS>(reinterpret_cast<const __half*>(r.z), begin, end, f);
+  else walk<U, LOGITS>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, f);
 }
 
 struct MaxSum { float mx, sum; };
@@ -199,16 +199,23 @@ __device__ __noinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
   if (x.sum == 0.f) x.mx = -INFINITY;             // (nothing but -infinity)
   return x;
 }
-// The largest value and its lowest index over this thread's share, as one number (argmax_key).
+// The largest value and its lowest index over this thread's share, as one number (argmax_key).  A word's maximum first, and its place where it is a new one.
 __device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
-  unsigned long long best = 0;
   float mx = -INFINITY;
-  walk<4>(r, begin, end, [&](int i, auto& v) {
+  int at = begin;
+  walk<4, false>(r, begin, end, [&](int i, auto& v) {
     constexpr int N = sizeof(v) / sizeof(float);
+    float m = v[0];
 #pragma unroll
-    for (int j = 0; j < N; ++j) if (v[j] > mx || best == 0) { mx = v[j]; best = argmax_key(v[j], i + j); }
+    for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);           // (NaN gives way)
+    m = fminf(m, FLT_MAX);
+    if (m > mx) {
+      mx = m;
+#pragma unroll
+      for (int j = N - 1; j >= 0; --j) if (fminf(v[j], FLT_MAX) == m) at = i + j;
+    }
   });
-  return best;
+  return begin < end ? argmax_key(mx, at) : 0;
 }
 
 // e^((z - m) / t) in 64 bits; nothing where z is -infinity
