@@ -474,13 +474,14 @@ struct RowWeights {                    // the weights of one row's logits, from 
   const Weights* w;
   const void* z;
   float m, inv_tf;
-  double md, inv_t;
+  double md, inv_t;                    // -m / temperature, 1 / temperature
   float log2_t, factor;                // of the 32-bit ones: log2(e) / temperature
   bool bf16;
   __device__ __forceinline__ double operator()(float v) const {
     if (!EXACT) return double(quick(v));
     const double magic = 6755399441055744.0;                  // 1.5 2^52: whole numbers end up in the low bits
-    const double x = (double(v) - md) * inv_t, t = fma(x, 369.32993046757655, magic);      // 256 / ln 2
+    // (-m / temperature is rounded once, alike in all of the row's weights)
+    const double x = fma(double(v), inv_t, md), t = fma(x, 369.32993046757655, magic);       // 256 / ln 2
     const int k = __double2loint(t);
     const double f = fma(t - magic, -0.0027076061740622863, x);                              // ln 2 / 256
     const double p = f * fma(f, fma(f, fma(f, 1.0 / 24.0, 1.0 / 6.0), 0.5), 1.0), y = w->table[k & 255];
@@ -557,8 +558,12 @@ __device__ __noinline__ double rest_sum(RowWeights<EXACT> p, RowWeights<EXACT> q
   auto add = [&](float (&t)[4], const float (&d)[4]) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (EXACT) s[u] += MINUS ? fmax(0.0, p(t[u]) - q(d[u])) : p(t[u]);
-      else t[u] = MINUS ? fmaxf(0.f, p.quick(t[u]) - q.quick(d[u])) : p.quick(t[u]);
+      if (EXACT) {
+        const double w = MINUS ? p(t[u]) - q(d[u]) : p(t[u]);
+        s[u] += !MINUS || w > 0.0 ? w : 0.0;                  // (never NaN; fmax looks for it)
+      } else {
+        t[u] = MINUS ? fmaxf(0.f, p.quick(t[u]) - q.quick(d[u])) : p.quick(t[u]);
+      }
     }
     if (!EXACT) s[0] += double((t[0] + t[1]) + (t[2] + t[3]));
   };
@@ -696,8 +701,8 @@ verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant
   const float inv_tf = fminf(float(inv_t), 3.0e38f);
   const bool t32 = c.t_dtype == CHUNK_F32, d32 = c.d_dtype == CHUNK_F32;
   const float log2_t = fminf(fmaxf(LOG2E / r.t, 1e-30f), 1e30f);
-  RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, double(mt), inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
-  RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, double(md), inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
+  RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, -double(mt) * inv_t, inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
+  RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, -double(md) * inv_t, inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
   const int gone_token = refused && !c.draft ? c.ids[at] : -1;        // the arg-max drafter's, which takes all of its q
   if (both) {
     int dbegin, dend;
