@@ -432,8 +432,9 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
 
 // One (position, request) per cluster, position by position.  verdict[b * k + i] = 1 if the draft would stand; the row maxima (and for greedy requests
 // the arg-max) are left for the kernel behind.  skip: first[b] holds the lowest position refused so far, and items behind it are passed over.
-// 128 requests of 16 drafts, 575 MB up to the first refused ones: 160 us and 770 MB, the rest read while the verdict in front was still out.  (Clusters
-// that walk the items themselves 205 us; leaving off a row whose request has been refused meanwhile 735 MB in 167 us.)
+// 128 requests of 16 drafts, 575 MB up to the first refused ones: 160 us and 960 MB, the rest read while the verdict in front was still out.  (Clusters
+// that walk the items themselves 205 us; leaving off a row whose request has been refused meanwhile saved some bytes and no time; two blocks a row
+// read fewer ahead in the same time, four are slower.)
 __global__ void __launch_bounds__(VT, 2)
 verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S, int skip) {
   pdl_wait();
