@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) chunk_few_kernel(const __grid_c
 // Joins the items that a cut went through; the part that an item begins in speaks for it.  A block looks at a part for every SM (a warp each), then
 // joins what there is to join, 16 warps to an item: a warp per row and share of the parts.  What it waits for in turn is the places, the rows' maxima
 // and sums, and the partial results.
-constexpr int JOIN_WARPS = 16;
+constexpr int JOIN_WARPS = 16, JOIN_AHEAD = 16;             // partial results under way at a time
 template <int DH, bool F16>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_few_join_kernel(const __grid_constant__ Args a) {
   pdl_wait();
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_few_join_kernel(const _
     if (n == 0) continue;
     const int rows = jobs[j].item.w, me = jobs[j].unit, first = jobs[j].first;
     const int wide = rows > 4 ? 8 : rows > 2 ? 4 : rows, shares = JOIN_WARPS / wide, r = warp % wide, share = warp / wide;
-    auto row_of = [&](int i) { return size_t(i == 0 ? first : 2 * (me + i * a.group)) * FEW_ROWS + r; };
+    auto row_of = [&](int i) { return unsigned(i == 0 ? first : 2 * (me + i * a.group)) * FEW_ROWS + r; };
     float m = NEG, sum = 0.f, acc[COLS];
 #pragma unroll
     for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
@@ -344,10 +344,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_few_join_kernel(const _
     for (int base = share; base < n && r < rows; base += 32 * shares) {
       const int mine = base + lane * shares, count = min(32, (n - base + shares - 1) / shares);
       const float2 ml = mine < n ? a.ws_ml[row_of(mine)] : make_float2(NEG, 0.f);
-      float v[8][COLS];
+      float v[JOIN_AHEAD][COLS];
       auto load = [&](int i) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < JOIN_AHEAD; ++u)
 #pragma unroll
           for (int e = 0; e < COLS; e += 2) {
             const float2 x = i + u < count ? *reinterpret_cast<const float2*>(a.ws_o + row_of(base + (i + u) * shares) * DH + lane * COLS + e) : make_float2(0.f, 0.f);
@@ -364,10 +364,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_few_join_kernel(const _
       sum = sum * f + s;
 #pragma unroll
       for (int e = 0; e < COLS; ++e) acc[e] *= f;
-      for (int i = 0; i < count; i += 8) {
+      for (int i = 0; i < count; i += JOIN_AHEAD) {
         if (i > 0) load(i);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < JOIN_AHEAD; ++u) {
           const float wi = __shfl_sync(0xffffffffu, w, (i + u) & 31);
 #pragma unroll
           for (int e = 0; e < COLS; ++e) acc[e] = i + u < count ? fmaf(wi, v[u][e], acc[e]) : acc[e];
