@@ -414,6 +414,7 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
       const float tol = (24.f + fabsf(xt) + fabsf(vd > -INFINITY ? xd : 0.f)) * 3.2e-7f;
       verdict = ratio >= alpha;
       near = !(ratio > 1e-30f) || !(alpha > 1e-30f) || fabsf(ratio - alpha) <= tol * alpha;
+      near |= xt < -1000.f || xd < -1000.f;       // (p or q may be nothing in 64 bits, or not whole: decided there)
     }
     s.verdict[at] = verdict;
     if (skip && !verdict && !near) atomicMin(s.first + b, i);

@@ -145,6 +145,18 @@ def test_uniform_numbers_next_to_a_cumulative_sum(hs):
     assert n.tolist() == [1] * 8 and tok[:, 1].tolist() == [0, 1, 2, V // 2, V - 1, V - 1, 0, V - 1]
 
 
+def test_probabilities_that_64_bits_do_not_hold(hs):
+    """A low temperature: p and q of the drafted token at 2^-900 .. 2^-1100, where they lose bits and become nothing, with their ratio near 1."""
+    B, V = 64, 12
+    z, d = torch.zeros((2 * B, V)), torch.zeros((B, 1, V))
+    depth = torch.linspace(620.0, 765.0, B)                  # of the token, in units of the temperature (2^-1022 is e^-708, the least is e^-745)
+    temperature = torch.full((B,), 2.0 ** -10)
+    z[0::2, 3] = -depth * 2.0 ** -10
+    d[:, 0, 3] = (-depth + torch.tensor([1.5, -1.5]).repeat(B // 2)) * 2.0 ** -10
+    n, _ = _check(hs, z, d, torch.full((B, 1), 3, dtype=torch.int32), torch.full((B, 1), 0.5), torch.full((B,), 0.4), temperature=temperature)
+    assert 0 < n.sum() < B // 2
+
+
 def test_what_an_argmax_drafter_leaves_over(hs):
     """The refused token holds nearly all of p: the rest is as small as 2^-39 of it, and its tokens are alike or far apart."""
     B, V = 240, 5003
