@@ -467,10 +467,11 @@ verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__
 // ------------------------------------------------------------------ the token behind the drafts that stand
 // A row is full of 64-bit exponentials here: e^x = 2^n 2^(i / 256) e^f with |f| <= ln 2 / 512, 2^(i / 256) from a table in shared memory (times the
 // factor that the row's weights need anyway) and e^f by its series up to f^4 / 24 (the next term is 4e-17): 10 operations in 64 bits, where the
-// library's function takes three times as many.  Nothing below e^-700, which no sum of weights with a 1 among them shows.
+// library's function, left to what lies below e^-700, takes three times as many.
 struct Weights {
   double table[256];
 };
+__device__ __noinline__ double exp_of(double x) { return exp(x); }
 template <bool EXACT>
 struct RowWeights {                    // the weights of one row's logits, from its maximum, temperature and factor
   const Weights* w;
@@ -488,7 +489,9 @@ struct RowWeights {                    // the weights of one row's logits, from 
     const double f = fma(t - magic, -0.0027076061740622863, x);                              // ln 2 / 256
     const double p = f * fma(f, fma(f, fma(f, 1.0 / 24.0, 1.0 / 6.0), 0.5), 1.0), y = w->table[k & 255];
     const double r = fma(y, p, y);
-    return (v - m) * inv_tf > -700.f ? __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r)) : 0.0;
+    const float depth = (v - m) * inv_tf;
+    if (depth > -700.f) return __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r));
+    return depth > -746.f ? exp_of(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
   }
   __device__ __forceinline__ float quick(float v) const { return ex2_ftz((v - m) * log2_t) * factor; }
   // A logit as it lies in memory, and what it says.  (Two steps, so that many loads go out before the first is looked at; no branch on the type.)

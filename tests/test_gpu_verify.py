@@ -157,6 +157,20 @@ def test_probabilities_that_64_bits_do_not_hold(hs):
     assert 0 < n.sum() < B // 2
 
 
+@pytest.mark.parametrize("draft", [True, False])
+def test_the_least_weights_at_u_zero(hs, draft):
+    """u = 0 takes the lowest token with any weight in 64 bits: one of e^-650 .. e^-760 of the largest, in front of it."""
+    B, V = 48, 600
+    z, d = torch.full((2 * B, V), -1.0e30), torch.full((B, 1, V), -1.0e30)
+    depth = torch.linspace(650.0, 760.0, B)
+    z[:, 400] = d[:, 0, 500] = 0.0
+    z[0::2, 7] = z[1::2, 7] = -depth * 2.0 ** -10
+    ids = torch.full((B, 1), 500, dtype=torch.int32)
+    for alpha in (0.5, 0.0):
+        n, tok = _check(hs, z, d if draft else None, ids, torch.full((B, 1), alpha), torch.zeros(B), temperature=torch.full((B,), 2.0 ** -10))
+        assert set(tok[:, 0].tolist()) == {7, 400}
+
+
 def test_what_an_argmax_drafter_leaves_over(hs):
     """The refused token holds nearly all of p: the rest is as small as 2^-39 of it, and its tokens are alike or far apart."""
     B, V = 240, 5003
