@@ -477,14 +477,14 @@ struct RowWeights {                    // the weights of one row's logits, from 
   const Weights* w;
   const void* z;
   float m, inv_tf;
-  double md, inv_t;                    // -m / temperature, 1 / temperature
+  double md, inv_t;
   float log2_t, factor;                // of the 32-bit ones: log2(e) / temperature
   bool bf16;
   __device__ __forceinline__ double operator()(float v) const {
     if (!EXACT) return double(quick(v));
     const double magic = 6755399441055744.0;                  // 1.5 2^52: whole numbers end up in the low bits
-    // (-m / temperature is rounded once, alike in all of the row's weights)
-    const double x = fma(double(v), inv_t, md), t = fma(x, 369.32993046757655, magic);       // 256 / ln 2
+    // (the difference first: the largest weight is 1 to the bit, and p - q nothing where either row has only that)
+    const double x = (double(v) - md) * inv_t, t = fma(x, 369.32993046757655, magic);        // 256 / ln 2
     const int k = __double2loint(t);
     const double f = fma(t - magic, -0.0027076061740622863, x);                              // ln 2 / 256
     const double p = f * fma(f, fma(f, fma(f, 1.0 / 24.0, 1.0 / 6.0), 0.5), 1.0), y = w->table[k & 255];
@@ -706,8 +706,8 @@ verify_sample_kernel(const __grid_constant__ VerifyCall c, const __grid_constant
   const float inv_tf = fminf(float(inv_t), 3.0e38f);
   const bool t32 = c.t_dtype == CHUNK_F32, d32 = c.d_dtype == CHUNK_F32;
   const float log2_t = fminf(fmaxf(LOG2E / r.t, 1e-30f), 1e30f);
-  RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, -double(mt) * inv_t, inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
-  RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, -double(md) * inv_t, inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
+  RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, double(mt), inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
+  RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, double(md), inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
   const int gone_token = refused && !c.draft ? c.ids[at] : -1;        // the arg-max drafter's, which takes all of its q
   if (both) {
     int dbegin, dend;

@@ -171,6 +171,23 @@ def test_the_least_weights_at_u_zero(hs, draft):
         assert set(tok[:, 0].tolist()) == {7, 400}
 
 
+def test_rows_that_agree_but_for_next_to_nothing(hs):
+    """p and q have the same token at 1 to the bit, and differ in another at e^-600: that is all of max(0, p - q)."""
+    B, V = 60, 103
+    g = torch.Generator().manual_seed(4)
+    top = torch.randint(0, 50, (B,), generator=g)
+    m = torch.randn(B, generator=g) * 9.0
+    z, d = (torch.full((B, V), -1.0e4) for _ in range(2))
+    at = torch.arange(B)
+    z[at, top] = d[at, top] = m
+    z[at, 50 + top] = m - 0.6
+    d[at, 102] = m - 0.5
+    both = torch.stack([z, z], 1).reshape(2 * B, V)
+    n, tok = _check(hs, both, d[:, None], torch.full((B, 1), 102, dtype=torch.int32), torch.full((B, 1), 0.9), torch.rand(B, generator=g),
+                    temperature=torch.full((B,), 1e-3))
+    assert n.sum() == 0 and tok[:, 0].tolist() == (50 + top).tolist()
+
+
 def test_what_an_argmax_drafter_leaves_over(hs):
     """The refused token holds nearly all of p: the rest is as small as 2^-39 of it, and its tokens are alike or far apart."""
     B, V = 240, 5003
