@@ -8,11 +8,12 @@
 // Both answers are integers that hang on a comparison of real numbers, and they are decided as if in 64 bits: each comparison is made with 32-bit
 // exponentials first and made again with 64-bit ones where the numbers come so near to one another that the first could be wrong.
 //
-// Three steps, a launch each, or the last two in one.  The first takes one (request, position) per cluster of blocks, reads the target's and the drafter's row once and decides whether
-// the position would be refused; items are started position by position, and one whose request is known to have been refused before is not read.
-// The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for the requests whose uniform
-// number came within some 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The first two are bound by
-// memory, the third by the 64-bit pipe (128 requests of 152 064 tokens: 238 us in 64 bits alone, 69 and 61 in two).
+// Three steps, a launch each, or the last two in one.  The first takes one (request, position) per cluster of blocks, reads the target's and the
+// drafter's row once and decides whether the position would be refused; items are started position by position, and one whose request is known to have
+// been refused before is not read.  The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for
+// the requests whose uniform number came within some 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The
+// first two are bound by memory, the third by the latency of its 64-bit operations (their pipe is busy for a fifth of the time; 128 requests of 152 064
+// tokens: 238 us in 64 bits alone, 69 and 61 in two steps).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -861,7 +862,7 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip);
     if (e != cudaSuccess) return e;
   }
-  // About one request in ten is left for the third kernel, and what it waits for is the 64-bit pipes of its SMs: 16 blocks each as long as there are SMs
+  // One request in five to ten is left for the third step, a chain of 64-bit operations for every token of a thread: 16 blocks each as long as there are SMs
   // for them (37 requests of 151 937 tokens: 45 us, 58 with 8; 128 of 152 064: 77, 60 with 8).
   const int S = blocks_for(c.B, MAX_S), S64 = blocks_for(1, c.B <= 64 ? MAX_S : 8);
   static bool done[MAX_DEVICES] = {};
