@@ -360,11 +360,12 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
   if (!id_ok && rank == 0 && threadIdx.x == 0) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
   if (r.greedy) {
     const unsigned long long key = cluster_max_key(sh_key, S, rank, key_row(zt, begin, end));
-    const int top = argmax_key_value(key) > -INFINITY ? int(0xffffffffu - uint32_t(key)) : 0;
+    const bool some = argmax_key_value(key) > -INFINITY;      // (of a row without any weight token 0 is taken, but no draft stands on it)
+    const int top = some ? int(0xffffffffu - uint32_t(key)) : 0, verdict = some && id == top;
     if (rank == 0 && threadIdx.x == 0) {
       s.top[at] = top;
-      s.verdict[at] = id == top;
-      if (skip && id != top) atomicMin(s.first + b, i);
+      s.verdict[at] = verdict;
+      if (skip && !verdict) atomicMin(s.first + b, i);
     }
     return;
   }

@@ -260,3 +260,15 @@ def test_streams_and_graphs(hs):
     torch.cuda.synchronize()
     again = _run(hs, **c)
     assert all(torch.equal(a, b) for a, b in zip(got, again)) and not torch.equal(got[0], want[0])
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+def test_no_draft_stands_on_a_row_without_weight(hs, kind):
+    """Greedy requests whose draft's row is -infinity all through: token 0 is what comes out of it, but as the target's, not as a draft that stands."""
+    V = 300
+    z = torch.randn((8, V), generator=torch.Generator().manual_seed(7)).to(kind)
+    z[0::2] = -float("inf")
+    for warm in (0.0, 1.0):
+        n, tok = _check(hs, z, None, torch.tensor([[0], [1], [0], [299]], dtype=torch.int32), torch.zeros((4, 1)), torch.full((4,), 0.5),
+                        temperature=torch.full((4,), warm))
+        assert n.tolist() == [0] * 4 and tok.tolist() == [[0, -1]] * 4
