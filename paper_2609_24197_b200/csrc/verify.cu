@@ -208,12 +208,12 @@ __device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
     constexpr int N = sizeof(v) / sizeof(float);
     float m = v[0];
 #pragma unroll
-    for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);           // (NaN gives way)
-    m = fminf(m, FLT_MAX);
+    for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);           // (NaN gives way to a number)
+    m = logit(m);                                             // (a word of nothing but NaN)
     if (m > mx) {
       mx = m;
 #pragma unroll
-      for (int j = N - 1; j >= 0; --j) if (fminf(v[j], FLT_MAX) == m) at = i + j;
+      for (int j = N - 1; j >= 0; --j) if (logit(v[j]) == m) at = i + j;
     }
   });
   return begin < end ? argmax_key(mx, at) : 0;

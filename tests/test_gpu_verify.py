@@ -272,3 +272,32 @@ def test_no_draft_stands_on_a_row_without_weight(hs, kind):
         n, tok = _check(hs, z, None, torch.tensor([[0], [1], [0], [299]], dtype=torch.int32), torch.zeros((4, 1)), torch.full((4,), 0.5),
                         temperature=torch.full((4,), warm))
         assert n.tolist() == [0] * 4 and tok.tolist() == [[0, -1]] * 4
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+def test_nan_logits_lose_every_argmax(hs, kind):
+    """Runs of NaN that fill whole 16-byte words, alone and beside +infinity, in the rows whose arg-max counts: a greedy request's draft rows, and the
+    row behind drafts that all stand, of greedy and of sampling requests."""
+    V, g = 1037, torch.Generator().manual_seed(31)          # (an odd pitch: words begin anywhere in a row)
+    runs = [(0, 16), (0, 1), (7, 9), (256, 288), (500, 541), (V - 16, V), (V - 37, V), (1, V), (0, V - 1), (0, V)]
+    top = [None, 0, 1, 5, 15]                               # place of a +infinity within the run
+    z, ids, warm, alpha = [], [], [], []
+    for first, end in runs:
+        for inf in top:
+            for how in range(4):
+                rows = (torch.randn((2, V), generator=g) * 3.0).to(kind)
+                drafted = int(rows[0].float().argmax())
+                bad = rows[0] if how in (0, 3) else rows[1]
+                bad[first:end] = float("nan")
+                if inf is not None and first + inf < end:
+                    bad[first + inf] = float("inf")
+                if how == 0:                                # the row's arg-max, where it has one
+                    drafted = int(torch.nan_to_num(bad.float(), nan=-float("inf"), posinf=3.4e38).argmax())
+                z.append(rows)
+                ids.append([drafted])
+                warm.append(0.0 if how < 2 else 1.0)
+                alpha.append([1.0 if how == 3 else 0.0])
+    B = len(ids)
+    n, tok = _check(hs, torch.cat(z), None, torch.tensor(ids, dtype=torch.int32), torch.tensor(alpha), torch.rand(B, generator=g),
+                    temperature=torch.tensor(warm))
+    assert (n[0::4][:-5] == 1).all() and (n[1::4] == 1).all()        # (the last five have nothing but NaN in the draft's row, or +infinity beside it)
