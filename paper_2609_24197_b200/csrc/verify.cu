@@ -469,7 +469,10 @@ verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__
 // ------------------------------------------------------------------ the token behind the drafts that stand
 // A row is full of 64-bit exponentials here: e^x = 2^n 2^(i / 256) e^f with |f| <= ln 2 / 512, 2^(i / 256) from a table in shared memory (times the
 // factor that the row's weights need anyway) and e^f by its series up to f^4 / 24 (the next term is 4e-17): 10 operations in 64 bits, where the
-// library's function, left to what lies below e^-700, takes three times as many.
+// library's function, left to what lies below e^-680, takes three times as many.
+// 2^n goes into the bits of a product that already holds the factor.  That is 1, or one over a sum of at most 2^30 weights: e^-680 is 2^-981.1, so that the
+// exponent stays at 2^-1013 or above, and 64 bits hold 2^-1022.
+constexpr float DEEP = -680.f;
 struct Weights {
   double table[256];
 };
@@ -492,7 +495,7 @@ struct RowWeights {                    // the weights of one row's logits, from 
     const double p = f * fma(f, fma(f, fma(f, 1.0 / 24.0, 1.0 / 6.0), 0.5), 1.0), y = w->table[k & 255];
     const double r = fma(y, p, y);
     const float depth = (v - m) * inv_tf;
-    if (depth > -700.f) return __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r));
+    if (depth > DEEP) return __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r));
     return depth > -746.f ? exp_of(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
   }
   __device__ __forceinline__ float quick(float v) const { return ex2_ftz((v - m) * log2_t) * factor; }
@@ -510,7 +513,7 @@ struct RowWeights {                    // the weights of one row's logits, from 
   template <bool F32>
   __device__ __forceinline__ uint32_t none() const { return F32 ? 0xff800000u : bf16 ? 0xff80u : 0xfc00u; }
 };
-// The table times a factor; e^700 has room above it.
+// The table times a factor.
 __device__ __forceinline__ void weights_init(Weights& w, double factor) {
   for (int i = threadIdx.x; i < 256; i += VT) w.table[i] = exp2(double(i) / 256.0) * factor;
 }

@@ -301,3 +301,25 @@ def test_nan_logits_lose_every_argmax(hs, kind):
     n, tok = _check(hs, torch.cat(z), None, torch.tensor(ids, dtype=torch.int32), torch.tensor(alpha), torch.rand(B, generator=g),
                     temperature=torch.tensor(warm))
     assert (n[0::4][:-5] == 1).all() and (n[1::4] == 1).all()        # (the last five have nothing but NaN in the draft's row, or +infinity beside it)
+
+
+@pytest.mark.parametrize("V", [50000, 152064])
+@pytest.mark.parametrize("where", ["draft", "target"])
+def test_deep_tokens_of_flat_rows(hs, where, V):
+    """Tokens some 700 temperatures below thousands of equal ones: next to nothing of a sum of V, which a 64-bit exponent holds only with care.  In the draft's
+    row they must not take the rest; in the target's, in front of all others, u = 0 takes the first of them that has any weight at all."""
+    depth = torch.arange(640.0, 725.0, 0.25)
+    z, d = torch.zeros((8, V)), torch.zeros((4, 1, V))
+    z[0::2, V - 20:] = 0.5                                  # what is left of p - q, and next to none of it: decided in 64 bits
+    if where == "draft":
+        z[0::2, 100:100 + depth.numel()] = d[:, 0, 100:100 + depth.numel()] = -depth
+        z[0::2, 100:100 + depth.numel()] -= 1.0
+        u = torch.tensor([0.0, 0.3, 0.7, 0.999])
+    else:
+        for b in range(4):
+            z[2 * b, 0] = -(697.0, 698.25, 699.0, 699.75)[b]
+        d[:, 0, 0] = -1.0e30
+        u = torch.zeros(4)
+    ids = torch.full((4, 1), V // 2, dtype=torch.int32)
+    n, tok = _check(hs, z, d, ids, torch.ones((4, 1)), u)
+    assert n.sum() == 0 and ((tok[:, 0] >= V - 20).all() if where == "draft" else (tok[:, 0] == 0).all())
