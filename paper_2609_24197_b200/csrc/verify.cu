@@ -18,6 +18,7 @@
 #include "kernels.h"
 
 #include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 namespace hspec {
@@ -120,9 +121,9 @@ __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c) {
   return MaxSum{m, (a.mx > -INFINITY ? a.sum * ex2_ftz((a.mx - m) * c) : 0.f) + (b.mx > -INFINITY ? b.sum * ex2_ftz((b.mx - m) * c) : 0.f)};
 }
 // One pass: the running maximum and the sum of 2^((z - max) c) over this thread's share.  16 values at a time with one maximum and one rescaling, two
-// values to an instruction where there is one (14 instructions a value were more than the memory leaves time for; these are 5).  Values are taken as
-// they are: NaN and +infinity make the sum NaN, and such a share is gone through once more with every value looked at.
-template <typename T>
+// values to an instruction where there is one (14 instructions a value were more than the memory leaves time for; these are 5).  Without LOGITS values
+// are taken as they are: NaN and +infinity make the sum NaN, and such a share is gone through once more with every value looked at.
+template <bool LOGITS, typename T>
 __device__ __forceinline__ MaxSum sum_share(const T* z, int begin, int end, float c) {
   constexpr int N = 16 / sizeof(T), U = 4, G = 16 / N;          // values of a word, words under way, words of 16 values
   float mx = -FLT_MAX, sum = 0.f;
@@ -133,8 +134,8 @@ __device__ __forceinline__ MaxSum sum_share(const T* z, int begin, int end, floa
   };
   const int off = int((reinterpret_cast<uintptr_t>(z + begin) & 15) / sizeof(T));
   const int head = min(end, begin + (off ? N - off : 0)), n16 = (end - head) / N;
-  for (int i = begin + int(threadIdx.x); i < head; i += VT) one(value_of(z[i]));
-  for (int i = head + n16 * N + int(threadIdx.x); i < end; i += VT) one(value_of(z[i]));
+  for (int i = begin + int(threadIdx.x); i < head; i += VT) one(LOGITS ? logit(value_of(z[i])) : value_of(z[i]));
+  for (int i = head + n16 * N + int(threadIdx.x); i < end; i += VT) one(LOGITS ? logit(value_of(z[i])) : value_of(z[i]));
   const uint4* p = reinterpret_cast<const uint4*>(z + head);
   const uint32_t none = nothing(T());
   uint4 next[U];
@@ -155,7 +156,7 @@ __device__ __forceinline__ MaxSum sum_share(const T* z, int begin, int end, floa
 #pragma unroll
       for (int u = 0; u < G; ++u) {
         float x[N];
-        unpack16<false>(w[g * G + u], x, T());
+        unpack16<LOGITS>(w[g * G + u], x, T());
 #pragma unroll
         for (int j = 0; j < N; ++j) v[u * N + j] = x[j];
       }
@@ -178,24 +179,21 @@ __device__ __forceinline__ MaxSum sum_share(const T* z, int begin, int end, floa
   }
   return MaxSum{mx, sum};
 }
-// (Functions of their own, so that the three types' loops do not share the registers of the kernel around them.)
+// (Functions of their own, so that the three types' loops do not share the registers of the kernel around them; the first with the second inside it keeps its
+// arguments past the loop, and 128 requests of 152 064 tokens take 292 us, not 288.)
 __device__ __noinline__ MaxSum sum_row_careful(Row r, int begin, int end, float c) {
-  float mx = -INFINITY, sum = 0.f;
-  walk<1>(r, begin, end, [&](int, auto& v) {
-    constexpr int N = sizeof(v) / sizeof(float);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float m = fmaxf(mx, v[j]);
-      if (m > -INFINITY) sum = sum * ex2_ftz((mx - m) * c) + ex2_ftz((v[j] - m) * c);
-      mx = m;
-    }
-  });
-  return MaxSum{mx, sum};
+  if (r.dtype == CHUNK_F32) return sum_share<true>(reinterpret_cast<const float*>(r.z), begin, end, c);
+  if (r.dtype == CHUNK_F16) return sum_share<true>(reinterpret_cast<const __half*>(r.z), begin, end, c);
+  return sum_share<true>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, c);
 }
-__device__ __noinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
-  MaxSum x = r.dtype == CHUNK_F32   ? sum_share(reinterpret_cast<const float*>(r.z), begin, end, c)
-             : r.dtype == CHUNK_F16 ? sum_share(reinterpret_cast<const __half*>(r.z), begin, end, c)
-                                    : sum_share(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, c);
+__device__ __noinline__ MaxSum sum_row_quick(Row r, int begin, int end, float c) {
+  MaxSum x = r.dtype == CHUNK_F32   ? sum_share<false>(reinterpret_cast<const float*>(r.z), begin, end, c)
+             : r.dtype == CHUNK_F16 ? sum_share<false>(reinterpret_cast<const __half*>(r.z), begin, end, c)
+                                    : sum_share<false>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, c);
+  return x;
+}
+__device__ __forceinline__ MaxSum sum_row(Row r, int begin, int end, float c) {
+  MaxSum x = sum_row_quick(r, begin, end, c);
   if (x.sum != x.sum) x = sum_row_careful(r, begin, end, c);
   if (x.sum == 0.f) x.mx = -INFINITY;             // (nothing but -infinity)
   return x;
@@ -350,7 +348,7 @@ __device__ __noinline__ void verify_row64(const VerifyCall& c, const VerifyScrat
 }
 
 __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScratch& s, int S, int rank, int skip, int i, int b, MaxSum (&sh_warp)[2][VW],
-                                           unsigned long long (&sh_block)[2][8], Reduce64& sh_sum, ReduceKey& sh_key, float (&sh_max)[2], int& sh_near) {
+                                           unsigned long long (&sh_block)[2][8], Reduce64& sh_sum, ReduceKey& sh_key, float (&sh_max)[2], int& sh_near, float err) {
   const Request r = request(c, b);
   const int at = b * c.k + i, id = c.ids[at];
   const Row zt = row_at(c.target, c.t_dtype, c.ld_t, r.row0 + i);
@@ -409,11 +407,11 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
     if (!(vt > -INFINITY) || !(alpha <= 1.f)) {
       verdict = 0;
     } else {
-      // p / q = 2^(xt - xd) sum_d / sum_t.  Each exponent is off by 2^-23 of its size (a subtraction and a product rounded, then the special
-      // function's 2^-22), so are the sums' terms, and a sum of n terms by a few roundings more: 2^-17 of the whole covers sizes up to 24.
+      // p / q = 2^(xt - xd) sum_d / sum_t, in 32 bits off by the sums' part (row_error) and, for an exponent of size x, 1.7 x + 1 units of 2^-23 (the
+      // difference, the temperature's factor and their product; the special function is in the former).
       const float xt = (vt - x[0].mx) * scale, xd = both ? (vd - x[1].mx) * scale : 0.f;
       const float ratio = both ? (vd > -INFINITY ? ex2_ftz(xt - xd) * (x[1].sum / x[0].sum) : INFINITY) : ex2_ftz(xt) / x[0].sum;
-      const float tol = (24.f + fabsf(xt) + fabsf(vd > -INFINITY ? xd : 0.f)) * 3.2e-7f;
+      const float tol = err + 2.7f * 0x1p-23f * (fabsf(xt) + fabsf(vd > -INFINITY ? xd : 0.f));
       verdict = ratio >= alpha;
       near = !(ratio > 1e-30f) || !(alpha > 1e-30f) || fabsf(ratio - alpha) <= tol * alpha;
       near |= xt < -1000.f || xd < -1000.f;       // (p or q may be nothing in 64 bits, or not whole: decided there)
@@ -439,7 +437,7 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
 // that walk the items themselves 205 us; leaving off a row whose request has been refused meanwhile saved some bytes and no time; two blocks a row
 // read fewer ahead in the same time, four are slower.)
 __global__ void __launch_bounds__(VT, 2)
-verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S, int skip) {
+verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__ VerifyScratch s, int S, int skip, float err) {
   pdl_wait();
   pdl_trigger();
   const int item = blockIdx.x / S, rank = blockIdx.x % S, i = item / c.B, b = item % c.B;
@@ -463,7 +461,7 @@ verify_rows_kernel(const __grid_constant__ VerifyCall c, const __grid_constant__
       return;
     }
   }
-  verify_row(c, s, S, rank, skip, i, b, sh_warp, sh_block, sh_sum, sh_key, sh_max, sh_near);
+  verify_row(c, s, S, rank, skip, i, b, sh_warp, sh_block, sh_sum, sh_key, sh_max, sh_near, err);
 }
 
 // ------------------------------------------------------------------ the token behind the drafts that stand
@@ -841,6 +839,16 @@ size_t verify_workspace_bytes(int B, int k) {
   return ((size_t(B) * 8 + 255) & ~size_t(255)) + size_t(B) * k * (sizeof(float2) + 8) + 256;
 }
 
+// How far the quotient of two sums (or of one and a weight) of the first step may be off relative to itself, added up as if every rounding went the same way,
+// in units of 2^-23.  The exponents' average by weight is log2 V at most, which gives 1.7 log2 V for what rounds in them and 2 for the special function.  A thread
+// rescales what it has and adds to it for every 16 values (3: the special function, a product, an addition; and 3 for the sum of the sixteen), and the same 27
+// times for what others have (5 lanes', 15 warps', 7 blocks').  152 064 tokens, a block each: 4e-5, which a ratio comes as near to alpha as once in some
+// thousand rows.
+static float row_error(const VerifyCall& c, int S) {
+  const float steps = float(c.V / (S * VT * 16) + 3), sum = 1.7f * log2f(float(c.V)) + 2.f + 3.f * (steps + 27.f) + 3.f;
+  return ((c.draft ? 2.f : 1.f) * sum + 4.f) * 0x1p-23f;
+}
+
 cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
   VerifyScratch s;
   uint8_t* ws = reinterpret_cast<uint8_t*>(c.ws);
@@ -863,7 +871,7 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
       e = launch_pdl(verify_init_kernel, dim3(1), dim3(256), 0, stream, s.first, c.B);
       if (e != cudaSuccess) return e;
     }
-    e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip);
+    e = launch_pdl_cluster(verify_rows_kernel, dim3(unsigned(items * S)), dim3(VT), dim3(S), 0, stream, c, s, S, skip, row_error(c, S));
     if (e != cudaSuccess) return e;
   }
   // One request in five to ten is left for the third step, a chain of 64-bit operations for every token of a thread: 16 blocks each as long as there are SMs

@@ -323,3 +323,19 @@ def test_deep_tokens_of_flat_rows(hs, where, V):
     ids = torch.full((4, 1), V // 2, dtype=torch.int32)
     n, tok = _check(hs, z, d, ids, torch.ones((4, 1)), u)
     assert n.sum() == 0 and ((tok[:, 0] >= V - 20).all() if where == "draft" else (tok[:, 0] == 0).all())
+
+
+@pytest.mark.parametrize("depth,side", [(2.8125, 1), (3.53125, -1)])
+def test_the_accept_test_of_a_huge_vocabulary(hs, depth, side):
+    """2^27 tokens, all but some of them `depth` below the largest: a running sum in 32 bits that comes by every 4096th word of an eighth of them is off by 2.9e-5
+    here (the same rounding of every addition, down for one depth and up for the other), and alpha lies halfway between the drafted token's share and what such a
+    sum makes of it."""
+    V, tops = 2 ** 27, 2 ** 12
+    p = np.exp(-depth) / (8 * tops + (V - 8 * tops) * np.exp(-depth))
+    z = torch.full((2, V), -depth, dtype=torch.float16, device="cuda")
+    z[0].view(8, -1)[:, :tops] = 0.0                         # (a running maximum that is there from the first word on)
+    alpha = np.float32(p * (1.0 + side * 1.45e-5))
+    assert (p >= float(alpha)) == (side < 0)
+    n, tok = _run(hs, z, None, torch.full((1, 1), V - 1, dtype=torch.int32, device="cuda"), torch.full((1, 1), float(alpha), device="cuda"),
+                  torch.zeros(1, device="cuda"))
+    assert n.tolist() == [int(side < 0)] and tok.tolist() == [[V - 1, 0] if side < 0 else [0, -1]]
