@@ -299,7 +299,7 @@ __device__ __forceinline__ Request request(const VerifyCall& c, int b) {
   int lo = b * (c.k + 1), hi = lo + c.k + 1;
   if (c.cu_q) { lo = c.cu_q[b]; hi = c.cu_q[b + 1]; }
   r.row0 = min(max(lo, 0), c.T);
-  r.drafts = min(max(min(hi, c.T) - r.row0 - 1, -1), c.k);         // -1: no row at all, nothing to sample from
+  r.drafts = min(min(max(hi, r.row0), c.T) - r.row0 - 1, c.k);     // -1: no row at all, nothing to sample from (held first: a far offset's difference wraps)
   r.t = c.temperature ? c.temperature[b] : 1.f;
   r.greedy = !(r.t > 0.f);
   return r;

@@ -339,3 +339,21 @@ def test_the_accept_test_of_a_huge_vocabulary(hs, depth, side):
     n, tok = _run(hs, z, None, torch.full((1, 1), V - 1, dtype=torch.int32, device="cuda"), torch.full((1, 1), float(alpha), device="cuda"),
                   torch.zeros(1, device="cuda"))
     assert n.tolist() == [int(side < 0)] and tok.tolist() == [[V - 1, 0] if side < 0 else [0, -1]]
+
+
+def test_offsets_far_outside_are_held(hs):
+    """Entries of cu_q at the ends of 32 bits: a request that they give no row has none, and the others are as they were."""
+    B, k, V = 5, 3, 50
+    c = _case(B, k, V, torch.float32, 41)
+    low, high = -2 ** 31, 2 ** 31 - 1
+    c["target"] = c["target"][:2].clone()                   # (fewer rows than a request may have)
+    for cu, rows in (([0, low, 2, 2, 2, 2], [0, 2, 0, 0, 0]), ([low, 1, high, 2, low, high], [1, 1, 0, 0, 2]), ([2, 2, high, high, 0, 1], [0, 0, 0, 0, 1]),
+                     ([high, low, high, low, low, 2], [0, 2, 0, 0, 2])):
+        offsets = torch.tensor(cu, dtype=torch.int32)
+        n, tok = _run(hs, **{x: None if y is None else y.cuda() for x, y in dict(c, cu_q=offsets).items()})
+        first = [min(max(x, 0), 2) for x in cu[:-1]]
+        for b in range(B):
+            one = to.verify(_wide(c["target"]), _wide(c["draft"][b:b + 1]), *(c[x][b:b + 1].numpy() for x in ("ids", "alpha", "u")),
+                            cu_q=[first[b], first[b] + rows[b]])
+            assert n[b].item() == one[0][0] and tok[b].tolist() == one[1][0].tolist(), (cu, b)
+    hs.hspec_op_device_status(clear=True)
