@@ -750,7 +750,9 @@ __device__ __forceinline__ void sample(const VerifyCall& c, const VerifyScratch&
     for (int j = 0; j < S; ++j) whole += sh.block[j];
     // (how far the 32-bit sums may be off: p and q weigh 1 each where both count, else p is all there is)
     const double tol = EXACT ? 0.0 : (both && less ? 2.0 : whole) * double(log2f(float(c.V)) + fmaxf(0.f, -log2f(float(whole))) + 4.f) * 0x1p-23;
-    if (!EXACT && both && less && !(whole > 64.0 * tol)) {    // nearly nothing left of p - q: left to the other kernel
+    // Nearly nothing left of p - q, or of p without an arg-max drafter's token (weights under 2^-126, up to 2^30 of them, are nothing here; beside 2^-60 they
+    // do not count): left to the other kernel.
+    if (!EXACT && ((both && less && !(whole > 64.0 * tol)) || (gone >= 0 && !(whole > 0x1p-60)))) {
       if (rank == 0 && threadIdx.x == 0) s.open[b] = 1;
       break;
     }

@@ -357,3 +357,25 @@ def test_offsets_far_outside_are_held(hs):
                             cu_q=[first[b], first[b] + rows[b]])
             assert n[b].item() == one[0][0] and tok[b].tolist() == one[1][0].tolist(), (cu, b)
     hs.hspec_op_device_status(clear=True)
+
+
+def test_the_rest_of_a_draft_that_no_ratio_reaches(hs):
+    """alpha above 1 refuses whatever stands: an arg-max drafter's token may then hold all of p but weights that 32 bits flush to nothing, one by one or
+    many of them beside a larger one."""
+    B, V = 60, 50021
+    g = torch.Generator().manual_seed(51)
+    z = torch.full((B, 2, V), -float("inf"))
+    at = torch.randint(0, V - 1, (B,), generator=g)
+    for b in range(B):
+        if b % 3 == 0:                                      # a few tokens, the largest at e^-80 .. e^-700
+            z[b, :, torch.randint(0, V, (30,), generator=g)] = -torch.linspace(80.0, 700.0, B)[b] - 3.0 * torch.rand(30, generator=g)
+        elif b % 3 == 1:                                    # all of them under 2^-126 = e^-87.3
+            z[b] = -88.0 - 4.0 * torch.rand(V, generator=g)
+        else:                                               # the same and one above it
+            z[b] = -88.0 - 0.5 * torch.rand(V, generator=g)
+            z[b, :, V - 1] = -87.0
+        z[b, :, at[b]] = 0.0
+    alpha = torch.full((B, 1), 2.0)
+    alpha[1::7] = float("nan")
+    n, tok = _check(hs, z.reshape(2 * B, V), None, at[:, None].to(torch.int32), alpha, torch.rand(B, generator=g))
+    assert n.sum() == 0 and (tok[:, 0] != at.numpy()).all()
