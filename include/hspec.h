@@ -396,7 +396,8 @@ size_t hspec_chunk_attention_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t dh
  *   draft_logits   device [B * k, ld_draft] (draft_dtype): what the drafts were sampled from at the same temperature; NULL: a drafter that takes
  *                  the arg-max, all of q on the drafted token.  V_draft = V, or with vocab_map (device int32 [V_draft], ascending) a pruned
  *                  vocabulary's size; q is 0 at tokens outside it
- *   draft_ids int32 [B, k] target token ids; temperature fp32 [B] or NULL (1); at 0 p is all on the arg-max (lowest on ties), q on the draft
+ *   draft_ids int32 [B, k] target token ids; temperature fp32 [B] or NULL (1); at 0 p is all on the arg-max (lowest on ties), q on the draft; above
+ *                  that it counts as 1e-36 at least and as 1e36 at most
  *   alpha fp32 [B, k], u fp32 [B] in [0, 1)
  *   n_accept int32 [B]; tokens int32 [B, k + 1]: the drafts that stand, the token behind them, then -1 (a request without rows: -1 all through)
  * A NaN logit counts as -infinity, +infinity as the largest finite number; from a row without any weight token 0 is taken.  A draft id outside

@@ -292,7 +292,7 @@ __device__ __forceinline__ unsigned long long cluster_max_key(ReduceKey& sh, int
   return k;
 }
 
-// Rows and drafts of a request, and its temperature (not above zero, or NaN: greedy).
+// Rows and drafts of a request, and its temperature (not above zero, or NaN: greedy).  That is held where it and its inverse are numbers of full 32 bits.
 struct Request { int row0, drafts; float t; bool greedy; };
 __device__ __forceinline__ Request request(const VerifyCall& c, int b) {
   Request r;
@@ -300,8 +300,9 @@ __device__ __forceinline__ Request request(const VerifyCall& c, int b) {
   if (c.cu_q) { lo = c.cu_q[b]; hi = c.cu_q[b + 1]; }
   r.row0 = min(max(lo, 0), c.T);
   r.drafts = min(min(max(hi, r.row0), c.T) - r.row0 - 1, c.k);     // -1: no row at all, nothing to sample from (held first: a far offset's difference wraps)
-  r.t = c.temperature ? c.temperature[b] : 1.f;
-  r.greedy = !(r.t > 0.f);
+  const float t = c.temperature ? c.temperature[b] : 1.f;
+  r.t = fminf(fmaxf(t, 1e-36f), 1e36f);
+  r.greedy = !(t > 0.f);
   return r;
 }
 // Place of a token in the drafter's vocabulary, or -1.
@@ -369,7 +370,7 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
   }
   const bool both = c.draft != nullptr;
   const Row zd = both ? row_at(c.draft, c.d_dtype, c.ld_d, at) : zt;
-  const float scale = fminf(fmaxf(LOG2E / r.t, 1e-30f), 1e30f);
+  const float scale = LOG2E / r.t;
   MaxSum mine[2] = {sum_row(zt, begin, end, scale), MaxSum{-INFINITY, 0.f}};
   int dbegin = 0, dend = 0;
   if (both) {
@@ -494,7 +495,7 @@ struct RowWeights {                    // the weights of one row's logits, from 
     const double r = fma(y, p, y);
     const float depth = (v - m) * inv_tf;
     if (depth > DEEP) return __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r));
-    return depth > -746.f ? exp_of(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
+    return x > -746.0 ? exp_of(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
   }
   __device__ __forceinline__ float quick(float v) const { return ex2_ftz((v - m) * log2_t) * factor; }
   // A logit as it lies in memory, and what it says.  (Two steps, so that many loads go out before the first is looked at; no branch on the type.)
@@ -701,9 +702,9 @@ __device__ __forceinline__ void sample(const VerifyCall& c, const VerifyScratch&
   const bool both = refused && c.draft != nullptr && md > -INFINITY;
   const Row zd = both ? row_at(c.draft, c.d_dtype, c.ld_d, at) : zt;
   const double inv_t = 1.0 / double(r.t);
-  const float inv_tf = fminf(float(inv_t), 3.0e38f);
+  const float inv_tf = float(inv_t);
   const bool t32 = c.t_dtype == CHUNK_F32, d32 = c.d_dtype == CHUNK_F32;
-  const float log2_t = fminf(fmaxf(LOG2E / r.t, 1e-30f), 1e30f);
+  const float log2_t = LOG2E / r.t;
   RowWeights<EXACT> p{&sh.p, zt.z, mt, inv_tf, double(mt), inv_t, log2_t, 1.f, c.t_dtype == CHUNK_BF16};
   RowWeights<EXACT> q{&sh.q, zd.z, md, inv_tf, double(md), inv_t, log2_t, 1.f, c.d_dtype == CHUNK_BF16};
   const int gone_token = refused && !c.draft ? c.ids[at] : -1;        // the arg-max drafter's, which takes all of its q

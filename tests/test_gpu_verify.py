@@ -379,3 +379,24 @@ def test_the_rest_of_a_draft_that_no_ratio_reaches(hs):
     alpha[1::7] = float("nan")
     n, tok = _check(hs, z.reshape(2 * B, V), None, at[:, None].to(torch.int32), alpha, torch.rand(B, generator=g))
     assert n.sum() == 0 and (tok[:, 0] != at.numpy()).all()
+
+
+@pytest.mark.parametrize("V", [40, 30000])
+def test_the_largest_and_the_smallest_temperatures(hs, V):
+    """Temperatures up to 1e36 and down to 1e-36 count as they are, over logits of their size; those beyond count as 1e36 and 1e-36."""
+    g = torch.Generator().manual_seed(61)
+    T = [1e29, 1e30, 3e30, 1e33, 9e35, 1e36, 3e38, float("inf"), 1e-29, 1e-30, 3e-31, 1e-33, 2e-36, 1e-36, 1e-38, 1e-45]
+    t = torch.tensor(T)
+    held = t.clamp(1e-36, 1e36)
+    B, k = len(T), 2
+    z, d = (torch.randn((B, n, V), generator=g) * 2.0 * held[:, None, None] for n in (k + 1, k))
+    z[:, 0] = d[:, 0] + 0.02 * z[:, 0]
+    z[:8, :, 7] = -float("inf")                             # masked tokens stay masked
+    z[:, :, 11] = -3.0e38
+    c = dict(target=z.reshape(-1, V), draft=d, ids=torch.randint(12, V, (B, k), generator=g, dtype=torch.int32), alpha=torch.rand((B, k), generator=g),
+             u=torch.rand(B, generator=g))
+    n, tok = _run(hs, **{x: y.cuda() for x, y in c.items()}, temperature=t.cuda())
+    want_n, want = to.verify(_wide(c["target"]), _wide(d), *(c[x].numpy() for x in ("ids", "alpha", "u")), temperature=held.numpy())
+    np.testing.assert_array_equal(n.cpu().numpy(), want_n)
+    np.testing.assert_array_equal(tok.cpu().numpy(), want)
+    assert 0 < want_n.sum() < B * k
