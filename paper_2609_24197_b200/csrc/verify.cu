@@ -654,7 +654,10 @@ __device__ __forceinline__ void sample(const VerifyCall& c, const VerifyScratch&
     weights_init(sh.p, 1.0);
     weights_init(sh.q, 1.0);
   }
-  if (!EXACT && rank == 0 && threadIdx.x == 0) s.open[b] = 0;
+  if (!EXACT && rank == 0 && threadIdx.x == 0) {
+    s.open[b] = 0;
+    if (c.cu_q && (c.cu_q[b] < 0 || c.cu_q[b + 1] < c.cu_q[b] || c.cu_q[b + 1] > c.T)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+  }
   if (threadIdx.x == 0) { sh.found = 0x7fffffff; sh.last = -1; }
   if (r.drafts >= 0 && S > 1) cluster_sync_all();  // from here every block of the cluster runs, and its shared memory may be written to
   if (warp == 0) {

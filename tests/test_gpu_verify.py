@@ -400,3 +400,13 @@ def test_the_largest_and_the_smallest_temperatures(hs, V):
     np.testing.assert_array_equal(n.cpu().numpy(), want_n)
     np.testing.assert_array_equal(tok.cpu().numpy(), want)
     assert 0 < want_n.sum() < B * k
+
+
+def test_offsets_outside_are_counted(hs):
+    c = {x: None if y is None else y.cuda() for x, y in _case(6, 2, 60, torch.float32, 71).items()}
+    hs.hspec_op_device_status(clear=True)
+    _run(hs, **c)
+    _run(hs, **dict(c, cu_q=torch.tensor([0, 3, 3, 4, 9, 12, 18], dtype=torch.int32, device="cuda")))
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 0
+    _run(hs, **dict(c, cu_q=torch.tensor([-1, 3, 2, 4, 9, 12, 19], dtype=torch.int32, device="cuda")))
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3          # in front of the rows, descending, behind them
