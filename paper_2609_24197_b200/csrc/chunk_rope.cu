@@ -117,6 +117,9 @@ __global__ void __launch_bounds__(256, 3) chunk_rope_kernel(const __grid_constan
     }
   };
   fetch();                                                // (under way while the rows are looked up)
+  // every request once, with rows or without, by threads that no row's look-up waits for where there are any
+  for (int b = int(blockIdx.x) * 256 + 255 - int(threadIdx.x); b < c.B; b += int(gridDim.x) * 256)
+    if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], c.kv_lens[b], c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
   for (int r = warp; r < rows; r += 8) {
     const int t = t0 + r, b = chunk_request_of(c.cu_q, c.B, t, lane);
     if (lane == 0) {
@@ -125,7 +128,6 @@ __global__ void __launch_bounds__(256, 3) chunk_rope_kernel(const __grid_constan
       if (b < c.B) {
         const int cu0 = c.cu_q[b], cu1 = c.cu_q[b + 1], len = c.kv_lens[b];
         const ChunkRequest q = chunk_request(cu0, cu1, len, c.T, c.max_len);
-        if (t == q.q0 && chunk_request_bad(cu0, cu1, len, c.T, c.max_len)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
         used = t >= q.q0 && t < q.q0 + q.n;               // (a cu_q that does not ascend may have counted t to a request that does not own it)
         at = q.len - q.n + (t - q.q0);
         if (used && at >= 0) {

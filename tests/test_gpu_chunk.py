@@ -559,3 +559,16 @@ def test_rope_in_a_graph(hs):
     graph.replay()
     for p, w in zip(got[1:], want[1:]):
         assert torch.equal(p[int(c.table[0, 117 // 16]), 117 % 16], w[int(c.table[0, 116 // 16]), 116 % 16])
+
+
+def test_rope_counts_requests_without_rows_too(hs):
+    """Lengths outside of requests that have no row in this chunk: as the attention over the same arrays counts them."""
+    Hq, Hkv, dh = HEADS["three"]
+    c = Chunk(HEADS["three"], torch.bfloat16, [2, 0, 0, 3], [8, 9, 9, 0], seed=2, poison=False)
+    kv = torch.tensor([10, -3, 10 ** 6, 1], dtype=torch.int32, device="cuda")       # a good one, two without rows, one with more rows than tokens
+    q = torch.empty((5, Hq, dh), dtype=torch.bfloat16, device="cuda")
+    hs.hspec_op_device_status(clear=True)
+    hs.hspec_op_chunk_rope_write(torch.randn((5, (Hq + 2 * Hkv) * dh), device="cuda"), None, None, c.cu, kv, c.table, q, c.k, c.v, 1.0e4)
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3
+    c.run(hs, kv=kv)
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3
