@@ -392,7 +392,8 @@ size_t hspec_chunk_attention_workspace_bytes(int32_t Hq, int32_t Hkv, int32_t dh
  * where draft n was refused (from p_n where that is nothing anywhere), from p_n where none was: the lowest token v with sum over w <= v above u
  * times the whole.
  *   target_logits  device [T, ld_target], fp32, bf16 or fp16 (target_dtype): request b's rows cu_q[b] .. cu_q[b+1]-1 are the logits behind its
- *                  last token and behind each draft, so it has min(k, rows - 1) drafts.  cu_q NULL: k + 1 rows each
+ *                  last token and behind each draft, so it has min(k, rows - 1) drafts.  cu_q NULL: k + 1 rows each.  T may be 0 (no request has a
+ *                  row), target_logits NULL then
  *   draft_logits   device [B * k, ld_draft] (draft_dtype): what the drafts were sampled from at the same temperature; NULL: a drafter that takes
  *                  the arg-max, all of q on the drafted token.  V_draft = V, or with vocab_map (device int32 [V_draft], ascending) a pruned
  *                  vocabulary's size; q is 0 at tokens outside it

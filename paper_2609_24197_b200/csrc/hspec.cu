@@ -1081,7 +1081,7 @@ int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_
                     const float* alpha, const float* u, int32_t* n_accept, int32_t* tokens, int32_t B, int32_t k, int32_t V, int32_t V_draft,
                     void* workspace, size_t workspace_bytes, void* stream) {
   const std::string who = "hspec_op_verify: ";
-  if (!target_logits || !draft_ids || !alpha || !u || !n_accept || !tokens || !workspace || B < 1 || k < 1 || V < 1 || T < 1 || ld_target < V)
+  if ((!target_logits && T > 0) || !draft_ids || !alpha || !u || !n_accept || !tokens || !workspace || B < 1 || k < 1 || V < 1 || T < 0 || ld_target < V)
     return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
   auto known = [](int32_t d) { return d == HSPEC_F32 || d == HSPEC_BF16 || d == HSPEC_F16; };
   if (!known(target_dtype) || (draft_logits && !known(draft_dtype))) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "logits must be fp32, bf16 or fp16");

@@ -410,3 +410,12 @@ def test_offsets_outside_are_counted(hs):
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 0
     _run(hs, **dict(c, cu_q=torch.tensor([-1, 3, 2, 4, 9, 12, 19], dtype=torch.int32, device="cuda")))
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3          # in front of the rows, descending, behind them
+
+
+def test_an_iteration_in_which_no_request_has_rows(hs):
+    c = {x: None if y is None else y.cuda() for x, y in _case(4, 3, 70, torch.bfloat16, 81).items()}
+    for draft in (c["draft"], None):
+        n, tok = _run(hs, **dict(c, target=c["target"][:0], draft=draft, cu_q=torch.zeros(5, dtype=torch.int32, device="cuda")))
+        assert n.tolist() == [0] * 4 and tok.tolist() == [[-1] * 4] * 4
+    with pytest.raises(hs.HSpecError, match="k \\+ 1 rows"):
+        _run(hs, **dict(c, target=c["target"][:0]))

@@ -93,3 +93,9 @@ def test_the_binding_refuses_before_the_library(lib):
     with pytest.raises(hs.HSpecError, match="current CUDA device"):
         hs.hspec_op_verify(torch.zeros((4, 9)), None, torch.zeros((1, 3), dtype=torch.int32), torch.zeros((1, 3)), torch.zeros(1), ints[:1],
                            torch.zeros((1, 4), dtype=torch.int32), torch.zeros(8, dtype=torch.uint8))
+
+
+def test_verify_without_rows_needs_their_offsets(lib):
+    for over, text in ((dict(T=0), "k + 1 rows"), (dict(T=0, target=None), "k + 1 rows"), (dict(T=-1, cu=A), "bad argument"), (dict(T=1, target=None, cu=A), "bad argument")):
+        rc, msg = _verify(lib, **over)
+        assert rc == -1 and "hspec_op_verify" in msg and text in msg
