@@ -375,7 +375,8 @@ int hspec_op_chunk_rope_write(const void* qkv, int32_t in_dtype, int64_t ld_qkv,
                               int32_t page_size, void* stream);
 /* Attention of a chunk over the paged cache, which holds the chunk's own keys and values already: row at position p sees keys
  * max(0, p - window + 1) .. p (window 0: from the first).  Single tokens, draft blocks and pieces of prompts may be mixed.
- *   q [T, Hq, dh] with row pitch ld_q, o likewise with ld_o (elements, multiples of 8; o of q's type); scale 0: 1 / sqrt(dh)
+ *   q [T, Hq, dh] with row pitch ld_q, o likewise with ld_o (elements, multiples of 8; o of q's type); scale 0: 1 / sqrt(dh);
+ *   it is at most 2.35e38 (times log2 e it has to be a number)
  * At most 8192 requests, and 512 query heads for a KV head.  A row at a negative position sees nothing: its o is zero.  Keys
  * and values at places that a row does not see never reach it, whatever they hold; page-table entries that no row of the request
  * sees are not read.  A bad page reads as zeros.

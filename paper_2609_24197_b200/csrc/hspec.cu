@@ -6,6 +6,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -1052,7 +1053,8 @@ int hspec_op_chunk_attention(const void* q, int64_t ld_q, const void* k_pool, co
                              void* workspace, size_t workspace_bytes, void* stream) {
   const std::string who = "hspec_op_chunk_attention: ";
   if (T == 0) return HSPEC_OK;
-  if (!q || !k_pool || !v_pool || !page_table || !cu_q || !kv_lens || !o || !workspace || window < 0 || !(scale >= 0.f) || scale > 3.0e38f)
+  if (!q || !k_pool || !v_pool || !page_table || !cu_q || !kv_lens || !o || !workspace || window < 0 || !(scale >= 0.f) ||
+      std::isinf(scale * 1.4426950408889634f))               // (what the kernels take it times)
     return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
   if (const char* why = chunk_refusal(B, T, Hq, Hkv, dh, page_size, page_table_stride, num_pages, dtype, q, k_pool, v_pool))
     return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + why);

@@ -99,3 +99,9 @@ def test_verify_without_rows_needs_their_offsets(lib):
     for over, text in ((dict(T=0), "k + 1 rows"), (dict(T=0, target=None), "k + 1 rows"), (dict(T=-1, cu=A), "bad argument"), (dict(T=1, target=None, cu=A), "bad argument")):
         rc, msg = _verify(lib, **over)
         assert rc == -1 and "hspec_op_verify" in msg and text in msg
+
+
+def test_a_scale_whose_product_with_log2_e_is_infinite(lib):
+    for scale in (2.36e38, 3.0e38):
+        rc, msg = _attn(lib, scale=scale)
+        assert rc == -1 and "hspec_op_chunk_attention" in msg and "bad argument" in msg
