@@ -8,7 +8,7 @@ namespace {
 
 constexpr int ITEM_ROWS = 256;
 constexpr int FEW_ROWS = 8;          // requests with this many rows of a KV head or fewer have a kernel of their own
-constexpr float NEG = -1.0e30f;
+constexpr float NEG = -3.402823466e38f;   // the maximum of scores that are not there: the lowest number, so that no score lies below it
 enum { KIND_ALL, KIND_FEW, KIND_MANY };
 
 struct Args {

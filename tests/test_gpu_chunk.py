@@ -572,3 +572,28 @@ def test_rope_counts_requests_without_rows_too(hs):
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3
     c.run(hs, kv=kv)
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 3
+
+
+def _one_score_above_all_others(heads, dtype, new, past, size, sign):
+    """q . k is sign 32 size^2 + order size^2 / 4096 with a whole number of its own for every key: exact in 32 bits, and no two scores of a row less than some
+    ten thousand apart, so that every row takes the value at its largest."""
+    c = Chunk(HEADS[heads], dtype, new, past, seed=17, poison=False)
+    order = torch.randperm(int(max(c.kv)), generator=_gen(5)).cuda()
+    c.q.zero_()
+    c.k.zero_()
+    c.q[..., 8:40], c.q[..., 4:6] = sign * size, size
+    for b in range(c.B):
+        at = torch.arange(c.kv[b], device="cuda")
+        page, at = c.table[b].long()[at // c.page], at % c.page
+        c.k[page, at, :, 8:40] = size
+        c.k[page, at, :, 4] = ((order[:c.kv[b]] // 64) * (size / 64.0)).to(dtype)[:, None]
+        c.k[page, at, :, 5] = ((order[:c.kv[b]] % 64) * (size / 4096.0)).to(dtype)[:, None]
+    return c
+
+
+@pytest.mark.parametrize("size", [2.0 ** 17, 2.0 ** 50, 2.0 ** 60])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size_of_few_rows(hs, sign, size):
+    """Scores of 7e10 to 5e36, all of one sign: far below zero is not the same as unseen."""
+    c = _one_score_above_all_others("tiny", torch.bfloat16, [1, 1, 1], [150, 5, 2000], size, sign)
+    c.check(c.run(hs), what=f"size {size} sign {sign}")
