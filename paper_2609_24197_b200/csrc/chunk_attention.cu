@@ -523,6 +523,26 @@ __device__ __noinline__ void add_not_finite(const Args& a, const Segment& s, int
   }
 }
 
+// The weights' reference is a rounded product with the scale, the scores' own products are exact (one fma with the difference): all weights of a row have the
+// same error, which the division by their sum takes away.  From 2^23 on that error could be more than a weight's type holds, and the scores' products have to be
+// rounded as the reference's was.  (Infinities and the maximum of nothing are not meant.)
+__device__ __forceinline__ bool far_score(float x) { return (__float_as_uint(x) & 0x7fffffffu) - 0x4b000000u < 0x7f7fffffu - 0x4b000000u; }
+// The 32 weights of a row in this way: 16 words of them over the first of the scores; returns their sum.  (A function of its own, because the inner loop has no
+// registers to spare: the look at the references costs a piece of 1024 tokens over 30777 others 1140 -> 1165 us and a prompt of 8192 nothing; with the
+// choice in the loop they take 7 % more.)
+template <bool F16>
+__device__ __noinline__ float far_weights(float* x, float scale, float ref) {
+  const bool far = far_score(ref);
+  float sum = 0.f;
+  for (int i = 0; i < 32; i += 2) {
+    const float p0 = ex2_ftz(far ? __fmul_rn(x[i], scale) - ref : fmaf(x[i], scale, -ref));
+    const float p1 = ex2_ftz(far ? __fmul_rn(x[i + 1], scale) - ref : fmaf(x[i + 1], scale, -ref));
+    sum += p0 + p1;
+    x[i / 2] = __uint_as_float(pack16<F16>(p0, p1));
+  }
+  return sum;
+}
+
 // The largest of three; NaN where one of them is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -602,6 +622,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
     int key0 = (s.ta + (turns ? h : 0)) * KT + ch * 64;       // first of this thread's keys
     const int key_step = turns ? 2 * KT : KT;
     float m_ref = NEG, m_next = NEG, l_sum = 0.f;
+    bool far = false;                                         // a row of this warp has a reference of 2^23 or more
     if (nt == 0 && q_of(seg + 1)) q_finish();
     const uint32_t done = h == 0 ? done0 : done1;
     for (int j = 0; j < nt; ++j, key0 += key_step) {
@@ -657,7 +678,18 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
         };
         uint64_t ls[2] = {0ull, 0ull};
         // Weights of the 32 keys, over scores of this thread that have been fetched.
-        auto weights_of = [&](int part, float ref) {
+        auto weights_of = [&](int part, float ref, bool any_far) {
+          if (any_far) {
+            float copy[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) copy[e] = x[e];
+            ls[0] = add_f32x2(ls[0], pack_f32x2(far_weights<F16>(copy, a.scale_log2, ref), 0.f));
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = __float_as_uint(copy[e]);
+            tmem_st16(t_s + ch * 64 + part * 16, p);
+            return;
+          }
           const uint64_t scale2 = pack_f32x2(a.scale_log2, a.scale_log2), neg_m2 = pack_f32x2(-ref, -ref);
           uint32_t p[16];
 #pragma unroll
@@ -681,7 +713,8 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
           x_pending = false;
           mx = exchange(mx);
           m_ref = max3(mx, NEG, NEG);
-          weights_of(0, m_ref);
+          far = __any_sync(0xffffffffu, far_score(m_ref));
+          weights_of(0, m_ref, far);
           fetch(1);
         } else {
           // The weights do not wait for the row's maximum: the reference is that of the tiles before.  Only where this tile is above it by more than
@@ -689,13 +722,14 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
           if (__any_sync(0xffffffffu, m_next != m_ref)) {
             const float factor = m_next != m_ref ? ex2_ftz(m_ref - m_next) : 1.f;
             m_ref = m_next;
+            far = __any_sync(0xffffffffu, far_score(m_ref));
             rescale(factor);
           }
           fetch(0);
           mx = largest();
           const float own = mx * a.scale_log2;
           const float ref0 = !(own <= m_ref + LIMIT) ? own : m_ref;                 // (NaN: it becomes the reference, and all of the row)
-          weights_of(0, ref0);
+          weights_of(0, ref0, __any_sync(0xffffffffu, far_score(ref0)));
           fetch(1);
           mx = exchange(max3(mx, largest(), largest()));
           const bool over = !(mx <= m_ref + LIMIT);
@@ -703,6 +737,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
             const float m_new = over ? mx : m_ref;
             const float factor = over ? ex2_ftz(m_ref - m_new) : 1.f, f0 = over ? ex2_ftz(ref0 - m_new) : 1.f;
             m_ref = m_new;
+            far = __any_sync(0xffffffffu, far_score(m_ref));
             rescale(factor);
             tmem_st_wait();
             uint32_t p[16];
@@ -724,7 +759,7 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->p_half[h]));
-        weights_of(1, m_ref);
+        weights_of(1, m_ref, far);
         tmem_st_wait();
         tc_fence_before();
         float s0, s1, s2, s3;

@@ -597,3 +597,13 @@ def test_scores_of_any_size_of_few_rows(hs, sign, size):
     """Scores of 7e10 to 5e36, all of one sign: far below zero is not the same as unseen."""
     c = _one_score_above_all_others("tiny", torch.bfloat16, [1, 1, 1], [150, 5, 2000], size, sign)
     c.check(c.run(hs), what=f"size {size} sign {sign}")
+
+
+@pytest.mark.parametrize("dtype,size", [(torch.bfloat16, 2.0 ** 17), (torch.bfloat16, 2.0 ** 50), (torch.bfloat16, 2.0 ** 60), (torch.float16, 2.0 ** 15)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("new,past", [([40, 300, 1], [150, 20, 700]), ([100, 17], [0, 3000])])
+@pytest.mark.parametrize("heads", ["tiny", "8b"])
+def test_scores_of_any_size(hs, heads, new, past, sign, dtype, size):
+    """Scores of 4e9 to 5e36, all of one sign: a score's exact product with the scale and the row's rounded maximum may be thousands apart."""
+    c = _one_score_above_all_others(heads, dtype, new, past, size, sign)
+    c.check(c.run(hs), what=f"size {size} sign {sign}")
