@@ -360,7 +360,7 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
   if (r.greedy) {
     const unsigned long long key = cluster_max_key(sh_key, S, rank, key_row(zt, begin, end));
     const bool some = argmax_key_value(key) > -INFINITY;      // (of a row without any weight token 0 is taken, but no draft stands on it)
-    const int top = some ? int(0xffffffffu - uint32_t(key)) : 0, verdict = some && id == top;
+    const int top = some ? int(0xffffffffu - uint32_t(key)) : 0, verdict = some && id == top && c.alpha[at] <= 1.f;
     if (rank == 0 && threadIdx.x == 0) {
       s.top[at] = top;
       s.verdict[at] = verdict;

@@ -419,3 +419,13 @@ def test_an_iteration_in_which_no_request_has_rows(hs):
         assert n.tolist() == [0] * 4 and tok.tolist() == [[-1] * 4] * 4
     with pytest.raises(hs.HSpecError, match="k \\+ 1 rows"):
         _run(hs, **dict(c, target=c["target"][:0]))
+
+
+@pytest.mark.parametrize("draft", [True, False])
+def test_greedy_drafts_that_no_ratio_reaches(hs, draft):
+    """min(1, p / q) is 1 for a greedy request's arg-max: an alpha above that, or NaN, refuses it, and the target's token is the same."""
+    c = _case(6, 3, 500, torch.float32, 91, draft=draft)
+    c["ids"] = c["target"].reshape(6, 4, 500)[:, :3].argmax(-1).to(torch.int32)
+    c["alpha"] = torch.tensor([[1.0, 1.0, 1.0], [1.0000001, 0.0, 0.0], [0.5, float("nan"), 0.5], [0.5, 0.5, 2.0], [-1.0, 0.0, 1.0], [float("inf"), 0.0, 0.0]])
+    n, tok = _check(hs, **c, temperature=torch.zeros(6))
+    assert n.tolist() == [3, 0, 1, 2, 3, 0]
