@@ -221,14 +221,48 @@ __device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
 __device__ __forceinline__ double weight64(float z, float m, double inv_t) {
   return z > -INFINITY ? exp((double(z) - double(m)) * inv_t) : 0.0;
 }
+// Calls f(4 U values) for this thread's share of [begin, end), begin a multiple of 4, by index and not by address as walk does: sums over equal rows are then equal
+// to the bit wherever the rows lie and whatever type holds them, so that p / q of them is 1 and p - q nothing.  Four neighbours at a time, one load where the row
+// begins on a boundary of four; behind the last: -infinity.
+template <int U, typename T, typename F>
+__device__ __forceinline__ void walk_by_index(const T* z, int begin, int end, F f) {
+  struct __align__(4 * sizeof(T)) Four { T v[4]; };
+  const bool whole = reinterpret_cast<uintptr_t>(z) % sizeof(Four) == 0;
+  Four next[U];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * 4 * VT;
+      if (whole && i + 4 <= end) {
+        next[u] = *reinterpret_cast<const Four*>(z + i);
+      } else if (i < end) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) next[u].v[j] = z[min(i + j, end - 1)];
+      }
+    }
+  };
+  fetch(begin + int(threadIdx.x) * 4);
+  for (int i0 = begin + int(threadIdx.x) * 4; i0 < end; i0 += U * 4 * VT) {
+    float v[4 * U];
+#pragma unroll
+    for (int j = 0; j < 4 * U; ++j) v[j] = i0 + (j / 4) * 4 * VT + j % 4 < end ? logit(value_of(next[j / 4].v[j % 4])) : -INFINITY;
+    fetch(i0 + U * 4 * VT);                       // (under way while these are dealt with)
+    f(v);
+  }
+}
+template <int U, typename F>
+__device__ __forceinline__ void walk_by_index(const Row& r, int begin, int end, F f) {
+  if (r.dtype == CHUNK_F32) walk_by_index<U>(reinterpret_cast<const float*>(r.z), begin, end, f);
+  else if (r.dtype == CHUNK_F16) walk_by_index<U>(reinterpret_cast<const __half*>(r.z), begin, end, f);
+  else walk_by_index<U>(reinterpret_cast<const __nv_bfloat16*>(r.z), begin, end, f);
+}
 template <typename W>
 __device__ __forceinline__ double sum_row64(const Row& r, int begin, int end, float m, W weigh) {
   double s0 = 0.0, s1 = 0.0;
   if (m > -INFINITY)
-    walk<2>(r, begin, end, [&](int, auto& v) {
-      constexpr int N = sizeof(v) / sizeof(float);
+    walk_by_index<1>(r, begin, end, [&](auto& v) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) (j & 1 ? s1 : s0) += weigh(v[j]);
+      for (int j = 0; j < 4; ++j) (j & 1 ? s1 : s0) += weigh(v[j]);
     });
   return s0 + s1;
 }
@@ -531,18 +565,20 @@ struct SampleShared {
 template <bool EXACT>
 __device__ __noinline__ double row_sum(RowWeights<EXACT> w, Row r, int begin, int end) {
   double s0 = 0.0, s1 = 0.0;
-  walk<EXACT ? 2 : 4>(r, begin, end, [&](int, auto& v) {
-    constexpr int N = sizeof(v) / sizeof(float);
-    if (EXACT) {
+  if (EXACT) {
+    walk_by_index<2>(r, begin, end, [&](auto& v) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) (j & 1 ? s1 : s0) += w(v[j]);
-    } else {
+      for (int j = 0; j < 8; ++j) (j & 1 ? s1 : s0) += w(v[j]);
+    });
+  } else {
+    walk<4>(r, begin, end, [&](int, auto& v) {
+      constexpr int N = sizeof(v) / sizeof(float);
       float part = 0.f;
 #pragma unroll
       for (int j = 0; j < N; ++j) part += w.quick(v[j]);
       s0 += double(part);
-    }
-  });
+    });
+  }
   return s0 + s1;
 }
 

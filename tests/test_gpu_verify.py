@@ -429,3 +429,22 @@ def test_greedy_drafts_that_no_ratio_reaches(hs, draft):
     c["alpha"] = torch.tensor([[1.0, 1.0, 1.0], [1.0000001, 0.0, 0.0], [0.5, float("nan"), 0.5], [0.5, 0.5, 2.0], [-1.0, 0.0, 1.0], [float("inf"), 0.0, 0.0]])
     n, tok = _check(hs, **c, temperature=torch.zeros(6))
     assert n.tolist() == [3, 0, 1, 2, 3, 0]
+
+
+@pytest.mark.parametrize("kinds", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float16), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("V,pitch", [(157, 160), (3001, 3001), (40009, 40013)])
+def test_equal_rows_at_any_alignment(hs, V, pitch, kinds):
+    """A drafter that is the target, its rows elsewhere in memory and of another type: every ratio is 1 to the bit, and nothing is left of p - q."""
+    B, k, g = 9, 4, torch.Generator().manual_seed(V)
+    d = (torch.randn((B, k, V), generator=g) * 2.0).to(torch.float16).to(torch.bfloat16)     # (values that all three types hold)
+    d = torch.where(d.abs() < 2.0 ** -6, torch.zeros_like(d), d).to(kinds[1]).cuda()
+    wide = torch.full((B * (k + 1), pitch), float("nan"), dtype=kinds[0], device="cuda")
+    wide[:, :V] = torch.cat([d, d[:, :1]], 1).reshape(-1, V).to(kinds[0])
+    ids, u = torch.randint(0, V, (B, k), generator=g, dtype=torch.int32), torch.rand(B, generator=g)
+    for alpha in (1.0, 1.5):
+        a = torch.full((B, k), alpha)
+        n, tok = _run(hs, wide[:, :V], d, ids.cuda(), a.cuda(), u.cuda())
+        want_n, want = to.verify(_wide(wide[:, :V]), _wide(d), ids.numpy(), a.numpy(), u.numpy())
+        assert (want_n == (k if alpha == 1.0 else 0)).all()
+        np.testing.assert_array_equal(n.cpu().numpy(), want_n)
+        np.testing.assert_array_equal(tok.cpu().numpy(), want)
