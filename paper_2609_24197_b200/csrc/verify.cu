@@ -217,9 +217,12 @@ __device__ __noinline__ unsigned long long key_row(Row r, int begin, int end) {
   return begin < end ? argmax_key(mx, at) : 0;
 }
 
-// e^((z - m) / t) in 64 bits; nothing where z is -infinity
+// e^((z - m) / t) in 64 bits; nothing where z is -infinity.  (As the square of e^(x / 2) where 64 bits end: the function itself may be off by 2^-1074 there,
+// which is all or nothing.)
 __device__ __forceinline__ double weight64(float z, float m, double inv_t) {
-  return z > -INFINITY ? exp((double(z) - double(m)) * inv_t) : 0.0;
+  if (!(z > -INFINITY)) return 0.0;
+  const double x = (double(z) - double(m)) * inv_t, e = exp(x > -700.0 ? x : 0.5 * x);
+  return x > -700.0 ? e : e * e;
 }
 // Calls f(4 U values) for this thread's share of [begin, end), begin a multiple of 4, by index and not by address as walk does: sums over equal rows are then equal
 // to the bit wherever the rows lie and whatever type holds them, so that p / q of them is 1 and p - q nothing.  Four neighbours at a time, one load where the row
@@ -509,7 +512,10 @@ constexpr float DEEP = -680.f;
 struct Weights {
   double table[256];
 };
-__device__ __noinline__ double exp_of(double x) { return exp(x); }
+__device__ __noinline__ double exp_of_deep(double x) {       // (see weight64)
+  const double e = exp(0.5 * x);
+  return e * e;
+}
 template <bool EXACT>
 struct RowWeights {                    // the weights of one row's logits, from its maximum, temperature and factor
   const Weights* w;
@@ -529,7 +535,7 @@ struct RowWeights {                    // the weights of one row's logits, from 
     const double r = fma(y, p, y);
     const float depth = (v - m) * inv_tf;
     if (depth > DEEP) return __hiloint2double(__double2hiint(r) + ((k >> 8) << 20), __double2loint(r));
-    return x > -746.0 ? exp_of(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
+    return x > -746.0 ? exp_of_deep(x) * w->table[0] : 0.0;    // (down to where 64 bits end: at u = 0 the lowest token with any weight is taken)
   }
   __device__ __forceinline__ float quick(float v) const { return ex2_ftz((v - m) * log2_t) * factor; }
   // A logit as it lies in memory, and what it says.  (Two steps, so that many loads go out before the first is looked at; no branch on the type.)

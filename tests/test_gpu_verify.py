@@ -448,3 +448,17 @@ def test_equal_rows_at_any_alignment(hs, V, pitch, kinds):
         assert (want_n == (k if alpha == 1.0 else 0)).all()
         np.testing.assert_array_equal(n.cpu().numpy(), want_n)
         np.testing.assert_array_equal(tok.cpu().numpy(), want)
+
+
+def test_the_least_number_of_64_bits(hs):
+    """Weights of half of 2^-1074 and more are that number: e^-745 is (2^-1075 is e^-745.13), e^-745.25 is nothing.  At u = 0 the first of them is taken, at alpha 0
+    a draft with it stands."""
+    depth = torch.tensor([-744.0, -744.5, -744.75, -745.0, -745.25, -745.5, -746.0, -747.0])
+    B, V = depth.numel(), 70
+    z = torch.full((B, 2, V), -1.0e30)
+    z[:, :, 50] = 64.0
+    z[:, :, 20] = 64.0 + depth[:, None]
+    for token in (20, 50):
+        n, tok = _check(hs, z.reshape(2 * B, V), None, torch.full((B, 1), token, dtype=torch.int32), torch.zeros((B, 1)), torch.zeros(B))
+        assert n.tolist() == ([1, 1, 1, 1, 0, 0, 0, 0] if token == 20 else [1] * B)
+        assert tok[:4, 1].tolist() == [20] * 4 and tok[4:, 1 if token == 50 else 0].tolist() == [50] * 4
