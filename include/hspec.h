@@ -351,9 +351,10 @@ int hspec_op_swiglu(const float* gu, void* h_f16, int32_t M, int32_t F, void* st
  * stands at cache position kv_lens[b] - n + i.  The cache is the paged one of the draft step: page_table int32
  * [B, page_table_stride], pools [num_pages, page_size, Hkv, dh].  Both may be bf16 or fp16 here (`dtype`), Hq a multiple of Hkv,
  * dh 64 or 128, any page size; q and the pools start on 16-byte boundaries.  Rows behind cu_q[B] (a batch padded to a captured
- * graph's size) are not written, and nothing depends on what they hold.  Outputs share no memory with inputs.  What the device arrays say is held inside T and page_table_stride * page_size; entries
- * outside, requests with more rows than cached tokens and page ids outside [0, num_pages) are counted (hspec_op_device_status).
- * The lengths are read on the device: a captured call follows the arrays' contents.
+ * graph's size) are not written, and no result depends on what they hold.  Outputs share no memory with inputs.  What the device
+ * arrays say is held inside T and page_table_stride * page_size; entries outside, requests with more rows than cached tokens and
+ * page ids outside [0, num_pages) are counted (hspec_op_device_status).  The lengths are read on the device: a captured call
+ * follows the arrays' contents.  The first call of a process may be a captured one.
  * ---------------------------------------------------------------------------------------------- */
 
 /* Norm, rotary positions on one or several axes and the cache write of a chunk.

@@ -158,9 +158,17 @@ uint32_t* global_status() {
   if (d < 0) return nullptr;
   std::lock_guard<std::mutex> lock(device_setup_mutex());
   if (!g_status[d]) {
+    // (The first call on a device may be one that is being captured: allocated outside of the capture, and zero on a stream of its own before anything runs.)
     uint32_t* p = nullptr;
-    if (cudaMalloc(&p, STATUS_WORDS * 4) != cudaSuccess) return nullptr;
-    if (cudaMemset(p, 0, STATUS_WORDS * 4) != cudaSuccess) { cudaFree(p); return nullptr; }
+    cudaStream_t own = nullptr;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) return nullptr;
+    const bool ok = cudaMalloc(&p, STATUS_WORDS * 4) == cudaSuccess && cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking) == cudaSuccess &&
+                    cudaMemsetAsync(p, 0, STATUS_WORDS * 4, own) == cudaSuccess && cudaStreamSynchronize(own) == cudaSuccess;
+    if (own) cudaStreamDestroy(own);
+    if (!ok && p) cudaFree(p);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (!ok) return nullptr;
     g_status[d] = p;
   }
   return g_status[d];

@@ -1,5 +1,9 @@
 """The target's side of an iteration run as it is used: rotary positions and cache write, attention over the cache, LM head, verification, all of it one
 captured graph that is replayed while requests grow by what was accepted and one of them ends."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -159,3 +163,43 @@ def test_iterations_of_a_target(hs):
         for pool in ("k", "v"):
             assert torch.isfinite(again[pool][i, j]).all() and torch.equal(cache[pool][i, j], again[pool][i, j])
     assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 0
+
+
+FIRST_CALL = """
+import sys, torch
+import paper_2609_24197_b200 as hs
+i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+half = lambda *s: torch.randn(s, device="cuda").to(torch.bfloat16)
+u8 = lambda n: torch.empty(n, dtype=torch.uint8, device="cuda")
+table = i32(0, 1, 2, 3)[None]
+k, v, q = half(4, 8, 2, 64), half(4, 8, 2, 64), half(3, 6, 64)
+if sys.argv[1] == "write":
+    qkv, out = half(3, 640), [torch.zeros_like(q), k, v]
+    call = lambda: hs.hspec_op_chunk_rope_write(qkv, None, None, i32_cu, i32_kv, table, *out, 1.0e4)
+elif sys.argv[1] == "attend":
+    out, ws = [torch.zeros_like(q)], u8(hs.hspec_chunk_attention_workspace_bytes(6, 2, 64))
+    call = lambda: hs.hspec_op_chunk_attention(q, k, v, table, i32_cu, i32_kv, out[0], ws)
+else:
+    z, ids, alpha, u, ws = torch.randn((3, 40), device="cuda"), i32(1, 2)[None], torch.rand((1, 2), device="cuda"), torch.rand(1, device="cuda"), u8(hs.hspec_verify_workspace_bytes(1, 2))
+    out = [i32(-9), i32(-9, -9, -9)[None]]
+    call = lambda: hs.hspec_op_verify(z, None, ids, alpha, u, out[0], out[1], ws)
+i32_cu, i32_kv = i32(0, 3), i32(20)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call()
+graph.replay()
+torch.cuda.synchronize()
+got = [x.clone() for x in out]
+call()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, out)) and any((x != 0).any() for x in got)
+assert not any(hs.hspec_op_device_status().values()), hs.hspec_op_device_status()
+"""
+
+
+@pytest.mark.parametrize("what", ["write", "attend", "verify"])
+def test_the_first_call_of_a_process_may_be_a_captured_one(what):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALL, what], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0, done.stderr[-1500:]
