@@ -26,7 +26,6 @@
 #include "chunk_plan.cuh"
 
 #include <cstddef>
-#include <cstdlib>
 #include <type_traits>
 
 namespace hspec {
@@ -40,7 +39,8 @@ constexpr int MAX_CTAS = 148;
 // place of 14 a prompt of 8192 tokens takes 638 us, not 548).
 constexpr int COST_TURNS = 3, COST_BOTH = 4, COST_ITEM = 14;
 constexpr float LAZY = 8.0f;         // the reference maximum moves, for the next tile, when the row's exceeds it by 2^8
-constexpr float LIMIT_BF16 = 60.0f, LIMIT_F16 = 15.0f;      // and at once when it exceeds it by more than the weights' type can hold
+// And at once when it exceeds it by more than the weights' type can hold, or 32 bits a tile's products with values up to 2^60.
+constexpr float LIMIT_BF16 = 60.0f, LIMIT_F16 = 15.0f;
 constexpr int THREADS = 640;
 
 template <int DH> struct Shape {
@@ -677,7 +677,9 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
           tmem_st_wait();
         };
         uint64_t ls[2] = {0ull, 0ull};
-        // Weights of the 32 keys, over scores of this thread that have been fetched.
+        // Weights of the 32 keys, over scores of this thread that have been fetched.  They are rounded to the pools' type, which the product with the values needs:
+        // half a step each, at most half a step of sum p |v| together.  In fp16 those under 2^-14 of the reference lose bits and those under 2^-25 all of them,
+        // while the sum, which is of 32-bit weights, has them: 2^-25 of the reference's weight for a key at most.
         auto weights_of = [&](int part, float ref, bool any_far) {
           if (any_far) {
             float copy[32];
@@ -718,7 +720,8 @@ __device__ __forceinline__ void softmax_half(const Args& a, uint8_t* sQ, Bars* b
           fetch(1);
         } else {
           // The weights do not wait for the row's maximum: the reference is that of the tiles before.  Only where this tile is above it by more than
-          // the weights' type can hold do they follow at once: the first 32 from their own maximum, then, when the row's is known, scaled to it.
+          // the weights' type can hold do they follow at once: the first 32 from their own maximum, then, when the row's is known, scaled to it (and
+          // rounded a second time).
           if (__any_sync(0xffffffffu, m_next != m_ref)) {
             const float factor = m_next != m_ref ? ex2_ftz(m_ref - m_next) : 1.f;
             m_ref = m_next;

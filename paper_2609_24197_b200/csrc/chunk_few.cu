@@ -12,7 +12,8 @@
 //      keys g and g + 8, and of Q's row g: each piece is the operand of two products.
 //   V: thread (g, c) loads columns 8 g .. 8 g + 7 of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9; neighbouring keys are paired by byte permutes, and its columns
 //      take rows g and g + 8 of four products.  The result then lies as 8 neighbouring columns of rows 2 c and 2 c + 1.
-//   P: weights come out transposed, and movmatrix turns them.
+//   P: weights come out transposed, and movmatrix turns them.  They are rounded to the pools' type for the product (see weights_of in chunk_attention.cu); their
+//      sums are of 32-bit ones.
 // The reference maximum moves when a score exceeds it by 2^8 (fp16 weights hold 2^15); sums are a thread's own until the item's end.
 #include "chunk_plan.cuh"
 

@@ -13,7 +13,7 @@
 // been refused before is not read.  The second takes one request per cluster and samples with 32-bit weights.  The third does so with 64-bit weights for
 // the requests whose uniform number came within some 2^-16 of a border between two tokens: what falls among the many tokens of next to no weight.  The
 // first two are bound by memory, the third by the latency of its 64-bit operations (their pipe is busy for a fifth of the time; 128 requests of 152 064
-// tokens: 238 us in 64 bits alone, 69 and 61 in two steps).
+// tokens: 238 us in 64 bits alone, 70 and 64 in two steps).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -471,7 +471,7 @@ __device__ __forceinline__ void verify_row(const VerifyCall& c, const VerifyScra
 
 // One (position, request) per cluster, position by position.  verdict[b * k + i] = 1 if the draft would stand; the row maxima (and for greedy requests
 // the arg-max) are left for the kernel behind.  skip: first[b] holds the lowest position refused so far, and items behind it are passed over.
-// 128 requests of 16 drafts, 575 MB up to the first refused ones: 160 us and 960 MB, the rest read while the verdict in front was still out.  (Clusters
+// 128 requests of 16 drafts, 575 MB up to the first refused ones: 163 us and 960 MB, the rest read while the verdict in front was still out.  (Clusters
 // that walk the items themselves 205 us; leaving off a row whose request has been refused meanwhile saved some bytes and no time; two blocks a row
 // read fewer ahead in the same time, four are slower.)
 __global__ void __launch_bounds__(VT, 2)
@@ -683,11 +683,11 @@ __device__ __noinline__ double rest_sum(RowWeights<EXACT> p, RowWeights<EXACT> q
   return all;
 }
 
-// One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by 2^-23 x
-// of itself for its exponent of size x, 2^-22 for the special function and 2^-23 for the factor and the sums of four, and from there on sums are
-// 64-bit ones.  Averaged by weight, the exponents' size is the entropy of the weights less log2 of their sum W, so at most log2 (V / W): V weights are off by
-// 2^-23 (log2 V - log2 W + 3) of their sum together (W is 1 or more, but where an arg-max drafter's token is left out).  A goal that is not that far
-// inside its token's share is left to the kernel with EXACT.
+// One request per cluster: counts the drafts that stand and takes the token behind them.  Without EXACT the weights are 32-bit ones, each off by up to 1.7 x 2^-23
+// of itself for its exponent of size x (as in row_error), 2^-22 for the special function and 2^-23 for the factor and the sums of four, and from there on sums
+// are 64-bit ones.  Averaged by weight, the exponents' size is the entropy of the weights less log2 of their sum W, so at most log2 (V / W): V weights are off by
+// 2^-23 (1.7 (log2 V - log2 W) + 3) of their sum together (W is 1 or more, but where an arg-max drafter's token is left out), and so is the distance from the goal
+// to a border.  A goal that is not 2^-22 (log2 V - log2 W + 4) of the sum inside its token's share is left to the kernel with EXACT.
 template <bool EXACT>
 __device__ __forceinline__ void sample(const VerifyCall& c, const VerifyScratch& s, int S, SampleShared& sh) {
   const int b = blockIdx.x / S, rank = blockIdx.x % S, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -923,7 +923,7 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
   }
   // One request in five to ten is left for the third step, a chain of 64-bit operations for every token of a thread: 16 blocks each as long as there are SMs
-  // for them (37 requests of 151 937 tokens: 45 us, 58 with 8; 128 of 152 064: 77, 60 with 8).
+  // for them (37 requests of 151 937 tokens: 45 us, 58 with 8; 128 of 152 064: 77, 64 with 8).
   const int S = blocks_for(c.B, MAX_S), S64 = blocks_for(1, c.B <= 64 ? MAX_S : 8);
   static bool done[MAX_DEVICES] = {};
   e = once_per_device(done, [](int) {
@@ -933,7 +933,7 @@ cudaError_t verify_launch(const VerifyCall& c, cudaStream_t stream) {
     return e1;
   });
   if (e != cudaSuccess) return e;
-  // With as many blocks a request in both, one launch: a loop of calls for a single request takes 19.0 us each, not 23.5.
+  // With as many blocks a request in both, one launch: a single request's step takes 13.8 us on the device.
   if (S == S64) return launch_pdl_cluster(verify_sample_kernel<SAMPLE_BOTH>, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
   e = launch_pdl_cluster(verify_sample_kernel<SAMPLE_32>, dim3(unsigned(c.B) * S), dim3(VT), dim3(S), 0, stream, c, s, S);
   if (e != cudaSuccess) return e;
