@@ -324,7 +324,7 @@ def _plain_logits(s):
     case = s["case"]
     B, V, T = case["batch"], case["vocab"], sum(s["new"])
     b, i = _places(s["cu_q"], T)
-    z = s["z"][:T].float()
+    z = s["z"][:T].to(torch.float32, copy=True)
     if s["history"] is not None:
         at = torch.arange(s["history"].shape[1], device="cuda")
         inside, mine = at < s["history_lens"].unsqueeze(1), at >= s["prompt_lens"].unsqueeze(1)
