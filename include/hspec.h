@@ -412,6 +412,55 @@ int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_
                     void* workspace, size_t workspace_bytes, void* stream);
 size_t hspec_verify_workspace_bytes(int32_t B, int32_t k);
 
+/* The recurrent layers of a hybrid target over a ragged chunk (Mamba-2: short causal convolution, selective scan, gate), from a carried state and back
+ * into it.  For every row t of a request, with u = SiLU(convolution of x | B | C over the request's last d_conv rows):
+ *   dt = softplus(dt_raw + dt_bias),  S <- exp(-dt e^A_log) S + dt x B^T  (per head, [P, N]),  y = (S C + Dskip x) SiLU(z)
+ *   zxbcdt      device [T, ld_in] fp32, bf16 or fp16 (in_dtype): columns z [Di] | x [Di] | B [G N] | C [G N] (| dt [H] when dt_raw is NULL), H = Di / P,
+ *               from any address.  T may be 0, zxbcdt NULL then
+ *   dt_raw      device fp32 [T, H] or NULL
+ *   conv_w fp32 [Di + 2 G N, d_conv], conv_b [Di + 2 G N], dt_bias, A_log, Dskip [H]; d_conv 1 to 4, N at most 256
+ *   conv_state  device [num_slots, d_conv - 1, Di + 2 G N] of in_dtype: the raw rows in front of the next one, oldest first (NULL when d_conv is 1)
+ *   ssm_state   device fp32 [num_slots, H, P, N], 16-byte aligned
+ *   slots       device int32 [B] or NULL (b): where request b's states lie.  Slots of requests in one call differ.  A request with rows whose slot lies
+ *               outside [0, num_slots) starts from zeros and keeps nothing (counted)
+ *   fresh       device int32 [B] or NULL: nonzero starts the request from zeros, whatever its slot holds
+ *   keep        device int32 [B] or NULL: the states behind the request's first keep[b] + keep_more rows are stored (held inside 0 .. its rows); NULL:
+ *               behind all of them.  A request of which nothing is kept leaves its states as they are (zeros, if it is fresh)
+ *   y           out [T, ld_y] fp32, bf16 or fp16 (y_dtype), all rows of all requests; NULL: the states alone
+ * Single tokens, draft blocks and pieces of prompts may be mixed.  A verification's pass runs with keep all zero (keep_more 0); once
+ * hspec_op_verify has counted the drafts that stand, the same rows with y NULL, keep = n_accept and keep_more = 1 move the states on.
+ * States that the call does not store keep their bits.  Accumulation and states are 32-bit.  At most 65535 requests.
+ * workspace: hspec_chunk_scan_workspace_bytes (it grows with T and B, so that of the largest call does for all), 256-byte aligned, contents undefined
+ * between calls; calls that may overlap on the GPU need one each. */
+int hspec_op_chunk_scan(const void* zxbcdt, int32_t in_dtype, int64_t ld_in, const float* dt_raw, const float* conv_w, const float* conv_b,
+                        const float* dt_bias, const float* A_log, const float* Dskip, const int32_t* cu_q, int32_t B, const int32_t* slots,
+                        const int32_t* fresh, const int32_t* keep, int32_t keep_more, void* conv_state, float* ssm_state, int32_t num_slots, void* y,
+                        int32_t y_dtype, int64_t ld_y, int32_t T, int32_t Di, int32_t P, int32_t N, int32_t G, int32_t d_conv, void* workspace,
+                        size_t workspace_bytes, void* stream);
+size_t hspec_chunk_scan_workspace_bytes(int32_t T, int32_t B, int32_t Di, int32_t P, int32_t N, int32_t G);
+/* What a request's rules do to logits between the LM head and the verification (or any sampling).  Row i of request b stands behind the text
+ * history[b, : len] and then drafts[b, : min(i, k)]; for every token v of the row, in this order:
+ *   z <- z / repetition if z > 0, else z repetition     where v is anywhere in the text
+ *   z <- z - frequency count - presence                 where v is `count` > 0 times in the answer (the text behind its first prompt_lens[b]) or the drafts
+ *   z <- z + the sum of v's biases
+ *   z <- -infinity                                      where the row's mask has bit v at zero
+ *   logits      device [T, ld_in] fp32, bf16 or fp16 (in_dtype); out [T, ld_out] of the same type or fp32: logits itself (only what changes is then
+ *               touched), or memory apart from it.  A finite result beyond fp16 is clamped there (counted)
+ *   cu_q        device int32 [B + 1], or NULL: B = T requests of one row.  Rows behind cu_q[B] are not written
+ *   history     device int32 [B, history_stride] or NULL; history_lens int32 [B] or NULL (all of it); prompt_lens int32 [B] or NULL (0)
+ *   drafts      device int32 [B, k] or NULL; a text has at most 2^20 - 1 tokens with its drafts
+ *   repetition, frequency, presence   device fp32 [B] or NULL each
+ *   bias_ids, bias_values   device int32, fp32 [B, n_bias] or NULL; bias_counts int32 [B] or NULL (all); at most 1024; a token may come several times
+ *   mask        device uint32 [n_masks, mask_stride], bit v % 32 of word v / 32 set where v is allowed; mask_rows int32 [T]: each row's mask, -1 for
+ *               none; NULL: row t has mask t
+ * Token ids outside [0, V) count for nothing; these, lengths outside their array and mask rows outside -1 .. n_masks - 1 (taken as none) are counted
+ * (hspec_op_device_status). */
+int hspec_op_adjust_logits(const void* logits, int32_t in_dtype, int64_t ld_in, void* out, int32_t out_dtype, int64_t ld_out, int32_t T, int32_t V,
+                           const int32_t* cu_q, int32_t B, const int32_t* history, int32_t history_stride, const int32_t* history_lens,
+                           const int32_t* prompt_lens, const int32_t* drafts, int32_t k, const float* repetition, const float* frequency,
+                           const float* presence, const int32_t* bias_ids, const float* bias_values, const int32_t* bias_counts, int32_t n_bias,
+                           const uint32_t* mask, int32_t n_masks, int32_t mask_stride, const int32_t* mask_rows, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

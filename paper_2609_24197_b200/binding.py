@@ -25,7 +25,7 @@ EXPORTS = [
     "hspec_op_accept", "hspec_op_token_probs", "hspec_op_markov_head", "hspec_markov_workspace_bytes",
     "hspec_op_kv_inject_write", "hspec_op_device_status", "hspec_debug_gemm_tiles",
     "hspec_op_chunk_rope_write", "hspec_op_chunk_attention", "hspec_chunk_attention_workspace_bytes", "hspec_op_verify",
-    "hspec_verify_workspace_bytes",
+    "hspec_verify_workspace_bytes", "hspec_op_chunk_scan", "hspec_chunk_scan_workspace_bytes", "hspec_op_adjust_logits",
 ]
 
 
@@ -133,6 +133,12 @@ def load_library(path=None):
     lib.hspec_op_verify.argtypes = [vp, i32, i64, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
     lib.hspec_verify_workspace_bytes.argtypes = [i32, i32]
     lib.hspec_verify_workspace_bytes.restype = sz
+    lib.hspec_op_chunk_scan.argtypes = [vp, i32, i64, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32, i64, i32, i32, i32, i32, i32,
+                                        i32, vp, sz, vp]
+    lib.hspec_chunk_scan_workspace_bytes.argtypes = [i32] * 6
+    lib.hspec_chunk_scan_workspace_bytes.restype = sz
+    lib.hspec_op_adjust_logits.argtypes = [vp, i32, i64, vp, i32, i64, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i32,
+                                           i32, vp, vp]
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -427,7 +433,7 @@ def _device():
 
 
 _HALF, _LOGITS = (torch.bfloat16, torch.float16), (torch.float32, torch.bfloat16, torch.float16)
-_I32, _F32, _U8 = (torch.int32,), (torch.float32,), (torch.uint8,)
+_I32, _F32, _U8, _WORDS = (torch.int32,), (torch.float32,), (torch.uint8,), (torch.int32, torch.uint32)
 
 
 def hspec_op_chunk_rope_write(qkv, pos, pair_axis, cu_q, kv_lens, page_table, q, k_pool, v_pool, theta, q_norm_w=None, k_norm_w=None, eps=1e-6):
@@ -500,6 +506,60 @@ def hspec_op_verify(target_logits, draft_logits, draft_ids, alpha, u, n_accept, 
         _arg("workspace", workspace, _U8, workspace.shape, dev), workspace.shape[0], _stream())
     if rc:
         _check(rc, None, "hspec_op_verify")
+
+
+def hspec_chunk_scan_workspace_bytes(T, B, Di, P, N, G):
+    return int(load_library().hspec_chunk_scan_workspace_bytes(T, B, Di, P, N, G))
+
+
+def _opt(name, t, dtypes, shape, dev):
+    return None if t is None else _arg(name, t, dtypes, shape, dev)
+
+
+def hspec_op_chunk_scan(zxbcdt, conv_w, conv_b, dt_bias, A_log, Dskip, cu_q, conv_state, ssm_state, y, workspace, dt_raw=None, slots=None, fresh=None,
+                        keep=None, keep_more=0):
+    """A recurrent layer over a ragged chunk: zxbcdt [T, z | x | B | C (| dt)] -> y [T, Di] (or None: the states alone), with the carried rows
+    conv_state [slots, d_conv - 1, Di + 2 G N] (None where the convolution is one wide) and states ssm_state [slots, H, P, N], in place."""
+    dev = _device()
+    T, B = zxbcdt.shape[0], cu_q.shape[0] - 1
+    d_xBC, d_conv = conv_w.shape
+    slots_n, H, P, N = ssm_state.shape
+    Di = H * P
+    G = (d_xBC - Di) // (2 * N) if N else 0
+    if G < 1 or d_xBC != Di + 2 * G * N:
+        raise HSpecError(f"conv_w: {d_xBC} channels are not those of {H} heads of {P} with states of {N}")
+    width, half = Di + d_xBC + (H if dt_raw is None else 0), (zxbcdt.dtype,)
+    rc = load_library().hspec_op_chunk_scan(
+        _arg("zxbcdt", zxbcdt, _LOGITS, (T, width), dev, True), _DT[zxbcdt.dtype], _row_pitch(zxbcdt, width), _opt("dt_raw", dt_raw, _F32, (T, H), dev),
+        _arg("conv_w", conv_w, _F32, (d_xBC, d_conv), dev), _arg("conv_b", conv_b, _F32, (d_xBC,), dev), _arg("dt_bias", dt_bias, _F32, (H,), dev),
+        _arg("A_log", A_log, _F32, (H,), dev), _arg("Dskip", Dskip, _F32, (H,), dev), _arg("cu_q", cu_q, _I32, (B + 1,), dev), B,
+        _opt("slots", slots, _I32, (B,), dev), _opt("fresh", fresh, _I32, (B,), dev), _opt("keep", keep, _I32, (B,), dev), keep_more,
+        _opt("conv_state", conv_state, half, (slots_n, d_conv - 1, d_xBC), dev), _arg("ssm_state", ssm_state, _F32, (slots_n, H, P, N), dev), slots_n,
+        None if y is None else _arg("y", y, _LOGITS, (T, Di), dev, True), 0 if y is None else _DT[y.dtype], Di if y is None else _row_pitch(y, Di), T, Di,
+        P, N, G, d_conv, _arg("workspace", workspace, _U8, workspace.shape, dev), workspace.shape[0], _stream())
+    if rc:
+        _check(rc, None, "hspec_op_chunk_scan")
+
+
+def hspec_op_adjust_logits(logits, out, cu_q=None, history=None, history_lens=None, prompt_lens=None, drafts=None, repetition=None, frequency=None,
+                           presence=None, bias_ids=None, bias_values=None, bias_counts=None, mask=None, mask_rows=None):
+    """Penalties, biases and allowed tokens: logits [T, V] -> out [T, V] (logits itself, or apart from it).  mask: int32 or uint32 words."""
+    dev = _device()
+    T, V = logits.shape
+    B = T if cu_q is None else cu_q.shape[0] - 1
+    h = 0 if history is None else history.shape[1]
+    k = 0 if drafts is None else drafts.shape[1]
+    n = 0 if bias_ids is None else bias_ids.shape[1]
+    masks = (0, 0) if mask is None else mask.shape
+    rc = load_library().hspec_op_adjust_logits(
+        _arg("logits", logits, _LOGITS, (T, V), dev, True), _DT[logits.dtype], _row_pitch(logits, V), _arg("out", out, _LOGITS, (T, V), dev, True),
+        _DT[out.dtype], _row_pitch(out, V), T, V, _opt("cu_q", cu_q, _I32, (B + 1,), dev), B, _opt("history", history, _I32, (B, h), dev), h,
+        _opt("history_lens", history_lens, _I32, (B,), dev), _opt("prompt_lens", prompt_lens, _I32, (B,), dev), _opt("drafts", drafts, _I32, (B, k), dev), k,
+        _opt("repetition", repetition, _F32, (B,), dev), _opt("frequency", frequency, _F32, (B,), dev), _opt("presence", presence, _F32, (B,), dev),
+        _opt("bias_ids", bias_ids, _I32, (B, n), dev), _opt("bias_values", bias_values, _F32, (B, n), dev), _opt("bias_counts", bias_counts, _I32, (B,), dev),
+        n, _opt("mask", mask, _WORDS, masks, dev), masks[0], masks[1], _opt("mask_rows", mask_rows, _I32, (T,), dev), _stream())
+    if rc:
+        _check(rc, None, "hspec_op_adjust_logits")
 
 
 # ----------------------------------------------------------------------------- convenience wrapper

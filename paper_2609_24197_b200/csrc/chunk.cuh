@@ -33,6 +33,34 @@ __device__ __forceinline__ int chunk_request_of(const int32_t* cu_q, int B, int 
   return n;
 }
 
+// Item `item` of a chunk whose requests are cut into items of `rows` rows (`least` of them at least: 1 where a request without rows has work too):
+// its request (-1: behind the last item), that request's first row and number of rows, and the item's first row among them.  There are at most
+// T / rows + B items (T / rows + min(B, T) with least = 0).  One warp.
+struct ChunkItem { int b, q0, n, first; };
+__device__ __forceinline__ ChunkItem chunk_item(const int32_t* cu_q, int B, int T, int rows, int least, int item, int lane) {
+  int before = 0;
+  for (int base = 0; base < B; base += 32) {
+    int c0 = 0, c1 = 0;
+    if (base + lane < B) { c0 = cu_q[base + lane]; c1 = cu_q[base + lane + 1]; }
+    const ChunkRequest r = chunk_request(c0, c1, 0, T, 0);
+    const int items = base + lane < B ? max((r.n + rows - 1) / rows, least) : 0;
+    int upto = items;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += up;
+    }
+    const uint32_t mine = __ballot_sync(0xffffffffu, before + upto > item);
+    if (mine) {
+      const int l = __ffs(mine) - 1;
+      return {base + l, __shfl_sync(0xffffffffu, r.q0, l), __shfl_sync(0xffffffffu, r.n, l),
+              (item - before - __shfl_sync(0xffffffffu, upto - items, l)) * rows};
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return {-1, 0, 0, 0};
+}
+
 __device__ __forceinline__ uint32_t pack_f16_sat(float lo, float hi, uint32_t* status) {
   const __half2 h = __halves2half2(f16_sat(lo, status), f16_sat(hi, status));
   return *reinterpret_cast<const uint32_t*>(&h);

@@ -1,0 +1,397 @@
+// Short causal convolution, selective scan and gate of a ragged chunk of new tokens, from a carried state and back into it.
+//
+//   u_t = SiLU(b + sum_j w_j raw_{t - K + 1 + j}),  u = x | B | C      raw rows in front of the chunk come from the request's carried ones
+//   dt_t = softplus(dt_raw_t + bias),  S_t = exp(-dt_t e^A_log) S_{t-1} + dt_t x_t B_t^T,  y_t = (S_t C_t + D x_t) SiLU(z_t)
+//
+// Two kernels.  The first one convolves the rows into a scratch of 32-bit rows, with their steps and decays; a thread takes four channels of some rows,
+// the thread of a request's first rows also moves the carried rows on, which nobody else reads.  The second one carries the states through the rows: a
+// block has some rows of a head's state in registers, from the first token to the last, and reads the convolved rows from shared memory, a few tokens
+// ahead of their use.  Up to some twenty rows it is bound by the state, which is read and written once.
+#include "chunk_scan.cuh"
+
+#include <climits>
+#include <type_traits>
+
+namespace hspec {
+
+namespace {
+
+constexpr int CONV_THREADS = 256;
+constexpr int CONV_TILE = 8;         // rows of a block
+
+struct ScanScratch {
+  float* xbc;                        // [T, pitch] convolved rows
+  float2* step;                      // [T, H] dt and the decay exp(dt A)
+  int pitch;
+};
+
+struct ConvArgs {
+  ChunkScanCall c;
+  ScanScratch s;
+  int ch_blocks, dt_blocks;          // blocks of an item: channels, then steps
+};
+
+// A word of W row values, widened.
+template <typename T, int W>
+__device__ __forceinline__ void load_wide(const T* p, float (&x)[W]) {
+  const Word<T, W> w = *reinterpret_cast<const Word<T, W>*>(p);
+#pragma unroll
+  for (int e = 0; e < W; ++e) x[e] = to_f32(w.v[e]);
+}
+
+template <typename TI, int W, int K>
+__global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
+  const ChunkScanCall& c = a.c;
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = blockIdx.x % blocks;
+  const ChunkItem item = chunk_item(c.cu_q, c.B, c.T, CONV_TILE, 1, blockIdx.x / blocks, tid & 31);
+  if (item.b < 0) return;
+  const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
+  if (part >= a.ch_blocks) {
+    // ---- steps and decays
+    const int i = (part - a.ch_blocks) * CONV_THREADS + tid, h = i % c.H, r = i / c.H;
+    if (r < rows) {
+      const size_t t = t0 + r;
+      const float raw = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
+      const float dt = softplus_f32(raw + c.dt_bias[h]);
+      a.s.step[t * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
+    }
+    return;
+  }
+  const ScanRequest r = scan_request(c, item.b);
+  if (part == 0 && item.first == 0 && tid == 0) {
+    const int slot = c.slots ? c.slots[item.b] : item.b;
+    if (chunk_request_bad(c.cu_q[item.b], c.cu_q[item.b + 1], INT_MAX, c.T, INT_MAX) || (item.n > 0 && r.slot != slot))
+      atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+  }
+  const int ch = (part * CONV_THREADS + tid) * W;
+  if (ch >= c.d_xBC) return;
+  float w[K][W], bias[W], raw[K - 1 + CONV_TILE][W];
+  // (a thread's weights are W rows of K)
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    bias[e] = c.conv_b[ch + e];
+#pragma unroll
+    for (int j = 0; j < K; ++j) w[j][e] = c.conv_w[size_t(ch + e) * K + j];
+  }
+  TI* carried = reinterpret_cast<TI*>(c.conv_state) + (r.slot < 0 ? 0 : size_t(r.slot) * (K - 1) * c.d_xBC) + ch;
+  const TI* src = reinterpret_cast<const TI*>(c.x) + size_t(t0) * c.ld_x + c.Di + ch;
+  if (item.first == 0) {
+    using V = Word<TI, W>;
+    V old[K - 1 > 0 ? K - 1 : 1];
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+      if (r.fresh) old[j] = V{};
+      else old[j] = *reinterpret_cast<const V*>(carried + size_t(j) * c.d_xBC);
+#pragma unroll
+      for (int e = 0; e < W; ++e) raw[j][e] = to_f32(old[j].v[e]);
+    }
+    if (r.stores()) {
+#pragma unroll
+      for (int j = 0; j < K - 1; ++j) {
+        const int from = r.keep + j - (K - 1);             // the chunk's row that comes to place j; below zero: a carried one
+        V v{};
+        if (from >= 0) {
+          v = *reinterpret_cast<const V*>(src + size_t(from) * c.ld_x);
+        } else {
+#pragma unroll
+          for (int o = 0; o < K - 1; ++o)
+            if (o == r.keep + j) v = old[o];
+        }
+        *reinterpret_cast<V*>(carried + size_t(j) * c.d_xBC) = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) load_wide<TI, W>(src + (j - (K - 1)) * (long long)(c.ld_x), raw[j]);
+  }
+#pragma unroll
+  for (int i = 0; i < CONV_TILE; ++i)
+    if (i < rows) load_wide<TI, W>(src + size_t(i) * c.ld_x, raw[K - 1 + i]);
+#pragma unroll
+  for (int i = 0; i < CONV_TILE; ++i) {
+    if (i >= rows) break;
+    Word<float, W> out;
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      float v = bias[e];
+#pragma unroll
+      for (int j = 0; j < K; ++j) v = fmaf(w[j][e], raw[i + j][e], v);
+      out.v[e] = silu_f32(v);
+    }
+    *reinterpret_cast<Word<float, W>*>(a.s.xbc + size_t(t0 + i) * a.s.pitch + ch) = out;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// The states through the rows.  A group of L lanes has PR rows of a head's state [P, N]: lane l of the group the elements n = 4 (l + L k) .. + 3.
+constexpr int STATE_THREADS = 128;
+constexpr int STATE_TILE = 8;        // tokens that are fetched together
+
+struct StateArgs {
+  ChunkScanCall c;
+  ScanScratch s;
+  int p_blocks, p_block;             // blocks of a head, rows of its state in each
+  int np;                            // padded N: row pitch of B and C in shared memory
+};
+
+template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
+__global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) {
+  constexpr int DUP = L / PR;                                // lanes that end up with the same row's sum
+  constexpr int ROWS = (STATE_TILE + DUP - 1) / DUP;         // tokens of a tile whose outputs a lane finishes
+  const ChunkScanCall& c = a.c;
+  const int tid = threadIdx.x, l = tid % L;
+  const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, g = h / (c.H / c.G);
+  const int p0 = (blockIdx.x % a.p_blocks) * a.p_block, pt = p0 + tid / L * PR;      // the block's and the thread's first rows
+  // (before the wait only what is at least two kernels back is read: the arrays that describe the chunk, and the states)
+  const ScanRequest r = scan_request(c, b);
+  const int upto = Y ? r.n : r.keep;
+  uint64_t S[PR][NPT / 2];
+  float* state = c.ssm_state + ((size_t(r.slot < 0 ? 0 : r.slot) * c.H + h) * c.P + pt) * c.N;
+#pragma unroll
+  for (int i = 0; i < PR; ++i) {
+#pragma unroll
+    for (int k = 0; k < NPT / 4; ++k) {
+      const int n = 4 * (l + L * k);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (!r.fresh && (upto > 0) && pt + i < c.P && n < c.N) {
+        const float* p = state + size_t(i) * c.N + n;
+        if (VECN) v = __ldcs(reinterpret_cast<const float4*>(p));
+        else {
+          v.x = p[0];
+          if (n + 1 < c.N) v.y = p[1];
+          if (n + 2 < c.N) v.z = p[2];
+          if (n + 3 < c.N) v.w = p[3];
+        }
+      }
+      S[i][2 * k] = pack_f32x2(v.x, v.y);
+      S[i][2 * k + 1] = pack_f32x2(v.z, v.w);
+    }
+  }
+  pdl_wait();
+  pdl_trigger();
+  if (upto == 0 && !r.stores()) return;
+  auto store = [&] {
+#pragma unroll
+    for (int i = 0; i < PR; ++i) {
+#pragma unroll
+      for (int k = 0; k < NPT / 4; ++k) {
+        const int n = 4 * (l + L * k);
+        if (pt + i >= c.P || n >= c.N) continue;
+        float4 v;
+        unpack_f32x2(S[i][2 * k], v.x, v.y);
+        unpack_f32x2(S[i][2 * k + 1], v.z, v.w);
+        float* p = state + size_t(i) * c.N + n;
+        if (VECN) __stcs(reinterpret_cast<float4*>(p), v);
+        else {
+          p[0] = v.x;
+          if (n + 1 < c.N) p[1] = v.y;
+          if (n + 2 < c.N) p[2] = v.z;
+          if (n + 3 < c.N) p[3] = v.w;
+        }
+      }
+    }
+  };
+  if (r.keep == 0 && r.stores()) store();                    // a fresh request of which nothing is kept: zeros
+  if (upto == 0) return;
+
+  extern __shared__ __align__(16) float sm[];
+  const int xw = (a.p_block + 3) / 4 * 4, width = 2 * a.np + xw + 2;   // B | C | x | dt, decay
+  const int per = (width + 3) / 4 * 4, stage = per * STATE_TILE;
+  for (int i = tid; i < 2 * stage; i += blockDim.x) sm[i] = 0.f;       // (what lies behind N and P stays zero)
+  __syncthreads();
+  // fetches tokens first .. first + STATE_TILE - 1 of the request into a stage
+  auto fetch = [&](int first, int buf) {
+    const int count = min(STATE_TILE, upto - first);
+    float* dst = sm + buf * stage;
+    const float* rows = a.s.xbc + size_t(r.q0 + first) * a.s.pitch;
+    const int xn = min(a.p_block, c.P - p0);
+    if (VECN && c.P % 4 == 0) {
+      const int nv = c.N / 4, xv = xn / 4, all = 2 * nv + xv;
+      for (int i = tid; i < count * all; i += blockDim.x) {
+        const int row = i / all, e = i % all;
+        const int from = e < nv ? c.Di + g * c.N + 4 * e : e < 2 * nv ? c.Di + (c.G + g) * c.N + 4 * (e - nv) : h * c.P + p0 + 4 * (e - 2 * nv);
+        const int to = e < nv ? 4 * e : e < 2 * nv ? a.np + 4 * (e - nv) : 2 * a.np + 4 * (e - 2 * nv);
+        cp_async16(smem_u32(dst + row * per + to), rows + size_t(row) * a.s.pitch + from, true);
+      }
+    } else {
+      const int all = 2 * c.N + xn;
+      for (int i = tid; i < count * all; i += blockDim.x) {
+        const int row = i / all, e = i % all;
+        const int from = e < c.N ? c.Di + g * c.N + e : e < 2 * c.N ? c.Di + (c.G + g) * c.N + e - c.N : h * c.P + p0 + e - 2 * c.N;
+        const int to = e < c.N ? e : e < 2 * c.N ? a.np + e - c.N : 2 * a.np + e - 2 * c.N;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst + row * per + to)), "l"(rows + size_t(row) * a.s.pitch + from) : "memory");
+      }
+    }
+    if (tid < count)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst + tid * per + 2 * a.np + xw)),
+                   "l"(a.s.step + size_t(r.q0 + first + tid) * c.H + h) : "memory");
+    cp_async_commit();
+  };
+  // the row of the state whose output the lane finishes, and its place among the lanes that do
+  const int mine = l / DUP, dup = l % DUP, pm = pt + mine;
+  const TI* z = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * c.P + pm;
+  const float D = Y && pm < c.P ? c.Dskip[h] : 0.f;
+  fetch(0, 0);
+  for (int first = 0, buf = 0; first < upto; first += STATE_TILE, buf ^= 1) {
+    const int count = min(STATE_TILE, upto - first);
+    float gate[ROWS];
+    if (Y) {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const int row = i * DUP + dup;
+        gate[i] = row < count && pm < c.P ? to_f32(z[size_t(first + row) * c.ld_x]) : 0.f;
+      }
+    }
+    if (first + STATE_TILE < upto) fetch(first + STATE_TILE, buf ^ 1);
+    else cp_async_commit();
+    cp_async_wait<1>();
+    __syncthreads();
+    const float* rows = sm + buf * stage;
+#pragma unroll
+    for (int row = 0; row < STATE_TILE; ++row) {
+      if (row >= count) break;
+      const float* now = rows + row * per;
+      const float2 step = *reinterpret_cast<const float2*>(now + 2 * a.np + xw);
+      const uint64_t decay = pack_f32x2(step.y, step.y);
+      uint64_t xd[PR], y2[PR];
+      float x[PR];
+#pragma unroll
+      for (int i = 0; i < PR; ++i) {
+        x[i] = now[2 * a.np + (pt - p0) + i];
+        xd[i] = pack_f32x2(step.x * x[i], step.x * x[i]);
+        y2[i] = 0ull;
+      }
+#pragma unroll
+      for (int k = 0; k < NPT / 4; ++k) {
+        const ulonglong2 Bv = *reinterpret_cast<const ulonglong2*>(now + 4 * (l + L * k));
+        ulonglong2 Cv;
+        if (Y) Cv = *reinterpret_cast<const ulonglong2*>(now + a.np + 4 * (l + L * k));
+#pragma unroll
+        for (int i = 0; i < PR; ++i) {
+          S[i][2 * k] = fma_f32x2(decay, S[i][2 * k], mul_f32x2(xd[i], Bv.x));
+          S[i][2 * k + 1] = fma_f32x2(decay, S[i][2 * k + 1], mul_f32x2(xd[i], Bv.y));
+          if (Y) {
+            y2[i] = fma_f32x2(S[i][2 * k], Cv.x, y2[i]);
+            y2[i] = fma_f32x2(S[i][2 * k + 1], Cv.y, y2[i]);
+          }
+        }
+      }
+      if (Y) {
+        // the group's sums: every step hands half of the rows to the partner, until a lane has one
+        float v[PR];
+#pragma unroll
+        for (int i = 0; i < PR; ++i) {
+          float lo, hi;
+          unpack_f32x2(y2[i], lo, hi);
+          v[i] = lo + hi;
+        }
+#pragma unroll
+        for (int half = PR / 2, off = L / 2; off >= 1; off /= 2, half /= 2) {
+          if (half >= 1) {
+            const bool up = (l & off) != 0;
+#pragma unroll
+            for (int i = 0; i < PR / 2; ++i) {
+              if (i >= half) break;
+              const float got = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + half], off);
+              v[i] = (up ? v[i + half] : v[i]) + got;
+            }
+          } else {
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+          }
+        }
+        if (row % DUP == dup && pm < c.P) {
+          float xm = x[0];
+#pragma unroll
+          for (int i = 1; i < PR; ++i)
+            if (i == mine) xm = x[i];
+          const float zz = gate[row / DUP];
+          store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, xm, v[0]) * silu_f32(zz), c.status);
+        }
+      }
+      if (first + row + 1 == r.keep && r.stores()) store();
+    }
+    __syncthreads();
+  }
+}
+
+template <typename TI, int L, int PR, int NPT>
+cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
+  const ChunkScanCall& c = a.c;
+  int groups = STATE_THREADS / L;
+  while (groups * L > 32 && (groups / 2) * PR >= c.P) groups /= 2;
+  a.p_block = groups * PR;
+  a.p_blocks = (c.P + a.p_block - 1) / a.p_block;
+  a.np = (c.N + 3) / 4 * 4 > L * NPT ? (c.N + 3) / 4 * 4 : L * NPT;
+  const int per = (2 * a.np + (a.p_block + 3) / 4 * 4 + 2 + 3) / 4 * 4;
+  const size_t smem = size_t(2) * STATE_TILE * per * 4;
+  const bool vec = c.N % 4 == 0 && c.Di % 4 == 0;
+  const dim3 grid(unsigned(c.H * a.p_blocks), unsigned(c.B));
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(unsigned(groups * L)), smem, stream, a); };
+  if (c.y) return vec ? go(scan_state_kernel<TI, L, PR, NPT, true, true>) : go(scan_state_kernel<TI, L, PR, NPT, false, true>);
+  return vec ? go(scan_state_kernel<TI, L, PR, NPT, true, false>) : go(scan_state_kernel<TI, L, PR, NPT, false, false>);
+}
+
+template <typename TI>
+cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
+  const int N = a.c.N;
+  if (N <= 4) return launch_state<TI, 1, 1, 4>(a, stream);
+  if (N <= 16) return launch_state<TI, 1, 1, 16>(a, stream);
+  if (N <= 32) return launch_state<TI, 2, 2, 16>(a, stream);
+  if (N <= 64) return launch_state<TI, 4, 4, 16>(a, stream);
+  if (N <= 128) return launch_state<TI, 8, 4, 16>(a, stream);
+  return launch_state<TI, 16, 4, 16>(a, stream);
+}
+
+template <typename TI, int W, int K>
+cudaError_t launch_rows_k(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
+  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), 0, stream, a);
+}
+template <typename TI, int W>
+cudaError_t launch_rows_w(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
+  switch (a.c.d_conv) {
+    case 1: return launch_rows_k<TI, W, 1>(a, blocks, stream);
+    case 2: return launch_rows_k<TI, W, 2>(a, blocks, stream);
+    case 3: return launch_rows_k<TI, W, 3>(a, blocks, stream);
+    default: return launch_rows_k<TI, W, 4>(a, blocks, stream);
+  }
+}
+
+template <typename TI>
+cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
+  const ChunkScanCall& c = a.c;
+  // words of four row values, where all rows and both parts of a row start on their boundaries
+  auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(TI)) == 0; };
+  const bool wide = c.Di % 4 == 0 && c.d_xBC % 4 == 0 && c.ld_x % 4 == 0 && aligned(c.x) && aligned(c.conv_state);
+  a.ch_blocks = (c.d_xBC + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
+  a.dt_blocks = (CONV_TILE * c.H + CONV_THREADS - 1) / CONV_THREADS;
+  const long long blocks = (long long)(c.T / CONV_TILE + c.B) * (a.ch_blocks + a.dt_blocks);
+  if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
+  const cudaError_t e = wide ? launch_rows_w<TI, 4>(a, unsigned(blocks), stream) : launch_rows_w<TI, 1>(a, unsigned(blocks), stream);
+  if (e != cudaSuccess) return e;
+  StateArgs s{};
+  s.c = c;
+  s.s = a.s;
+  return launch_states<TI>(s, stream);
+}
+
+int scratch_pitch(int Di, int N, int G) { return (Di + 2 * G * N + 3) / 4 * 4; }
+
+}  // namespace
+
+size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) {
+  return (size_t(T) * scratch_pitch(Di, N, G) * 4 + 255) / 256 * 256 + size_t(T) * (Di / P) * 8 + 256;
+}
+
+cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
+  ConvArgs a{};
+  a.c = c;
+  a.s.pitch = scratch_pitch(c.Di, c.N, c.G);
+  a.s.xbc = reinterpret_cast<float*>(c.ws);
+  a.s.step = reinterpret_cast<float2*>(reinterpret_cast<char*>(c.ws) + (size_t(c.T) * a.s.pitch * 4 + 255) / 256 * 256);
+  if (c.in_dtype == CHUNK_F32) return launch_all<float>(a, stream);
+  return c.in_dtype == CHUNK_F16 ? launch_all<__half>(a, stream) : launch_all<__nv_bfloat16>(a, stream);
+}
+
+}  // namespace hspec

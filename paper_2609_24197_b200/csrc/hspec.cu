@@ -1113,4 +1113,73 @@ int hspec_op_verify(const void* target_logits, int32_t target_dtype, int64_t ld_
   return HSPEC_OK;
 }
 
+size_t hspec_chunk_scan_workspace_bytes(int32_t T, int32_t B, int32_t Di, int32_t P, int32_t N, int32_t G) {
+  return T < 0 || B < 1 || Di < 1 || P < 1 || N < 1 || G < 1 || Di % P ? 0 : chunk_scan_workspace_bytes(T, B, Di, P, N, G);
+}
+
+int hspec_op_chunk_scan(const void* zxbcdt, int32_t in_dtype, int64_t ld_in, const float* dt_raw, const float* conv_w, const float* conv_b,
+                        const float* dt_bias, const float* A_log, const float* Dskip, const int32_t* cu_q, int32_t B, const int32_t* slots,
+                        const int32_t* fresh, const int32_t* keep, int32_t keep_more, void* conv_state, float* ssm_state, int32_t num_slots, void* y,
+                        int32_t y_dtype, int64_t ld_y, int32_t T, int32_t Di, int32_t P, int32_t N, int32_t G, int32_t d_conv, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  const std::string who = "hspec_op_chunk_scan: ";
+  if ((!zxbcdt && T > 0) || !conv_w || !conv_b || !dt_bias || !A_log || !Dskip || !cu_q || !ssm_state || !workspace || B < 1 || T < 0 || num_slots < 1)
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
+  auto known = [](int32_t d) { return d == HSPEC_F32 || d == HSPEC_BF16 || d == HSPEC_F16; };
+  if (!known(in_dtype) || (y && !known(y_dtype))) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "rows must be fp32, bf16 or fp16");
+  if (Di < 1 || P < 1 || N < 1 || G < 1 || Di % P || (Di / P) % G) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "heads of P channels in G groups must fill Di");
+  if (N > 256) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 256 state elements a channel");
+  if (d_conv < 1 || d_conv > 4) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "the convolution must be 1 to 4 wide");
+  if (d_conv > 1 && !conv_state) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "a convolution needs its carried rows");
+  const int64_t d_xBC = int64_t(Di) + 2 * int64_t(G) * N;
+  if (d_xBC > 1 << 24) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "rows of more than 2^24 channels");
+  if (B > 65535) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 65535 requests");
+  if (ld_in < Di + d_xBC + (dt_raw ? 0 : Di / P) || (y && ld_y < Di)) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "row pitch too small");
+  if (reinterpret_cast<uintptr_t>(ssm_state) & 15) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the states must start on a 16-byte boundary");
+  if (workspace_bytes < chunk_scan_workspace_bytes(T, B, Di, P, N, G)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");
+  std::string errtxt;
+  ChunkScanCall c{};
+  c.x = zxbcdt; c.in_dtype = in_dtype; c.ld_x = ld_in; c.dt_raw = dt_raw; c.conv_w = conv_w; c.conv_b = conv_b; c.dt_bias = dt_bias; c.A_log = A_log;
+  c.Dskip = Dskip; c.cu_q = cu_q; c.slots = slots; c.fresh = fresh; c.keep = keep; c.keep_more = keep_more; c.conv_state = conv_state;
+  c.ssm_state = ssm_state; c.num_slots = num_slots; c.y = y; c.y_dtype = y_dtype; c.ld_y = ld_y; c.B = B; c.T = T; c.Di = Di; c.P = P; c.N = N;
+  c.G = G; c.H = Di / P; c.d_conv = d_conv; c.d_xBC = int(d_xBC); c.ws = workspace;
+  c.status = global_status();
+  if (!c.status) return fail(nullptr, HSPEC_ERR_CUDA, who + "cannot allocate the status word");
+  OP_TRY(chunk_scan_launch(c, reinterpret_cast<cudaStream_t>(stream)));
+  return HSPEC_OK;
+}
+
+int hspec_op_adjust_logits(const void* logits, int32_t in_dtype, int64_t ld_in, void* out, int32_t out_dtype, int64_t ld_out, int32_t T, int32_t V,
+                           const int32_t* cu_q, int32_t B, const int32_t* history, int32_t history_stride, const int32_t* history_lens,
+                           const int32_t* prompt_lens, const int32_t* drafts, int32_t k, const float* repetition, const float* frequency,
+                           const float* presence, const int32_t* bias_ids, const float* bias_values, const int32_t* bias_counts, int32_t n_bias,
+                           const uint32_t* mask, int32_t n_masks, int32_t mask_stride, const int32_t* mask_rows, void* stream) {
+  const std::string who = "hspec_op_adjust_logits: ";
+  if (T == 0) return HSPEC_OK;
+  if (!logits || !out || T < 0 || V < 1 || B < 1 || ld_in < V || ld_out < V || !bias_ids != !bias_values) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "bad argument");
+  auto known = [](int32_t d) { return d == HSPEC_F32 || d == HSPEC_BF16 || d == HSPEC_F16; };
+  if (!known(in_dtype) || (out_dtype != in_dtype && out_dtype != HSPEC_F32))
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "logits must be fp32, bf16 or fp16, and the result of their type or fp32");
+  const size_t item = in_dtype == HSPEC_F32 ? 4 : 2, out_item = out_dtype == HSPEC_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(logits) % item || reinterpret_cast<uintptr_t>(out) % out_item) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "misaligned logits");
+  if (logits == out && (in_dtype != out_dtype || ld_in != ld_out)) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "in place the type and the row pitch are one");
+  if (!cu_q && B != T) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "without cu_q every request has one row");
+  if ((history && history_stride < 1) || (drafts && k < 1) || (bias_ids && n_bias < 1) || (mask && (n_masks < 1 || mask_stride < (V - 1) / 32 + 1)))
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "a rule's array is too small");
+  if (int64_t(history ? history_stride : 0) + (drafts ? k : 0) > (1 << 20) - 1) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 2^20 - 1 tokens in a text");
+  if (bias_ids && n_bias > 1024) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 1024 biases for a request");
+  if (V > 1 << 30) return fail(nullptr, HSPEC_ERR_BAD_SHAPE, who + "more than 2^30 tokens");
+  std::string errtxt;
+  LogitsCall c{};
+  c.in = logits; c.in_dtype = in_dtype; c.ld_in = ld_in; c.out = out; c.out_dtype = out_dtype; c.ld_out = ld_out; c.T = T; c.V = V; c.cu_q = cu_q; c.B = B;
+  c.history = history; c.history_stride = history_stride; c.history_lens = history_lens; c.prompt_lens = prompt_lens; c.drafts = drafts; c.k = k;
+  c.repetition = repetition; c.frequency = frequency; c.presence = presence; c.bias_ids = bias_ids; c.bias_values = bias_values;
+  c.bias_counts = bias_counts; c.n_bias = n_bias; c.mask = mask; c.n_masks = n_masks; c.mask_stride = mask_stride; c.mask_rows = mask_rows;
+  c.status = global_status();
+  if (!c.status) return fail(nullptr, HSPEC_ERR_CUDA, who + "cannot allocate the status word");
+  OP_TRY(adjust_logits_launch(c, reinterpret_cast<cudaStream_t>(stream)));
+  return HSPEC_OK;
+}
+
 }  // extern "C"

@@ -317,6 +317,41 @@ bool chunk_few_takes(const ChunkAttnCall& c);
 bool chunk_few_takes_all(const ChunkAttnCall& c);
 size_t chunk_few_workspace_bytes(int dh);
 cudaError_t chunk_few_launch(const ChunkAttnCall& c, void* ws, cudaStream_t stream);
+struct ChunkScanCall {              // chunk_scan.cu
+  const void* x; int in_dtype; long long ld_x;          // [T, z | x | B | C (| dt)]
+  const float* dt_raw;                                  // [T, H] or null: the row's last H values
+  const float *conv_w, *conv_b, *dt_bias, *A_log, *Dskip;
+  const int32_t *cu_q, *slots, *fresh, *keep;           // [B + 1]; [B] or null each: slot b, none fresh, all rows kept
+  int keep_more;
+  void* conv_state;                                     // [num_slots, d_conv - 1, d_xBC] of the rows' type
+  float* ssm_state;                                     // [num_slots, H, P, N]
+  int num_slots;
+  void* y; int y_dtype; long long ld_y;                 // [T, Di] or null: only the states
+  int B, T, Di, P, N, G, H, d_conv, d_xBC;
+  void* ws;
+  uint32_t* status;
+};
+size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G);
+cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream);
+struct LogitsCall {                 // logits.cu
+  const void* in; int in_dtype; long long ld_in;        // [T, V]
+  void* out; int out_dtype; long long ld_out;           // [T, V]; `in` itself, or apart from it
+  const int32_t* cu_q;                                  // [B + 1] or null: a row each
+  const int32_t *history, *history_lens, *prompt_lens;  // [B, history_stride], [B] or null (all of it), [B] or null (none of it)
+  int history_stride;
+  const int32_t* drafts;                                // [B, k] or null
+  int k;
+  const float *repetition, *frequency, *presence;       // [B] or null each
+  const int32_t *bias_ids, *bias_counts;                // [B, n_bias] or null, [B] or null (all of them)
+  const float* bias_values;
+  int n_bias;
+  const uint32_t* mask;                                 // [n_masks, mask_stride] or null
+  int n_masks, mask_stride;
+  const int32_t* mask_rows;                             // [T] or null: row t has mask t
+  int B, T, V;
+  uint32_t* status;
+};
+cudaError_t adjust_logits_launch(const LogitsCall& c, cudaStream_t stream);
 struct VerifyCall {                 // verify.cu
   const void* target; int t_dtype; long long ld_t;      // [T, V]
   const void* draft; int d_dtype; long long ld_d;       // [B * k, Vd] or null: the arg-max drafter
