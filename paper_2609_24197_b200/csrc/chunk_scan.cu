@@ -20,16 +20,116 @@ constexpr int CONV_THREADS = 256;
 constexpr int CONV_TILE = 8;         // rows of a block
 
 struct ScanScratch {
-  float* xbc;                        // [T, pitch] convolved rows
-  float2* step;                      // [T, H] dt and the decay exp(dt A)
+  float* xbc;                        // [.., pitch] convolved rows
+  float2* step;                      // [.., H] dt and the decay exp(dt A)
   int pitch;
+  int few;                           // requests with more rows than this go another way
+  int apart;                         // 0: row t of the chunk lies at t; else row i of request b at b * apart + i
+  __device__ __forceinline__ size_t row(int b, int q0, int i) const { return apart ? size_t(b) * apart + i : size_t(q0) + i; }
 };
 
 struct ConvArgs {
   ChunkScanCall c;
   ScanScratch s;
   int ch_blocks, dt_blocks;          // blocks of an item: channels, then steps
+  int32_t *plan, *list, *chunks;     // of the requests with many rows (LongArgs); null: there are none
+  int max_long, max_chunks;
 };
+
+// Item `item`: CONV_TILE rows of a request that has few (one item at least, for what its carried rows need).  One warp.
+__device__ __forceinline__ ChunkItem few_item(const ChunkScanCall& c, int few, int item, int lane) {
+  int before = 0;
+  for (int base = 0; base < c.B; base += 32) {
+    int items = 0, q0 = 0, n = 0;
+    if (base + lane < c.B) {
+      const ScanRequest r = scan_request(c, base + lane);
+      q0 = r.q0;
+      n = scan_upto(c, r);
+      items = n > few ? 0 : max((n + CONV_TILE - 1) / CONV_TILE, 1);
+    }
+    int upto = items;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += up;
+    }
+    const uint32_t mine = __ballot_sync(0xffffffffu, before + upto > item);
+    if (mine) {
+      const int l = __ffs(mine) - 1;
+      return {base + l, __shfl_sync(0xffffffffu, q0, l), __shfl_sync(0xffffffffu, n, l), (item - before - __shfl_sync(0xffffffffu, upto - items, l)) * CONV_TILE};
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return {-1, 0, 0, 0};
+}
+
+// The requests with many rows: a list, longest first, and their chunks in the order of the requests.  One block.
+constexpr int PLAN_SORT = 1024;
+__device__ __forceinline__ int chunks_of(const ChunkScanCall& c, const ScanRequest& r) {
+  const int upto = scan_upto(c, r), k = min(r.keep, upto);
+  return (k + SCAN_CHUNK - 1) / SCAN_CHUNK + (upto - k + SCAN_CHUNK - 1) / SCAN_CHUNK;
+}
+__device__ void plan_long(const ConvArgs& a) {
+  const ChunkScanCall& c = a.c;
+  __shared__ int key[PLAN_SORT], who[PLAN_SORT], front[PLAN_SORT];
+  __shared__ int sums[2][CONV_THREADS / 32], totals[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int n_long = 0, n_chunks = 0;
+  bool full = false;
+  for (int base = 0; base < c.B; base += CONV_THREADS) {
+    const int b = base + tid;
+    int upto = 0, count = 0;
+    if (b < c.B) {
+      const ScanRequest r = scan_request(c, b);
+      upto = scan_upto(c, r);
+      if (upto > a.s.few) count = chunks_of(c, r);
+    }
+    const int one = count > 0 ? 1 : 0;
+    int i1 = one, i2 = count;                                // sums up to and with this request
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int u1 = __shfl_up_sync(0xffffffffu, i1, off), u2 = __shfl_up_sync(0xffffffffu, i2, off);
+      if (lane >= off) { i1 += u1; i2 += u2; }
+    }
+    if (lane == 31) { sums[0][warp] = i1; sums[1][warp] = i2; }
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) { i1 += sums[0][w]; i2 += sums[1][w]; }
+    i1 += n_long;
+    i2 += n_chunks;
+    // (offsets that do not ascend could ask for more than there is room for: these requests are left out, and counted)
+    const bool fits = i1 <= a.max_long && i2 <= a.max_chunks && !full;
+    if (one && !fits) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+    if (one && fits) {
+      const int at = i1 - 1, first = i2 - count;
+      if (at < PLAN_SORT) { key[at] = upto; who[at] = b; front[at] = first; }
+      a.list[2 * at] = b;
+      a.list[2 * at + 1] = first;
+      for (int j = 0; j < count; ++j) {
+        a.chunks[2 * (first + j)] = b;
+        a.chunks[2 * (first + j) + 1] = j;
+      }
+    }
+    // the last one that fits ends the sums
+    if (tid == 0) { totals[0] = n_long; totals[1] = n_chunks; }
+    __syncthreads();
+    if (fits) { atomicMax(&totals[0], i1); atomicMax(&totals[1], i2); }
+    full = __syncthreads_or(one && !fits) || full;
+    n_long = totals[0];
+    n_chunks = totals[1];
+    __syncthreads();
+  }
+  if (n_long <= PLAN_SORT)
+    for (int i = tid; i < n_long; i += CONV_THREADS) {
+      int rank = 0;
+      for (int j = 0; j < n_long; ++j) rank += key[j] > key[i] || (key[j] == key[i] && j < i);
+      a.list[2 * rank] = who[i];
+      a.list[2 * rank + 1] = front[i];
+    }
+  if (tid == 0) {
+    a.plan[0] = n_long;
+    a.plan[1] = n_chunks;
+  }
+}
 
 // A word of W row values, widened.
 template <typename T, int W>
@@ -44,10 +144,20 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
   const ChunkScanCall& c = a.c;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = blockIdx.x % blocks;
-  const ChunkItem item = chunk_item(c.cu_q, c.B, c.T, CONV_TILE, 1, blockIdx.x / blocks, tid & 31);
+  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1) % blocks;
+  if (blockIdx.x == 0) {
+    for (int b = tid; b < c.B; b += CONV_THREADS) {
+      const ScanRequest r = scan_request(c, b);
+      if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], INT_MAX, c.T, INT_MAX) || (r.n > 0 && r.slot != (c.slots ? c.slots[b] : b)))
+        atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+    }
+    if (a.plan) plan_long(a);
+    return;
+  }
+  const ChunkItem item = few_item(c, a.s.few, (blockIdx.x - 1) / blocks, tid & 31);
   if (item.b < 0) return;
   const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
+  const size_t out0 = a.s.row(item.b, item.q0, item.first);
   if (part >= a.ch_blocks) {
     // ---- steps and decays
     const int i = (part - a.ch_blocks) * CONV_THREADS + tid, h = i % c.H, r = i / c.H;
@@ -55,16 +165,11 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
       const size_t t = t0 + r;
       const float raw = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
       const float dt = softplus_f32(raw + c.dt_bias[h]);
-      a.s.step[t * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
+      a.s.step[(out0 + r) * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
     }
     return;
   }
   const ScanRequest r = scan_request(c, item.b);
-  if (part == 0 && item.first == 0 && tid == 0) {
-    const int slot = c.slots ? c.slots[item.b] : item.b;
-    if (chunk_request_bad(c.cu_q[item.b], c.cu_q[item.b + 1], INT_MAX, c.T, INT_MAX) || (item.n > 0 && r.slot != slot))
-      atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-  }
   const int ch = (part * CONV_THREADS + tid) * W;
   if (ch >= c.d_xBC) return;
   float w[K][W], bias[W], raw[K - 1 + CONV_TILE][W];
@@ -120,7 +225,7 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
       for (int j = 0; j < K; ++j) v = fmaf(w[j][e], raw[i + j][e], v);
       out.v[e] = silu_f32(v);
     }
-    *reinterpret_cast<Word<float, W>*>(a.s.xbc + size_t(t0 + i) * a.s.pitch + ch) = out;
+    *reinterpret_cast<Word<float, W>*>(a.s.xbc + (out0 + i) * a.s.pitch + ch) = out;
   }
 }
 
@@ -146,7 +251,8 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   const int p0 = (blockIdx.x % a.p_blocks) * a.p_block, pt = p0 + tid / L * PR;      // the block's and the thread's first rows
   // (before the wait only what is at least two kernels back is read: the arrays that describe the chunk, and the states)
   const ScanRequest r = scan_request(c, b);
-  const int upto = Y ? r.n : r.keep;
+  const int upto = scan_upto(c, r);
+  if (upto > a.s.few) { pdl_wait(); return; }
   uint64_t S[PR][NPT / 2];
   float* state = c.ssm_state + ((size_t(r.slot < 0 ? 0 : r.slot) * c.H + h) * c.P + pt) * c.N;
 #pragma unroll
@@ -196,6 +302,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   if (r.keep == 0 && r.stores()) store();                    // a fresh request of which nothing is kept: zeros
   if (upto == 0) return;
 
+  const size_t at0 = a.s.row(b, r.q0, 0);
   extern __shared__ __align__(16) float sm[];
   const int xw = (a.p_block + 3) / 4 * 4, width = 2 * a.np + xw + 2;   // B | C | x | dt, decay
   const int per = (width + 3) / 4 * 4, stage = per * STATE_TILE;
@@ -205,7 +312,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   auto fetch = [&](int first, int buf) {
     const int count = min(STATE_TILE, upto - first);
     float* dst = sm + buf * stage;
-    const float* rows = a.s.xbc + size_t(r.q0 + first) * a.s.pitch;
+    const float* rows = a.s.xbc + (at0 + first) * a.s.pitch;
     const int xn = min(a.p_block, c.P - p0);
     if (VECN && c.P % 4 == 0) {
       const int nv = c.N / 4, xv = xn / 4, all = 2 * nv + xv;
@@ -226,7 +333,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     }
     if (tid < count)
       asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst + tid * per + 2 * a.np + xw)),
-                   "l"(a.s.step + size_t(r.q0 + first + tid) * c.H + h) : "memory");
+                   "l"(a.s.step + (at0 + first + tid) * c.H + h) : "memory");
     cp_async_commit();
   };
   // the row of the state whose output the lane finishes, and its place among the lanes that do
@@ -366,7 +473,9 @@ cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   const bool wide = c.Di % 4 == 0 && c.d_xBC % 4 == 0 && c.ld_x % 4 == 0 && aligned(c.x) && aligned(c.conv_state);
   a.ch_blocks = (c.d_xBC + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
   a.dt_blocks = (CONV_TILE * c.H + CONV_THREADS - 1) / CONV_THREADS;
-  const long long blocks = (long long)(c.T / CONV_TILE + c.B) * (a.ch_blocks + a.dt_blocks);
+  long long items = c.T / CONV_TILE + c.B;
+  if (a.plan && items > (long long)(c.B) * (SCAN_FEW / CONV_TILE)) items = (long long)(c.B) * (SCAN_FEW / CONV_TILE);
+  const long long blocks = 1 + items * (a.ch_blocks + a.dt_blocks);
   if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
   const cudaError_t e = wide ? launch_rows_w<TI, 4>(a, unsigned(blocks), stream) : launch_rows_w<TI, 1>(a, unsigned(blocks), stream);
   if (e != cudaSuccess) return e;
@@ -376,22 +485,55 @@ cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   return launch_states<TI>(s, stream);
 }
 
-int scratch_pitch(int Di, int N, int G) { return (Di + 2 * G * N + 3) / 4 * 4; }
+// Where everything lies in the caller's scratch.
+struct Scratch {
+  size_t step, plan, list, chunks, images, total;
+  int pitch;
+  bool tensor;                       // requests with many rows go through the tensor cores
+  Scratch(long long T, int B, int Di, int P, int N, int G) {
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    pitch = (Di + 2 * G * N + 3) / 4 * 4;
+    tensor = P == 64 && N == 128 && T > SCAN_FEW;
+    const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
+    step = up(rows * pitch * 4);
+    plan = step + up(rows * (Di / P) * 8);
+    list = plan + 256;
+    chunks = list + (tensor ? up(size_t(scan_max_long(T, B)) * 8) : 0);
+    images = chunks + (tensor ? up(size_t(scan_max_chunks(T, B)) * 8) : 0);
+    total = images + (tensor ? size_t(scan_max_chunks(T, B)) * G * SCAN_IMAGE_BYTES : 0);
+  }
+};
 
 }  // namespace
 
-size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) {
-  return (size_t(T) * scratch_pitch(Di, N, G) * 4 + 255) / 256 * 256 + size_t(T) * (Di / P) * 8 + 256;
-}
+size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) { return Scratch(T, B, Di, P, N, G).total; }
 
 cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
+  const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G);
+  char* ws = reinterpret_cast<char*>(c.ws);
   ConvArgs a{};
   a.c = c;
-  a.s.pitch = scratch_pitch(c.Di, c.N, c.G);
-  a.s.xbc = reinterpret_cast<float*>(c.ws);
-  a.s.step = reinterpret_cast<float2*>(reinterpret_cast<char*>(c.ws) + (size_t(c.T) * a.s.pitch * 4 + 255) / 256 * 256);
-  if (c.in_dtype == CHUNK_F32) return launch_all<float>(a, stream);
-  return c.in_dtype == CHUNK_F16 ? launch_all<__half>(a, stream) : launch_all<__nv_bfloat16>(a, stream);
+  a.s.pitch = at.pitch;
+  a.s.xbc = reinterpret_cast<float*>(ws);
+  a.s.step = reinterpret_cast<float2*>(ws + at.step);
+  a.s.few = INT_MAX;
+  if (at.tensor) {
+    a.s.few = SCAN_FEW;
+    a.s.apart = c.T > (long long)(SCAN_FEW) * c.B ? SCAN_FEW : 0;
+    a.plan = reinterpret_cast<int32_t*>(ws + at.plan);
+    a.list = reinterpret_cast<int32_t*>(ws + at.list);
+    a.chunks = reinterpret_cast<int32_t*>(ws + at.chunks);
+    a.max_long = int(scan_max_long(c.T, c.B));
+    a.max_chunks = int(scan_max_chunks(c.T, c.B));
+  }
+  const cudaError_t e = c.in_dtype == CHUNK_F32 ? launch_all<float>(a, stream) : c.in_dtype == CHUNK_F16 ? launch_all<__half>(a, stream)
+                                                                                                         : launch_all<__nv_bfloat16>(a, stream);
+  if (e != cudaSuccess || !at.tensor) return e;
+  LongArgs l{};
+  l.c = c;
+  l.plan = a.plan; l.list = a.list; l.chunks = a.chunks;
+  l.images = reinterpret_cast<uint8_t*>(ws + at.images);
+  return scan_long_launch(l, stream);
 }
 
 }  // namespace hspec

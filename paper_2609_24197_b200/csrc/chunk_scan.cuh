@@ -19,6 +19,24 @@ __device__ __forceinline__ ScanRequest scan_request(const ChunkScanCall& c, int 
   return r;
 }
 
+// rows that have to be gone through: all of them for outputs, the kept ones for the states alone
+__device__ __forceinline__ int scan_upto(const ChunkScanCall& c, const ScanRequest& r) { return c.y ? r.n : r.keep; }
+
+// Requests with more than SCAN_FEW such rows go through the tensor cores in chunks of SCAN_CHUNK rows (chunk_scan_tc.cu), where the shape allows it.
+constexpr int SCAN_FEW = 32, SCAN_CHUNK = 128, SCAN_IMAGE_BYTES = 131072 + 40960;
+struct LongArgs {
+  ChunkScanCall c;
+  const int32_t* plan;               // [0] requests with many rows, [1] their chunks
+  const int32_t* list;               // [.., 2] request and its first chunk, longest requests first
+  const int32_t* chunks;             // [.., 2] request and the chunk's index in it
+  uint8_t* images;
+  int vec, y_vec;                    // rows start on the boundaries of four values; of 16 bytes
+};
+inline long long scan_max_long(long long T, int B) { return T / (SCAN_FEW + 1) < B ? T / (SCAN_FEW + 1) : B; }
+// (a request's chunks end where its kept rows do: up to two of them are not full)
+inline long long scan_max_chunks(long long T, int B) { return T / SCAN_CHUNK + 2 * scan_max_long(T, B); }
+cudaError_t scan_long_launch(const LongArgs& a, cudaStream_t stream);
+
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
