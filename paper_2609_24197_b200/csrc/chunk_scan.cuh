@@ -30,7 +30,7 @@ struct LongArgs {
   const int32_t* list;               // [.., 2] request and its first chunk, longest requests first
   const int32_t* chunks;             // [.., 2] request and the chunk's index in it
   uint8_t* images;
-  int vec, y_vec;                    // rows start on the boundaries of four values; of 16 bytes
+  int y_vec, z_vec;                  // rows of y, and of x, start on 32-byte boundaries
 };
 inline long long scan_max_long(long long T, int B) { return T / (SCAN_FEW + 1) < B ? T / (SCAN_FEW + 1) : B; }
 // (a request's chunks end where its kept rows do: up to two of them are not full)

@@ -16,6 +16,7 @@
 
 #include <atomic>
 #include <climits>
+#include <cstddef>
 
 namespace hspec {
 
@@ -51,46 +52,95 @@ __device__ __forceinline__ int chunk_count(int keep, int upto) {
   return (k + Q - 1) / Q + (upto - k + Q - 1) / Q;
 }
 
-// v = head + remainder, both bf16, for two values; packed with the first in the low half
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+template <bool VEC, int N, typename TI>
+__device__ __forceinline__ Word<TI, N> load_word(const TI* p) {
+  Word<TI, N> w;
+  if (VEC) w = *reinterpret_cast<const Word<TI, N>*>(p);
+  else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) w.v[e] = p[e];
+  }
+  return w;
+}
+
+// Two values at a time.
+__device__ __forceinline__ uint64_t dup2(float v) { return pack_f32x2(v, v); }
+__device__ __forceinline__ uint64_t silu2(uint64_t v) {
+  float a, b;
+  unpack_f32x2(mul_f32x2(v, dup2(-1.4426950408889634f)), a, b);
+  unpack_f32x2(add_f32x2(pack_f32x2(ex2_ftz(a), ex2_ftz(b)), dup2(1.f)), a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return mul_f32x2(v, pack_f32x2(a, b));
+}
+// v = head + remainder, both bf16; packed with the first value in the low half
+__device__ __forceinline__ void split2(uint64_t v, uint32_t& hi, uint32_t& lo) {
+  float a, b;
+  unpack_f32x2(v, a, b);
   hi = pack_bf16(a, b);
-  const float ra = a - __uint_as_float(hi << 16), rb = b - __uint_as_float(hi & 0xffff0000u);
-  lo = pack_bf16(ra, rb);
+  unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), dup2(-1.f), v), a, b);
+  lo = pack_bf16(a, b);
+}
+template <typename TI, int N>
+__device__ __forceinline__ void widen(const Word<TI, N>& w, uint64_t (&v)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) v[i] = pack_f32x2(to_f32(w.v[2 * i]), to_f32(w.v[2 * i + 1]));
 }
 
-// Row i of the request (raw, four channels from ch on); below zero a carried one, or nothing.
-template <typename TI>
-__device__ __forceinline__ void raw4(const LongArgs& a, const ScanRequest& r, int ch, int i, int end, float (&x)[4]) {
-  const ChunkScanCall& c = a.c;
-  const TI* p = nullptr;
-  if (i >= 0) {
-    if (i < end) p = reinterpret_cast<const TI*>(c.x) + size_t(r.q0 + i) * c.ld_x + c.Di + ch;
-  } else if (!r.fresh && i + c.d_conv - 1 >= 0) {
-    p = reinterpret_cast<const TI*>(c.conv_state) + (size_t(r.slot) * (c.d_conv - 1) + i + c.d_conv - 1) * c.d_xBC + ch;
+// N raw channels (from `ch` on) of a request's rows; below row zero the carried ones, or nothing.  Addresses are chosen and no loads skipped, so
+// that those of several rows are under way together.
+template <bool VEC, int N, typename TI>
+struct RawRows {
+  const TI* x;                       // the request's first row
+  const TI* carried;                 // row -(d_conv - 1); null: nothing is carried
+  long long ld;
+  int d_xBC, K1;
+  __device__ __forceinline__ RawRows(const LongArgs& a, const ScanRequest& r, int ch)
+      : x(reinterpret_cast<const TI*>(a.c.x) + size_t(r.q0) * a.c.ld_x + a.c.Di + ch),
+        carried(r.fresh || a.c.d_conv == 1 ? nullptr : reinterpret_cast<const TI*>(a.c.conv_state) + size_t(r.slot) * (a.c.d_conv - 1) * a.c.d_xBC + ch),
+        ld(a.c.ld_x), d_xBC(a.c.d_xBC), K1(a.c.d_conv - 1) {}
+  // row i; behind `last` row `last` again
+  __device__ __forceinline__ Word<TI, N> row(int i, int last) const { return load_word<VEC, N>(x + size_t(min(i, last)) * ld); }
+  // rows i - 3 .. i - 1 (front_value: those that are not there are zero)
+  __device__ __forceinline__ void front(Word<TI, N> (&w)[3], int i, int last) const {
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      const int row = i - 3 + j;
+      w[j] = load_word<VEC, N>(row < 0 && there(row) ? carried + size_t(row + K1) * d_xBC : x + size_t(max(min(row, last), 0)) * ld);
+    }
   }
-  if (!p) {
+  __device__ __forceinline__ bool there(int row) const { return row >= 0 || (carried && row + K1 >= 0); }
+  __device__ __forceinline__ void front_value(const Word<TI, N> (&w)[3], int i, uint64_t (&before)[3][N / 2]) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = 0.f;
-  } else if (a.vec) {
-    const Word<TI, 4> w = *reinterpret_cast<const Word<TI, 4>*>(p);
+    for (int j = 0; j < 3; ++j) {
+      widen(w[j], before[j]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = to_f32(w.v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = to_f32(p[e]);
+      for (int h = 0; h < N / 2; ++h)
+        if (!there(i - 3 + j)) before[j][h] = 0ull;
+    }
   }
-}
+};
 
-// Weights of four channels: taps in front of a narrower convolution are zero.
+// The convolution of 2 H channels: taps in front of a narrower one are zero.
+template <int H>
 struct Taps {
-  float w[4][4], b[4];               // [tap][channel]
+  uint64_t w[4][H], b[H];            // [tap][channels]
   __device__ __forceinline__ void load(const ChunkScanCall& c, int ch) {
     const int K = c.d_conv;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      b[e] = c.conv_b[ch + e];
+    for (int h = 0; h < H; ++h) {
+      const float* f = c.conv_w + size_t(ch + 2 * h) * K;
+      b[h] = pack_f32x2(c.conv_b[ch + 2 * h], c.conv_b[ch + 2 * h + 1]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j][e] = j >= 4 - K ? c.conv_w[size_t(ch + e) * K + j - (4 - K)] : 0.f;
+      for (int j = 0; j < 4; ++j) w[j][h] = j >= 4 - K ? pack_f32x2(f[j - (4 - K)], f[j - (4 - K) + K]) : 0ull;
+    }
+  }
+  // SiLU of the convolution at the row behind `before` (oldest first), which moves on by that row
+  __device__ __forceinline__ void next(uint64_t (&before)[3][H], const uint64_t (&now)[H], uint64_t (&v)[H]) const {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      v[h] = silu2(fma_f32x2(w[3][h], now[h], fma_f32x2(w[2][h], before[2][h], fma_f32x2(w[1][h], before[1][h], fma_f32x2(w[0][h], before[0][h], b[h])))));
+      before[0][h] = before[1][h]; before[1][h] = before[2][h]; before[2][h] = now[h];
     }
   }
 };
@@ -98,7 +148,7 @@ struct Taps {
 constexpr int PREP_PITCH = NS + 8;   // bf16 of a staged row: the rows of an ldmatrix spread over the banks
 constexpr int PREP_SMEM = 4 * Q * PREP_PITCH * 2;
 
-template <typename TI>
+template <typename TI, bool VEC>
 __global__ void __launch_bounds__(256) scan_prep_kernel(LongArgs a) {
   const ChunkScanCall& c = a.c;
   pdl_wait();
@@ -117,29 +167,33 @@ __global__ void __launch_bounds__(256) scan_prep_kernel(LongArgs a) {
       const int cg = tid & 63, first = (tid >> 6) * 32;
       const bool isC = cg >= 32;
       const int n = (cg & 31) * 4, ch = c.Di + ((isC ? c.G : 0) + g) * NS + n, end = range.start + range.len;
-      Taps t;
+      Taps<2> t;
       t.load(c, ch);
-      float w0[4], w1[4], w2[4];
-      raw4<TI>(a, r, ch, range.start + first - 3, end, w0);
-      raw4<TI>(a, r, ch, range.start + first - 2, end, w1);
-      raw4<TI>(a, r, ch, range.start + first - 1, end, w2);
-      for (int i0 = 0; i0 < 32; i0 += 8) {
-        float x[8][4];
+      const RawRows<VEC, 4, TI> raw(a, r, ch);
+      Word<TI, 4> next[8], front[3];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) raw4<TI>(a, r, ch, range.start + first + i0 + i, end, x[i]);
+      for (int i = 0; i < 8; ++i) next[i] = raw.row(range.start + first + i, end - 1);
+      raw.front(front, range.start + first, end - 1);
+      uint64_t before[3][2];
+      raw.front_value(front, range.start + first, before);
+      for (int i0 = 0; i0 < 32; i0 += 8) {
+        Word<TI, 4> x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = next[i];
+        if (i0 < 24) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) next[i] = raw.row(range.start + first + i0 + 8 + i, end - 1);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int row = first + i0 + i;
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float s = fmaf(t.w[3][e], x[i][e], fmaf(t.w[2][e], w2[e], fmaf(t.w[1][e], w1[e], fmaf(t.w[0][e], w0[e], t.b[e]))));
-            v[e] = row < range.len ? silu_f32(s) : 0.f;
-            w0[e] = w1[e]; w1[e] = w2[e]; w2[e] = x[i][e];
-          }
+          uint64_t now[2], v[2];
+          widen(x[i], now);
+          t.next(before, now, v);
+          if (row >= range.len) v[0] = v[1] = 0ull;
           uint2 hi, lo;
-          split2(v[0], v[1], hi.x, lo.x);
-          split2(v[2], v[3], hi.y, lo.y);
+          split2(v[0], hi.x, lo.x);
+          split2(v[1], hi.y, lo.y);
           uint16_t* s = staged + (isC ? 2 : 0) * Q * PREP_PITCH + row * PREP_PITCH + n;
           *reinterpret_cast<uint2*>(s) = hi;
           *reinterpret_cast<uint2*>(s + Q * PREP_PITCH) = lo;
@@ -198,8 +252,13 @@ __global__ void __launch_bounds__(256) scan_prep_kernel(LongArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------
-constexpr int LONG_THREADS = 640;    // four warps for control, then scores, x, state and outputs
-constexpr int SM_B = 0, SM_X = 65536, SM_XW = SM_X + 32768, SM_S = SM_XW + 32768, SM_STEPS = SM_S + 32768;    // head, remainder each
+// All warps go through a chunk's work together, two block barriers a chunk: what the products need (x split and the scores into place), then, under the
+// products, what can be done ahead (the next chunk's convolution and steps, this one's gates), then what the products gave (outputs, state).  (With a
+// role for every four to eight warps and barriers in shared memory between them a chunk took 16 thousand clocks: a warp alone on its scheduler runs at its
+// instructions' latency, and those that wait take the others' issue slots with their polling.)
+constexpr int LONG_THREADS = 512;
+constexpr int SM_B = 0, SM_X = 65536, SM_XW = SM_X + 32768, SM_S = SM_XW + 32768;    // head, remainder each
+constexpr int SM_G = SM_S + 32768, SM_STEPS = SM_G + IMG_BYTES - IMG_G;
 struct LongSteps {
   float n_hi[Q], n_lo[Q];            // log2 of dt_s e^{-c_s}, in two parts
   float c_hi[Q], c_lo[Q];            // log2 of e^{c_t}
@@ -209,35 +268,27 @@ struct LongSteps {
   float pad[31];
 };
 struct __align__(8) LongBars {
-  uint64_t b_full, x_full, c_full, g_full, s_full;           // operands in place
-  uint64_t m_state, m_next, m_near;                          // products done: with the state, of the next state, inside the chunk
-  uint64_t next_free, out_free;                              // their results read
-  uint64_t x_read;                                           // the carried rows read
-  uint64_t steps_full[2], steps_free[2];
+  uint64_t b_full, scores_full;      // copies landed
+  uint64_t products;                 // done
+  double sums[4];                    // of 32 steps each
   uint32_t tmem;
-  uint32_t stop;
+  uint32_t stop;                     // a wait gave up
+  int any_odd[2], first_odd[2][NH];  // of a chunk (by its parity): whether x is finite, each channel's first row where not
 };
 constexpr int LONG_SMEM = SM_STEPS + 2 * int(sizeof(LongSteps)) + int(sizeof(LongBars));
 // tensor memory, columns
 constexpr uint32_t TM_C = 0, TM_G = 128, TM_NEAR = 256, TM_STATE = 320, TM_NEXT = 384;
 
-// Waits with a limit of about two seconds; false ends the block's work (the status word says so).
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, LongBars* bars, uint32_t* status, uint32_t code) {
+// Waits for a phase, with a limit (four million polls, some 0.1 to 4 s), after which the block's work ends (the status word says so).
+__device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, LongBars* bars, uint32_t* status, uint32_t code) {
   const uint32_t at = smem_u32(bar);
-  uint64_t t0 = 0;
-  for (uint32_t i = 0;; ++i) {
-    if (mbar_try_wait(at, parity)) return true;
-    if ((i & 255u) == 255u) {
-      if (*reinterpret_cast<volatile uint32_t*>(&bars->stop)) return false;
-      const uint64_t now = global_timer_ns();
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > 2000000000ull) {
-        atomicExch(status, code);
-        *reinterpret_cast<volatile uint32_t*>(&bars->stop) = 1;
-        return false;
-      }
+  uint32_t left = 1u << 22;
+  while (!mbar_try_wait(at, parity))
+    if (--left == 0) {
+      atomicExch(status, code);
+      *reinterpret_cast<volatile uint32_t*>(&bars->stop) = 1;
+      return;
     }
-  }
 }
 
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {             // rows of 64 values, 16-byte pieces exchanged; halves of 64 16 KB apart
@@ -249,31 +300,42 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {             // rows
   d |= uint64_t(2) << 61;
   return d;
 }
-// fp32 results, bf16 operands, 128 x 64; B (and A, where it is in shared memory) with its rows along the terms
-__device__ __forceinline__ constexpr uint32_t long_idesc(bool a_rows) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((a_rows ? 1u : 0u) << 15) | (1u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+// fp32 results, bf16 operands, 128 x n; B (and A, where it is in shared memory) with its rows along the terms
+__device__ __forceinline__ constexpr uint32_t long_idesc(bool a_rows, uint32_t n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((a_rows ? 1u : 0u) << 15) | (1u << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
+// Shared memory by its own address.
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ void sts4(uint32_t at, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts16(uint32_t at, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// One copy of a multiple of 16 bytes from and to 16-byte boundaries, counted by the barrier.
+__device__ __forceinline__ void bulk_load(uint8_t* dst, const uint8_t* src, uint32_t bytes, uint64_t* bar) {
+  mbar_expect_tx(smem_u32(bar), bytes);
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes),
+               "r"(smem_u32(bar)) : "memory");
 }
 
 // The block's n-th item; the list is sorted longest first, and the rounds run through the blocks forth and back.
 __device__ __forceinline__ int long_item(int n) { return n * int(gridDim.x) + ((n & 1) ? int(gridDim.x) - 1 - int(blockIdx.x) : int(blockIdx.x)); }
 
-struct LongItem {
-  ScanRequest r;
-  int h, g, upto, chunks, base;      // base: the request's first chunk among all
-};
-__device__ __forceinline__ LongItem long_load(const LongArgs& a, int item) {
-  const int2 at = *reinterpret_cast<const int2*>(a.list + 2 * (item / a.c.H));
-  LongItem i;
-  i.r = scan_request(a.c, at.x);
-  i.h = item % a.c.H;
-  i.g = i.h / (a.c.H / a.c.G);
-  i.upto = scan_upto(a.c, i.r);
-  i.chunks = chunk_count(i.r.keep, i.upto);
-  i.base = at.y;
-  return i;
-}
+template <typename TI> __device__ __forceinline__ TI from_bits(uint32_t v);
+template <> __device__ __forceinline__ float from_bits(uint32_t v) { return __uint_as_float(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_bits(uint32_t v) { return __ushort_as_bfloat16(uint16_t(v)); }
+template <> __device__ __forceinline__ __half from_bits(uint32_t v) { return __ushort_as_half(uint16_t(v)); }
 
-template <typename TI, bool Y>
+template <typename TI, bool Y, bool VEC>
 __global__ void __launch_bounds__(LONG_THREADS, 1) scan_long_kernel(LongArgs a) {
   const ChunkScanCall& c = a.c;
   pdl_wait();
@@ -287,20 +349,10 @@ __global__ void __launch_bounds__(LONG_THREADS, 1) scan_long_kernel(LongArgs a) 
   if (warp == 0) {
     if (lane == 0) {
       mbar_init(smem_u32(&bars->b_full), 1);
-      mbar_init(smem_u32(&bars->x_full), 128);
-      mbar_init(smem_u32(&bars->c_full), 128);
-      mbar_init(smem_u32(&bars->g_full), 128);
-      mbar_init(smem_u32(&bars->s_full), 128);
-      mbar_init(smem_u32(&bars->m_state), 1);
-      mbar_init(smem_u32(&bars->m_next), 1);
-      mbar_init(smem_u32(&bars->m_near), 1);
-      mbar_init(smem_u32(&bars->next_free), 128);
-      mbar_init(smem_u32(&bars->out_free), 128);
-      mbar_init(smem_u32(&bars->x_read), 128);
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(smem_u32(&bars->steps_full[i]), 32);
-        mbar_init(smem_u32(&bars->steps_free[i]), Y ? 512 : 256);
-      }
+      mbar_init(smem_u32(&bars->scores_full), 1);
+      mbar_init(smem_u32(&bars->products), 1);
+      for (int i = 0; i < 2 * NH; ++i) bars->first_odd[i / NH][i % NH] = Q;
+      bars->any_odd[0] = bars->any_odd[1] = 0;
       bars->stop = (smem_u32(smem) & 1023) ? 1u : 0u;
       if (bars->stop) atomicExch(c.status, STATUS_BAD_SMEM_BASE);
       fence_mbar_init();
@@ -313,445 +365,468 @@ __global__ void __launch_bounds__(LONG_THREADS, 1) scan_long_kernel(LongArgs a) 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
-  const bool broken = bars->stop != 0;
-  // (a role of whole warps goes on or gives up as a warp)
-#define WAIT_ONE(bar, parity, code) \
-  if (!wait_for(&bars->bar, parity, bars, c.status, code)) goto done
-#define WAIT(bar, parity, code) \
-  if (!__all_sync(0xffffffffu, wait_for(&bars->bar, parity, bars, c.status, code))) goto done
-
-  if (broken) goto done;
-  if (warp == 0) {
-    // ---- B's image, a chunk at a time
-    if (lane == 0) {
-      uint32_t k = 0;
-      bool ok = true;
-      for (int n = 0; ok && long_item(n) < items; ++n) {
-        const LongItem it = long_load(a, long_item(n));
-        for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-          ok = !k || wait_for(&bars->m_next, (k - 1) & 1, bars, c.status, STATUS_TIMEOUT_PRODUCER);
-          if (!ok) break;
-          const uint8_t* src = a.images + (size_t(it.base + ci) * c.G + it.g) * IMG_BYTES + IMG_B;
-          const uint32_t bar = smem_u32(&bars->b_full);
-          mbar_expect_tx(bar, 65536);
+  // a thread's lane of tensor memory (a row of the chunk, or a state element), and its quarter of the columns
+  const int row = (warp & 3) * 32 + lane, quarter = warp >> 2;
+  const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);
+  if (Y) {
+    uint32_t zero[16] = {};
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem + SM_B + i * 16384)),
-                         "l"(src + i * 16384), "r"(16384), "r"(bar) : "memory");
+    for (int i = 0; i < 2; ++i) tmem_st16(lanes + TM_G + quarter * 32 + i * 16, zero);      // above the diagonal it stays so
+    tmem_st_wait();
+  }
+  const int cp = lane * 2, first = warp * 8;                 // its two channels of x and its eight rows of them
+  uint32_t k = 0;                                            // chunks so far
+  volatile uint32_t* stop = &bars->stop;
+  for (int n = 0; long_item(n) < items && !*stop; ++n) {
+    const int item = long_item(n);
+    const int2 at = *reinterpret_cast<const int2*>(a.list + 2 * (item / c.H));
+    const int h = item % c.H, g = h / (c.H / c.G);
+    const ScanRequest r = scan_request(c, at.x);
+    const int upto = scan_upto(c, r), chunks = chunk_count(r.keep, upto);
+    const uint8_t* img = a.images + (size_t(at.y) * c.G + g) * IMG_BYTES;
+    const TI* rows0 = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * NH;             // the request's gates; x stands Di behind them
+    float* mem = c.ssm_state + (((size_t(r.slot < 0 ? 0 : r.slot) * c.H + h) * NH) + quarter * 16) * NS + row;
+    if (tid == 0) {
+      bulk_load(smem + SM_B, img + IMG_B, 65536, &bars->b_full);
+      if (Y) bulk_load(smem + SM_G, img + IMG_G, IMG_BYTES - IMG_G, &bars->scores_full);
+    }
+    Taps<1> taps;
+    taps.load(c, h * NH + cp);
+    const RawRows<VEC, 2, TI> raw(a, r, h * NH + cp);
+    const double rate = -exp(double(c.A_log[h])) * 1.4426950408889634;
+    const float dt_bias = c.dt_bias[h], D = c.Dskip[h];
+    // the raw value that a row's step comes from (a row each for the second four warps: the first warp issues the products)
+    auto raw_step = [&](const ChunkRange& range) {
+      const size_t t = size_t(r.q0 + range.start + row);
+      return quarter != 1 || row >= range.len ? 0.f
+             : c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
+    };
+    // The steps of a chunk.  Their sums are 64-bit: at a sum of 100 a 32-bit one is off by 4e-6, and so would be every weight.
+    auto make_steps = [&](LongSteps& s, float raw, int len) {
+      const float dt = row < len ? softplus_f32(raw + dt_bias) : 0.f;
+      double ct = double(dt) * rate;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const double up = __shfl_up_sync(0xffffffffu, ct, off);
+        if (lane >= off) ct += up;
+      }
+      if (lane == 31) bars->sums[warp & 3] = ct;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      double all = 0.0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const double part = bars->sums[i];
+        if (i < (warp & 3)) ct += part;
+        all += part;
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      const float hi = float(ct);
+      s.c_hi[row] = hi;
+      s.c_lo[row] = float(ct - double(hi));
+      s.ec[row] = ex2_ftz(hi);
+      s.w[row] = dt * ex2_ftz(float(all - ct));
+      const double nd = dt > 0.f ? double(__log2f(dt)) - ct : dt == 0.f ? -INFINITY : double(dt);
+      const float nh = float(nd);
+      s.n_hi[row] = nh;
+      s.n_lo[row] = dt > 0.f ? float(nd - double(nh)) : 0.f;
+      if (row == 0) s.total = ex2_ftz(float(all));
+    };
+    // x: eight raw rows become v, and `odd`: zero times every value, NaN where one is not finite
+    Word<TI, 2> held[8], front[3];
+    uint64_t v[8], odd;
+    auto fetch_x = [&](const ChunkRange& range) {
+      const int last = range.start + range.len - 1;
+      if (range.len == Q && range.start >= 3) {
+        const TI* p = raw.x + size_t(range.start + first - 3) * raw.ld;
+#pragma unroll
+        for (int i = 0; i < 3; ++i, p += raw.ld) front[i] = load_word<VEC, 2>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i, p += raw.ld) held[i] = load_word<VEC, 2>(p);
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) held[i] = raw.row(range.start + first + i, last);
+      raw.front(front, range.start + first, last);
+    };
+    auto convolve = [&](const ChunkRange& range) {
+      uint64_t before[3][1];
+      raw.front_value(front, range.start + first, before);
+      odd = 0ull;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint64_t now[1], u[1];
+        widen(held[i], now);
+        taps.next(before, now, u);
+        odd = fma_f32x2(u[0], 0ull, odd);
+        v[i] = u[0];
+      }
+    };
+    // state: one element of 16 channels
+    float S[16];
+    auto put_state = [&] {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t to = smem_u32(smem + SM_S) + (row >> 3) * 1024 + (row & 7) * 128 + (((quarter * 2 + i) ^ (row & 7)) << 4);
+        uint4 hi, lo;
+        split2(pack_f32x2(S[8 * i], S[8 * i + 1]), hi.x, lo.x);
+        split2(pack_f32x2(S[8 * i + 2], S[8 * i + 3]), hi.y, lo.y);
+        split2(pack_f32x2(S[8 * i + 4], S[8 * i + 5]), hi.z, lo.z);
+        split2(pack_f32x2(S[8 * i + 6], S[8 * i + 7]), hi.w, lo.w);
+        sts16(to, hi);
+        sts16(to + 16384, lo);
+      }
+    };
+    ChunkRange range = chunk_range(r.keep, upto, 0);
+    fetch_x(range);
+    float step = raw_step(range);
+#pragma unroll
+    for (int p = 0; p < 16; ++p) S[p] = r.fresh ? 0.f : __ldcs(mem + p * NS);
+    if (r.keep == 0 && r.stores()) {
+#pragma unroll
+      for (int p = 0; p < 16; ++p) __stcs(mem + p * NS, 0.f);
+    }
+    if (Y) put_state();
+    if (quarter == 1) make_steps(steps[k & 1], step, range.len);
+    convolve(range);
+    if (chunks > 1) {
+      const ChunkRange next = chunk_range(r.keep, upto, 1);
+      fetch_x(next);
+      step = raw_step(next);
+    }
+    __syncthreads();
+    for (int ci = 0; ci < chunks; ++ci, ++k) {
+      const LongSteps& s = steps[k & 1];
+      const uint32_t s_at = smem_u32(&s);
+      // ---- operands of the products: C
+      uint32_t cw[32];
+      if (Y) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(img + IMG_C + ((quarter * 8 + i) * Q + row) * 16));
+          cw[4 * i] = x.x; cw[4 * i + 1] = x.y; cw[4 * i + 2] = x.z; cw[4 * i + 3] = x.w;
         }
       }
-      if (k) mbar_wait(smem_u32(&bars->b_full), (k - 1) & 1);       // (no copy is under way when the block ends)
-    }
-  } else if (warp == 1) {
-    // ---- products
-    if (elect_one()) {
-      uint32_t k = 0;
-      const uint32_t b_hi = smem_u32(smem + SM_B), b_lo = b_hi + 32768, x_hi = smem_u32(smem + SM_X), x_lo = x_hi + 16384;
-      const uint32_t w_hi = smem_u32(smem + SM_XW), w_lo = w_hi + 16384, s_hi = smem_u32(smem + SM_S), s_lo = s_hi + 16384;
-      for (int n = 0; long_item(n) < items; ++n) {
-        const LongItem it = long_load(a, long_item(n));
-        for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-          const uint32_t now = k & 1, before = now ^ 1;
-          // the next state's: B^T (x w)
-          WAIT_ONE(b_full, now, STATUS_TIMEOUT_MMA);
-          WAIT_ONE(x_full, now, STATUS_TIMEOUT_MMA);
-          if (k) WAIT_ONE(next_free, before, STATUS_TIMEOUT_MMA);
-          tc_fence_after();
-#pragma unroll
-          for (int p = 0; p < 3; ++p)
-#pragma unroll
-            for (int ks = 0; ks < Q / 16; ++ks)
-              umma_bf16(tmem + TM_NEXT, desc_mn((p == 2 ? b_lo : b_hi) + ks * 2048), desc_mn((p == 1 ? w_lo : w_hi) + ks * 2048), long_idesc(true), p || ks);
-          umma_commit(smem_u32(&bars->m_next));
-          if (Y) {
-            // with the state: C S
-            WAIT_ONE(c_full, now, STATUS_TIMEOUT_MMA);
-            WAIT_ONE(s_full, now, STATUS_TIMEOUT_MMA);
-            if (k) WAIT_ONE(out_free, before, STATUS_TIMEOUT_MMA);
-            tc_fence_after();
-#pragma unroll
-            for (int p = 0; p < 3; ++p)
-#pragma unroll
-              for (int ks = 0; ks < NS / 16; ++ks)
-                umma_bf16_ts(tmem + TM_STATE, tmem + TM_C + (p == 2 ? 64 : 0) + ks * 8, desc_mn((p == 1 ? s_lo : s_hi) + ks * 2048), long_idesc(false), p || ks);
-            umma_commit(smem_u32(&bars->m_state));
-            // inside the chunk
-            WAIT_ONE(g_full, now, STATUS_TIMEOUT_MMA);
-            tc_fence_after();
-#pragma unroll
-            for (int p = 0; p < 3; ++p)
-#pragma unroll
-              for (int ks = 0; ks < Q / 16; ++ks)
-                umma_bf16_ts(tmem + TM_NEAR, tmem + TM_G + (p == 2 ? 64 : 0) + ks * 8, desc_mn((p == 1 ? x_lo : x_hi) + ks * 2048), long_idesc(false), p || ks);
-            umma_commit(smem_u32(&bars->m_near));
-          }
-        }
-      }
-    }
-  } else if (warp == 2) {
-    // ---- steps: a lane has four rows.  The sums are 64-bit: at a sum of 100 a 32-bit one is off by 4e-6, and so would be every weight.
-    uint32_t k = 0;
-    for (int n = 0; long_item(n) < items; ++n) {
-      const LongItem it = long_load(a, long_item(n));
-      const double rate = -exp(double(c.A_log[it.h])) * 1.4426950408889634;
-      const float bias = c.dt_bias[it.h];
-      for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-        const ChunkRange range = chunk_range(it.r.keep, it.upto, ci);
-        float dt[4];
-        double sum[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = lane * 4 + e;
-          float raw = 0.f;
-          const size_t t = size_t(it.r.q0 + range.start + i);
-          if (i < range.len) raw = c.dt_raw ? c.dt_raw[t * c.H + it.h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + it.h]);
-          dt[e] = i < range.len ? softplus_f32(raw + bias) : 0.f;
-          sum[e] = (e ? sum[e - 1] : 0.0) + double(dt[e]) * rate;
-        }
-        double upto = sum[3];
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const double up = __shfl_up_sync(0xffffffffu, upto, off);
-          if (lane >= off) upto += up;
-        }
-        const double all = __shfl_sync(0xffffffffu, upto, 31), front = upto - sum[3];
-        if (k >= 2) WAIT(steps_free[k & 1], ((k >> 1) - 1) & 1, STATUS_TIMEOUT_PRODUCER);
-        LongSteps& s = steps[k & 1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = lane * 4 + e;
-          const double ct = front + sum[e];
-          const float hi = float(ct);
-          s.c_hi[i] = hi;
-          s.c_lo[i] = float(ct - double(hi));
-          s.ec[i] = exp2f(hi);
-          s.w[i] = dt[e] * exp2f(float(all - ct));
-          const double nd = dt[e] > 0.f ? double(log2f(dt[e])) - ct : -INFINITY;
-          const float nh = float(nd);
-          s.n_hi[i] = nh;
-          s.n_lo[i] = dt[e] > 0.f ? float(nd - double(nh)) : 0.f;
-        }
-        if (lane == 0) s.total = exp2f(float(all));
-        mbar_arrive(smem_u32(&bars->steps_full[k & 1]));
-      }
-    }
-  } else if (warp >= 4 && warp < 8) {
-    // ---- scores: C into tensor memory, then the scores times the decays
-    if (Y) {
-      const int row = tid - 128;
-      const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);
-      uint32_t k = 0;
+      // ---- x
       {
-        uint32_t zero[16] = {};
+        const uint32_t to = smem_u32(smem + SM_X) + warp * 1024 + (lane & 3) * 4;
+        const uint4 wa = lds16(s_at + offsetof(LongSteps, w) + first * 4), wb = lds16(s_at + offsetof(LongSteps, w) + first * 4 + 16);
+        const uint32_t w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tmem_st16(lanes + TM_G + i * 16, zero);      // above the diagonal it stays so
-        tmem_st_wait();
-      }
-      for (int n = 0; long_item(n) < items; ++n) {
-        const LongItem it = long_load(a, long_item(n));
-        const float D = c.Dskip[it.h];
-        for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-          const uint8_t* img = a.images + (size_t(it.base + ci) * c.G + it.g) * IMG_BYTES;
-          if (k) WAIT(m_state, (k - 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          tc_fence_after();
-#pragma unroll
-          for (int part = 0; part < 4; ++part) {             // head, head, remainder, remainder
-            uint32_t v[32];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint4 x = __ldg(reinterpret_cast<const uint4*>(img + IMG_C + part * 16384 + (i * Q + row) * 16));
-              v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
-            }
-            tmem_st32(lanes + TM_C + part * 32, v);
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t at = to + i * 128 + (((lane >> 2) ^ i) << 4);
+          uint32_t hi, lo;
+          if (Y) {
+            split2(v[i], hi, lo);
+            sts4(at, hi);
+            sts4(at + 16384, lo);
           }
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive(smem_u32(&bars->c_full));
-          WAIT(steps_full[k & 1], (k >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          const LongSteps& s = steps[k & 1];
-          const uint64_t chi = pack_f32x2(s.c_hi[row], s.c_hi[row]), clo = pack_f32x2(s.c_lo[row], s.c_lo[row]);
-          if (k) WAIT(m_near, (k - 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          tc_fence_after();
-          for (int cb = 0; cb <= (warp & 3); ++cb) {
-            const uint8_t* gsrc = img + g_block(cb) + (row - 32 * cb) * 16;
-            const int pitch = (Q - 32 * cb) * 16;
-            const bool diag = cb == (warp & 3);
-            float4 g4[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g4[i] = __ldg(reinterpret_cast<const float4*>(gsrc + i * pitch));
-            uint32_t hi[16], lo[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int col = cb * 32 + 2 * i;
-              const uint64_t e2 = add_f32x2(add_f32x2(chi, *reinterpret_cast<const uint64_t*>(&s.n_hi[col])),
-                                            add_f32x2(clo, *reinterpret_cast<const uint64_t*>(&s.n_lo[col])));
-              float e0, e1;
-              unpack_f32x2(e2, e0, e1);
-              if (diag) { e0 = fminf(e0, 126.f); e1 = fminf(e1, 126.f); }      // (above the diagonal: times zero)
-              const float4 gg = g4[i >> 1];
-              float v0 = ex2_ftz(e0) * ((i & 1) ? gg.z : gg.x), v1 = ex2_ftz(e1) * ((i & 1) ? gg.w : gg.y);
-              if (diag) {
-                if (2 * i == lane) v0 += D;
-                if (2 * i + 1 == lane) v1 += D;
+          split2(mul_f32x2(v[i], dup2(__uint_as_float(w[i]))), hi, lo);
+          sts4(at + SM_XW - SM_X, hi);
+          sts4(at + SM_XW - SM_X + 16384, lo);
+        }
+        // A value that is not finite would reach the rows in front of it too, as zero times itself: it leaves the operands, and what it reaches is made
+        // NaN where the products are read.  (Rows behind the last one repeat it, with weight zero: they are cleared as well.)
+        float odd0, odd1;
+        unpack_f32x2(odd, odd0, odd1);
+        if (odd0 + odd1 != 0.f) {
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            uint8_t* at = smem + SM_X + warp * 1024 + i * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3) * 4;
+#pragma unroll 1
+            for (int e = 0; e < 2; ++e) {
+              uint16_t* x = reinterpret_cast<uint16_t*>(at) + e;
+              uint16_t* w = reinterpret_cast<uint16_t*>(at + SM_XW - SM_X) + e;
+              const bool bad = (Y && (x[0] & 0x7f80) == 0x7f80) || (Y && (x[8192] & 0x7f80) == 0x7f80) || (w[0] & 0x7f80) == 0x7f80 || (w[8192] & 0x7f80) == 0x7f80;
+              if (!bad) continue;
+              if (Y) x[0] = x[8192] = 0;
+              w[0] = w[8192] = 0;
+              if (first + i < range.len) {
+                atomicMin(&bars->first_odd[k & 1][cp + e], first + i);
+                *reinterpret_cast<volatile int*>(&bars->any_odd[k & 1]) = 1;
               }
-              split2(v0, v1, hi[i], lo[i]);
             }
-            tmem_st16(lanes + TM_G + cb * 16, hi);
-            tmem_st16(lanes + TM_G + 64 + cb * 16, lo);
           }
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive(smem_u32(&bars->g_full));
-          mbar_arrive(smem_u32(&bars->steps_free[k & 1]));
         }
       }
-    }
-  } else if (warp >= 8 && warp < 12) {
-    // ---- x: a thread has four channels of 16 rows
-    const int t = tid - 256, cg = t & 15, first = (t >> 4) * 16;
-    uint32_t k = 0, reads = 0;
-    for (int n = 0; long_item(n) < items; ++n) {
-      const LongItem it = long_load(a, long_item(n));
-      const int ch = it.h * NH + cg * 4;
-      Taps taps;
-      taps.load(c, ch);
-      for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-        const ChunkRange range = chunk_range(it.r.keep, it.upto, ci);
-        const int end = range.start + range.len;
-        float w0[4], w1[4], w2[4], x[8][4];
-        raw4<TI>(a, it.r, ch, range.start + first - 3, end, w0);
-        raw4<TI>(a, it.r, ch, range.start + first - 2, end, w1);
-        raw4<TI>(a, it.r, ch, range.start + first - 1, end, w2);
+      // ---- scores times decays: every fourth block of 8 columns up to the diagonal's
+      if (Y) {
+        wait_for(&bars->scores_full, k & 1, bars, c.status, STATUS_TIMEOUT_EPILOGUE);
+        tmem_st32(lanes + TM_C + quarter * 32, cw);
+        const uint64_t chi = dup2(s.c_hi[row]), clo = dup2(s.c_lo[row]);
+        auto two = [](uint32_t a, uint32_t b) { return pack_f32x2(__uint_as_float(a), __uint_as_float(b)); };
+        uint4 gg[2], nh[2], nl[2];
+        auto fetch = [&](int cb) {
+          const int pitch = (Q - 32 * cb) * 16, o = cb * 4 + quarter;
+          const uint32_t from = smem_u32(smem + SM_G) - IMG_G + g_block(cb) + (row - 32 * cb) * 16 + quarter * 2 * pitch;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) raw4<TI>(a, it.r, ch, range.start + first + i, end, x[i]);
-        WAIT(steps_full[k & 1], (k >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-        const LongSteps& s = steps[k & 1];
-        if (k) {
-          WAIT(m_next, (k - 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          if (Y) WAIT(m_near, (k - 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-        }
-#pragma unroll
-        for (int i0 = 0; i0 < 16; i0 += 8) {
-          if (i0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) raw4<TI>(a, it.r, ch, range.start + first + i0 + i, end, x[i]);
+          for (int i = 0; i < 2; ++i) {
+            gg[i] = lds16(from + i * pitch);
+            nh[i] = lds16(s_at + (o * 8 + 4 * i) * 4);
+            nl[i] = lds16(s_at + (Q + o * 8 + 4 * i) * 4);
           }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int row = first + i0 + i;
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float u = fmaf(taps.w[3][e], x[i][e], fmaf(taps.w[2][e], w2[e], fmaf(taps.w[1][e], w1[e], fmaf(taps.w[0][e], w0[e], taps.b[e]))));
-              v[e] = row < range.len ? silu_f32(u) : 0.f;
-              w0[e] = w1[e]; w1[e] = w2[e]; w2[e] = x[i][e];
-            }
-            uint8_t* d = smem + SM_X + (row >> 3) * 1024 + (row & 7) * 128 + (((cg >> 1) ^ (row & 7)) << 4) + (cg & 1) * 8;
-            uint2 hi, lo;
-            if (Y) {
-              split2(v[0], v[1], hi.x, lo.x);
-              split2(v[2], v[3], hi.y, lo.y);
-              *reinterpret_cast<uint2*>(d) = hi;
-              *reinterpret_cast<uint2*>(d + 16384) = lo;
-            }
-            const float w = s.w[row];
-            split2(v[0] * w, v[1] * w, hi.x, lo.x);
-            split2(v[2] * w, v[3] * w, hi.y, lo.y);
-            *reinterpret_cast<uint2*>(d + SM_XW - SM_X) = hi;
-            *reinterpret_cast<uint2*>(d + SM_XW - SM_X + 16384) = lo;
-          }
-        }
-        fence_proxy_async();
-        mbar_arrive(smem_u32(&bars->x_full));
-        mbar_arrive(smem_u32(&bars->steps_free[k & 1]));
-      }
-      // ---- the carried rows of this head's channels, and of its group's B and C for the group's first head: all of it read before any is written
-      const int K1 = c.d_conv - 1;
-      if (it.r.stores() && K1 > 0) {
-        const bool all = it.h % (c.H / c.G) == 0;
-        const int width = NH + (all ? 2 * NS : 0);
-        TI* carried = reinterpret_cast<TI*>(c.conv_state) + size_t(it.r.slot) * K1 * c.d_xBC;
-        auto place = [&](int i, int& j) {
-          const int e = i % width;
-          j = i / width;
-          return e < NH ? it.h * NH + e : e < NH + NS ? c.Di + it.g * NS + e - NH : c.Di + (c.G + it.g) * NS + e - NH - NS;
         };
-        TI v[8];                                             // 3 (64 + 256) values over 128 threads
+        fetch(0);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int i = t + q * 128;
-          if (i >= K1 * width) continue;
-          int j;
-          const int at = place(i, j), from = it.r.keep + j - K1;
-          if (from >= 0) v[q] = reinterpret_cast<const TI*>(c.x)[size_t(it.r.q0 + from) * c.ld_x + c.Di + at];
-          else if (it.r.fresh) v[q] = TI(0.f);
-          else v[q] = carried[size_t(from + K1) * c.d_xBC + at];
-        }
-        mbar_arrive(smem_u32(&bars->x_read));
-        WAIT(x_read, reads & 1, STATUS_TIMEOUT_EPILOGUE);
-        ++reads;
+        for (int cb = 0; cb < 4; ++cb) {
+          if (cb > (warp & 3)) break;
+          const int o = cb * 4 + quarter;
+          uint64_t u[4];
+          float e[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int i = t + q * 128;
-          if (i >= K1 * width) continue;
-          int j;
-          const int at = place(i, j);
-          carried[size_t(j) * c.d_xBC + at] = v[q];
-        }
-      }
-    }
-  } else if (warp >= 12 && warp < 16) {
-    // ---- state: a thread has one state element of all 64 channels
-    const int e = tid - 384;
-    const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);
-    uint32_t k = 0;
-    for (int n = 0; long_item(n) < items; ++n) {
-      const LongItem it = long_load(a, long_item(n));
-      float* mem = c.ssm_state + ((size_t(it.r.slot < 0 ? 0 : it.r.slot) * c.H + it.h) * NH) * NS + e;
-      float S[NH];
-#pragma unroll
-      for (int p = 0; p < NH; ++p) S[p] = it.r.fresh ? 0.f : __ldcs(mem + p * NS);
-      if (it.r.keep == 0 && it.r.stores()) {
-#pragma unroll
-        for (int p = 0; p < NH; ++p) __stcs(mem + p * NS, 0.f);
-      }
-      for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-        if (Y) {
-          if (k) WAIT(m_state, (k - 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          uint8_t* d = smem + SM_S + (e >> 3) * 1024 + (e & 7) * 128;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            uint4 hi, lo;
-            split2(S[8 * i], S[8 * i + 1], hi.x, lo.x);
-            split2(S[8 * i + 2], S[8 * i + 3], hi.y, lo.y);
-            split2(S[8 * i + 4], S[8 * i + 5], hi.z, lo.z);
-            split2(S[8 * i + 6], S[8 * i + 7], hi.w, lo.w);
-            const int at = (i ^ (e & 7)) << 4;
-            *reinterpret_cast<uint4*>(d + at) = hi;
-            *reinterpret_cast<uint4*>(d + 16384 + at) = lo;
+          for (int i = 0; i < 2; ++i) {
+            unpack_f32x2(add_f32x2(add_f32x2(chi, two(nh[i].x, nh[i].y)), add_f32x2(clo, two(nl[i].x, nl[i].y))), e[4 * i], e[4 * i + 1]);
+            unpack_f32x2(add_f32x2(add_f32x2(chi, two(nh[i].z, nh[i].w)), add_f32x2(clo, two(nl[i].z, nl[i].w))), e[4 * i + 2], e[4 * i + 3]);
+            u[2 * i] = mul_f32x2(pack_f32x2(ex2_ftz(e[4 * i]), ex2_ftz(e[4 * i + 1])), two(gg[i].x, gg[i].y));
+            u[2 * i + 1] = mul_f32x2(pack_f32x2(ex2_ftz(e[4 * i + 2]), ex2_ftz(e[4 * i + 3])), two(gg[i].z, gg[i].w));
           }
-          fence_proxy_async();
-          mbar_arrive(smem_u32(&bars->s_full));
-        }
-        WAIT(steps_full[k & 1], (k >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-        const float total = steps[k & 1].total;
-        mbar_arrive(smem_u32(&bars->steps_free[k & 1]));
-        WAIT(m_next, k & 1, STATUS_TIMEOUT_EPILOGUE);
-        tc_fence_after();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t v[16];
-          tmem_ld16(lanes + TM_NEXT + q * 16, v);
-          tmem_wait_ld16(v);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) S[q * 16 + i] = fmaf(total, S[q * 16 + i], __uint_as_float(v[i]));
-        }
-        tc_fence_before();
-        mbar_arrive(smem_u32(&bars->next_free));
-        const ChunkRange range = chunk_range(it.r.keep, it.upto, ci);
-        if (range.start + range.len == it.r.keep && it.r.stores()) {
-#pragma unroll
-          for (int p = 0; p < NH; ++p) __stcs(mem + p * NS, S[p]);
-        }
-      }
-    }
-  } else if (warp >= 16) {
-    // ---- outputs: a thread has one row's 64 channels
-    if (Y) {
-      const int row = tid - 512;
-      const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);
-      uint32_t k = 0;
-      for (int n = 0; long_item(n) < items; ++n) {
-        const LongItem it = long_load(a, long_item(n));
-        for (int ci = 0; ci < it.chunks; ++ci, ++k) {
-          const ChunkRange range = chunk_range(it.r.keep, it.upto, ci);
-          const bool on = row < range.len;
-          const size_t t = size_t(it.r.q0 + range.start + row);
-          const TI* z = reinterpret_cast<const TI*>(c.x) + t * c.ld_x + it.h * NH;
-          WAIT(steps_full[k & 1], (k >> 1) & 1, STATUS_TIMEOUT_EPILOGUE);
-          const float ec = steps[k & 1].ec[row];
-          mbar_arrive(smem_u32(&bars->steps_free[k & 1]));
-          WAIT(m_near, k & 1, STATUS_TIMEOUT_EPILOGUE);
-          tc_fence_after();
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float zz[16];
+          if (cb < (warp & 3)) {
+            fetch(cb + 1);
+          } else {                                             // (above the diagonal the weights may be anything)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              if (on && a.vec) {
-                const Word<TI, 4> w = *reinterpret_cast<const Word<TI, 4>*>(z + q * 16 + i * 4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) zz[4 * i + j] = to_f32(w.v[j]);
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) zz[4 * i + j] = on ? to_f32(z[q * 16 + i * 4 + j]) : 0.f;
-              }
-            }
-            uint32_t near[16], state[16];
-            tmem_ld16(lanes + TM_NEAR + q * 16, near);
-            tmem_ld16(lanes + TM_STATE + q * 16, state);
-            tmem_wait_ld16(near);
-            tmem_wait_ld16(state);
-            if (q == 3) {
-              tc_fence_before();
-              mbar_arrive(smem_u32(&bars->out_free));
-            }
-            float y[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = fmaf(ec, __uint_as_float(state[i]), __uint_as_float(near[i])) * silu_f32(zz[i]);
-            if (!on) continue;
-            const size_t at = t * c.ld_y + it.h * NH + q * 16;
-            if (!a.y_vec) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) store_row(c.y, c.y_dtype, at + i, y[i], c.status);
-            } else if (c.y_dtype == CHUNK_F32) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(reinterpret_cast<float*>(c.y) + at)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-            } else {
-              uint32_t o[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = c.y_dtype == CHUNK_BF16 ? pack_bf16(y[2 * i], y[2 * i + 1]) : pack_f16_sat(y[2 * i], y[2 * i + 1], c.status);
-              uint4* d = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(c.y) + at);
-              d[0] = make_uint4(o[0], o[1], o[2], o[3]);
-              d[1] = make_uint4(o[4], o[5], o[6], o[7]);
+              const int col = o * 8 + 2 * i;
+              float u0, u1;
+              unpack_f32x2(u[i], u0, u1);
+              u[i] = pack_f32x2(col < row ? u0 : col == row ? u0 + D : 0.f, col + 1 < row ? u1 : col + 1 == row ? u1 + D : 0.f);
             }
           }
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) split2(u[i], hi[i], lo[i]);
+          tmem_st4(lanes + TM_G + o * 4, hi);
+          tmem_st4(lanes + TM_G + 64 + o * 4, lo);
         }
+        tmem_st_wait();
+      }
+      fence_proxy_async();
+      tc_fence_before();
+      __syncthreads();
+      // ---- the products, in eight parts that the first warp issues between its own work: it would wait for the tensor core otherwise
+      img += size_t(c.G) * IMG_BYTES;
+      auto issue = [&](int part) {
+        if (warp == 0) {
+          if (elect_one()) {
+            constexpr uint64_t REST = 16384 >> 4;            // from an operand's head to its remainder (B: twice that)
+            if (part == 0) {
+              tc_fence_after();
+              wait_for(&bars->b_full, k & 1, bars, c.status, STATUS_TIMEOUT_MMA);
+            }
+            if (part < 2) {
+              // the next state's: B's head times the head and the remainder of x at once (their places are as far apart as the halves of a 128-column
+              // operand), next to one another, then its remainder times the head: A comes from shared memory, which is what bounds this one
+              const uint64_t b_at = desc_mn(smem_u32(smem + SM_B)) + (part ? 2 * REST : 0), w_at = desc_mn(smem_u32(smem + SM_XW));
+#pragma unroll
+              for (int ks = 0; ks < Q / 16; ++ks) umma_bf16(tmem + TM_NEXT, b_at + ks * 128, w_at + ks * 128, part ? long_idesc(true, 64) : long_idesc(true, 128), part || ks);
+            } else {
+              // inside the chunk, then with the state: head x head, head x remainder, remainder x head
+              const int p = part < 5 ? part - 2 : part - 5;
+              const uint32_t a_at = tmem + (part < 5 ? TM_G : TM_C) + (p == 2 ? 64 : 0), to = tmem + (part < 5 ? TM_NEAR : TM_STATE);
+              const uint64_t o_at = desc_mn(smem_u32(smem + (part < 5 ? SM_X : SM_S))) + (p == 1 ? REST : 0);
+#pragma unroll
+              for (int ks = 0; ks < Q / 16; ++ks) umma_bf16_ts(to, a_at + ks * 8, o_at + ks * 128, long_idesc(false, 64), p || ks);
+            }
+            if (part == (Y ? 7 : 1)) umma_commit(smem_u32(&bars->products));
+            if (part == 2 && ci + 1 < chunks) bulk_load(smem + SM_G, img + IMG_G, IMG_BYTES - IMG_G, &bars->scores_full);
+          }
+          __syncwarp();
+        }
+      };
+      issue(0);
+      issue(1);
+      if (Y) issue(2);
+      // ---- meanwhile: gates of this chunk, steps and convolution of the next one, raw rows of the one behind that
+      const bool on = row < range.len, keeps = range.start + range.len == r.keep && r.stores();
+      const size_t t = size_t(range.start + (on ? row : 0));
+      uint64_t gate[8];
+      if (Y) {
+        // (a thread's 16 values in one load where they lie on a 32-byte boundary: every load of a warp goes to 32 rows, and takes its time for that)
+        const TI* z = rows0 + t * c.ld_x + quarter * 16;
+        Word<TI, 2> w[8];
+        if (sizeof(TI) == 2 && a.z_vec) {
+          uint4 lo, hi;
+          ldg_nc_32B(z, lo, hi);
+          const uint32_t bits[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) { w[i].v[0] = from_bits<TI>(bits[i]); w[i].v[1] = from_bits<TI>(bits[i] >> 16); }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const Word<TI, 4> four = load_word<VEC, 4>(z + 4 * i);
+            w[2 * i].v[0] = four.v[0]; w[2 * i].v[1] = four.v[1];
+            w[2 * i + 1].v[0] = four.v[2]; w[2 * i + 1].v[1] = four.v[3];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint64_t one[1];
+          widen(w[i], one);
+          gate[i] = one[0];
+        }
+      }
+      const int len = range.len;
+      if (ci + 1 < chunks) {
+        range = chunk_range(r.keep, upto, ci + 1);
+        const float now = step;
+        convolve(range);
+        if (Y) issue(3);
+        if (ci + 2 < chunks) {
+          const ChunkRange next = chunk_range(r.keep, upto, ci + 2);
+          fetch_x(next);
+          step = raw_step(next);
+        }
+        if (Y) issue(4);
+        if (quarter == 1) make_steps(steps[(k + 1) & 1], now, range.len);
+      } else if (Y) {
+        issue(3);
+        issue(4);
+      }
+      if (Y) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gate[i] = silu2(gate[i]);
+        issue(5);
+        issue(6);
+        issue(7);
+      }
+      if (warp == 1 && bars->any_odd[(k + 1) & 1]) {           // (the chunk in front of this one has been read)
+        bars->first_odd[(k + 1) & 1][lane] = bars->first_odd[(k + 1) & 1][lane + 32] = Q;
+        __syncwarp();
+        if (lane == 0) bars->any_odd[(k + 1) & 1] = 0;
+      }
+      if (tid == 0) wait_for(&bars->products, k & 1, bars, c.status, STATUS_TIMEOUT_MMA);
+      __syncthreads();
+      if (*stop) break;
+      if (tid == 0 && ci + 1 < chunks) bulk_load(smem + SM_B, img + IMG_B, 65536, &bars->b_full);
+      // ---- what the products gave: outputs
+      tc_fence_after();
+      const bool any_odd = bars->any_odd[k & 1] != 0;
+      const int* first_odd = bars->first_odd[k & 1] + quarter * 16;
+      if (Y) {
+        uint32_t near[16], state[16];
+        tmem_ld16(lanes + TM_NEAR + quarter * 16, near);
+        tmem_ld16(lanes + TM_STATE + quarter * 16, state);
+        const uint64_t ec = dup2(s.ec[row]);
+        tmem_wait_ld16(near);
+        tmem_wait_ld16(state);
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          unpack_f32x2(mul_f32x2(fma_f32x2(ec, pack_f32x2(__uint_as_float(state[2 * i]), __uint_as_float(state[2 * i + 1])),
+                                           pack_f32x2(__uint_as_float(near[2 * i]), __uint_as_float(near[2 * i + 1]))), gate[i]), y[2 * i], y[2 * i + 1]);
+        if (any_odd) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (row >= first_odd[i]) y[i] = NAN;
+        }
+        if (on) {
+          const size_t to = (size_t(r.q0) + t) * c.ld_y + h * NH + quarter * 16;
+          if (!a.y_vec) {                                      // (no 32-byte boundary)
+            for (int i = 0; i < 16; ++i) store_row(c.y, c.y_dtype, to + i, y[i], c.status);
+          } else if (c.y_dtype == CHUNK_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(reinterpret_cast<float*>(c.y) + to)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          } else {
+            uint32_t o[8];
+            if (c.y_dtype == CHUNK_BF16) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = pack_f16_sat(y[2 * i], y[2 * i + 1], c.status);
+            }
+            uint16_t* d = reinterpret_cast<uint16_t*>(c.y) + to;
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(d), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]),
+                         "r"(o[6]), "r"(o[7]) : "memory");
+          }
+        }
+        __syncwarp();
+      }
+      // ---- the state
+      {
+        uint32_t next[16], rest[16];
+        tmem_ld16(lanes + TM_NEXT + quarter * 16, next);
+        tmem_ld16(lanes + TM_NEXT + 64 + quarter * 16, rest);
+        const float total = s.total;
+        tmem_wait_ld16(next);
+        tmem_wait_ld16(rest);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = fmaf(total, S[i], __uint_as_float(next[i]) + __uint_as_float(rest[i]));
+        if (any_odd) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (first_odd[i] < len) S[i] = NAN;
+        }
+        if (Y && ci + 1 < chunks) put_state();
+        if (keeps) {
+#pragma unroll
+          for (int p = 0; p < 16; ++p) __stcs(mem + p * NS, S[p]);
+        }
+      }
+      tc_fence_before();
+    }
+    // ---- the carried rows of this head's channels, and of its group's B and C for the group's first head, once everyone has read them
+    __syncthreads();
+    if (*stop) break;
+    const int K1 = c.d_conv - 1;
+    if (r.stores() && K1 > 0) {
+      const int width = NH + (h % (c.H / c.G) == 0 ? 2 * NS : 0);
+      TI* carried = reinterpret_cast<TI*>(c.conv_state) + size_t(r.slot) * K1 * c.d_xBC;
+      const TI* rows = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + c.Di;
+      if (tid < width) {
+        const int ch = tid < NH ? h * NH + tid : tid < NH + NS ? c.Di + g * NS + tid - NH : c.Di + (c.G + g) * NS + tid - NH - NS;
+        TI old[3];
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+          const int from = r.keep + j - K1;
+          old[j] = TI(0.f);
+          if (j < K1 && (from >= 0 || !r.fresh)) old[j] = from >= 0 ? rows[size_t(from) * c.ld_x + ch] : carried[size_t(from + K1) * c.d_xBC + ch];
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (j < K1) carried[size_t(j) * c.d_xBC + ch] = old[j];
       }
     }
   }
-done:
-#undef WAIT
-#undef WAIT_ONE
-  __syncwarp();
+  // (a copy that was asked for has landed before the block ends)
   tc_fence_before();
   __syncthreads();
+  if (*stop && tid == 0) {
+    mbar_wait(smem_u32(&bars->b_full), k & 1, 100000000ull);
+    if (Y) mbar_wait(smem_u32(&bars->scores_full), k & 1, 100000000ull);
+  }
+  __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+template <typename TI, bool VEC>
+cudaError_t launch_vec(const LongArgs& a, cudaStream_t stream) {
+  const ChunkScanCall& c = a.c;
+  static std::atomic<uint32_t> ready{0};                     // devices on which the kernels have been told their shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 32 || !(ready.load() >> dev & 1u)) {
+    e = cudaFuncSetAttribute(scan_prep_kernel<TI, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, PREP_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(scan_long_kernel<TI, true, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, LONG_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(scan_long_kernel<TI, false, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, LONG_SMEM);
+    if (e != cudaSuccess) return e;
+    if (dev < 32) ready.fetch_or(1u << dev);
+  }
+  const long long chunks = (long long)(scan_max_chunks(c.T, c.B)) * c.G, heads = (long long)(scan_max_long(c.T, c.B)) * c.H;
+  e = launch_pdl(scan_prep_kernel<TI, VEC>, dim3(unsigned(chunks < 148 ? chunks : 148)), dim3(256), PREP_SMEM, stream, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(c.y ? scan_long_kernel<TI, true, VEC> : scan_long_kernel<TI, false, VEC>, dim3(unsigned(heads < 148 ? heads : 148)), dim3(LONG_THREADS),
+                    LONG_SMEM, stream, a);
 }
 
 template <typename TI>
 cudaError_t launch_for(LongArgs a, cudaStream_t stream) {
   const ChunkScanCall& c = a.c;
   auto on = [](const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; };
-  a.vec = c.Di % 4 == 0 && c.ld_x % 4 == 0 && on(c.x, 4 * sizeof(TI)) && on(c.conv_state, 4 * sizeof(TI)) ? 1 : 0;
   const int item = c.y_dtype == CHUNK_F32 ? 4 : 2;
-  a.y_vec = c.y && on(c.y, 16) && c.ld_y % (16 / item) == 0 ? 1 : 0;
-  static std::atomic<uint32_t> ready{0};                     // devices on which the kernels have been told their shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 32 || !(ready.load() >> dev & 1u)) {
-    e = cudaFuncSetAttribute(scan_prep_kernel<TI>, cudaFuncAttributeMaxDynamicSharedMemorySize, PREP_SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(scan_long_kernel<TI, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, LONG_SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(scan_long_kernel<TI, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, LONG_SMEM);
-    if (e != cudaSuccess) return e;
-    if (dev < 32) ready.fetch_or(1u << dev);
-  }
-  const long long chunks = (long long)(scan_max_chunks(c.T, c.B)) * c.G, heads = (long long)(scan_max_long(c.T, c.B)) * c.H;
-  e = launch_pdl(scan_prep_kernel<TI>, dim3(unsigned(chunks < 148 ? chunks : 148)), dim3(256), PREP_SMEM, stream, a);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(c.y ? scan_long_kernel<TI, true> : scan_long_kernel<TI, false>, dim3(unsigned(heads < 148 ? heads : 148)), dim3(LONG_THREADS), LONG_SMEM,
-                    stream, a);
+  a.y_vec = c.y && on(c.y, 32) && c.ld_y % (32 / item) == 0 ? 1 : 0;
+  a.z_vec = sizeof(TI) == 2 && on(c.x, 32) && c.ld_x % 16 == 0 ? 1 : 0;
+  const bool vec = c.Di % 4 == 0 && c.ld_x % 4 == 0 && on(c.x, 4 * sizeof(TI)) && on(c.conv_state, 4 * sizeof(TI));
+  return vec ? launch_vec<TI, true>(a, stream) : launch_vec<TI, false>(a, stream);
 }
 
 }  // namespace
