@@ -6,10 +6,12 @@
 //   z <- z + bias;   z <- -infinity where the row's bits forbid the token
 // Bound by memory: every logit is read and written once (in place: only what changes).  A block takes a slice of the vocabulary and some rows of one
 // request.  It counts the request's tokens that fall into the slice in shared memory (whole numbers, so that the order of the additions does not
-// matter), marks the tokens that any rule but the bits touches in a bitmap, and then streams the rows: a 16-byte word of logits costs one look at the
-// bitmap and one at the allowed bits, and the counts are read where a bit is set.  Between two rows the draft in front of the second is counted.
+// matter) and lists those that any rule but the bits touches.  A row is then streamed in 16-byte words, which knows of the allowed bits alone, and the
+// listed tokens are put right behind it: every warp has some of them, and with the rules inside the stream it is bound by its instructions (32 requests,
+// 17 rows of 128 256, texts of 512 to 8192 tokens: 246 us).  Between two rows the draft in front of the second is counted.
 #include "chunk_scan.cuh"
 
+#include <atomic>
 #include <climits>
 #include <type_traits>
 
@@ -19,14 +21,15 @@ namespace {
 
 constexpr int RULE_THREADS = 256;
 constexpr int MOST_ROWS = 32;                     // of a block
-constexpr int RULE_AHEAD = 4;                      // 16-byte words of a thread under way
+constexpr int RULE_AHEAD = 4;                     // 16-byte words of a row that a thread has
 constexpr uint32_t IN_PROMPT = 0x80000000u;       // a token's word: said in the prompt, bias entry + 1, times said since
 constexpr int BIAS_SHIFT = 20;
 constexpr uint32_t BIAS_BITS = 0x7ff, COUNT_BITS = (1u << BIAS_SHIFT) - 1;
 
 struct RuleArgs {
   LogitsCall c;
-  int slice, slices, rows;                        // tokens of a slice, slices, rows of a block
+  int slice, slices, rows;                        // tokens of a slice (at most 2^16), slices, rows of a block
+  int biases;                                     // room for biases, in multiples of four
   int tables;                                     // penalties or biases are asked for: counts are needed
 };
 
@@ -56,16 +59,18 @@ __device__ __forceinline__ float ruled(float z, uint32_t word, const Rules& u, c
   return e ? z + bias[e - 1] : z;
 }
 
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(RULE_THREADS) adjust_logits_kernel(RuleArgs a) {
+// STAGED: with tables and out of place, the rows come through shared memory, the next one under way, so that the listed tokens find theirs there.
+template <typename TI, typename TO, bool STAGED>
+__global__ void __launch_bounds__(RULE_THREADS, 4) adjust_logits_kernel(RuleArgs a) {
   constexpr int VEC = 16 / sizeof(TI);
   const LogitsCall& c = a.c;
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) uint32_t table[];          // [slice] words of the tokens
-  uint32_t* marked = table + a.slice;                        // [slice / 32] bits
-  float* bias = reinterpret_cast<float*>(marked + a.slice / 32);
-  __shared__ int s_draft[MOST_ROWS], s_mask[MOST_ROWS];
+  uint16_t* list = reinterpret_cast<uint16_t*>(table + a.slice);       // [slice] those that are not zero
+  float* bias = reinterpret_cast<float*>(list + a.slice);
+  uint8_t* stage = reinterpret_cast<uint8_t*>(bias + a.biases);                  // two rows of the slice, then two of its allowed bits
+  __shared__ int s_draft[MOST_ROWS], s_mask[MOST_ROWS], listed;
   const int tid = threadIdx.x, lane = tid & 31;
   const int lo = (blockIdx.x % a.slices) * a.slice, hi = min(lo + a.slice, c.V);
 
@@ -79,8 +84,8 @@ __global__ void __launch_bounds__(RULE_THREADS) adjust_logits_kernel(RuleArgs a)
   const int b = item.b, first = item.first, t0 = item.q0 + first, rows = min(a.rows, item.n - first);
   Rules u{};
   if (a.tables) {
-    for (int i = tid; i < a.slice; i += RULE_THREADS) table[i] = 0;
-    for (int i = tid; i < a.slice / 32; i += RULE_THREADS) marked[i] = 0;
+    for (int i = tid; i < a.slice / 4; i += RULE_THREADS) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) listed = 0;
   }
   // row i's rule, and the draft in front of it (-1: none that counts)
   if (tid < rows) {
@@ -119,10 +124,10 @@ __global__ void __launch_bounds__(RULE_THREADS) adjust_logits_kernel(RuleArgs a)
       if (report && tid == 0 && (l < 0 || l > c.history_stride || p < 0 || p > len)) ++bad;
     }
     auto count = [&](int id, int j) {
-      if (id >= lo && id < hi) {
-        if (j < prompt) atomicOr(&table[id - lo], IN_PROMPT);
-        else atomicAdd(&table[id - lo], 1u);
-        atomicOr(&marked[(id - lo) >> 5], 1u << ((id - lo) & 31));
+      if (uint32_t(id - lo) < uint32_t(hi - lo)) {
+        // (the first one to find a token lists it: in any order, no result depends on it)
+        const uint32_t had = j < prompt ? atomicOr(&table[id - lo], IN_PROMPT) : atomicAdd(&table[id - lo], 1u);
+        if (!had) list[atomicAdd(&listed, 1)] = uint16_t(id - lo);
       } else if (report && (id < 0 || id >= c.V)) ++bad;
     };
     // 16-byte loads from the first boundary on
@@ -177,8 +182,8 @@ __global__ void __launch_bounds__(RULE_THREADS) adjust_logits_kernel(RuleArgs a)
         if (owner) {
           bias[at] = sum;
           if (!had) {
+            if (!table[id - lo]) list[atomicAdd(&listed, 1)] = uint16_t(id - lo);
             table[id - lo] |= uint32_t(at + 1) << BIAS_SHIFT;
-            atomicOr(&marked[(id - lo) >> 5], 1u << ((id - lo) & 31));
           }
         }
         used += __popc(fresh);
@@ -192,82 +197,170 @@ __global__ void __launch_bounds__(RULE_THREADS) adjust_logits_kernel(RuleArgs a)
   // ---- the rows
   const int mask_words = (c.V + 31) / 32;
   const bool in_place = c.in == c.out;
-  for (int i = 0; i < rows; ++i) {
-    const int t = t0 + i;
-    const int draft = i && a.tables ? s_draft[i] : -1;
+  // a row as the block sees it: 16-byte words from its first boundary in the slice on, single logits in front of them and behind
+  struct Row {
+    const uint32_t* allowed;
+    const TI* src;
+    TO* dst;
+    int from, words;
+  };
+  const TI* src = reinterpret_cast<const TI*>(c.in) + size_t(t0) * c.ld_in;
+  TO* dst = reinterpret_cast<TO*>(c.out) + size_t(t0) * c.ld_out;
+  auto row_of = [&](int i) {                                 // (rows come one after another)
+    Row r;
+    r.allowed = s_mask[i] < 0 ? nullptr : c.mask + size_t(s_mask[i]) * c.mask_stride;
+    r.src = src;
+    r.dst = dst;
+    src += c.ld_in;
+    dst += c.ld_out;
+    r.from = min(hi, lo + int((16 - (reinterpret_cast<uintptr_t>(r.src + lo) & 15)) & 15) / int(sizeof(TI)));
+    r.words = in_place && !r.allowed ? 0 : (hi - r.from) / VEC;
+    return r;
+  };
+  constexpr uint32_t ALL = (1u << VEC) - 1u;
+  Word<TI, VEC> x[RULE_AHEAD];
+  uint32_t out[RULE_AHEAD];                                  // tokens of the word that are not allowed
+  auto load = [&](const Row& r) {
+#pragma unroll
+    for (int e = 0; e < RULE_AHEAD; ++e) {
+      const int w = tid + e * RULE_THREADS, v = r.from + w * VEC;
+      out[e] = 0;
+      if (w >= r.words) continue;
+      if (r.allowed) out[e] = ~bits_from(r.allowed, v, mask_words) & ALL;
+      x[e] = *reinterpret_cast<const Word<TI, VEC>*>(r.src + v);          // (without waiting for the bits)
+    }
+  };
+  auto store = [&](const Row& r) {
+    const bool out_words = (reinterpret_cast<uintptr_t>(r.dst + r.from) & (sizeof(Word<TO, VEC>) - 1)) == 0;
+#pragma unroll
+    for (int e = 0; e < RULE_AHEAD; ++e) {
+      const int w = tid + e * RULE_THREADS, v = r.from + w * VEC;
+      if (e * RULE_THREADS >= r.words) break;
+      if (w >= r.words || (in_place && !out[e])) continue;
+      Word<TO, VEC> y;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        if constexpr (std::is_same<TI, TO>::value) y.v[j] = x[e].v[j];
+        else y.v[j] = from_f32<TO>(to_f32(x[e].v[j]), c.status);
+      }
+      if (r.allowed) {                                       // (of the whole row: no branch for each word)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if ((out[e] >> j) & 1u) y.v[j] = from_f32<TO>(-INFINITY, c.status);
+      }
+      if (out_words) {
+        // (eight 32-bit logits in one store: two of 16 bytes would each leave every other half of a sector to the other one)
+        if constexpr (sizeof(y) == 32)
+          asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(r.dst + v), "f"(float(y.v[0])), "f"(float(y.v[1])), "f"(float(y.v[2])),
+                       "f"(float(y.v[3])), "f"(float(y.v[4 % VEC])), "f"(float(y.v[5 % VEC])), "f"(float(y.v[6 % VEC])), "f"(float(y.v[7 % VEC])) : "memory");
+        else
+          *reinterpret_cast<uint4*>(r.dst + v) = *reinterpret_cast<const uint4*>(&y);
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) r.dst[v + j] = y.v[j];
+      }
+    }
+    // (at most 7 logits on either side)
+    const int rest = r.from + (hi - r.from) / VEC * VEC;
+    if ((r.from > lo || rest < hi) && (!in_place || r.allowed)) {
+      const int single = tid < 8 ? lo + tid : rest + tid - 8;
+      if (tid < 16 && (tid < 8 ? single < r.from : single < hi)) {
+        if (r.allowed && !((r.allowed[single >> 5] >> (single & 31)) & 1u)) r.dst[single] = from_f32<TO>(-INFINITY, c.status);
+        else if (!in_place) r.dst[single] = from_f32<TO>(to_f32(r.src[single]), c.status);
+      }
+    }
+  };
+  auto listed_tokens = [&](int i, const Row& r, const TI* staged) {
+    const int draft = i ? s_draft[i] : -1;                   // with the draft in front of this row among them
     if (draft >= lo && draft < hi) {                         // (the same for the whole block)
-      __syncthreads();
       if (tid == 0) {
+        if (table[draft - lo] == 0) list[listed++] = uint16_t(draft - lo);
         table[draft - lo] += 1;
-        marked[(draft - lo) >> 5] |= 1u << ((draft - lo) & 31);
       }
       __syncthreads();
     }
-    const uint32_t* allowed = s_mask[i] < 0 ? nullptr : c.mask + size_t(s_mask[i]) * c.mask_stride;
-    if (in_place && !a.tables && !allowed) continue;
-    const TI* src = reinterpret_cast<const TI*>(c.in) + size_t(t) * c.ld_in;
-    TO* dst = reinterpret_cast<TO*>(c.out) + size_t(t) * c.ld_out;
-    auto one = [&](int v) {
-      const bool touched = a.tables && ((marked[(v - lo) >> 5] >> ((v - lo) & 31)) & 1u);
-      const bool out = allowed && !((allowed[v >> 5] >> (v & 31)) & 1u);
-      if (in_place && !touched && !out) return;
-      if (out) { dst[v] = from_f32<TO>(-INFINITY, c.status); return; }
-      const TI x = src[v];
-      if (touched) dst[v] = from_f32<TO>(ruled(to_f32(x), table[v - lo], u, bias), c.status);
-      else if constexpr (std::is_same<TI, TO>::value) dst[v] = x;
-      else dst[v] = from_f32<TO>(to_f32(x), c.status);
+    const int many = listed;
+    for (int l = tid; l < many; l += RULE_THREADS) {
+      const int at = list[l], v = lo + at, w = v - r.from;
+      if (r.allowed && !((r.allowed[v >> 5] >> (v & 31)) & 1u)) continue;
+      const TI z = STAGED && w >= 0 && w < r.words * VEC ? staged[w] : r.src[v];
+      r.dst[v] = from_f32<TO>(ruled(to_f32(z), table[at], u, bias), c.status);
+    }
+  };
+  Row row = row_of(0);
+  if constexpr (STAGED) {
+    constexpr int BYTES = RULE_AHEAD * RULE_THREADS * 16;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(stage + 2 * BYTES);
+    const int bit_words = (hi - lo + 31) / 32;
+    auto fetch = [&](const Row& r, int buf) {
+      for (int w = tid; w < r.words; w += RULE_THREADS) cp_async16(smem_u32(stage + buf * BYTES + w * 16), r.src + r.from + w * VEC, true);
+      if (r.allowed && tid < bit_words)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(bits + buf * (a.slice / 32) + tid)), "l"(r.allowed + lo / 32 + tid) : "memory");
+      cp_async_commit();
     };
-    // single logits up to the row's first 16-byte boundary in the slice and behind its last, 16-byte words between
-    const int from = min(hi, lo + int((16 - (reinterpret_cast<uintptr_t>(src + lo) & 15)) & 15) / int(sizeof(TI)));
-    const int words = (hi - from) / VEC, rest = from + words * VEC;
-    const bool out_words = (reinterpret_cast<uintptr_t>(dst + from) & 15) == 0;
-    if (lo + tid < from) one(lo + tid);
-    if (rest + tid < hi) one(rest + tid);
-    for (int w = tid; w < words; w += RULE_AHEAD * RULE_THREADS) {
-      Word<TI, VEC> x[RULE_AHEAD];
-      uint32_t touched[RULE_AHEAD], out[RULE_AHEAD];
-      constexpr uint32_t ALL = (1u << VEC) - 1u;
+    fetch(row, 0);
+    for (int i = 0; i < rows; ++i) {
+      Row now = row;
+      const bool ruled_out = now.allowed != nullptr;
+      now.allowed = bits + (i & 1) * (a.slice / 32) - lo / 32;
+      if (!ruled_out) now.allowed = nullptr;
+      if (i + 1 < rows) {
+        row = row_of(i + 1);
+        fetch(row, (i + 1) & 1);                             // (its place was read before the barrier at the row's end)
+      } else {
+        cp_async_commit();
+      }
+      cp_async_wait<1>();                                    // (a thread streams the words that it has fetched itself; the bits are others')
+      if (ruled_out) __syncthreads();
+      const uint8_t* mine = stage + (i & 1) * BYTES;
 #pragma unroll
       for (int e = 0; e < RULE_AHEAD; ++e) {
-        const int we = w + e * RULE_THREADS;
-        touched[e] = out[e] = 0;
-        x[e] = Word<TI, VEC>{};
-        if (we >= words) continue;
-        const int v = from + we * VEC;
-        if (a.tables) touched[e] = bits_from(marked, v - lo, a.slice / 32) & ALL;
-        if (allowed) out[e] = ~bits_from(allowed, v, mask_words) & ALL;
-        touched[e] &= ~out[e];                               // (what is forbidden is nothing else)
-        if (in_place ? ((touched[e] | out[e]) && out[e] != ALL) : out[e] != ALL) x[e] = *reinterpret_cast<const Word<TI, VEC>*>(src + v);
+        const int w = tid + e * RULE_THREADS;
+        out[e] = 0;
+        if (e * RULE_THREADS >= now.words) break;
+        if (w >= now.words) continue;
+        if (now.allowed) out[e] = ~bits_from(now.allowed, now.from + w * VEC, lo / 32 + bit_words) & ALL;
+        x[e] = *reinterpret_cast<const Word<TI, VEC>*>(mine + w * 16);
       }
-#pragma unroll
-      for (int e = 0; e < RULE_AHEAD; ++e) {
-        const int we = w + e * RULE_THREADS;
-        if (we >= words) continue;
-        if (in_place && !(touched[e] | out[e])) continue;
-        const int v = from + we * VEC;
-        Word<TO, VEC> y;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          if constexpr (std::is_same<TI, TO>::value) y.v[j] = x[e].v[j];
-          else y.v[j] = from_f32<TO>(to_f32(x[e].v[j]), c.status);
-          if ((touched[e] >> j) & 1u) y.v[j] = from_f32<TO>(ruled(to_f32(x[e].v[j]), table[v + j - lo], u, bias), c.status);
-          if ((out[e] >> j) & 1u) y.v[j] = from_f32<TO>(-INFINITY, c.status);
-        }
-        if (out_words) {
-#pragma unroll
-          for (int k = 0; k < int(sizeof(TO)) * VEC / 16; ++k) reinterpret_cast<uint4*>(dst + v)[k] = reinterpret_cast<const uint4*>(&y)[k];
-        } else {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) dst[v + j] = y.v[j];
-        }
+      store(now);
+      __syncthreads();                                       // (the row is streamed, and all of it is in shared memory for everyone)
+      listed_tokens(i, now, reinterpret_cast<const TI*>(mine));
+      __syncthreads();
+    }
+  } else {
+    load(row);
+    for (int i = 0; i < rows; ++i) {
+      store(row);
+      const Row now = row;
+      if (i + 1 < rows) {                                    // the next row is under way while the listed tokens of this one are dealt with
+        row = row_of(i + 1);
+        load(row);
       }
+      if (!a.tables) continue;
+      __syncthreads();                                       // (the row is streamed, the listed tokens of the one before are done)
+      listed_tokens(i, now, nullptr);
     }
   }
 }
 
+template <typename TI, typename TO, bool STAGED>
+cudaError_t launch_as(const RuleArgs& a, unsigned blocks, size_t smem, cudaStream_t stream) {
+  if (smem > 40 * 1024) {                                    // (with what the kernel has besides, up to 48 KB go without asking)
+    static std::atomic<uint32_t> ready{0};                   // devices on which the kernel has been told how much it may take
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 32 || !(ready.load() >> dev & 1u)))
+      e = cudaFuncSetAttribute(adjust_logits_kernel<TI, TO, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+    if (e != cudaSuccess) return e;
+    if (dev < 32) ready.fetch_or(1u << dev);
+  }
+  return launch_pdl(adjust_logits_kernel<TI, TO, STAGED>, dim3(blocks), dim3(RULE_THREADS), smem, stream, a);
+}
 template <typename TI, typename TO>
-cudaError_t launch_for(const RuleArgs& a, unsigned blocks, size_t smem, cudaStream_t stream) {
-  return launch_pdl(adjust_logits_kernel<TI, TO>, dim3(blocks), dim3(RULE_THREADS), smem, stream, a);
+cudaError_t launch_for(const RuleArgs& a, unsigned blocks, cudaStream_t stream) {
+  const size_t smem = a.tables ? size_t(a.slice) * 6 + size_t(a.biases) * 4 : 0;
+  return a.tables && a.c.in != a.c.out ? launch_as<TI, TO, true>(a, blocks, smem + 2 * (RULE_AHEAD * RULE_THREADS * 16 + a.slice / 8), stream)
+                                       : launch_as<TI, TO, false>(a, blocks, smem, stream);
 }
 
 }  // namespace
@@ -278,24 +371,27 @@ cudaError_t adjust_logits_launch(const LogitsCall& c, cudaStream_t stream) {
   a.tables = (c.repetition || c.frequency || c.presence) && (c.history || c.drafts) ? 1 : 0;
   if (!a.tables) a.c.history = a.c.drafts = nullptr;
   if (c.bias_ids) a.tables = 1;
-  // A block reads its request's whole text, so its slice is wide and its rows are many while there are four blocks for every SM.
-  a.slice = 8192;
-  a.rows = MOST_ROWS;
+  a.biases = c.bias_ids ? (c.n_bias + 3) / 4 * 4 : 0;
+  // With tables a block reads its request's whole text, so its slice is wide and its rows are many while there are several waves of blocks.  Without,
+  // nothing is shared between its rows.
+  a.slice = RULE_AHEAD * RULE_THREADS * 4;                   // (a row of 32-bit logits; 16-bit ones take half the words)
+  if (!a.tables && c.in_dtype != CHUNK_F32) a.slice *= 2;
+  a.rows = a.tables ? MOST_ROWS : 1;
   auto blocks = [&] {
     a.slices = (c.V + a.slice - 1) / a.slice;
     return (long long)(a.slices) * (c.cu_q ? c.T / a.rows + (c.B < c.T ? c.B : c.T) : c.T);
   };
+  while (a.rows > 8 && blocks() < 8 * 148) a.rows /= 2;
   while (a.rows > 4 && blocks() < 4 * 148) a.rows /= 2;
   while (a.slice > 1024 && blocks() < 4 * 148) a.slice /= 2;
   while (a.rows > 1 && blocks() < 4 * 148) a.rows /= 2;
   const long long n = blocks();
   if (n > INT_MAX) return cudaErrorInvalidConfiguration;
-  const size_t smem = a.tables ? size_t(a.slice) * 4 + a.slice / 8 + (c.bias_ids ? size_t(c.n_bias) * 4 : 0) : 0;
-  if (c.in_dtype == CHUNK_F32) return launch_for<float, float>(a, unsigned(n), smem, stream);
+  if (c.in_dtype == CHUNK_F32) return launch_for<float, float>(a, unsigned(n), stream);
   if (c.in_dtype == CHUNK_F16)
-    return c.out_dtype == CHUNK_F32 ? launch_for<__half, float>(a, unsigned(n), smem, stream) : launch_for<__half, __half>(a, unsigned(n), smem, stream);
-  return c.out_dtype == CHUNK_F32 ? launch_for<__nv_bfloat16, float>(a, unsigned(n), smem, stream)
-                                  : launch_for<__nv_bfloat16, __nv_bfloat16>(a, unsigned(n), smem, stream);
+    return c.out_dtype == CHUNK_F32 ? launch_for<__half, float>(a, unsigned(n), stream) : launch_for<__half, __half>(a, unsigned(n), stream);
+  return c.out_dtype == CHUNK_F32 ? launch_for<__nv_bfloat16, float>(a, unsigned(n), stream)
+                                  : launch_for<__nv_bfloat16, __nv_bfloat16>(a, unsigned(n), stream);
 }
 
 }  // namespace hspec
