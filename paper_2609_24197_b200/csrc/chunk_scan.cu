@@ -19,19 +19,12 @@ namespace {
 constexpr int CONV_THREADS = 256;
 constexpr int CONV_TILE = 8;         // rows of a block
 
-struct ScanScratch {
-  float* xbc;                        // [.., pitch] convolved rows
-  float2* step;                      // [.., H] dt and the decay exp(dt A)
-  int pitch;
-  int few;                           // requests with more rows than this go another way
-  int apart;                         // 0: row t of the chunk lies at t; else row i of request b at b * apart + i
-  __device__ __forceinline__ size_t row(int b, int q0, int i) const { return apart ? size_t(b) * apart + i : size_t(q0) + i; }
-};
-
 struct ConvArgs {
   ChunkScanCall c;
   ScanScratch s;
+  int channels;                      // that the channel blocks take: all of them, or those of x (the group blocks take the others)
   int ch_blocks, dt_blocks;          // blocks of an item: channels, then steps
+  int group_blocks;                  // behind the items: one for every request and group
   int32_t *plan, *list, *chunks;     // of the requests with many rows (LongArgs); null: there are none
   int max_long, max_chunks;
 };
@@ -139,12 +132,91 @@ __device__ __forceinline__ void load_wide(const T* p, float (&x)[W]) {
   for (int e = 0; e < W; ++e) x[e] = to_f32(w.v[e]);
 }
 
+// B and C of a group, for a request with up to SCAN_FEW rows (N = 128): a thread a channel.  B goes into the scratch's rows, C into its two parts; their
+// products by pairs of rows.
+constexpr int CB_PITCH = 128 + 4;
+template <typename TI, int K>
+__device__ void rows_of_group(const ConvArgs& a, int b, int g) {
+  const ChunkScanCall& c = a.c;
+  extern __shared__ __align__(16) float rows_sm[];           // B, then C: [SCAN_FEW][CB_PITCH] each
+  const ScanRequest r = scan_request(c, b);
+  const int n = scan_upto(c, r), tid = threadIdx.x, e = tid & 127;
+  const bool isC = tid >= 128;
+  if (n > a.s.few || (n == 0 && !r.stores())) return;
+  const int ch = c.Di + ((isC ? c.G : 0) + g) * 128 + e;
+  float w[K], raw[K];
+  const float bias = c.conv_b[ch];
+#pragma unroll
+  for (int j = 0; j < K; ++j) w[j] = c.conv_w[size_t(ch) * K + j];
+  TI* carried = reinterpret_cast<TI*>(c.conv_state) + (r.slot < 0 ? 0 : size_t(r.slot) * (K - 1) * c.d_xBC) + ch;
+  const TI* src = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + c.Di + ch;
+  TI old[K];
+#pragma unroll
+  for (int j = 0; j < K - 1; ++j) {
+    old[j] = r.fresh ? TI(0.f) : carried[size_t(j) * c.d_xBC];
+    raw[j] = to_f32(old[j]);
+  }
+  if (r.stores()) {
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+      const int from = r.keep + j - (K - 1);
+      TI v = TI(0.f);
+      if (from >= 0) v = src[size_t(from) * c.ld_x];
+#pragma unroll
+      for (int o = 0; o < K - 1; ++o)
+        if (from < 0 && o == r.keep + j) v = old[o];
+      carried[size_t(j) * c.d_xBC] = v;
+    }
+  }
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    TI next[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) next[i] = src[size_t(min(i0 + i, n - 1)) * c.ld_x];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i >= n) break;
+      raw[K - 1] = to_f32(next[i]);
+      float v = bias;
+#pragma unroll
+      for (int j = 0; j < K; ++j) v = fmaf(w[j], raw[j], v);
+#pragma unroll
+      for (int j = 0; j < K - 1; ++j) raw[j] = raw[j + 1];
+      v = silu_f32(v);
+      rows_sm[((isC ? SCAN_FEW : 0) + i0 + i) * CB_PITCH + e] = v;
+      const size_t row = a.s.row(b, r.q0, i0 + i);
+      if (isC) {
+        const __nv_bfloat16 hi = __float2bfloat16_rn(v);
+        __nv_bfloat16* parts = reinterpret_cast<__nv_bfloat16*>(a.s.c_parts) + (row * c.G + g) * 256 + e;
+        parts[0] = hi;
+        parts[128] = __float2bfloat16_rn(v - __bfloat162float(hi));
+      } else {
+        a.s.xbc[row * a.s.pitch + ch] = v;
+      }
+    }
+  }
+  if (!c.y) return;
+  __syncthreads();
+  for (int pair = tid; pair < n * n; pair += CONV_THREADS) {
+    const int t = pair / n, s = pair % n;
+    if (s > t) continue;
+    const float4* ct = reinterpret_cast<const float4*>(rows_sm + (SCAN_FEW + t) * CB_PITCH);
+    const float4* bs = reinterpret_cast<const float4*>(rows_sm + s * CB_PITCH);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+      const float4 x = ct[i], y = bs[i];
+      sum.x = fmaf(x.x, y.x, sum.x); sum.y = fmaf(x.y, y.y, sum.y); sum.z = fmaf(x.z, y.z, sum.z); sum.w = fmaf(x.w, y.w, sum.w);
+    }
+    a.s.cb[((size_t(b) * c.G + g) * SCAN_FEW + t) * SCAN_FEW + s] = (sum.x + sum.y) + (sum.z + sum.w);
+  }
+}
+
 template <typename TI, int W, int K>
 __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
   const ChunkScanCall& c = a.c;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1) % blocks;
+  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1 - a.group_blocks) % blocks;
   if (blockIdx.x == 0) {
     for (int b = tid; b < c.B; b += CONV_THREADS) {
       const ScanRequest r = scan_request(c, b);
@@ -154,7 +226,11 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
     if (a.plan) plan_long(a);
     return;
   }
-  const ChunkItem item = few_item(c, a.s.few, (blockIdx.x - 1) / blocks, tid & 31);
+  if (int(blockIdx.x) <= a.group_blocks) {
+    rows_of_group<TI, K>(a, (blockIdx.x - 1) / c.G, (blockIdx.x - 1) % c.G);
+    return;
+  }
+  const ChunkItem item = few_item(c, a.s.few, (blockIdx.x - 1 - a.group_blocks) / blocks, tid & 31);
   if (item.b < 0) return;
   const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
   const size_t out0 = a.s.row(item.b, item.q0, item.first);
@@ -171,7 +247,7 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
   }
   const ScanRequest r = scan_request(c, item.b);
   const int ch = (part * CONV_THREADS + tid) * W;
-  if (ch >= c.d_xBC) return;
+  if (ch >= a.channels) return;
   float w[K][W], bias[W], raw[K - 1 + CONV_TILE][W];
   // (a thread's weights are W rows of K)
 #pragma unroll
@@ -233,13 +309,6 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
 // The states through the rows.  A group of L lanes has PR rows of a head's state [P, N]: lane l of the group the elements n = 4 (l + L k) .. + 3.
 constexpr int STATE_THREADS = 128;
 constexpr int STATE_TILE = 8;        // tokens that are fetched together
-
-struct StateArgs {
-  ChunkScanCall c;
-  ScanScratch s;
-  int p_blocks, p_block;             // blocks of a head, rows of its state in each
-  int np;                            // padded N: row pitch of B and C in shared memory
-};
 
 template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
 __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) {
@@ -453,7 +522,7 @@ cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
 
 template <typename TI, int W, int K>
 cudaError_t launch_rows_k(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
-  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), 0, stream, a);
+  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), a.group_blocks ? size_t(2) * SCAN_FEW * CB_PITCH * 4 : 0, stream, a);
 }
 template <typename TI, int W>
 cudaError_t launch_rows_w(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
@@ -471,32 +540,38 @@ cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   // words of four row values, where all rows and both parts of a row start on their boundaries
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(TI)) == 0; };
   const bool wide = c.Di % 4 == 0 && c.d_xBC % 4 == 0 && c.ld_x % 4 == 0 && aligned(c.x) && aligned(c.conv_state);
-  a.ch_blocks = (c.d_xBC + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
+  a.channels = a.s.c_parts ? c.Di : c.d_xBC;
+  a.group_blocks = a.s.c_parts ? c.B * c.G : 0;
+  a.ch_blocks = (a.channels + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
   a.dt_blocks = (CONV_TILE * c.H + CONV_THREADS - 1) / CONV_THREADS;
   long long items = c.T / CONV_TILE + c.B;
   if (a.plan && items > (long long)(c.B) * (SCAN_FEW / CONV_TILE)) items = (long long)(c.B) * (SCAN_FEW / CONV_TILE);
-  const long long blocks = 1 + items * (a.ch_blocks + a.dt_blocks);
+  const long long blocks = 1 + a.group_blocks + items * (a.ch_blocks + a.dt_blocks);
   if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
   const cudaError_t e = wide ? launch_rows_w<TI, 4>(a, unsigned(blocks), stream) : launch_rows_w<TI, 1>(a, unsigned(blocks), stream);
   if (e != cudaSuccess) return e;
   StateArgs s{};
   s.c = c;
   s.s = a.s;
+  if (a.s.c_parts) return scan_block_launch(s, stream);
   return launch_states<TI>(s, stream);
 }
 
 // Where everything lies in the caller's scratch.
 struct Scratch {
-  size_t step, plan, list, chunks, images, total;
+  size_t step, c_parts, cb, plan, list, chunks, images, total;
   int pitch;
-  bool tensor;                       // requests with many rows go through the tensor cores
+  bool blocks, tensor;               // requests with few rows go through scan_block_kernel, those with many through the tensor cores
   Scratch(long long T, int B, int Di, int P, int N, int G) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     pitch = (Di + 2 * G * N + 3) / 4 * 4;
-    tensor = P == 64 && N == 128 && T > SCAN_FEW;
+    blocks = P == 64 && N == 128;
+    tensor = blocks && T > SCAN_FEW;
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
     step = up(rows * pitch * 4);
-    plan = step + up(rows * (Di / P) * 8);
+    c_parts = step + up(rows * (Di / P) * 8);
+    cb = c_parts + (blocks ? up(rows * G * N * 4) : 0);
+    plan = cb + (blocks ? up(size_t(B) * G * SCAN_FEW * SCAN_FEW * 4) : 0);
     list = plan + 256;
     chunks = list + (tensor ? up(size_t(scan_max_long(T, B)) * 8) : 0);
     images = chunks + (tensor ? up(size_t(scan_max_chunks(T, B)) * 8) : 0);
@@ -517,6 +592,10 @@ cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
   a.s.xbc = reinterpret_cast<float*>(ws);
   a.s.step = reinterpret_cast<float2*>(ws + at.step);
   a.s.few = INT_MAX;
+  if (at.blocks) {
+    a.s.c_parts = reinterpret_cast<uint16_t*>(ws + at.c_parts);
+    a.s.cb = reinterpret_cast<float*>(ws + at.cb);
+  }
   if (at.tensor) {
     a.s.few = SCAN_FEW;
     a.s.apart = c.T > (long long)(SCAN_FEW) * c.B ? SCAN_FEW : 0;

@@ -37,6 +37,27 @@ inline long long scan_max_long(long long T, int B) { return T / (SCAN_FEW + 1) <
 inline long long scan_max_chunks(long long T, int B) { return T / SCAN_CHUNK + 2 * scan_max_long(T, B); }
 cudaError_t scan_long_launch(const LongArgs& a, cudaStream_t stream);
 
+struct ScanScratch {
+  float* xbc;                        // [.., pitch] convolved rows
+  float2* step;                      // [.., H] dt and the decay exp(dt A)
+  // blocks of rows (scan_block_kernel) have their C apart, split into two bf16 parts, and the products C_t . B_s of a request's rows
+  uint16_t* c_parts;                 // [.., G, 2, N]; null: requests with few rows go through scan_state_kernel
+  float* cb;                         // [B, G, SCAN_FEW, SCAN_FEW]
+  int pitch;
+  int few;                           // requests with more rows than this go another way
+  int apart;                         // 0: row t of the chunk lies at t; else row i of request b at b * apart + i
+  __device__ __forceinline__ size_t row(int b, int q0, int i) const { return apart ? size_t(b) * apart + i : size_t(q0) + i; }
+};
+
+struct StateArgs {
+  ChunkScanCall c;
+  ScanScratch s;
+  int p_blocks, p_block;             // blocks of a head, rows of its state in each
+  int np;                            // padded N: row pitch of B and C in shared memory
+  int y_vec;                         // four outputs start on their boundary
+};
+cudaError_t scan_block_launch(const StateArgs& a, cudaStream_t stream);
+
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
