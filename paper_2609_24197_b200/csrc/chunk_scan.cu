@@ -22,15 +22,22 @@ constexpr int CONV_TILE = 8;         // rows of a block
 struct ConvArgs {
   ChunkScanCall c;
   ScanScratch s;
-  int channels;                      // that the channel blocks take: all of them, or those of x (the group blocks take the others)
   int ch_blocks, dt_blocks;          // blocks of an item: channels, then steps
-  int group_blocks;                  // behind the items: one for every request and group
   int32_t *plan, *list, *chunks;     // of the requests with many rows (LongArgs); null: there are none
   int max_long, max_chunks;
 };
 
-// Item `item`: CONV_TILE rows of a request that has few (one item at least, for what its carried rows need).  One warp.
-__device__ __forceinline__ ChunkItem few_item(const ChunkScanCall& c, int few, int item, int lane) {
+// The requests that say what cannot be.  One block.
+__device__ void count_bad(const ChunkScanCall& c) {
+  for (int b = threadIdx.x; b < c.B; b += CONV_THREADS) {
+    const ScanRequest r = scan_request(c, b);
+    if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], INT_MAX, c.T, INT_MAX) || (r.n > 0 && r.slot != (c.slots ? c.slots[b] : b)))
+      atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
+  }
+}
+
+// Item `item`: CONV_TILE rows of a request (one item at least, for what its carried rows need).  One warp.
+__device__ __forceinline__ ChunkItem few_item(const ChunkScanCall& c, int item, int lane) {
   int before = 0;
   for (int base = 0; base < c.B; base += 32) {
     int items = 0, q0 = 0, n = 0;
@@ -38,7 +45,7 @@ __device__ __forceinline__ ChunkItem few_item(const ChunkScanCall& c, int few, i
       const ScanRequest r = scan_request(c, base + lane);
       q0 = r.q0;
       n = scan_upto(c, r);
-      items = n > few ? 0 : max((n + CONV_TILE - 1) / CONV_TILE, 1);
+      items = max((n + CONV_TILE - 1) / CONV_TILE, 1);
     }
     int upto = items;
 #pragma unroll
@@ -62,9 +69,9 @@ __device__ __forceinline__ int chunks_of(const ChunkScanCall& c, const ScanReque
   const int upto = scan_upto(c, r), k = min(r.keep, upto);
   return (k + SCAN_CHUNK - 1) / SCAN_CHUNK + (upto - k + SCAN_CHUNK - 1) / SCAN_CHUNK;
 }
-__device__ void plan_long(const ConvArgs& a) {
+__device__ void plan_long(const ConvArgs& a, int* room) {     // room for 3 PLAN_SORT numbers
   const ChunkScanCall& c = a.c;
-  __shared__ int key[PLAN_SORT], who[PLAN_SORT], front[PLAN_SORT];
+  int *key = room, *who = room + PLAN_SORT, *front = room + 2 * PLAN_SORT;
   __shared__ int sums[2][CONV_THREADS / 32], totals[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int n_long = 0, n_chunks = 0;
@@ -132,13 +139,182 @@ __device__ __forceinline__ void load_wide(const T* p, float (&x)[W]) {
   for (int e = 0; e < W; ++e) x[e] = to_f32(w.v[e]);
 }
 
-// B and C of a group, for a request with up to SCAN_FEW rows (N = 128): a thread a channel.  B goes into the scratch's rows, C into its two parts; their
+template <typename TI, int W, int K>
+__global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
+  const ChunkScanCall& c = a.c;
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1) % blocks;
+  if (blockIdx.x == 0) {
+    count_bad(c);
+    return;
+  }
+  const ChunkItem item = few_item(c, (blockIdx.x - 1) / blocks, tid & 31);
+  if (item.b < 0) return;
+  const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
+  const size_t out0 = a.s.row(item.b, item.q0, item.first);
+  if (part >= a.ch_blocks) {
+    // ---- steps and decays
+    const int i = (part - a.ch_blocks) * CONV_THREADS + tid, h = i % c.H, r = i / c.H;
+    if (r < rows) {
+      const size_t t = t0 + r;
+      const float raw = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
+      const float dt = softplus_f32(raw + c.dt_bias[h]);
+      a.s.step[(out0 + r) * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
+    }
+    return;
+  }
+  const ScanRequest r = scan_request(c, item.b);
+  const int ch = (part * CONV_THREADS + tid) * W;
+  if (ch >= c.d_xBC) return;
+  float w[K][W], bias[W], raw[K - 1 + CONV_TILE][W];
+  // (a thread's weights are W rows of K)
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    bias[e] = c.conv_b[ch + e];
+#pragma unroll
+    for (int j = 0; j < K; ++j) w[j][e] = c.conv_w[size_t(ch + e) * K + j];
+  }
+  TI* carried = reinterpret_cast<TI*>(c.conv_state) + (r.slot < 0 ? 0 : size_t(r.slot) * (K - 1) * c.d_xBC) + ch;
+  const TI* src = reinterpret_cast<const TI*>(c.x) + size_t(t0) * c.ld_x + c.Di + ch;
+  if (item.first == 0) {
+    using V = Word<TI, W>;
+    V old[K - 1 > 0 ? K - 1 : 1];
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) {
+      if (r.fresh) old[j] = V{};
+      else old[j] = *reinterpret_cast<const V*>(carried + size_t(j) * c.d_xBC);
+#pragma unroll
+      for (int e = 0; e < W; ++e) raw[j][e] = to_f32(old[j].v[e]);
+    }
+    if (r.stores()) {
+#pragma unroll
+      for (int j = 0; j < K - 1; ++j) {
+        const int from = r.keep + j - (K - 1);             // the chunk's row that comes to place j; below zero: a carried one
+        V v{};
+        if (from >= 0) {
+          v = *reinterpret_cast<const V*>(src + size_t(from) * c.ld_x);
+        } else {
+#pragma unroll
+          for (int o = 0; o < K - 1; ++o)
+            if (o == r.keep + j) v = old[o];
+        }
+        *reinterpret_cast<V*>(carried + size_t(j) * c.d_xBC) = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < K - 1; ++j) load_wide<TI, W>(src + (j - (K - 1)) * (long long)(c.ld_x), raw[j]);
+  }
+#pragma unroll
+  for (int i = 0; i < CONV_TILE; ++i)
+    if (i < rows) load_wide<TI, W>(src + size_t(i) * c.ld_x, raw[K - 1 + i]);
+#pragma unroll
+  for (int i = 0; i < CONV_TILE; ++i) {
+    if (i >= rows) break;
+    Word<float, W> out;
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      float v = bias[e];
+#pragma unroll
+      for (int j = 0; j < K; ++j) v = fmaf(w[j][e], raw[i + j][e], v);
+      out.v[e] = silu_f32(v);
+    }
+    *reinterpret_cast<Word<float, W>*>(a.s.xbc + (out0 + i) * a.s.pitch + ch) = out;
+  }
+}
+
+// B and C of a group, for a request with up to SCAN_FEW rows (N = 128): a thread a channel.  B goes into the scratch as it is, C in its two parts; their
 // products by pairs of rows.
 constexpr int CB_PITCH = 128 + 4;
-template <typename TI, int K>
-__device__ void rows_of_group(const ConvArgs& a, int b, int g) {
+// x of a request with few rows: a thread two channels.
+template <typename TI, bool VEC>
+__device__ void x_of_request(const ConvArgs& a, int b, int ch) {
   const ChunkScanCall& c = a.c;
+  const ScanRequest r = scan_request(c, b);
+  const int n = scan_upto(c, r), K1 = c.d_conv - 1;
+  if (n > a.s.few || ch >= c.Di || (n == 0 && !r.stores())) return;
+  const RawRows<VEC, 2, TI> raw(c, r, ch);
+  Taps<1> taps;
+  taps.load(c, ch);
+  Word<TI, 2> front[3] = {};
+  uint64_t before[3][1];
+  if (n > 0) {
+    raw.front(front, 0, n - 1);
+    raw.front_value(front, 0, before);
+  }
+  if (r.stores()) {
+    TI* carried = reinterpret_cast<TI*>(c.conv_state) + size_t(r.slot) * K1 * c.d_xBC + ch;
+    for (int j = 0; j < K1; ++j) {
+      const int from = r.keep + j - K1;                      // the row that comes to place j; below zero: a carried one (front: rows -3 .. -1)
+      Word<TI, 2> v = from == -3 ? front[0] : from == -2 ? front[1] : front[2];
+      if (from >= 0) v = raw.row(from, n - 1);
+      else if (r.fresh) v = Word<TI, 2>{};
+      carried[size_t(j) * c.d_xBC] = v.v[0];
+      carried[size_t(j) * c.d_xBC + 1] = v.v[1];
+    }
+  }
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    Word<TI, 2> rows[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rows[i] = raw.row(i0 + i, n - 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i >= n) break;
+      uint64_t now[1], v[1];
+      widen(rows[i], now);
+      taps.next(before, now, v);
+      *reinterpret_cast<uint64_t*>(a.s.xbc + a.s.row(b, r.q0, i0 + i) * a.s.pitch + ch) = v[0];
+    }
+  }
+}
+
+// The steps of a request with few rows: a thread a head.  The log-decays' sums are 64-bit and stored in two parts.
+template <typename TI>
+__device__ void steps_of_request(const ConvArgs& a, int b) {
+  const ChunkScanCall& c = a.c;
+  const ScanRequest r = scan_request(c, b);
+  const int n = scan_upto(c, r);
+  if (n > a.s.few) return;
+  for (int h = threadIdx.x; h < c.H; h += CONV_THREADS) {
+    const float bias = c.dt_bias[h];
+    const double rate = double(-expf(c.A_log[h]));
+    double sum = 0.0;
+    for (int i0 = 0; i0 < n; i0 += 8) {
+      float in[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const size_t t = size_t(r.q0) + min(i0 + i, n - 1);
+        in[i] = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i0 + i >= n) break;
+        const float dt = softplus_f32(in[i] + bias);
+        sum += double(dt) * rate;
+        const float hi = float(sum);
+        a.s.sums[a.s.row(b, r.q0, i0 + i) * c.H + h] = make_float4(dt, expf(hi), hi, float(sum - double(hi)));
+      }
+    }
+  }
+}
+
+template <typename TI, int K, bool VEC>
+__global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
+  const ChunkScanCall& c = a.c;
+  pdl_wait();
+  pdl_trigger();
   extern __shared__ __align__(16) float rows_sm[];           // B, then C: [SCAN_FEW][CB_PITCH] each
+  if (blockIdx.x == 0) {
+    count_bad(c);
+    if (a.plan) plan_long(a, reinterpret_cast<int*>(rows_sm));
+    return;
+  }
+  // (a request's blocks: its groups, its steps, 512 channels of x each)
+  const int x_blocks = (c.Di + 2 * CONV_THREADS - 1) / (2 * CONV_THREADS), each = c.G + 1 + x_blocks;
+  const int b = (blockIdx.x - 1) / each, g = (blockIdx.x - 1) % each;
+  if (g > c.G) { x_of_request<TI, VEC>(a, b, (g - c.G - 1) * 2 * CONV_THREADS + 2 * threadIdx.x); return; }
+  if (g == c.G) { steps_of_request<TI>(a, b); return; }
   const ScanRequest r = scan_request(c, b);
   const int n = scan_upto(c, r), tid = threadIdx.x, e = tid & 127;
   const bool isC = tid >= 128;
@@ -208,100 +384,6 @@ __device__ void rows_of_group(const ConvArgs& a, int b, int g) {
       sum.x = fmaf(x.x, y.x, sum.x); sum.y = fmaf(x.y, y.y, sum.y); sum.z = fmaf(x.z, y.z, sum.z); sum.w = fmaf(x.w, y.w, sum.w);
     }
     a.s.cb[((size_t(b) * c.G + g) * SCAN_FEW + t) * SCAN_FEW + s] = (sum.x + sum.y) + (sum.z + sum.w);
-  }
-}
-
-template <typename TI, int W, int K>
-__global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
-  const ChunkScanCall& c = a.c;
-  pdl_wait();
-  pdl_trigger();
-  const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1 - a.group_blocks) % blocks;
-  if (blockIdx.x == 0) {
-    for (int b = tid; b < c.B; b += CONV_THREADS) {
-      const ScanRequest r = scan_request(c, b);
-      if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], INT_MAX, c.T, INT_MAX) || (r.n > 0 && r.slot != (c.slots ? c.slots[b] : b)))
-        atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
-    }
-    if (a.plan) plan_long(a);
-    return;
-  }
-  if (int(blockIdx.x) <= a.group_blocks) {
-    rows_of_group<TI, K>(a, (blockIdx.x - 1) / c.G, (blockIdx.x - 1) % c.G);
-    return;
-  }
-  const ChunkItem item = few_item(c, a.s.few, (blockIdx.x - 1 - a.group_blocks) / blocks, tid & 31);
-  if (item.b < 0) return;
-  const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
-  const size_t out0 = a.s.row(item.b, item.q0, item.first);
-  if (part >= a.ch_blocks) {
-    // ---- steps and decays
-    const int i = (part - a.ch_blocks) * CONV_THREADS + tid, h = i % c.H, r = i / c.H;
-    if (r < rows) {
-      const size_t t = t0 + r;
-      const float raw = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
-      const float dt = softplus_f32(raw + c.dt_bias[h]);
-      a.s.step[(out0 + r) * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
-    }
-    return;
-  }
-  const ScanRequest r = scan_request(c, item.b);
-  const int ch = (part * CONV_THREADS + tid) * W;
-  if (ch >= a.channels) return;
-  float w[K][W], bias[W], raw[K - 1 + CONV_TILE][W];
-  // (a thread's weights are W rows of K)
-#pragma unroll
-  for (int e = 0; e < W; ++e) {
-    bias[e] = c.conv_b[ch + e];
-#pragma unroll
-    for (int j = 0; j < K; ++j) w[j][e] = c.conv_w[size_t(ch + e) * K + j];
-  }
-  TI* carried = reinterpret_cast<TI*>(c.conv_state) + (r.slot < 0 ? 0 : size_t(r.slot) * (K - 1) * c.d_xBC) + ch;
-  const TI* src = reinterpret_cast<const TI*>(c.x) + size_t(t0) * c.ld_x + c.Di + ch;
-  if (item.first == 0) {
-    using V = Word<TI, W>;
-    V old[K - 1 > 0 ? K - 1 : 1];
-#pragma unroll
-    for (int j = 0; j < K - 1; ++j) {
-      if (r.fresh) old[j] = V{};
-      else old[j] = *reinterpret_cast<const V*>(carried + size_t(j) * c.d_xBC);
-#pragma unroll
-      for (int e = 0; e < W; ++e) raw[j][e] = to_f32(old[j].v[e]);
-    }
-    if (r.stores()) {
-#pragma unroll
-      for (int j = 0; j < K - 1; ++j) {
-        const int from = r.keep + j - (K - 1);             // the chunk's row that comes to place j; below zero: a carried one
-        V v{};
-        if (from >= 0) {
-          v = *reinterpret_cast<const V*>(src + size_t(from) * c.ld_x);
-        } else {
-#pragma unroll
-          for (int o = 0; o < K - 1; ++o)
-            if (o == r.keep + j) v = old[o];
-        }
-        *reinterpret_cast<V*>(carried + size_t(j) * c.d_xBC) = v;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < K - 1; ++j) load_wide<TI, W>(src + (j - (K - 1)) * (long long)(c.ld_x), raw[j]);
-  }
-#pragma unroll
-  for (int i = 0; i < CONV_TILE; ++i)
-    if (i < rows) load_wide<TI, W>(src + size_t(i) * c.ld_x, raw[K - 1 + i]);
-#pragma unroll
-  for (int i = 0; i < CONV_TILE; ++i) {
-    if (i >= rows) break;
-    Word<float, W> out;
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-      float v = bias[e];
-#pragma unroll
-      for (int j = 0; j < K; ++j) v = fmaf(w[j][e], raw[i + j][e], v);
-      out.v[e] = silu_f32(v);
-    }
-    *reinterpret_cast<Word<float, W>*>(a.s.xbc + (out0 + i) * a.s.pitch + ch) = out;
   }
 }
 
@@ -522,7 +604,7 @@ cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
 
 template <typename TI, int W, int K>
 cudaError_t launch_rows_k(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
-  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), a.group_blocks ? size_t(2) * SCAN_FEW * CB_PITCH * 4 : 0, stream, a);
+  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), 0, stream, a);
 }
 template <typename TI, int W>
 cudaError_t launch_rows_w(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
@@ -534,26 +616,48 @@ cudaError_t launch_rows_w(const ConvArgs& a, unsigned blocks, cudaStream_t strea
   }
 }
 
+template <typename TI, int K>
+cudaError_t launch_groups_k(const ConvArgs& a, cudaStream_t stream) {
+  const ChunkScanCall& c = a.c;
+  const long long blocks = 1 + (long long)(c.B) * (c.G + 1 + (c.Di + 2 * CONV_THREADS - 1) / (2 * CONV_THREADS));
+  if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
+  auto on = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % (2 * sizeof(TI)) == 0; };
+  const bool vec = c.ld_x % 2 == 0 && on(c.x) && on(c.conv_state);
+  return launch_pdl(vec ? scan_groups_kernel<TI, K, true> : scan_groups_kernel<TI, K, false>, dim3(unsigned(blocks)), dim3(CONV_THREADS),
+                    size_t(2) * SCAN_FEW * CB_PITCH * 4, stream, a);
+}
+template <typename TI>
+cudaError_t launch_groups(const ConvArgs& a, cudaStream_t stream) {
+  switch (a.c.d_conv) {
+    case 1: return launch_groups_k<TI, 1>(a, stream);
+    case 2: return launch_groups_k<TI, 2>(a, stream);
+    case 3: return launch_groups_k<TI, 3>(a, stream);
+    default: return launch_groups_k<TI, 4>(a, stream);
+  }
+}
+
 template <typename TI>
 cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   const ChunkScanCall& c = a.c;
+  if (a.s.c_parts) {
+    const cudaError_t e = launch_groups<TI>(a, stream);
+    StateArgs s{};
+    s.c = c;
+    s.s = a.s;
+    return e != cudaSuccess ? e : scan_block_launch(s, stream);
+  }
   // words of four row values, where all rows and both parts of a row start on their boundaries
   auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(TI)) == 0; };
   const bool wide = c.Di % 4 == 0 && c.d_xBC % 4 == 0 && c.ld_x % 4 == 0 && aligned(c.x) && aligned(c.conv_state);
-  a.channels = a.s.c_parts ? c.Di : c.d_xBC;
-  a.group_blocks = a.s.c_parts ? c.B * c.G : 0;
-  a.ch_blocks = (a.channels + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
+  a.ch_blocks = (c.d_xBC + CONV_THREADS * (wide ? 4 : 1) - 1) / (CONV_THREADS * (wide ? 4 : 1));
   a.dt_blocks = (CONV_TILE * c.H + CONV_THREADS - 1) / CONV_THREADS;
-  long long items = c.T / CONV_TILE + c.B;
-  if (a.plan && items > (long long)(c.B) * (SCAN_FEW / CONV_TILE)) items = (long long)(c.B) * (SCAN_FEW / CONV_TILE);
-  const long long blocks = 1 + a.group_blocks + items * (a.ch_blocks + a.dt_blocks);
+  const long long blocks = 1 + (long long)(c.T / CONV_TILE + c.B) * (a.ch_blocks + a.dt_blocks);
   if (blocks > INT_MAX) return cudaErrorInvalidConfiguration;
   const cudaError_t e = wide ? launch_rows_w<TI, 4>(a, unsigned(blocks), stream) : launch_rows_w<TI, 1>(a, unsigned(blocks), stream);
   if (e != cudaSuccess) return e;
   StateArgs s{};
   s.c = c;
   s.s = a.s;
-  if (a.s.c_parts) return scan_block_launch(s, stream);
   return launch_states<TI>(s, stream);
 }
 
@@ -564,12 +668,12 @@ struct Scratch {
   bool blocks, tensor;               // requests with few rows go through scan_block_kernel, those with many through the tensor cores
   Scratch(long long T, int B, int Di, int P, int N, int G) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    pitch = (Di + 2 * G * N + 3) / 4 * 4;
     blocks = P == 64 && N == 128;
+    pitch = (Di + 2 * G * N + 3) / 4 * 4;
     tensor = blocks && T > SCAN_FEW;
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
     step = up(rows * pitch * 4);
-    c_parts = step + up(rows * (Di / P) * 8);
+    c_parts = step + up(rows * (Di / P) * (blocks ? 16 : 8));
     cb = c_parts + (blocks ? up(rows * G * N * 4) : 0);
     plan = cb + (blocks ? up(size_t(B) * G * SCAN_FEW * SCAN_FEW * 4) : 0);
     list = plan + 256;
@@ -593,6 +697,7 @@ cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
   a.s.step = reinterpret_cast<float2*>(ws + at.step);
   a.s.few = INT_MAX;
   if (at.blocks) {
+    a.s.sums = reinterpret_cast<float4*>(ws + at.step);
     a.s.c_parts = reinterpret_cast<uint16_t*>(ws + at.c_parts);
     a.s.cb = reinterpret_cast<float*>(ws + at.cb);
   }

@@ -41,6 +41,7 @@ struct ScanScratch {
   float* xbc;                        // [.., pitch] convolved rows
   float2* step;                      // [.., H] dt and the decay exp(dt A)
   // blocks of rows (scan_block_kernel) have their C apart, split into two bf16 parts, and the products C_t . B_s of a request's rows
+  float4* sums;                      // [.., H] dt, e^c, and c, the sum of the log-decays so far, in two parts
   uint16_t* c_parts;                 // [.., G, 2, N]; null: requests with few rows go through scan_state_kernel
   float* cb;                         // [B, G, SCAN_FEW, SCAN_FEW]
   int pitch;
@@ -54,7 +55,7 @@ struct StateArgs {
   ScanScratch s;
   int p_blocks, p_block;             // blocks of a head, rows of its state in each
   int np;                            // padded N: row pitch of B and C in shared memory
-  int y_vec;                         // four outputs start on their boundary
+  int y_vec;                         // two outputs start on their boundary
 };
 cudaError_t scan_block_launch(const StateArgs& a, cudaStream_t stream);
 
@@ -79,5 +80,98 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+
+template <bool VEC, int N, typename TI>
+__device__ __forceinline__ Word<TI, N> load_word(const TI* p) {
+  Word<TI, N> w;
+  if (VEC) w = *reinterpret_cast<const Word<TI, N>*>(p);
+  else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) w.v[e] = p[e];
+  }
+  return w;
+}
+
+// Two values at a time.
+__device__ __forceinline__ uint64_t dup2(float v) { return pack_f32x2(v, v); }
+__device__ __forceinline__ uint64_t silu2(uint64_t v) {
+  float a, b;
+  unpack_f32x2(mul_f32x2(v, dup2(-1.4426950408889634f)), a, b);
+  unpack_f32x2(add_f32x2(pack_f32x2(ex2_ftz(a), ex2_ftz(b)), dup2(1.f)), a, b);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+  return mul_f32x2(v, pack_f32x2(a, b));
+}
+// v = head + remainder, both bf16; packed with the first value in the low half
+__device__ __forceinline__ void split2(uint64_t v, uint32_t& hi, uint32_t& lo) {
+  float a, b;
+  unpack_f32x2(v, a, b);
+  hi = pack_bf16(a, b);
+  unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), dup2(-1.f), v), a, b);
+  lo = pack_bf16(a, b);
+}
+template <typename TI, int N>
+__device__ __forceinline__ void widen(const Word<TI, N>& w, uint64_t (&v)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) v[i] = pack_f32x2(to_f32(w.v[2 * i]), to_f32(w.v[2 * i + 1]));
+}
+
+// N raw channels (from `ch` on) of a request's rows; below row zero the carried ones, or nothing.  Addresses are chosen and no loads skipped, so
+// that those of several rows are under way together.
+template <bool VEC, int N, typename TI>
+struct RawRows {
+  const TI* x;                       // the request's first row
+  const TI* carried;                 // row -(d_conv - 1); null: nothing is carried
+  long long ld;
+  int d_xBC, K1;
+  __device__ __forceinline__ RawRows(const ChunkScanCall& c, const ScanRequest& r, int ch)
+      : x(reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + c.Di + ch),
+        carried(r.fresh || c.d_conv == 1 ? nullptr : reinterpret_cast<const TI*>(c.conv_state) + size_t(r.slot) * (c.d_conv - 1) * c.d_xBC + ch),
+        ld(c.ld_x), d_xBC(c.d_xBC), K1(c.d_conv - 1) {}
+  // row i; behind `last` row `last` again
+  __device__ __forceinline__ Word<TI, N> row(int i, int last) const { return load_word<VEC, N>(x + size_t(min(i, last)) * ld); }
+  // rows i - 3 .. i - 1 (front_value: those that are not there are zero)
+  __device__ __forceinline__ void front(Word<TI, N> (&w)[3], int i, int last) const {
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      const int row = i - 3 + j;
+      w[j] = load_word<VEC, N>(row < 0 && there(row) ? carried + size_t(row + K1) * d_xBC : x + size_t(max(min(row, last), 0)) * ld);
+    }
+  }
+  __device__ __forceinline__ bool there(int row) const { return row >= 0 || (carried && row + K1 >= 0); }
+  __device__ __forceinline__ void front_value(const Word<TI, N> (&w)[3], int i, uint64_t (&before)[3][N / 2]) const {
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      widen(w[j], before[j]);
+#pragma unroll
+      for (int h = 0; h < N / 2; ++h)
+        if (!there(i - 3 + j)) before[j][h] = 0ull;
+    }
+  }
+};
+
+// The convolution of 2 H channels: taps in front of a narrower one are zero.
+template <int H>
+struct Taps {
+  uint64_t w[4][H], b[H];            // [tap][channels]
+  __device__ __forceinline__ void load(const ChunkScanCall& c, int ch) {
+    const int K = c.d_conv;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const float* f = c.conv_w + size_t(ch + 2 * h) * K;
+      b[h] = pack_f32x2(c.conv_b[ch + 2 * h], c.conv_b[ch + 2 * h + 1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j][h] = j >= 4 - K ? pack_f32x2(f[j - (4 - K)], f[j - (4 - K) + K]) : 0ull;
+    }
+  }
+  // SiLU of the convolution at the row behind `before` (oldest first), which moves on by that row
+  __device__ __forceinline__ void next(uint64_t (&before)[3][H], const uint64_t (&now)[H], uint64_t (&v)[H]) const {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      v[h] = silu2(fma_f32x2(w[3][h], now[h], fma_f32x2(w[2][h], before[2][h], fma_f32x2(w[1][h], before[1][h], fma_f32x2(w[0][h], before[0][h], b[h])))));
+      before[0][h] = before[1][h]; before[1][h] = before[2][h]; before[2][h] = now[h];
+    }
+  }
+};
 
 }  // namespace hspec

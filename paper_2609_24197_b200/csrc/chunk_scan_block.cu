@@ -20,14 +20,10 @@ constexpr int NH = 64, NS = 128, FEW = SCAN_FEW;
 constexpr int X_PITCH = NH + 4, W_PITCH = FEW + 4, C_PITCH = NS + 16;            // of rows in shared memory, in their own elements
 struct BlockShared {
   float x[FEW][X_PITCH];
-  float w[FEW][W_PITCH];                     // e^{c_t - c_s} dt_s (C_t . B_s), with D on the diagonal
-  union {
-    uint16_t c[2][FEW][C_PITCH];             // C's head and remainder
-    float y[FEW][X_PITCH];                   // later the outputs, before the gate
-  };
+  float cb[FEW][W_PITCH];                    // C_t . B_s, up to the diagonal
+  uint16_t c[2][FEW][C_PITCH];               // C's head and remainder
   float b[FEW][NS];
-  double sum[FEW];                           // c_t
-  float dt[FEW], ec[FEW], kept[FEW];         // dt, e^{c_t}, e^{c_m - c_s} dt_s
+  float4 sums[FEW];                          // dt_t, e^{c_t}, c_t in two parts
 };
 
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -56,76 +52,42 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
   extern __shared__ __align__(16) uint8_t block_sm[];
   BlockShared& s = *reinterpret_cast<BlockShared*>(block_sm);
   const size_t at0 = a.s.row(b, r.q0, 0);
-  if (n > 0) {
-    // ---- the rows: x, B, C; their steps
-    for (int i = tid; i < n * (NH / 4); i += 128) {
-      const int row = i >> 4, e = (i & 15) * 4;
-      cp_async16(smem_u32(&s.x[row][e]), a.s.xbc + (at0 + row) * a.s.pitch + h * NH + e, true);
+  // ---- the rows: steps, x, C, B and their products
+  if (tid < n) cp_async16(smem_u32(&s.sums[tid]), a.s.sums + (at0 + tid) * c.H + h, true);
+  for (int i = tid; i < n * (NH / 4); i += 128) cp_async16(smem_u32(&s.x[i >> 4][(i & 15) * 4]), a.s.xbc + (at0 + (i >> 4)) * a.s.pitch + h * NH + (i & 15) * 4, true);
+  for (int i = tid; i < r.keep * (NS / 4); i += 128)
+    cp_async16(smem_u32(&s.b[i >> 5][(i & 31) * 4]), a.s.xbc + (at0 + (i >> 5)) * a.s.pitch + c.Di + g * NS + (i & 31) * 4, true);
+  if (Y) {
+    for (int i = tid; i < n * 32; i += 128) {
+      const int row = i >> 5, part = (i >> 4) & 1, e = (i & 15) * 8;
+      cp_async16(smem_u32(&s.c[part][row][e]), a.s.c_parts + ((at0 + row) * c.G + g) * 2 * NS + part * NS + e, true);
     }
-    if (Y)
-      for (int i = tid; i < n * 32; i += 128) {
-        const int row = i >> 5, part = (i >> 4) & 1, e = (i & 15) * 8;
-        cp_async16(smem_u32(&s.c[part][row][e]), a.s.c_parts + ((at0 + row) * c.G + g) * 2 * NS + part * NS + e, true);
-      }
-    if (r.keep > 0)
-      for (int i = tid; i < r.keep * (NS / 4); i += 128) {
-        const int row = i >> 5, e = (i & 31) * 4;
-        cp_async16(smem_u32(&s.b[row][e]), a.s.xbc + (at0 + row) * a.s.pitch + c.Di + g * NS + e, true);
-      }
-    cp_async_commit();
-    if (tid < 32) {
-      const float dt = tid < n ? a.s.step[(at0 + tid) * c.H + h].x : 0.f;
-      double sum = double(dt) * double(-expf(c.A_log[h]));
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const double up = __shfl_up_sync(0xffffffffu, sum, off);
-        if (tid >= off) sum += up;
-      }
-      const double end = r.keep > 0 ? __shfl_sync(0xffffffffu, sum, max(r.keep - 1, 0)) : 0.0;
-      s.sum[tid] = sum;
-      s.dt[tid] = dt;
-      s.ec[tid] = __expf(float(sum));
-      s.kept[tid] = tid < r.keep ? dt * __expf(float(end - sum)) : 0.f;
-    }
+    for (int i = tid; i < n * (FEW / 4); i += 128)
+      if ((i & 7) * 4 <= i >> 3) cp_async16(smem_u32(&s.cb[i >> 3][(i & 7) * 4]), a.s.cb + ((size_t(b) * c.G + g) * FEW + (i >> 3)) * FEW + (i & 7) * 4, true);
   }
-  Word<TI, 4> z[FEW * NH / 4 / 128];
-  const TI* gates = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * NH;
+  cp_async_commit();
+  // (what lies behind the last row is read as zeros, never as what happens to be there)
+  const int padded = (n + 15) / 16 * 16;
+  for (int i = tid; i < (padded - n) * NH; i += 128) s.x[n + i / NH][i % NH] = 0.f;
+  for (int i = tid; i < padded - n; i += 128) s.sums[n + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (Y)
+    for (int i = tid; i < (padded - n) * (NS / 8); i += 128)
+      *reinterpret_cast<uint4*>(&s.c[0][n + i / (NS / 8)][i % (NS / 8) * 8]) = *reinterpret_cast<uint4*>(&s.c[1][n + i / (NS / 8)][i % (NS / 8) * 8]) = make_uint4(0, 0, 0, 0);
+  // A lane has channels p and p + 8 of rows 8 j + 2 q and + 1; after a swap with the lane four on (or back) two adjacent channels of one of the rows.
+  const int odd_lane = gl & 1, out_row = 2 * q + odd_lane, out_ch = warp * 16 + (gl & ~1);
+  const TI* gates = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * NH + out_ch;
+  Word<TI, 2> z[4][2];
   if (Y) {
 #pragma unroll
-    for (int i = 0; i < FEW * NH / 4 / 128; ++i) {
-      const int row = (tid + i * 128) >> 4, e = (tid & 15) * 4;
-      if (row >= n) continue;
-      if (VEC) z[i] = *reinterpret_cast<const Word<TI, 4>*>(gates + size_t(row) * c.ld_x + e);
-      else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[i].v[j] = gates[size_t(row) * c.ld_x + e + j];
+    for (int j = 0; j < 4; ++j)
+      if (j * 8 + out_row < n) {
+        z[j][0] = load_word<VEC, 2>(gates + size_t(j * 8 + out_row) * c.ld_x);
+        z[j][1] = load_word<VEC, 2>(gates + size_t(j * 8 + out_row) * c.ld_x + 8);
       }
-    }
   }
-  __syncthreads();
-  if (Y && n > 0) {
-    const float D = c.Dskip[h];
-    const int padded = (n + 15) / 16 * 16;                   // (what lies behind the last row is read as zeros, never as what happens to be there)
-    for (int i = tid; i < padded * padded; i += 128) {
-      const int t = i / padded, u = i % padded;
-      float w = 0.f;
-      if (u <= t && t < n) {
-        w = a.s.cb[((size_t(b) * c.G + g) * FEW + t) * FEW + u] * s.dt[u] * __expf(float(s.sum[t] - s.sum[u]));
-        if (u == t) w += D;
-      }
-      s.w[t][u] = w;
-    }
-    for (int i = tid; i < (padded - n) * NH; i += 128) s.x[n + i / NH][i % NH] = 0.f;
-    for (int i = tid; i < (padded - n) * NS; i += 128) s.c[0][n + i / NS][i % NS] = s.c[1][n + i / NS][i % NS] = 0;
-  }
+  const float D = c.Dskip[h];
   cp_async_wait<0>();
-  bool odd = false;                                          // x is not finite (a thread looks at what it has copied)
-  if (Y)
-    for (int i = tid; i < n * (NH / 4); i += 128) {
-      const float4 v = *reinterpret_cast<const float4*>(&s.x[i >> 4][(i & 15) * 4]);
-      odd |= fmaf(v.x, 0.f, fmaf(v.y, 0.f, fmaf(v.z, 0.f, v.w * 0.f))) != 0.f;
-    }
-  odd = __syncthreads_or(odd);
+  __syncthreads();
   if (Y && n > 0) {
     float acc[4][4] = {};
     // ---- with the state
@@ -145,84 +107,98 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
         mma_bf16_16816(acc[j], lo, ch.x, ch.y);
       }
     }
-    // (a lane has channels gl and gl + 8 of its warp's, of rows 8 j + 2 q and + 1)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (j * 8 >= n) break;
-      const float e0 = s.ec[j * 8 + 2 * q], e1 = s.ec[j * 8 + 2 * q + 1];
+      const float e0 = s.sums[j * 8 + 2 * q].y, e1 = s.sums[j * 8 + 2 * q + 1].y;
       acc[j][0] *= e0; acc[j][1] *= e1; acc[j][2] *= e0; acc[j][3] *= e1;
     }
-    // ---- among the rows
-    if (odd) {
-      // (in a product a value that is not finite would reach the rows in front of it too, as zero times itself)
+    // ---- among the rows: weight e^{c_t - c_u} dt_u (C_t . B_u) of row u for row t, with D on the diagonal
+    auto weight = [&](int t, int u) {
+      const float4 st = s.sums[t], su = s.sums[u];
+      const float w = s.cb[t][u] * su.x * __expf((st.z - su.z) + (st.w - su.w));
+      return u < t ? w : u == t ? w + D : 0.f;               // (behind the diagonal anything may be there)
+    };
+    bool odd = false;                                        // x is not finite
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k * 16 >= n) break;
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                          // channel gl (+ 8), rows 16 k + 2 q (+ 8) and the one behind it
+        const int p = warp * 16 + gl + (i & 1) * 8, u = k * 16 + 2 * q + (i >> 1) * 8;
+        const float x0 = s.x[u][p], x1 = s.x[u + 1][p];
+        odd |= fmaf(x0, 0.f, x1 * 0.f) != 0.f;
+        split_pair(x0, x1, hi[i], lo[i]);
+      }
+      if (__any_sync(0xffffffffu, odd)) break;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j * 8 >= n) break;
+        if (j * 8 + 7 < k * 16) continue;                    // (rows in front of the terms: nothing)
+        const int t = j * 8 + gl, u = k * 16 + 2 * q;
+        uint32_t wh[2], wl[2];
+        split_pair(weight(t, u), weight(t, u + 1), wh[0], wl[0]);
+        split_pair(weight(t, u + 8), weight(t, u + 9), wh[1], wl[1]);
+        mma_bf16_16816(acc[j], hi, wh[0], wh[1]);
+        mma_bf16_16816(acc[j], hi, wl[0], wl[1]);
+        mma_bf16_16816(acc[j], lo, wh[0], wh[1]);
+      }
+    }
+    if (__any_sync(0xffffffffu, odd)) {
+      // In a product a value that is not finite would reach the rows in front of it too, as zero times itself.  (Where the first sixteen rows have gone
+      // into the products before one was found, those stay, and the others are added here.)
+      bool early = false;
+      for (int u = 0; u < min(n, 16); ++u) {
+        const float x0 = s.x[u][warp * 16 + gl], x1 = s.x[u][warp * 16 + gl + 8];
+        early |= fmaf(x0, 0.f, x1 * 0.f) != 0.f;
+      }
+      const int from = __any_sync(0xffffffffu, early) ? 0 : 16;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = j * 8 + 2 * q + (i & 1);
 #pragma unroll 1
-          for (int u = 0; u <= t && t < n; ++u) acc[j][i] = fmaf(s.w[t][u], s.x[u][warp * 16 + gl + (i >> 1) * 8], acc[j][i]);
+          for (int u = from; u <= t && t < n; ++u) acc[j][i] = fmaf(weight(t, u), s.x[u][warp * 16 + gl + (i >> 1) * 8], acc[j][i]);
         }
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (odd || k * 16 >= n) break;
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {                          // channel gl (+ 8), rows 16 k + 2 q (+ 8) and the one behind it
-        const int p = warp * 16 + gl + (i & 1) * 8, u = k * 16 + 2 * q + (i >> 1) * 8;
-        split_pair(s.x[u][p], s.x[u + 1][p], hi[i], lo[i]);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j * 8 >= n) break;
-        if (j * 8 + 7 < k * 16) continue;                    // (rows in front of the terms: nothing)
-        const float2 w0 = *reinterpret_cast<const float2*>(&s.w[j * 8 + gl][k * 16 + 2 * q]), w1 = *reinterpret_cast<const float2*>(&s.w[j * 8 + gl][k * 16 + 2 * q + 8]);
-        uint32_t wh[2], wl[2];
-        split_pair(w0.x, w0.y, wh[0], wl[0]);
-        split_pair(w1.x, w1.y, wh[1], wl[1]);
-        mma_bf16_16816(acc[j], hi, wh[0], wh[1]);
-        mma_bf16_16816(acc[j], hi, wl[0], wl[1]);
-        mma_bf16_16816(acc[j], lo, wh[0], wh[1]);
-      }
-    }
-    __syncthreads();                                         // (C has been read: the outputs take its place)
+    // ---- outputs
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (j * 8 >= n) break;
+      const int row = j * 8 + out_row;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s.y[j * 8 + 2 * q + (i & 1)][warp * 16 + gl + (i >> 1) * 8] = acc[j][i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < FEW * NH / 4 / 128; ++i) {
-      const int row = (tid + i * 128) >> 4, e = (tid & 15) * 4;
-      if (row >= n) continue;
-      const float4 y = *reinterpret_cast<const float4*>(&s.y[row][e]);
-      const float v[4] = {y.x * silu_f(to_f32(z[i].v[0])), y.y * silu_f(to_f32(z[i].v[1])), y.z * silu_f(to_f32(z[i].v[2])), y.w * silu_f(to_f32(z[i].v[3]))};
-      const size_t to = (size_t(r.q0) + row) * c.ld_y + h * NH + e;
-      if (!a.y_vec) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) store_row(c.y, c.y_dtype, to + j, v[j], c.status);
-      } else if (c.y_dtype == CHUNK_F32) {
-        *reinterpret_cast<float4*>(reinterpret_cast<float*>(c.y) + to) = make_float4(v[0], v[1], v[2], v[3]);
-      } else {
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(c.y) + to) =
-            c.y_dtype == CHUNK_BF16 ? make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])) : make_uint2(pack_f16_sat(v[0], v[1], c.status), pack_f16_sat(v[2], v[3], c.status));
+      for (int i = 0; i < 2; ++i) {                          // channels out_ch and + 1, then both + 8
+        const float mine = odd_lane ? acc[j][2 * i + 1] : acc[j][2 * i];
+        const float got = __shfl_xor_sync(0xffffffffu, odd_lane ? acc[j][2 * i] : acc[j][2 * i + 1], 4);
+        if (row >= n) continue;
+        const float v0 = (odd_lane ? got : mine) * silu_f(to_f32(z[j][i].v[0])), v1 = (odd_lane ? mine : got) * silu_f(to_f32(z[j][i].v[1]));
+        const size_t to = (size_t(r.q0) + row) * c.ld_y + h * NH + out_ch + i * 8;
+        if (!a.y_vec) {
+          store_row(c.y, c.y_dtype, to, v0, c.status);
+          store_row(c.y, c.y_dtype, to + 1, v1, c.status);
+        } else if (c.y_dtype == CHUNK_F32) {
+          *reinterpret_cast<float2*>(reinterpret_cast<float*>(c.y) + to) = make_float2(v0, v1);
+        } else {
+          *reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(c.y) + to) = c.y_dtype == CHUNK_BF16 ? pack_bf16(v0, v1) : pack_f16_sat(v0, v1, c.status);
+        }
       }
     }
   }
   if (!r.stores()) return;
   // ---- the state behind the kept rows
   if (r.keep > 0) {
-    const float end = s.ec[r.keep - 1];
+    const float4 last = s.sums[r.keep - 1];
+    const float end = last.y;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int k = 0; k < 8; ++k) S[i][k] = make_float4(S[i][k].x * end, S[i][k].y * end, S[i][k].z * end, S[i][k].w * end);
 #pragma unroll 1
     for (int u = 0; u < r.keep; ++u) {
-      const float kept = s.kept[u], x0 = kept * s.x[u][warp * 16 + gl], x1 = kept * s.x[u][warp * 16 + gl + 8];
+      const float4 su = s.sums[u];
+      const float kept = su.x * __expf((last.z - su.z) + (last.w - su.w)), x0 = kept * s.x[u][warp * 16 + gl], x1 = kept * s.x[u][warp * 16 + gl + 8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float4 v = *reinterpret_cast<const float4*>(&s.b[u][k * 16 + q * 4]);
@@ -253,9 +229,9 @@ template <typename TI>
 cudaError_t launch_for(StateArgs a, cudaStream_t stream) {
   const ChunkScanCall& c = a.c;
   const int item = c.y_dtype == CHUNK_F32 ? 4 : 2;
-  a.y_vec = c.y && reinterpret_cast<uintptr_t>(c.y) % (4 * item) == 0 && c.ld_y % 4 == 0 ? 1 : 0;
-  if (!c.y) return launch_vec<TI, false, true>(a, stream);
-  const bool vec = c.ld_x % 4 == 0 && reinterpret_cast<uintptr_t>(c.x) % (4 * sizeof(TI)) == 0;
+  a.y_vec = c.y && reinterpret_cast<uintptr_t>(c.y) % (2 * item) == 0 && c.ld_y % 2 == 0 ? 1 : 0;
+  const bool vec = c.ld_x % 2 == 0 && reinterpret_cast<uintptr_t>(c.x) % (2 * sizeof(TI)) == 0;
+  if (!c.y) return vec ? launch_vec<TI, false, true>(a, stream) : launch_vec<TI, false, false>(a, stream);
   return vec ? launch_vec<TI, true, true>(a, stream) : launch_vec<TI, true, false>(a, stream);
 }
 
