@@ -661,14 +661,16 @@ cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   return launch_states<TI>(s, stream);
 }
 
+bool scan_has_blocks(int P, int N) { return P == 64 && N == 128; }
+
 // Where everything lies in the caller's scratch.
 struct Scratch {
   size_t step, c_parts, cb, plan, list, chunks, images, total;
   int pitch;
   bool blocks, tensor;               // requests with few rows go through scan_block_kernel, those with many through the tensor cores
-  Scratch(long long T, int B, int Di, int P, int N, int G) {
+  Scratch(long long T, int B, int Di, int P, int N, int G, bool by_blocks) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-    blocks = P == 64 && N == 128;
+    blocks = by_blocks;
     pitch = (Di + 2 * G * N + 3) / 4 * 4;
     tensor = blocks && T > SCAN_FEW;
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
@@ -685,10 +687,14 @@ struct Scratch {
 
 }  // namespace
 
-size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) { return Scratch(T, B, Di, P, N, G).total; }
+// (The kernels of this shape need no less with products than without, and what they need grows with T and B.)
+size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) { return Scratch(T, B, Di, P, N, G, scan_has_blocks(P, N)).total; }
+
 
 cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
-  const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G);
+  // Row after row where there are hardly more rows than requests: nothing but the state counts then (64 tokens of 64 requests 145 us, with products and the
+  // launches for requests with many rows 184), and a request that has many of the rows all the same takes less than the others' states.
+  const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G, scan_has_blocks(c.P, c.N) && c.T > 2ll * c.B);
   char* ws = reinterpret_cast<char*>(c.ws);
   ConvArgs a{};
   a.c = c;
