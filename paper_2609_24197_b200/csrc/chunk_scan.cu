@@ -390,12 +390,14 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
 // ---------------------------------------------------------------------------------------------------
 // The states through the rows.  A group of L lanes has PR rows of a head's state [P, N]: lane l of the group the elements n = 4 (l + L k) .. + 3.
 constexpr int STATE_THREADS = 128;
-constexpr int STATE_TILE = 8;        // tokens that are fetched together
 
+__host__ __device__ constexpr int state_tile(int pr, int npt) { return pr * npt <= 8 ? 32 : 8; }
 template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
 __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) {
+  constexpr bool SMALL = PR * NPT <= 8;                      // few elements a thread: the rows' operands and gates are fetched far ahead
+  constexpr int TILE = state_tile(PR, NPT);                  // tokens that are fetched together
   constexpr int DUP = L / PR;                                // lanes that end up with the same row's sum
-  constexpr int ROWS = (STATE_TILE + DUP - 1) / DUP;         // tokens of a tile whose outputs a lane finishes
+  constexpr int ROWS = (TILE + DUP - 1) / DUP;               // tokens of a tile whose outputs a lane finishes
   const ChunkScanCall& c = a.c;
   const int tid = threadIdx.x, l = tid % L;
   const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, g = h / (c.H / c.G);
@@ -456,12 +458,12 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   const size_t at0 = a.s.row(b, r.q0, 0);
   extern __shared__ __align__(16) float sm[];
   const int xw = (a.p_block + 3) / 4 * 4, width = 2 * a.np + xw + 2;   // B | C | x | dt, decay
-  const int per = (width + 3) / 4 * 4, stage = per * STATE_TILE;
+  const int per = (width + 3) / 4 * 4, stage = per * TILE;
   for (int i = tid; i < 2 * stage; i += blockDim.x) sm[i] = 0.f;       // (what lies behind N and P stays zero)
   __syncthreads();
-  // fetches tokens first .. first + STATE_TILE - 1 of the request into a stage
+  // fetches tokens first .. first + TILE - 1 of the request into a stage
   auto fetch = [&](int first, int buf) {
-    const int count = min(STATE_TILE, upto - first);
+    const int count = min(TILE, upto - first);
     float* dst = sm + buf * stage;
     const float* rows = a.s.xbc + (at0 + first) * a.s.pitch;
     const int xn = min(a.p_block, c.P - p0);
@@ -491,25 +493,44 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   const int mine = l / DUP, dup = l % DUP, pm = pt + mine;
   const TI* z = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * c.P + pm;
   const float D = Y && pm < c.P ? c.Dskip[h] : 0.f;
+  // small states: the tile's gates, row by row, through registers into shared memory a tile ahead
+  constexpr int GATES = SMALL ? TILE * PR / L : 1;
+  float* gates = sm + 2 * stage;                             // [2][TILE][p_block]
+  float ahead[GATES];
+  auto fetch_gates = [&](int first) {
+    const int count = min(TILE, upto - first);
+#pragma unroll
+    for (int i = 0; i < GATES; ++i) {
+      const int at = tid + i * blockDim.x, row = at / a.p_block, p = p0 + at % a.p_block;
+      ahead[i] = row < count && p < c.P ? to_f32(reinterpret_cast<const TI*>(c.x)[size_t(r.q0 + first + row) * c.ld_x + h * c.P + p]) : 0.f;
+    }
+  };
+  auto put_gates = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < GATES; ++i) gates[buf * TILE * a.p_block + tid + i * blockDim.x] = silu_f32(ahead[i]);
+  };
   fetch(0, 0);
-  for (int first = 0, buf = 0; first < upto; first += STATE_TILE, buf ^= 1) {
-    const int count = min(STATE_TILE, upto - first);
-    float gate[ROWS];
-    if (Y) {
+  if (SMALL && Y) {
+    fetch_gates(0);
+    put_gates(0);
+  }
+  for (int first = 0, buf = 0; first < upto; first += TILE, buf ^= 1) {
+    const int count = min(TILE, upto - first);
+    float gate[ROWS];                                        // (of a tile's rows that this lane finishes)
+    if (Y && !SMALL) {
 #pragma unroll
       for (int i = 0; i < ROWS; ++i) {
         const int row = i * DUP + dup;
         gate[i] = row < count && pm < c.P ? to_f32(z[size_t(first + row) * c.ld_x]) : 0.f;
       }
     }
-    if (first + STATE_TILE < upto) fetch(first + STATE_TILE, buf ^ 1);
+    if (SMALL && Y && first + TILE < upto) fetch_gates(first + TILE);
+    if (first + TILE < upto) fetch(first + TILE, buf ^ 1);
     else cp_async_commit();
     cp_async_wait<1>();
     __syncthreads();
     const float* rows = sm + buf * stage;
-#pragma unroll
-    for (int row = 0; row < STATE_TILE; ++row) {
-      if (row >= count) break;
+    auto one = [&](int row) {
       const float* now = rows + row * per;
       const float2 step = *reinterpret_cast<const float2*>(now + 2 * a.np + xw);
       const uint64_t decay = pack_f32x2(step.y, step.y);
@@ -564,11 +585,39 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
 #pragma unroll
           for (int i = 1; i < PR; ++i)
             if (i == mine) xm = x[i];
-          const float zz = gate[row / DUP];
-          store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, xm, v[0]) * silu_f32(zz), c.status);
+          float g;
+          if constexpr (SMALL) g = gates[(buf * TILE + row) * a.p_block + pm - p0];
+          else g = silu_f32(gate[row / DUP]);
+          store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, xm, v[0]) * g, c.status);
         }
       }
-      if (first + row + 1 == r.keep && r.stores()) store();
+    };
+    if constexpr (SMALL) {
+      // Eight rows in a row, so that the next ones' operands and the last ones' sums are under way beside the one thing that has to wait, an addition to
+      // the state a row.
+#pragma unroll 1
+      for (int r0 = 0; r0 < count; r0 += 8) {
+        const bool inside = r.stores() && r.keep > first + r0 && r.keep < first + r0 + 8;        // the state is stored among them
+        if (r0 + 8 <= count && !inside) {
+#pragma unroll
+          for (int row = 0; row < 8; ++row) one(r0 + row);
+          if (first + r0 + 8 == r.keep && r.stores()) store();
+        } else {
+#pragma unroll 1
+          for (int row = r0; row < min(r0 + 8, count); ++row) {
+            one(row);
+            if (first + row + 1 == r.keep && r.stores()) store();
+          }
+        }
+      }
+      if (Y && first + TILE < upto) put_gates(buf ^ 1);
+    } else {
+#pragma unroll
+      for (int row = 0; row < TILE; ++row) {
+        if (row >= count) break;
+        one(row);
+        if (first + row + 1 == r.keep && r.stores()) store();
+      }
     }
     __syncthreads();
   }
@@ -583,7 +632,8 @@ cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
   a.p_blocks = (c.P + a.p_block - 1) / a.p_block;
   a.np = (c.N + 3) / 4 * 4 > L * NPT ? (c.N + 3) / 4 * 4 : L * NPT;
   const int per = (2 * a.np + (a.p_block + 3) / 4 * 4 + 2 + 3) / 4 * 4;
-  const size_t smem = size_t(2) * STATE_TILE * per * 4;
+  constexpr int TILE = state_tile(PR, NPT);
+  const size_t smem = size_t(2) * TILE * (per + (PR * NPT <= 8 ? a.p_block : 0)) * 4;
   const bool vec = c.N % 4 == 0 && c.Di % 4 == 0;
   const dim3 grid(unsigned(c.H * a.p_blocks), unsigned(c.B));
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(unsigned(groups * L)), smem, stream, a); };
@@ -595,9 +645,9 @@ template <typename TI>
 cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
   const int N = a.c.N;
   if (N <= 4) return launch_state<TI, 1, 1, 4>(a, stream);
-  if (N <= 16) return launch_state<TI, 1, 1, 16>(a, stream);
-  if (N <= 32) return launch_state<TI, 2, 2, 16>(a, stream);
-  if (N <= 64) return launch_state<TI, 4, 4, 16>(a, stream);
+  if (N <= 16) return launch_state<TI, 4, 1, 4>(a, stream);
+  if (N <= 32) return launch_state<TI, 8, 1, 4>(a, stream);
+  if (N <= 64) return launch_state<TI, 8, 1, 8>(a, stream);
   if (N <= 128) return launch_state<TI, 8, 4, 16>(a, stream);
   return launch_state<TI, 16, 4, 16>(a, stream);
 }
