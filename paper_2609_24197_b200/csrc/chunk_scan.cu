@@ -530,16 +530,16 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     cp_async_wait<1>();
     __syncthreads();
     const float* rows = sm + buf * stage;
-    auto one = [&](int row) {
+    // a row's addition to the state; the sum of this lane's row of the state with C
+    auto add = [&](int row) {
       const float* now = rows + row * per;
       const float2 step = *reinterpret_cast<const float2*>(now + 2 * a.np + xw);
       const uint64_t decay = pack_f32x2(step.y, step.y);
       uint64_t xd[PR], y2[PR];
-      float x[PR];
 #pragma unroll
       for (int i = 0; i < PR; ++i) {
-        x[i] = now[2 * a.np + (pt - p0) + i];
-        xd[i] = pack_f32x2(step.x * x[i], step.x * x[i]);
+        const float x = now[2 * a.np + (pt - p0) + i];
+        xd[i] = pack_f32x2(step.x * x, step.x * x);
         y2[i] = 0ull;
       }
 #pragma unroll
@@ -557,6 +557,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
           }
         }
       }
+      float sum = 0.f;
       if (Y) {
         // the group's sums: every step hands half of the rows to the partner, until a lane has one
         float v[PR];
@@ -580,17 +581,20 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
             v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
           }
         }
-        if (row % DUP == dup && pm < c.P) {
-          float xm = x[0];
-#pragma unroll
-          for (int i = 1; i < PR; ++i)
-            if (i == mine) xm = x[i];
-          float g;
-          if constexpr (SMALL) g = gates[(buf * TILE + row) * a.p_block + pm - p0];
-          else g = silu_f32(gate[row / DUP]);
-          store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, xm, v[0]) * g, c.status);
-        }
+        sum = v[0];
       }
+      return sum;
+    };
+    auto finish = [&](int row, float sum) {
+      if (pm >= c.P) return;
+      float g;
+      if constexpr (SMALL) g = gates[(buf * TILE + row) * a.p_block + pm - p0];
+      else g = silu_f32(gate[row / DUP]);
+      store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, rows[row * per + 2 * a.np + pm - p0], sum) * g, c.status);
+    };
+    auto one = [&](int row) {
+      const float sum = add(row);
+      if (Y && row % DUP == dup) finish(row, sum);
     };
     if constexpr (SMALL) {
       // Eight rows in a row, so that the next ones' operands and the last ones' sums are under way beside the one thing that has to wait, an addition to
@@ -599,8 +603,19 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
       for (int r0 = 0; r0 < count; r0 += 8) {
         const bool inside = r.stores() && r.keep > first + r0 && r.keep < first + r0 + 8;        // the state is stored among them
         if (r0 + 8 <= count && !inside) {
+          constexpr int MINE = (8 + DUP - 1) / DUP;          // of the eight that this lane finishes
+          float sums[MINE];
 #pragma unroll
-          for (int row = 0; row < 8; ++row) one(r0 + row);
+          for (int row = 0; row < 8; ++row) {
+            const float sum = add(r0 + row);
+            if (row % DUP == 0) sums[row / DUP] = sum;
+            else sums[row / DUP] = row % DUP == dup ? sum : sums[row / DUP];
+          }
+          if (Y) {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i)
+              if (DUP <= 8 || dup < 8) finish(r0 + i * DUP + dup, sums[i]);
+          }
           if (first + r0 + 8 == r.keep && r.stores()) store();
         } else {
 #pragma unroll 1
