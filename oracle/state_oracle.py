@@ -30,6 +30,7 @@ def chunk_scan(rows, conv_w, conv_b, dt_bias, A_log, Dskip, cu_q, conv_state, ss
     y = np.zeros((int(cu_q[-1]), Di))
     A = -np.exp(np.asarray(A_log, np.float64))
     mag = np.abs if sizes else (lambda v: v)
+    ssm = mag(ssm)
     for r in range(len(cu_q) - 1):
         lo, n = int(cu_q[r]), int(cu_q[r + 1]) - int(cu_q[r])
         slot = r if slots is None else int(slots[r])
@@ -37,7 +38,7 @@ def chunk_scan(rows, conv_w, conv_b, dt_bias, A_log, Dskip, cu_q, conv_state, ss
         new = not there or (fresh is not None and bool(fresh[r]))
         kept = n if keep is None else min(max(int(keep[r]) + keep_more, 0), n)
         past = np.zeros((K - 1, dx)) if new else conv[slot].copy()
-        S = np.zeros((H, P, N)) if new else mag(ssm[slot]).copy()
+        S = np.zeros((H, P, N)) if new else ssm[slot].copy()
         raw = np.concatenate([past, np.asarray(rows[lo:lo + n, Di:Di + dx], np.float64)])
         at = [S.copy()]
         for t in range(n):

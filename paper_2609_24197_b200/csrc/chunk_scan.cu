@@ -31,7 +31,7 @@ struct ConvArgs {
 __device__ void count_bad(const ChunkScanCall& c) {
   for (int b = threadIdx.x; b < c.B; b += CONV_THREADS) {
     const ScanRequest r = scan_request(c, b);
-    if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], INT_MAX, c.T, INT_MAX) || (r.n > 0 && r.slot != (c.slots ? c.slots[b] : b)))
+    if (chunk_request_bad(c.cu_q[b], c.cu_q[b + 1], INT_MAX, c.T, INT_MAX) || (r.n > 0 && r.slot < 0))
       atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);
   }
 }
