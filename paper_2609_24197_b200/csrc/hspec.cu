@@ -1138,6 +1138,9 @@ int hspec_op_chunk_scan(const void* zxbcdt, int32_t in_dtype, int64_t ld_in, con
   if (reinterpret_cast<uintptr_t>(ssm_state) & 15) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the states must start on a 16-byte boundary");
   if (workspace_bytes < chunk_scan_workspace_bytes(T, B, Di, P, N, G)) return fail(nullptr, HSPEC_ERR_WORKSPACE_TOO_SMALL, who + "workspace too small");
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "the workspace must be 256-byte aligned");
+  const size_t item = in_dtype == HSPEC_F32 ? 4 : 2, y_item = y_dtype == HSPEC_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(zxbcdt) % item || reinterpret_cast<uintptr_t>(conv_state) % item || (y && reinterpret_cast<uintptr_t>(y) % y_item))
+    return fail(nullptr, HSPEC_ERR_INVALID_ARG, who + "misaligned rows");
   std::string errtxt;
   ChunkScanCall c{};
   c.x = zxbcdt; c.in_dtype = in_dtype; c.ld_x = ld_in; c.dt_raw = dt_raw; c.conv_w = conv_w; c.conv_b = conv_b; c.dt_bias = dt_bias; c.A_log = A_log;

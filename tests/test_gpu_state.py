@@ -248,6 +248,49 @@ def test_scan_of_thousands_of_requests(hs):
     Layer(2, 8, 16, 1, [2, 0, 1] * 900, dtype=torch.float32, seed=9).check(hs)
 
 
+def test_scan_without_any_row(hs):
+    for shape in ((2, 64, 128, 1), (2, 40, 24, 1)):
+        a = Layer(*shape, [0, 0], seed=14)
+        conv, ssm = a.conv.clone(), a.ssm.clone()
+        a.run(hs, fresh=torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+        own = int(a.slots[1])
+        conv[own], ssm[own] = 0, 0
+        assert torch.equal(a.conv, conv) and torch.equal(a.ssm, ssm)
+
+
+@pytest.mark.parametrize("H,P,N,G,new", [(2, 64, 128, 1, [40000, 20, 29990, 1]), (2, 64, 128, 1, [2] * 34998 + [1, 1]), (8, 64, 16, 1, [3] * 20000 + [9000, 2, 1010])])
+def test_scan_behind_2_to_the_31_elements(hs, H, P, N, G, new):
+    """Rows, outputs and states whose places pass 32 bits: the bits that they have in small arrays."""
+    B, T = len(new), sum(new)
+    a = Layer(H, P, N, G, new[-4:], seed=15)                   # (the weights)
+    width = a.rows.shape[1]
+    g = torch.Generator(device="cuda").manual_seed(15)
+    pitch = 2 ** 31 // T // 16 * 16 + 32
+    far, far_y = (torch.empty((T, pitch), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    near, near_y = torch.empty((T, (width + 15) // 16 * 16), dtype=torch.bfloat16, device="cuda"), torch.empty((T, H * P), dtype=torch.bfloat16, device="cuda")
+    near.normal_(generator=g)
+    far[:, :width] = near[:, :width]
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32).cuda()
+    conv = torch.randn((B, a.K - 1, a.dx), dtype=torch.float32, device="cuda", generator=g).to(torch.bfloat16)
+    ws = torch.empty(hs.hspec_chunk_scan_workspace_bytes(T, B, a.Di, P, N, G), dtype=torch.uint8, device="cuda")
+    fresh = torch.ones(B, dtype=torch.int32, device="cuda")
+    fresh[-3:] = 0
+    last = torch.randn((3, H, P, N), device="cuda", generator=g)
+    results = []
+    n_far = 2 ** 31 // (H * P * N) + B
+    for rows, y, n in ((near, near_y, B), (far, far_y, n_far)):
+        ssm = torch.empty((n, H, P, N), device="cuda")
+        ssm[n - 3:] = last
+        slots = torch.arange(n - B, n, dtype=torch.int32, device="cuda")
+        carried = conv.clone() if n == B else torch.cat([torch.zeros((n - B, a.K - 1, a.dx), dtype=conv.dtype, device="cuda"), conv])
+        hs.hspec_op_chunk_scan(rows[:, :width], a.cw, a.cb, a.bias, a.A_log, a.D, cu, carried, ssm, y[:, :a.Di], ws, slots=slots, fresh=fresh)
+        results.append((y[:, :a.Di].clone(), carried[n - B:].clone(), ssm[n - B:].clone()))
+        del ssm
+    for x, y in zip(*results):
+        assert torch.equal(x, y) and torch.isfinite(x).all()
+    assert hs.hspec_op_device_status(clear=True)["bad_inputs"] == 0
+
+
 def test_scan_of_a_prompt_in_pieces(hs):
     """A prompt at once, in pieces and token by token: the same outputs and states within what both may be off by."""
     whole = Layer(2, 64, 128, 1, [290], dtype=torch.float32, seed=11)
@@ -427,6 +470,18 @@ def test_rules_clamp_what_leaves_fp16(hs):
                               bias_values=torch.tensor([[1e5]], device="cuda"))
     assert out.tolist() == [[65504.0, -65504.0, 1.0]]
     assert hs.hspec_op_device_status(clear=True)["f16_range_events"] == 2
+
+
+def test_rules_behind_2_to_the_31_elements(hs):
+    z, rules = _rules(1000, [200, 300, 20], seed=10, dtype=torch.bfloat16, drafts=30)
+    out = torch.empty_like(z)
+    hs.hspec_op_adjust_logits(z, out, **rules)
+    far, far_out = (torch.empty((520, 2 ** 31 // 520 // 8 * 8 + 16), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far[:, :1000] = z
+    hs.hspec_op_adjust_logits(far[:, :1000], far_out[:, :1000], **rules)
+    assert torch.equal(far_out[:, :1000], out)
+    hs.hspec_op_adjust_logits(far[:, :1000], far[:, :1000], **rules)
+    assert torch.equal(far[:, :1000], out)
 
 
 def test_rules_captured_and_on_another_stream(hs):

@@ -29,6 +29,7 @@ def _scan(lib, **over):
     (dict(n_slots=0), -1, "bad argument"), (dict(in_dtype=I32), -1, "rows must be"), (dict(y_dtype=9), -1, "rows must be"),
     (dict(Di=500), -2, "fill Di"), (dict(G=3), -2, "fill Di"), (dict(P=0), -2, "fill Di"), (dict(N=257), -2, "256 state"), (dict(K=0), -2, "1 to 4"),
     (dict(K=5), -2, "1 to 4"), (dict(conv=None), -1, "carried rows"), (dict(ld=2 * 512 + 2 * 128 + 7), -1, "row pitch"), (dict(ldy=511), -1, "row pitch"),
+    (dict(x=A + 1), -1, "misaligned"), (dict(conv=A + 1), -1, "misaligned"), (dict(y=A + 2, y_dtype=F32), -1, "misaligned"),
     (dict(ssm=A + 4), -1, "16-byte"), (dict(ws_bytes=100), -4, "workspace too small"), (dict(ws=A + 16), -1, "256-byte"), (dict(B=65536), -2, "65535"),
     (dict(Di=1 << 25, ld=1 << 28, ldy=1 << 25), -2, "2^24")])
 def test_scan_refuses(lib, over, code, text):
