@@ -1,5 +1,9 @@
 """GPU parity of a hybrid target's recurrent layers (hspec_op_chunk_scan) and of the rules of its logits (hspec_op_adjust_logits) against
 oracle/state_oracle.py: odd sizes, mixed requests, padded batches, kept rows, values that are not finite, captured calls, other streams."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -579,3 +583,33 @@ def test_iterations_of_a_hybrid_target(hs):
         np.testing.assert_array_equal(_wide(a.conv), conv)
         assert (np.abs(_wide(a.ssm) - ssm) <= SCAN * size).all()
     assert max(counts) > 1 and hs.hspec_op_device_status(clear=True)["bad_inputs"] == 0
+
+
+FIRST_CALL = """
+import sys, torch
+import paper_2609_24197_b200 as hs
+sys.path.insert(0, "tests")
+import test_gpu_state as t
+a, b = (t.Layer(2, 64, 128, 1, [3, 200, 20], dtype=torch.float32, seed=40) for _ in range(2))
+z, rules = t._rules(5001, [3, 0, 9], seed=41)
+out, ws = torch.empty_like(z), a.workspace(hs)
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    if sys.argv[1] == "scan": a.run(hs, ws=ws)
+    else: hs.hspec_op_adjust_logits(z, out, **rules)
+graph.replay()
+torch.cuda.synchronize()
+if sys.argv[1] == "scan":
+    b.run(hs)
+    torch.cuda.synchronize()
+    assert torch.equal(a.y, b.y) and torch.equal(a.ssm, b.ssm)
+else:
+    t._check_rules(hs, z, rules)
+"""
+
+
+@pytest.mark.parametrize("what", ["scan", "rules"])
+def test_the_first_call_of_a_process_may_be_a_captured_one(what):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALL, what], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0, done.stderr[-1500:]
