@@ -429,7 +429,9 @@ size_t hspec_verify_workspace_bytes(int32_t B, int32_t k);
  *   y           out [T, ld_y] fp32, bf16 or fp16 (y_dtype), all rows of all requests; NULL: the states alone
  * Single tokens, draft blocks and pieces of prompts may be mixed.  A verification's pass runs with keep all zero (keep_more 0); once
  * hspec_op_verify has counted the drafts that stand, the same rows with y NULL, keep = n_accept and keep_more = 1 move the states on.
- * States that the call does not store keep their bits.  Accumulation and states are 32-bit.  At most 65535 requests.
+ * States that the call does not store keep their bits.  Accumulation and states are 32-bit.  Where P is 64 and N 128 and there are more than 2 B rows, outputs
+ * come from tensor-core products of operands in 16 bits (two bf16 parts): off by some 5e-6 of their size, elsewhere by 2e-7, before they are
+ * rounded to y_dtype.  At most 65535 requests.
  * workspace: hspec_chunk_scan_workspace_bytes (it grows with T and B, so that of the largest call does for all), 256-byte aligned, contents undefined
  * between calls; calls that may overlap on the GPU need one each. */
 int hspec_op_chunk_scan(const void* zxbcdt, int32_t in_dtype, int64_t ld_in, const float* dt_raw, const float* conv_w, const float* conv_b,

@@ -6,12 +6,15 @@
 // chunk one after another, the heads of a request side by side.
 //
 // The tensor cores take 16-bit operands, the states want more: every operand is split into a bf16 head and a bf16 remainder (16 bits together, any
-// exponent of 32 bits), and three products, head x head + head x remainder + remainder x head, leave a relative error of about 2^-18 a term.
+// exponent of 32 bits), and three products, head x head + head x remainder + remainder x head, leave a relative error of some 2^-18 a term, 3 x 2^-16 at
+// most (32-bit outputs are off by 5e-6 of their size; the states, sums of many terms of one sign and kept in 32 bits from chunk to chunk, by 3e-7).
 //
 //   scan_prep_kernel   a block a chunk and group: convolves B and C, writes both split in the layouts in which the next kernel's products take them,
 //                      and the scores C_t . B_s below the diagonal (mma.sync: the heads of a group share them, so they are little work)
-//   scan_long_kernel   one block an SM over (request, head) items, longest requests first: a warp each to fetch B, to issue the products and to sum up the
-//                      steps; and four warps each for scores (times decays, into tensor memory), x (convolved and split), state, and outputs
+//   scan_long_kernel   one block an SM over (request, head) items, longest requests first; all its warps go through a chunk's work together
+//
+// A prompt of 8192 rows, 128 heads: 532 us, of them 505 in the second kernel and 31 in the first (they overlap at their ends).  A chunk and head takes 15 000
+// clocks: 4800 are instructions to issue, some 4000 the products, the rest the latency of one phase after another with 16 warps on the SM.
 #include "chunk_scan.cuh"
 
 #include <atomic>
@@ -161,7 +164,7 @@ __global__ void __launch_bounds__(256) scan_prep_kernel(LongArgs a) {
 // ---------------------------------------------------------------------------------------------------
 // All warps go through a chunk's work together, two block barriers a chunk: what the products need (x split and the scores into place), then, under the
 // products, what can be done ahead (the next chunk's convolution and steps, this one's gates), then what the products gave (outputs, state).  (With a
-// role for every four to eight warps and barriers in shared memory between them a chunk took 16 thousand clocks: a warp alone on its scheduler runs at its
+// role for every four to eight warps and barriers in shared memory between them the 8192 rows took 1514 us, then 560 without: a warp alone on its scheduler runs at its
 // instructions' latency, and those that wait take the others' issue slots with their polling.)
 constexpr int LONG_THREADS = 512;
 constexpr int SM_B = 0, SM_X = 65536, SM_XW = SM_X + 32768, SM_S = SM_XW + 32768;    // head, remainder each

@@ -16,10 +16,10 @@ pytestmark = pytest.mark.gpu
 HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}       # half a step, relative to the value
 # fp16 has the same step for all values below 2^-14, 2^-24: half of it is what they may be off by, whatever their size (bf16 and fp32 go on to 2^-126).
 SMALL = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
-# What a scan's results may be off by, relative to the sum of the absolute values that enter them.  A product of operands in two bf16 parts: 2^-18 for each
-# operand's rest and 2^-18 for the product of the remainders, for C . B, its weights with x, and C with the state: 9 x 2^-18.  Sums of up to 256 terms in 32
-# bits: 2^8 x 2^-24 = 2^-16.  Convolutions, SiLU, steps and exponentials (arguments up to some 60, so 2^-18 in the power) each a few 2^-20.  Together below
-# 2^-14.
+# What a scan's results may be off by, relative to the sum of the absolute values that enter them.  A product of operands in two bf16 parts: 2^-16 at most and
+# some 2^-18 in the mean for each operand's rest and for the product of the remainders; C . B, its weights with x, and C with the state: 9 x 2^-18 where not all
+# are off by their most in one direction (these are sums of a hundred terms, or of one whose factors are such sums).  Sums of up to 256 terms in 32 bits:
+# 2^8 x 2^-24 = 2^-16.  Convolutions, SiLU, steps and exponentials (arguments up to some 60, so 2^-18 in the power) each a few 2^-20.  Together below 2^-14.
 SCAN = 2.0 ** -14
 
 
