@@ -399,6 +399,8 @@ template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
 __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) {
   constexpr bool SMALL = PR * NPT <= 8;                      // few elements a thread: the rows' operands and gates are fetched far ahead
   constexpr int TILE = state_tile(PR, NPT);                  // tokens that are fetched together
+  constexpr int NP = L * NPT;                                // N is not above it
+  constexpr int B_AT = 4, C_AT = B_AT + NP, X_AT = C_AT + NP;          // of a row in shared memory: dt, decay | B | C | x
   constexpr int DUP = L / PR;                                // lanes that end up with the same row's sum
   constexpr int ROWS = (TILE + DUP - 1) / DUP;               // tokens of a tile whose outputs a lane finishes
   const ChunkScanCall& c = a.c;
@@ -460,8 +462,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
 
   const size_t at0 = a.s.row(b, r.q0, 0);
   extern __shared__ __align__(16) float sm[];
-  const int xw = (a.p_block + 3) / 4 * 4, width = 2 * a.np + xw + 2;   // B | C | x | dt, decay
-  const int per = (width + 3) / 4 * 4, stage = per * TILE;
+  const int per = X_AT + (a.p_block + 3) / 4 * 4, stage = per * TILE;
   for (int i = tid; i < 2 * stage; i += blockDim.x) sm[i] = 0.f;       // (what lies behind N and P stays zero)
   __syncthreads();
   // fetches tokens first .. first + TILE - 1 of the request into a stage
@@ -470,26 +471,32 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     float* dst = sm + buf * stage;
     const float* rows = a.s.xbc + (at0 + first) * a.s.pitch;
     const int xn = min(a.p_block, c.P - p0);
+    // (a thread's elements lie blockDim apart: a step forward in the rows and in the row)
     if (VECN && c.P % 4 == 0) {
-      const int nv = c.N / 4, xv = xn / 4, all = 2 * nv + xv;
-      for (int i = tid; i < count * all; i += blockDim.x) {
-        const int row = i / all, e = i % all;
+      const int nv = c.N / 4, all = 2 * nv + xn / 4, step = blockDim.x % all, down = blockDim.x / all;
+      for (int row = tid / all, e = tid % all; row < count; row += down, e += step) {
+        if (e >= all) {
+          e -= all;
+          if (++row >= count) break;
+        }
         const int from = e < nv ? c.Di + g * c.N + 4 * e : e < 2 * nv ? c.Di + (c.G + g) * c.N + 4 * (e - nv) : h * c.P + p0 + 4 * (e - 2 * nv);
-        const int to = e < nv ? 4 * e : e < 2 * nv ? a.np + 4 * (e - nv) : 2 * a.np + 4 * (e - 2 * nv);
+        const int to = e < nv ? B_AT + 4 * e : e < 2 * nv ? C_AT + 4 * (e - nv) : X_AT + 4 * (e - 2 * nv);
         cp_async16(smem_u32(dst + row * per + to), rows + size_t(row) * a.s.pitch + from, true);
       }
     } else {
-      const int all = 2 * c.N + xn;
-      for (int i = tid; i < count * all; i += blockDim.x) {
-        const int row = i / all, e = i % all;
+      const int all = 2 * c.N + xn, step = blockDim.x % all, down = blockDim.x / all;
+      for (int row = tid / all, e = tid % all; row < count; row += down, e += step) {
+        if (e >= all) {
+          e -= all;
+          if (++row >= count) break;
+        }
         const int from = e < c.N ? c.Di + g * c.N + e : e < 2 * c.N ? c.Di + (c.G + g) * c.N + e - c.N : h * c.P + p0 + e - 2 * c.N;
-        const int to = e < c.N ? e : e < 2 * c.N ? a.np + e - c.N : 2 * a.np + e - 2 * c.N;
+        const int to = e < c.N ? B_AT + e : e < 2 * c.N ? C_AT + e - c.N : X_AT + e - 2 * c.N;
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst + row * per + to)), "l"(rows + size_t(row) * a.s.pitch + from) : "memory");
       }
     }
     if (tid < count)
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst + tid * per + 2 * a.np + xw)),
-                   "l"(a.s.step + (at0 + first + tid) * c.H + h) : "memory");
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst + tid * per)), "l"(a.s.step + (at0 + first + tid) * c.H + h) : "memory");
     cp_async_commit();
   };
   // the row of the state whose output the lane finishes, and its place among the lanes that do
@@ -500,13 +507,12 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   constexpr int GATES = SMALL ? TILE * PR / L : 1;
   float* gates = sm + 2 * stage;                             // [2][TILE][p_block]
   float ahead[GATES];
+  const int gate_row = tid / a.p_block, gate_p = p0 + tid % a.p_block, gate_rows = L / PR;       // (blockDim / p_block of them a step)
   auto fetch_gates = [&](int first) {
-    const int count = min(TILE, upto - first);
+    const int count = gate_p < c.P ? min(TILE, upto - first) : 0;
+    const TI* from = reinterpret_cast<const TI*>(c.x) + size_t(r.q0 + first + gate_row) * c.ld_x + h * c.P + gate_p;
 #pragma unroll
-    for (int i = 0; i < GATES; ++i) {
-      const int at = tid + i * blockDim.x, row = at / a.p_block, p = p0 + at % a.p_block;
-      ahead[i] = row < count && p < c.P ? to_f32(reinterpret_cast<const TI*>(c.x)[size_t(r.q0 + first + row) * c.ld_x + h * c.P + p]) : 0.f;
-    }
+    for (int i = 0; i < GATES; ++i) ahead[i] = gate_row + i * gate_rows < count ? to_f32(from[size_t(i * gate_rows) * c.ld_x]) : 0.f;
   };
   auto put_gates = [&](int buf) {
 #pragma unroll
@@ -536,20 +542,20 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     // a row's addition to the state; the sum of this lane's row of the state with C
     auto add = [&](int row) {
       const float* now = rows + row * per;
-      const float2 step = *reinterpret_cast<const float2*>(now + 2 * a.np + xw);
+      const float2 step = *reinterpret_cast<const float2*>(now);
       const uint64_t decay = pack_f32x2(step.y, step.y);
       uint64_t xd[PR], y2[PR];
 #pragma unroll
       for (int i = 0; i < PR; ++i) {
-        const float x = now[2 * a.np + (pt - p0) + i];
+        const float x = now[X_AT + (pt - p0) + i];
         xd[i] = pack_f32x2(step.x * x, step.x * x);
         y2[i] = 0ull;
       }
 #pragma unroll
       for (int k = 0; k < NPT / 4; ++k) {
-        const ulonglong2 Bv = *reinterpret_cast<const ulonglong2*>(now + 4 * (l + L * k));
+        const ulonglong2 Bv = *reinterpret_cast<const ulonglong2*>(now + B_AT + 4 * (l + L * k));
         ulonglong2 Cv;
-        if (Y) Cv = *reinterpret_cast<const ulonglong2*>(now + a.np + 4 * (l + L * k));
+        if (Y) Cv = *reinterpret_cast<const ulonglong2*>(now + C_AT + 4 * (l + L * k));
 #pragma unroll
         for (int i = 0; i < PR; ++i) {
           S[i][2 * k] = fma_f32x2(decay, S[i][2 * k], mul_f32x2(xd[i], Bv.x));
@@ -593,7 +599,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
       float g;
       if constexpr (SMALL) g = gates[(buf * TILE + row) * a.p_block + pm - p0];
       else g = silu_f32(gate[row / DUP]);
-      store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, rows[row * per + 2 * a.np + pm - p0], sum) * g, c.status);
+      store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, rows[row * per + X_AT + pm - p0], sum) * g, c.status);
     };
     auto one = [&](int row) {
       const float sum = add(row);
@@ -648,8 +654,7 @@ cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
   while (groups * L > 32 && (groups / 2) * PR >= c.P) groups /= 2;
   a.p_block = groups * PR;
   a.p_blocks = (c.P + a.p_block - 1) / a.p_block;
-  a.np = (c.N + 3) / 4 * 4 > L * NPT ? (c.N + 3) / 4 * 4 : L * NPT;
-  const int per = (2 * a.np + (a.p_block + 3) / 4 * 4 + 2 + 3) / 4 * 4;
+  const int per = 4 + 2 * L * NPT + (a.p_block + 3) / 4 * 4;
   constexpr int TILE = state_tile(PR, NPT);
   const size_t smem = size_t(2) * TILE * (per + (PR * NPT <= 8 ? a.p_block : 0)) * 4;
   const bool vec = c.N % 4 == 0 && c.Di % 4 == 0;

@@ -54,7 +54,6 @@ struct StateArgs {
   ChunkScanCall c;
   ScanScratch s;
   int p_blocks, p_block;             // blocks of a head, rows of its state in each
-  int np;                            // padded N: row pitch of B and C in shared memory
   int y_vec;                         // two outputs start on their boundary
 };
 cudaError_t scan_block_launch(const StateArgs& a, cudaStream_t stream);
