@@ -6,8 +6,8 @@
 // Row after row, any shape, two kernels.  scan_rows_kernel convolves the rows into a scratch of 32-bit rows, with their steps and decays; a thread takes four
 // channels of some rows, the thread of a request's first rows also moves the carried rows on, which nobody else reads.  scan_state_kernel carries the states
 // through the rows: a block has some rows of a head's state in registers, from the first token to the last, and reads the convolved rows from shared
-// memory, a few tokens ahead of their use.  Single tokens are bound by the state, which is read and written once (64 of 160 heads of 64 x 128: 132 us,
-// 5.2 TB/s), long requests with small states by the chain of their rows (170 ns a row; 29 requests of up to 700 rows, 8 heads of 64 x 16: 124 us).
+// memory, a few tokens ahead of their use.  Single tokens are bound by the state, which is read and written once (64 of 160 heads of 64 x 128: 119 us,
+// 5.7 TB/s), long requests with small states by the chain of their rows (100 ns a row; 29 requests of up to 700 rows, 8 heads of 64 x 16: 84 us).
 // By products, heads of 64 channels with 128 state elements: scan_groups_kernel convolves, sums up the steps and multiplies C with B for requests of up to 32
 // rows, which scan_block_kernel finishes; scan_prep_kernel and scan_long_kernel take those with more.  Where these are chosen stands at chunk_scan_launch.
 #include "chunk_scan.cuh"
@@ -306,7 +306,7 @@ template <typename TI, int K, bool VEC>
 __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
   const ChunkScanCall& c = a.c;
   pdl_wait();
-  pdl_trigger();
+  // (nor does the next one here: 17 rows of 32 requests 94 us with an early start, 82 without)
   extern __shared__ __align__(16) float rows_sm[];           // B, then C: [SCAN_FEW][CB_PITCH] each
   if (blockIdx.x == 0) {
     count_bad(c);
@@ -765,8 +765,8 @@ size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int 
 
 
 cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
-  // Row after row where there are hardly more rows than requests: nothing but the state counts then (64 tokens of 64 requests 137 us, with products and the
-  // launches for requests with many rows 184; 17 rows of 32 requests 182 and 103), and a request that has many of the rows all the same takes less than the others' states.
+  // Row after row where there are hardly more rows than requests: nothing but the state counts then (64 tokens of 64 requests 119 us, with products and the
+  // launches for requests with many rows 184; 17 rows of 32 requests 182 and 82), and a request that has many of the rows all the same takes less than the others' states.
   const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G, scan_has_blocks(c.P, c.N) && c.T > 2ll * c.B);
   char* ws = reinterpret_cast<char*>(c.ws);
   ConvArgs a{};

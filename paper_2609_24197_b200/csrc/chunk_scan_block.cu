@@ -8,7 +8,7 @@
 // and C in the same one.  Operands are split into a bf16 head and a bf16 remainder, three products for one (a
 // relative error of some 2^-18 a term, 3 x 2^-16 at most: 32-bit outputs are off by 5e-6 of their size, 16-bit ones round more away).
 // The kept rows are added to the state in 32 bits.  (Row after row through the state, 17 rows of 32 requests of 128 heads take 182 us, three operations an element
-// and row; so they take 92, 1.8 TB/s: 13 to 18 for the kernel in front, 70 here for 150 MB of states and rows with 2 x 10^9 multiply-adds of the fragments.)
+// and row; so they take 80, 2 TB/s: 13 to 18 for the kernel in front, 70 here for 150 MB of states and rows with 2 x 10^9 multiply-adds of the fragments.)
 #include "chunk_scan.cuh"
 
 #include <atomic>
