@@ -439,21 +439,29 @@ __global__ void __launch_bounds__(LONG_THREADS, 1) scan_long_kernel(LongArgs a) 
         float odd0, odd1;
         unpack_f32x2(odd, odd0, odd1);
         if (odd0 + odd1 != 0.f) {
+          // (x alone decides: its weighted form is NaN in every row of a chunk that has a step without a number, and stays so for the state)
+          uint32_t bad = Y ? 0xffff : 0;
+          if (!Y) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float x0, x1;
+              unpack_f32x2(v[i], x0, x1);
+              bad |= (fabsf(x0) < INFINITY ? 0u : 1u << 2 * i) | (fabsf(x1) < INFINITY ? 0u : 2u << 2 * i);
+            }
+          }
 #pragma unroll 1
-          for (int i = 0; i < 8; ++i) {
-            uint8_t* at = smem + SM_X + warp * 1024 + i * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3) * 4;
-#pragma unroll 1
-            for (int e = 0; e < 2; ++e) {
-              uint16_t* x = reinterpret_cast<uint16_t*>(at) + e;
-              uint16_t* w = reinterpret_cast<uint16_t*>(at + SM_XW - SM_X) + e;
-              const bool bad = (Y && (x[0] & 0x7f80) == 0x7f80) || (Y && (x[8192] & 0x7f80) == 0x7f80) || (w[0] & 0x7f80) == 0x7f80 || (w[8192] & 0x7f80) == 0x7f80;
-              if (!bad) continue;
-              if (Y) x[0] = x[8192] = 0;
-              w[0] = w[8192] = 0;
-              if (first + i < range.len) {
-                atomicMin(&bars->first_odd[k & 1][cp + e], first + i);
-                *reinterpret_cast<volatile int*>(&bars->any_odd[k & 1]) = 1;
-              }
+          for (; bad; bad &= bad - 1) {
+            const int i = (__ffs(bad) - 1) >> 1, e = (__ffs(bad) - 1) & 1;
+            uint16_t* x = reinterpret_cast<uint16_t*>(smem + SM_X + warp * 1024 + i * 128 + (((lane >> 2) ^ i) << 4) + (lane & 3) * 4) + e;
+            uint16_t* w = x + (SM_XW - SM_X) / 2;
+            if (Y) {
+              if ((x[0] & 0x7f80) != 0x7f80) continue;
+              x[0] = x[8192] = 0;
+            }
+            w[0] = w[8192] = 0;
+            if (first + i < range.len) {
+              atomicMin(&bars->first_odd[k & 1][cp + e], first + i);
+              *reinterpret_cast<volatile int*>(&bars->any_odd[k & 1]) = 1;
             }
           }
         }

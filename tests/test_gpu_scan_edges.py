@@ -1,0 +1,61 @@
+"""Edges of hspec_op_chunk_scan on the GPU: rows that are no numbers, narrow states, long chains of rows, narrow convolutions, errors that others left."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_state import HALF, SCAN, Layer, _wide
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hs():
+    import paper_2609_24197_b200 as m
+    m.load_library()
+    m.hspec_op_device_status(clear=True)
+    return m
+
+
+def _near(got, want, size, half=0.0, bound=SCAN):
+    return np.abs(got - want) <= half * np.abs(want) + bound * size
+
+
+# chunks of 128 rows, blocks of up to 32, row after row
+WAYS = [((2, 64, 128, 1), [300], 40), ((2, 64, 128, 1), [300], 130), ((2, 64, 128, 1), [300], 299), ((2, 64, 128, 1), [20], 5), ((2, 64, 128, 1), [20], 18),
+        ((2, 40, 24, 1), [300], 130), ((4, 64, 16, 1), [300], 40)]
+
+
+@pytest.mark.parametrize("shape,new,where", WAYS)
+def test_a_row_without_numbers_reaches_no_row_in_front_of_it(hs, shape, new, where):
+    """All of a row NaN: gate, x, B, C and dt.  Every row is kept."""
+    a, b = (Layer(*shape, new, dtype=torch.float32, seed=50) for _ in range(2))
+    a.rows[where] = float("nan")
+    a.run(hs)
+    torch.cuda.synchronize()
+    got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
+    assert _near(got, want, size, HALF[torch.float32])[:where].all()
+    assert not np.isfinite(got[where:]).any()
+    assert not torch.isfinite(a.ssm[a.slots.long()]).any()
+
+
+@pytest.mark.parametrize("shape,new,where", WAYS)
+@pytest.mark.parametrize("behind", [1, 20, -2])
+@pytest.mark.parametrize("value,step", [(float("inf"), float("nan")), (float("nan"), float("inf"))])
+def test_x_and_a_step_that_are_no_numbers_in_different_rows(hs, shape, new, where, behind, value, step):
+    a, b = (Layer(*shape, new, dtype=torch.float32, seed=51) for _ in range(2))
+    H, P, N, G = shape
+    at = min(where + behind, new[0] - 1)
+    a.rows[where, a.Di + 3] = value                            # a channel of x of the first head
+    a.rows[at, 2 * a.Di + 2 * G * N] = step                    # that head's step
+    a.run(hs)
+    torch.cuda.synchronize()
+    got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
+    near = _near(got, want, size, HALF[torch.float32])
+    assert near[:min(where, at)].all() and near[:, P:].all()   # rows in front of both, and all other heads
+    others = [p for p in range(P) if p != 3]
+    assert near[:at, others].all()                             # the head's other channels, up to its step
+    assert not np.isfinite(got[where:, 3]).any() and not np.isfinite(got[at + 1:, :P]).any()
