@@ -650,13 +650,17 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
 template <typename TI, int L, int PR, int NPT>
 cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
   const ChunkScanCall& c = a.c;
-  int groups = STATE_THREADS / L;
+  // (at most 64 rows of the state where a lane has one of them: x and the gates of more, 32 tokens twice, would not fit)
+  constexpr int MOST = L == 1 ? 64 : STATE_THREADS / L;
+  constexpr auto smem_of = [](int p_block) {
+    return size_t(2) * state_tile(PR, NPT) * (4 + 2 * L * NPT + (p_block + 3) / 4 * 4 + (PR * NPT <= 8 ? p_block : 0)) * 4;
+  };
+  static_assert(smem_of(MOST * PR) <= 48 * 1024, "more shared memory than a kernel has without asking: the launch would fail behind the rows' kernel");
+  int groups = MOST;
   while (groups * L > 32 && (groups / 2) * PR >= c.P) groups /= 2;
   a.p_block = groups * PR;
   a.p_blocks = (c.P + a.p_block - 1) / a.p_block;
-  const int per = 4 + 2 * L * NPT + (a.p_block + 3) / 4 * 4;
-  constexpr int TILE = state_tile(PR, NPT);
-  const size_t smem = size_t(2) * TILE * (per + (PR * NPT <= 8 ? a.p_block : 0)) * 4;
+  const size_t smem = smem_of(a.p_block);
   const bool vec = c.N % 4 == 0 && c.Di % 4 == 0;
   const dim3 grid(unsigned(c.H * a.p_blocks), unsigned(c.B));
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(unsigned(groups * L)), smem, stream, a); };

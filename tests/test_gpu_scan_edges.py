@@ -59,3 +59,17 @@ def test_x_and_a_step_that_are_no_numbers_in_different_rows(hs, shape, new, wher
     others = [p for p in range(P) if p != 3]
     assert near[:at, others].all()                             # the head's other channels, up to its step
     assert not np.isfinite(got[where:, 3]).any() and not np.isfinite(got[at + 1:, :P]).any()
+
+
+@pytest.mark.parametrize("H,P,N,G", [(2, 65, 4, 1), (1, 128, 3, 1), (2, 65, 1, 2), (4, 128, 4, 2), (1, 256, 3, 1), (1, 200, 1, 1), (2, 64, 2, 1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_states_of_up_to_four_elements_and_wide_heads(hs, H, P, N, G, dtype):
+    new = [1, 17, 0, 33, 70]
+    keep = torch.tensor([1, 9, 0, 33, 64], dtype=torch.int32, device="cuda")
+    Layer(H, P, N, G, new, dtype=dtype, pad=3, seed=52).check(hs)
+    a = Layer(H, P, N, G, new, dtype=dtype, seed=53)
+    _, conv, ssm = a.reference(keep=keep)
+    size = a.reference(sizes=True, keep=keep)[2]
+    a.run(hs, y=None, keep=keep)
+    np.testing.assert_array_equal(_wide(a.conv), conv)
+    assert _near(_wide(a.ssm), ssm, size).all()
