@@ -731,8 +731,7 @@ cudaError_t launch_vec(const LongArgs& a, cudaStream_t stream) {
   }
   const long long chunks = (long long)(scan_max_chunks(c.T, c.B)) * c.G, heads = (long long)(scan_max_long(c.T, c.B)) * c.H;
   // (not to start early: its blocks would take the room of those of the kernel in front, which has most of the work where no request has many rows)
-  scan_prep_kernel<TI, VEC><<<unsigned(chunks < 148 ? chunks : 148), 256, PREP_SMEM, stream>>>(a);
-  e = cudaGetLastError();
+  e = launch_behind(scan_prep_kernel<TI, VEC>, dim3(unsigned(chunks < 148 ? chunks : 148)), dim3(256), PREP_SMEM, stream, a);
   if (e != cudaSuccess) return e;
   return launch_pdl(c.y ? scan_long_kernel<TI, true, VEC> : scan_long_kernel<TI, false, VEC>, dim3(unsigned(heads < 148 ? heads : 148)), dim3(LONG_THREADS),
                     LONG_SMEM, stream, a);

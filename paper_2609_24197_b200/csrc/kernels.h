@@ -96,7 +96,17 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
   return e;
 }
 
-// The same with the grid's CTAs in clusters of the given shape.
+// One that does not start before the kernel in front of it has ended.  (The code is this launch's own, not what an earlier call of the thread left behind.)
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_behind(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e;
+}
+
+// launch_pdl() with the grid's CTAs in clusters of the given shape.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, dim3 cluster, size_t smem, cudaStream_t stream, Args&&... args) {
   if (cluster.x * cluster.y * cluster.z == 1) return launch_pdl(kernel, grid, block, smem, stream, args...);

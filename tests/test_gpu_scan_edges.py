@@ -73,3 +73,30 @@ def test_states_of_up_to_four_elements_and_wide_heads(hs, H, P, N, G, dtype):
     a.run(hs, y=None, keep=keep)
     np.testing.assert_array_equal(_wide(a.conv), conv)
     assert _near(_wide(a.ssm), ssm, size).all()
+
+
+LEFT_ERROR = """
+import sys, ctypes, torch
+import paper_2609_24197_b200 as hs
+sys.path.insert(0, "tests")
+import test_gpu_state as t
+a, b = (t.Layer(2, 64, 128, 1, [300, 20], dtype=torch.float32, seed=54) for _ in range(2))
+for x in (b, a):
+    ws = x.workspace(hs)
+    if x is a:                                                 # a call on the legacy stream fails while a stream that waits for that one is captured
+        cudart = ctypes.CDLL("libcudart.so.12")
+        side, none = ctypes.c_void_p(), ctypes.c_void_p()
+        assert cudart.cudaStreamCreate(ctypes.byref(side)) == 0 and cudart.cudaStreamBeginCapture(side, 0) == 0
+        assert hs.hspec_op_device_status()["rc"] == -6
+        cudart.cudaStreamEndCapture(side, ctypes.byref(none))
+        cudart.cudaGetLastError()
+    x.run(hs, ws=ws)
+torch.cuda.synchronize()
+assert torch.equal(a.y, b.y) and torch.equal(a.ssm, b.ssm) and torch.equal(a.conv, b.conv)
+"""
+
+
+def test_an_error_that_another_call_left_does_not_end_the_scan_in_the_middle():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", LEFT_ERROR], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0, done.stderr[-1500:]
