@@ -231,14 +231,15 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
 // products by pairs of rows.
 constexpr int CB_PITCH = 128 + 4;
 // x of a request with few rows: a thread two channels.
-template <typename TI, bool VEC>
+template <typename TI, int K, bool VEC>
 __device__ void x_of_request(const ConvArgs& a, int b, int ch) {
   const ChunkScanCall& c = a.c;
   const ScanRequest r = scan_request(c, b);
-  const int n = scan_upto(c, r), K1 = c.d_conv - 1;
+  const int n = scan_upto(c, r);
+  constexpr int K1 = K - 1;
   if (n > a.s.few || ch >= c.Di || (n == 0 && !r.stores())) return;
   const RawRows<VEC, 2, TI> raw(c, r, ch);
-  Taps<1> taps;
+  Taps<1, K> taps;
   taps.load(c, ch);
   Word<TI, 2> front[3] = {};
   uint64_t before[3][1];
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
   // (a request's blocks: its groups, its steps, 512 channels of x each)
   const int x_blocks = (c.Di + 2 * CONV_THREADS - 1) / (2 * CONV_THREADS), each = c.G + 1 + x_blocks;
   const int b = (blockIdx.x - 1) / each, g = (blockIdx.x - 1) % each;
-  if (g > c.G) { x_of_request<TI, VEC>(a, b, (g - c.G - 1) * 2 * CONV_THREADS + 2 * threadIdx.x); return; }
+  if (g > c.G) { x_of_request<TI, K, VEC>(a, b, (g - c.G - 1) * 2 * CONV_THREADS + 2 * threadIdx.x); return; }
   if (g == c.G) { steps_of_request<TI>(a, b); return; }
   const ScanRequest r = scan_request(c, b);
   const int n = scan_upto(c, r), tid = threadIdx.x, e = tid & 127;

@@ -149,25 +149,32 @@ struct RawRows {
   }
 };
 
-// The convolution of 2 H channels: taps in front of a narrower one are zero.
-template <int H>
+// The convolution of 2 H channels.  A narrower one has the last of four taps; the rows in front of these are left out, not taken times zero: they may be
+// no numbers.  K: its width, or 0: the call's.  (In the kernels of long requests the questions cost registers: those for rows on word boundaries are for K = 4.)
+template <int H, int K>
 struct Taps {
   uint64_t w[4][H], b[H];            // [tap][channels]
+  int width;
   __device__ __forceinline__ void load(const ChunkScanCall& c, int ch) {
-    const int K = c.d_conv;
+    const int taps = width = K ? K : c.d_conv;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      const float* f = c.conv_w + size_t(ch + 2 * h) * K;
+      const float* f = c.conv_w + size_t(ch + 2 * h) * taps;
       b[h] = pack_f32x2(c.conv_b[ch + 2 * h], c.conv_b[ch + 2 * h + 1]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j][h] = j >= 4 - K ? pack_f32x2(f[j - (4 - K)], f[j - (4 - K) + K]) : 0ull;
+      for (int j = 0; j < 4; ++j) w[j][h] = j >= 4 - taps ? pack_f32x2(f[j - (4 - taps)], f[j - (4 - taps) + taps]) : 0ull;
     }
   }
   // SiLU of the convolution at the row behind `before` (oldest first), which moves on by that row
   __device__ __forceinline__ void next(uint64_t (&before)[3][H], const uint64_t (&now)[H], uint64_t (&v)[H]) const {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      v[h] = silu2(fma_f32x2(w[3][h], now[h], fma_f32x2(w[2][h], before[2][h], fma_f32x2(w[1][h], before[1][h], fma_f32x2(w[0][h], before[0][h], b[h])))));
+      const int taps = K ? K : width;
+      uint64_t sum = b[h];
+      if (taps > 3) sum = fma_f32x2(w[0][h], before[0][h], sum);
+      if (taps > 2) sum = fma_f32x2(w[1][h], before[1][h], sum);
+      if (taps > 1) sum = fma_f32x2(w[2][h], before[2][h], sum);
+      v[h] = silu2(fma_f32x2(w[3][h], now[h], sum));
       before[0][h] = before[1][h]; before[1][h] = before[2][h]; before[2][h] = now[h];
     }
   }

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) scan_prep_kernel(LongArgs a) {
       const int cg = tid & 63, first = (tid >> 6) * 32;
       const bool isC = cg >= 32;
       const int n = (cg & 31) * 4, ch = c.Di + ((isC ? c.G : 0) + g) * NS + n, end = range.start + range.len;
-      Taps<2> t;
+      Taps<2, VEC ? 4 : 0> t;
       t.load(c, ch);
       const RawRows<VEC, 4, TI> raw(c, r, ch);
       Word<TI, 4> next[8], front[3];
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(LONG_THREADS, 1) scan_long_kernel(LongArgs a) 
       bulk_load(smem + SM_B, img + IMG_B, 65536, &bars->b_full);
       if (Y) bulk_load(smem + SM_G, img + IMG_G, IMG_BYTES - IMG_G, &bars->scores_full);
     }
-    Taps<1> taps;
+    Taps<1, VEC ? 4 : 0> taps;
     taps.load(c, h * NH + cp);
     const RawRows<VEC, 2, TI> raw(c, r, h * NH + cp);
     const double rate = -exp(double(c.A_log[h])) * 1.4426950408889634;
@@ -744,7 +744,7 @@ cudaError_t launch_for(LongArgs a, cudaStream_t stream) {
   const int item = c.y_dtype == CHUNK_F32 ? 4 : 2;
   a.y_vec = c.y && on(c.y, 32) && c.ld_y % (32 / item) == 0 ? 1 : 0;
   a.z_vec = sizeof(TI) == 2 && on(c.x, 32) && c.ld_x % 16 == 0 ? 1 : 0;
-  const bool vec = c.Di % 4 == 0 && c.ld_x % 4 == 0 && on(c.x, 4 * sizeof(TI)) && on(c.conv_state, 4 * sizeof(TI));
+  const bool vec = c.d_conv == 4 && c.Di % 4 == 0 && c.ld_x % 4 == 0 && on(c.x, 4 * sizeof(TI)) && on(c.conv_state, 4 * sizeof(TI));
   return vec ? launch_vec<TI, true>(a, stream) : launch_vec<TI, false>(a, stream);
 }
 

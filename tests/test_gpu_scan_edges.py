@@ -100,3 +100,23 @@ def test_an_error_that_another_call_left_does_not_end_the_scan_in_the_middle():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", LEFT_ERROR], cwd=root, capture_output=True, text=True, timeout=100)
     assert done.returncode == 0, done.stderr[-1500:]
+
+
+@pytest.mark.parametrize("K", [1, 2, 3, 4])
+@pytest.mark.parametrize("shape,new,where", [((2, 64, 128, 1), [300], 130), ((2, 64, 128, 1), [300, 9], 250), ((2, 64, 128, 1), [20], 5), ((2, 40, 24, 1), [40], 9)])
+@pytest.mark.parametrize("place", ["x", "C"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_value_that_is_no_number_reaches_as_far_as_the_convolution(hs, shape, new, where, place, value, K):
+    a, b = (Layer(*shape, new, K=K, dtype=torch.float32, seed=55) for _ in range(2))
+    H, P, N, G = shape
+    a.rows[where, a.Di + (3 if place == "x" else a.Di + G * N + 5)] = value
+    a.run(hs)
+    torch.cuda.synchronize()
+    got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
+    near = _near(got, want, size, HALF[torch.float32])
+    assert near[:where].all() and near[new[0]:].all()
+    if place == "C":                                           # nothing of it stays in the state
+        assert near[where + K:].all() and not np.isfinite(got[where]).any()
+        assert _near(_wide(a.ssm), b.reference()[2], b.reference(sizes=True)[2]).all()
+    else:                                                      # from its row on, in its channel
+        assert np.delete(near, 3, axis=1).all() and not np.isfinite(got[where:new[0], 3]).any()
