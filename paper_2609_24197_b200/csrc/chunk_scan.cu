@@ -163,7 +163,9 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
       const size_t t = t0 + r;
       const float raw = c.dt_raw ? c.dt_raw[t * c.H + h] : to_f32(reinterpret_cast<const TI*>(c.x)[t * c.ld_x + c.Di + c.d_xBC + h]);
       const float dt = softplus_f32(raw + c.dt_bias[h]);
-      a.s.step[(out0 + r) * c.H + h] = make_float2(dt, expf(-dt * expf(c.A_log[h])));
+      const float fall = -dt * expf(c.A_log[h]), less = expm1f(fall);
+      const float decay = less > -0.5f ? 1.f + less : expf(fall);            // (what falls by half in a row does not add up errors)
+      a.s.step[(out0 + r) * c.H + h] = make_float4(dt, decay, less > -0.5f ? less - (decay - 1.f) : 0.f, 0.f);
     }
     return;
   }
@@ -393,26 +395,26 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
 
 // ---------------------------------------------------------------------------------------------------
 // The states through the rows.  A group of L lanes has PR rows of a head's state [P, N]: lane l of the group the elements n = 4 (l + L k) .. + 3.
-constexpr int STATE_THREADS = 128;
+// Decays are next to one, and there may be thousands of rows.  So a decay comes in two parts, and (CARRY) what a row's rounding leaves out of the state is
+// carried to the next: otherwise both add up, in one direction where rows are alike (8000 equal rows: 4e-4 of the sum of all that entered, so 1e-6).  It
+// costs 2 % where the chain of rows bounds (29 requests of up to 700 rows 84 -> 86 us), and 13 % for blocks (17 rows of 32 requests, 24 heads of 40 x 24: 31 ->
+// 35).  Requests of up to STATE_FEW rows go without in calls with hardly more rows than requests: the registers are those of their loads (64 tokens of 160
+// heads of 64 x 128 124 us; 145 with the rest carried).
+constexpr int STATE_THREADS = 128, STATE_FEW = 8;
 
 __host__ __device__ constexpr int state_tile(int pr, int npt) { return pr * npt <= 8 ? 32 : 8; }
-template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
-__global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) {
+template <typename TI, int L, int PR, int NPT, bool VECN, bool Y, bool CARRY>
+__device__ __forceinline__ void scan_state(const StateArgs& a, const ScanRequest& r, const int upto, const int h, const int b, const int p0, const int p_block) {
   constexpr bool SMALL = PR * NPT <= 8;                      // few elements a thread: the rows' operands and gates are fetched far ahead
   constexpr int TILE = state_tile(PR, NPT);                  // tokens that are fetched together
   constexpr int NP = L * NPT;                                // N is not above it
-  constexpr int B_AT = 4, C_AT = B_AT + NP, X_AT = C_AT + NP;          // of a row in shared memory: dt, decay | B | C | x
+  constexpr int B_AT = 4, C_AT = B_AT + NP, X_AT = C_AT + NP;          // of a row in shared memory: dt, decay, its rest | B | C | x
   constexpr int DUP = L / PR;                                // lanes that end up with the same row's sum
   constexpr int ROWS = (TILE + DUP - 1) / DUP;               // tokens of a tile whose outputs a lane finishes
   const ChunkScanCall& c = a.c;
-  const int tid = threadIdx.x, l = tid % L;
-  const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, g = h / (c.H / c.G);
-  const int p0 = (blockIdx.x % a.p_blocks) * a.p_block, pt = p0 + tid / L * PR;      // the block's and the thread's first rows
-  // (before the wait only what is at least two kernels back is read: the arrays that describe the chunk, and the states)
-  const ScanRequest r = scan_request(c, b);
-  const int upto = scan_upto(c, r);
-  if (upto > a.s.few) { pdl_wait(); return; }
-  uint64_t S[PR][NPT / 2];
+  const int tid = threadIdx.x, l = tid % L, g = h / (c.H / c.G);
+  const int pt = p0 + tid / L * PR;                          // the thread's first row (p0: the block's, p_block: as many)
+  uint64_t S[PR][NPT / 2], rest[CARRY ? PR : 1][CARRY ? NPT / 2 : 1] = {};         // the state, and what its rounding has left out so far
   float* state = c.ssm_state + ((size_t(r.slot < 0 ? 0 : r.slot) * c.H + h) * c.P + pt) * c.N;
 #pragma unroll
   for (int i = 0; i < PR; ++i) {
@@ -445,8 +447,10 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
         const int n = 4 * (l + L * k);
         if (pt + i >= c.P || n >= c.N) continue;
         float4 v;
-        unpack_f32x2(S[i][2 * k], v.x, v.y);
-        unpack_f32x2(S[i][2 * k + 1], v.z, v.w);
+        uint64_t lo = S[i][2 * k], hi = S[i][2 * k + 1];
+        if constexpr (CARRY) { lo = add_f32x2(lo, rest[i][2 * k]); hi = add_f32x2(hi, rest[i][2 * k + 1]); }
+        unpack_f32x2(lo, v.x, v.y);
+        unpack_f32x2(hi, v.z, v.w);
         float* p = state + size_t(i) * c.N + n;
         if (VECN) __stcs(reinterpret_cast<float4*>(p), v);
         else {
@@ -463,15 +467,17 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
 
   const size_t at0 = a.s.row(b, r.q0, 0);
   extern __shared__ __align__(16) float sm[];
-  const int per = X_AT + (a.p_block + 3) / 4 * 4, stage = per * TILE;
-  for (int i = tid; i < 2 * stage; i += blockDim.x) sm[i] = 0.f;       // (what lies behind N and P stays zero)
-  __syncthreads();
+  const int per = X_AT + (p_block + 3) / 4 * 4, stage = per * TILE;
+  if (c.N < NP || c.P - p0 < p_block) {                      // what lies behind N and P stays zero
+    for (int i = tid; i < 2 * stage; i += blockDim.x) sm[i] = 0.f;
+    __syncthreads();
+  }
   // fetches tokens first .. first + TILE - 1 of the request into a stage
   auto fetch = [&](int first, int buf) {
     const int count = min(TILE, upto - first);
     float* dst = sm + buf * stage;
     const float* rows = a.s.xbc + (at0 + first) * a.s.pitch;
-    const int xn = min(a.p_block, c.P - p0);
+    const int xn = min(p_block, c.P - p0);
     // (a thread's elements lie blockDim apart: a step forward in the rows and in the row)
     if (VECN && c.P % 4 == 0) {
       const int nv = c.N / 4, all = 2 * nv + xn / 4, step = blockDim.x % all, down = blockDim.x / all;
@@ -497,7 +503,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
       }
     }
     if (tid < count)
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(dst + tid * per)), "l"(a.s.step + (at0 + first + tid) * c.H + h) : "memory");
+      cp_async16(smem_u32(dst + tid * per), a.s.step + (at0 + first + tid) * c.H + h, true);
     cp_async_commit();
   };
   // the row of the state whose output the lane finishes, and its place among the lanes that do
@@ -508,7 +514,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   constexpr int GATES = SMALL ? TILE * PR / L : 1;
   float* gates = sm + 2 * stage;                             // [2][TILE][p_block]
   float ahead[GATES];
-  const int gate_row = tid / a.p_block, gate_p = p0 + tid % a.p_block, gate_rows = L / PR;       // (blockDim / p_block of them a step)
+  const int gate_row = tid / p_block, gate_p = p0 + tid % p_block, gate_rows = L / PR;       // (blockDim / p_block of them a step)
   auto fetch_gates = [&](int first) {
     const int count = gate_p < c.P ? min(TILE, upto - first) : 0;
     const TI* from = reinterpret_cast<const TI*>(c.x) + size_t(r.q0 + first + gate_row) * c.ld_x + h * c.P + gate_p;
@@ -517,7 +523,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
   };
   auto put_gates = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < GATES; ++i) gates[buf * TILE * a.p_block + tid + i * blockDim.x] = silu_f32(ahead[i]);
+    for (int i = 0; i < GATES; ++i) gates[buf * TILE * p_block + tid + i * blockDim.x] = silu_f32(ahead[i]);
   };
   fetch(0, 0);
   if (SMALL && Y) {
@@ -543,8 +549,8 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     // a row's addition to the state; the sum of this lane's row of the state with C
     auto add = [&](int row) {
       const float* now = rows + row * per;
-      const float2 step = *reinterpret_cast<const float2*>(now);
-      const uint64_t decay = pack_f32x2(step.y, step.y);
+      const float4 step = *reinterpret_cast<const float4*>(now);
+      const uint64_t decay = dup2(step.y), decay_rest = dup2(step.z), minus = dup2(-step.y);
       uint64_t xd[PR], y2[PR];
 #pragma unroll
       for (int i = 0; i < PR; ++i) {
@@ -559,8 +565,17 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
         if (Y) Cv = *reinterpret_cast<const ulonglong2*>(now + C_AT + 4 * (l + L * k));
 #pragma unroll
         for (int i = 0; i < PR; ++i) {
-          S[i][2 * k] = fma_f32x2(decay, S[i][2 * k], mul_f32x2(xd[i], Bv.x));
-          S[i][2 * k + 1] = fma_f32x2(decay, S[i][2 * k + 1], mul_f32x2(xd[i], Bv.y));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint64_t s = S[i][2 * k + e], more = fma_f32x2(decay_rest, s, mul_f32x2(xd[i], e ? Bv.y : Bv.x));
+            if constexpr (CARRY) {
+              const uint64_t all = fma_f32x2(decay, rest[i][2 * k + e], more), next = fma_f32x2(decay, s, all);
+              rest[i][2 * k + e] = fma_f32x2(fma_f32x2(minus, s, next), dup2(-1.f), all);
+              S[i][2 * k + e] = next;
+            } else {
+              S[i][2 * k + e] = fma_f32x2(decay, s, more);
+            }
+          }
           if (Y) {
             y2[i] = fma_f32x2(S[i][2 * k], Cv.x, y2[i]);
             y2[i] = fma_f32x2(S[i][2 * k + 1], Cv.y, y2[i]);
@@ -598,7 +613,7 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
     auto finish = [&](int row, float sum) {
       if (pm >= c.P) return;
       float g;
-      if constexpr (SMALL) g = gates[(buf * TILE + row) * a.p_block + pm - p0];
+      if constexpr (SMALL) g = gates[(buf * TILE + row) * p_block + pm - p0];
       else g = silu_f32(gate[row / DUP]);
       store_row(c.y, c.y_dtype, size_t(r.q0 + first + row) * c.ld_y + h * c.P + pm, fmaf(D, rows[row * per + X_AT + pm - p0], sum) * g, c.status);
     };
@@ -637,18 +652,54 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_state_kernel(StateArgs a) 
       }
       if (Y && first + TILE < upto) put_gates(buf ^ 1);
     } else {
-#pragma unroll
-      for (int row = 0; row < TILE; ++row) {
-        if (row >= count) break;
+      auto step = [&](int row) {
         one(row);
         if (first + row + 1 == r.keep && r.stores()) store();
+      };
+      if constexpr (CARRY) {                                 // (all eight mixed take more registers than there are)
+#pragma unroll 4
+        for (int row = 0; row < TILE; ++row) {
+          if (row >= count) break;
+          step(row);
+        }
+      } else {
+#pragma unroll
+        for (int row = 0; row < TILE; ++row) {
+          if (row >= count) break;
+          step(row);
+        }
       }
     }
     __syncthreads();
   }
 }
 
-template <typename TI, int L, int PR, int NPT>
+template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
+__global__ void __launch_bounds__(STATE_THREADS, NPT == 16 ? 3 : 5) scan_state_kernel(StateArgs a) {
+  const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, p0 = blockIdx.x % a.p_blocks * a.p_block;
+  // (before the wait only what is at least two kernels back is read: the arrays that describe the chunk, and the states)
+  const ScanRequest r = scan_request(a.c, b);
+  scan_state<TI, L, PR, NPT, VECN, Y, true>(a, r, scan_upto(a.c, r), h, b, p0, a.p_block);
+}
+// The same for calls with hardly more rows than requests.  (A request that has many of them all the same goes through half of the block's part at a time,
+// where a thread has many elements.)
+template <typename TI, int L, int PR, int NPT, bool VECN, bool Y>
+__global__ void __launch_bounds__(STATE_THREADS) scan_few_kernel(StateArgs a) {
+  const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, p0 = blockIdx.x % a.p_blocks * a.p_block;
+  const ScanRequest r = scan_request(a.c, b);
+  const int upto = scan_upto(a.c, r);
+  if (upto <= STATE_FEW) {
+    scan_state<TI, L, PR, NPT, VECN, Y, false>(a, r, upto, h, b, p0, a.p_block);
+  } else if constexpr (PR == 1) {
+    scan_state<TI, L, PR, NPT, VECN, Y, true>(a, r, upto, h, b, p0, a.p_block);
+  } else {
+#pragma unroll 1
+    for (int half = 0; half < a.p_block && p0 + half < a.c.P; half += a.p_block / 2)
+      scan_state<TI, L, PR / 2, NPT, VECN, Y, true>(a, r, upto, h, b, p0 + half, a.p_block / 2);
+  }
+}
+
+template <typename TI, int L, int PR, int NPT, bool CARRY>
 cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
   const ChunkScanCall& c = a.c;
   // (at most 64 rows of the state where a lane has one of them: x and the gates of more, 32 tokens twice, would not fit)
@@ -665,19 +716,25 @@ cudaError_t launch_state(StateArgs a, cudaStream_t stream) {
   const bool vec = c.N % 4 == 0 && c.Di % 4 == 0;
   const dim3 grid(unsigned(c.H * a.p_blocks), unsigned(c.B));
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(unsigned(groups * L)), smem, stream, a); };
-  if (c.y) return vec ? go(scan_state_kernel<TI, L, PR, NPT, true, true>) : go(scan_state_kernel<TI, L, PR, NPT, false, true>);
-  return vec ? go(scan_state_kernel<TI, L, PR, NPT, true, false>) : go(scan_state_kernel<TI, L, PR, NPT, false, false>);
+  auto pick = [&](auto with, auto without) { return c.y ? go(with) : go(without); };
+  if constexpr (CARRY)
+    return vec ? pick(scan_state_kernel<TI, L, PR, NPT, true, true>, scan_state_kernel<TI, L, PR, NPT, true, false>)
+               : pick(scan_state_kernel<TI, L, PR, NPT, false, true>, scan_state_kernel<TI, L, PR, NPT, false, false>);
+  else
+    return vec ? pick(scan_few_kernel<TI, L, PR, NPT, true, true>, scan_few_kernel<TI, L, PR, NPT, true, false>)
+               : pick(scan_few_kernel<TI, L, PR, NPT, false, true>, scan_few_kernel<TI, L, PR, NPT, false, false>);
 }
 
-template <typename TI>
+template <typename TI, bool CARRY>
 cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
   const int N = a.c.N;
-  if (N <= 4) return launch_state<TI, 1, 1, 4>(a, stream);
-  if (N <= 16) return launch_state<TI, 4, 1, 4>(a, stream);
-  if (N <= 32) return launch_state<TI, 8, 1, 4>(a, stream);
-  if (N <= 64) return launch_state<TI, 8, 1, 8>(a, stream);
-  if (N <= 128) return launch_state<TI, 8, 4, 16>(a, stream);
-  return launch_state<TI, 16, 4, 16>(a, stream);
+  constexpr int PR = CARRY ? 2 : 4;                          // (64 elements a thread, or 32 and what their roundings left out)
+  if (N <= 4) return launch_state<TI, 1, 1, 4, CARRY>(a, stream);
+  if (N <= 16) return launch_state<TI, 4, 1, 4, CARRY>(a, stream);
+  if (N <= 32) return launch_state<TI, 8, 1, 4, CARRY>(a, stream);
+  if (N <= 64) return launch_state<TI, 8, 1, 8, CARRY>(a, stream);
+  if (N <= 128) return launch_state<TI, 8, PR, 16, CARRY>(a, stream);
+  return launch_state<TI, 16, PR, 16, CARRY>(a, stream);
 }
 
 template <typename TI, int W, int K>
@@ -736,7 +793,7 @@ cudaError_t launch_all(ConvArgs a, cudaStream_t stream) {
   StateArgs s{};
   s.c = c;
   s.s = a.s;
-  return launch_states<TI>(s, stream);
+  return c.T > 2ll * c.B ? launch_states<TI, true>(s, stream) : launch_states<TI, false>(s, stream);
 }
 
 bool scan_has_blocks(int P, int N) { return P == 64 && N == 128; }
@@ -753,7 +810,7 @@ struct Scratch {
     tensor = blocks && T > SCAN_FEW;
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
     step = up(rows * pitch * 4);
-    c_parts = step + up(rows * (Di / P) * (blocks ? 16 : 8));
+    c_parts = step + up(rows * (Di / P) * 16);
     cb = c_parts + (blocks ? up(rows * G * N * 4) : 0);
     plan = cb + (blocks ? up(size_t(B) * G * SCAN_FEW * SCAN_FEW * 4) : 0);
     list = plan + 256;
@@ -778,7 +835,7 @@ cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
   a.c = c;
   a.s.pitch = at.pitch;
   a.s.xbc = reinterpret_cast<float*>(ws);
-  a.s.step = reinterpret_cast<float2*>(ws + at.step);
+  a.s.step = reinterpret_cast<float4*>(ws + at.step);
   a.s.few = INT_MAX;
   if (at.blocks) {
     a.s.sums = reinterpret_cast<float4*>(ws + at.step);

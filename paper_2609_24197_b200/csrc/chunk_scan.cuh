@@ -39,7 +39,7 @@ cudaError_t scan_long_launch(const LongArgs& a, cudaStream_t stream);
 
 struct ScanScratch {
   float* xbc;                        // [.., pitch] convolved rows
-  float2* step;                      // [.., H] dt and the decay exp(dt A)
+  float4* step;                      // [.., H] dt, and the decay exp(dt A) with what its rounding left out
   // blocks of rows (scan_block_kernel) have their C apart, split into two bf16 parts, and the products C_t . B_s of a request's rows
   float4* sums;                      // [.., H] dt, e^c, and c, the sum of the log-decays so far, in two parts
   uint16_t* c_parts;                 // [.., G, 2, N]; null: requests with few rows go through scan_state_kernel

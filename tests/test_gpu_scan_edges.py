@@ -120,3 +120,55 @@ def test_a_value_that_is_no_number_reaches_as_far_as_the_convolution(hs, shape, 
         assert _near(_wide(a.ssm), b.reference()[2], b.reference(sizes=True)[2]).all()
     else:                                                      # from its row on, in its channel
         assert np.delete(near, 3, axis=1).all() and not np.isfinite(got[where:new[0], 3]).any()
+
+
+# Row after row, relative to the sum of the absolute values that enter a result, in roundings of 32 bits: a convolved value 5 for its terms and 7 for SiLU (two
+# units for its exponential and one for the argument's product at |v| of a few, its sum, its division); a step 4; a decay as much as its step and its rate,
+# 9 times c e^c <= 0.37, however many rows there are; the state 8 (one for each of up to eight rows; two where there are more, which carry the rest on).
+# A state has x, B and the step: 40 of them.  An output has C beside these, a sum of 16 products in a lane, one of up to 16 lanes, Dskip, and its gate with
+# 8: 40 + 12 + 20 + 2 + 8, below 84.
+STATE_ROWS, ROWS = 40 * 2.0 ** -24, 84 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("H,P,N,G", [(4, 64, 16, 1), (2, 40, 24, 1), (2, 20, 100, 1), (1, 16, 4, 1), (1, 8, 200, 1), (2, 16, 64, 2)])
+@pytest.mark.parametrize("rows", [700, 8000])
+@pytest.mark.parametrize("kind", ["same", "same step", "any"])
+def test_errors_do_not_grow_with_the_rows(hs, H, P, N, G, rows, kind):
+    """Decays next to one, row after row: what rounding leaves out of them and of the state must not add up."""
+    a = Layer(H, P, N, G, [rows, 3], dtype=torch.float32, step=-8.5, seed=56)
+    if kind == "same":
+        a.rows[:] = a.rows[0].clone()
+    elif kind == "same step":
+        a.rows[:, -H:] = a.rows[0, -H:].clone()
+    y, _, ssm = a.reference()
+    sy, _, ss = a.reference(sizes=True)
+    a.run(hs)
+    torch.cuda.synchronize()
+    off, far = np.abs(_wide(a.ssm) - ssm)[a.slots.cpu().numpy()], np.abs(_wide(a.y) - y)
+    assert (off <= STATE_ROWS * ss[a.slots.cpu().numpy()]).all(), (off / ss[a.slots.cpu().numpy()]).max()
+    assert (far <= ROWS * sy).all(), (far / sy).max()
+
+
+@pytest.mark.parametrize("shape", [(2, 64, 128, 1), (1, 130, 100, 1), (2, 8, 256, 1), (2, 20, 110, 2), (4, 64, 16, 1), (2, 20, 4, 1)])
+@pytest.mark.parametrize("new", [[40] + [0] * 60, [1] * 30 + [20] + [0] * 40, [0] * 300 + [500, 1, 8, 9], [8, 9, 0, 0, 0, 0, 0, 0, 0]])
+def test_requests_with_many_rows_among_empty_ones(hs, shape, new):
+    """Hardly more rows than requests, and most of them one request's."""
+    a = Layer(*shape, new, dtype=torch.float32, pad=2, seed=58)
+    n = len(new)
+    a.check(hs, fresh=(torch.arange(n, device="cuda") % 3 == 0).int(), keep=torch.tensor([x - x // 3 for x in new], dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("shape", [(2, 64, 128, 1), (2, 40, 24, 1), (2, 16, 100, 1), (1, 8, 4, 1)])
+@pytest.mark.parametrize("new", [[1], [6], [40], [200]])
+def test_an_infinite_state_is_no_number_in_its_own_channel_alone(hs, shape, new):
+    a, b = (Layer(*shape, new, dtype=torch.float32, seed=57) for _ in range(2))
+    own = int(a.slots[0])
+    a.ssm[own, 0, 3, 2], a.ssm[own, 0, 5, 1] = float("inf"), -float("inf")
+    a.run(hs)
+    torch.cuda.synchronize()
+    got, want, size = _wide(a.ssm)[own], b.reference()[2][own], b.reference(sizes=True)[2][own]
+    at = np.zeros(got.shape, bool)
+    at[0, 3, 2] = at[0, 5, 1] = True
+    assert not np.isfinite(got[at]).any() and _near(got, want, size)[~at].all()
+    y, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
+    assert not np.isfinite(y[:, [3, 5]]).any() and np.delete(_near(y, want, size, HALF[torch.float32]), [3, 5], axis=1).all()
