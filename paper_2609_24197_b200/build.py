@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libhspec.so")
 SOURCES = ["hspec.cu", "gemm.cu", "gemm_2sm.cu", "attention.cu", "attention_tc.cu", "scan.cu", "elementwise.cu",
            "noalloc.cu", "next_ops.cu", "markov_chain.cu", "chunk_rope.cu", "chunk_attention.cu", "chunk_few.cu", "verify.cu",
-           "chunk_scan.cu", "chunk_scan_block.cu", "chunk_scan_tc.cu", "logits.cu"]
+           "chunk_scan.cu", "chunk_scan_block.cu", "chunk_scan_tc.cu", "chunk_scan_tc_wide.cu", "logits.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 
 

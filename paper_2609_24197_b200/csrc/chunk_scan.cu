@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
   }
 }
 
-// B and C of a group, for a request with up to SCAN_FEW rows (N = 128): a thread a channel.  B goes into the scratch as it is, C in its two parts; their
+// B and C of a group, for a request with up to SCAN_FEW rows (N = 128): a thread a channel.  B goes into the scratch as it is, C in its bf16 parts; their
 // products by pairs of rows.
 constexpr int CB_PITCH = 128 + 4;
 // x of a request with few rows: a thread two channels.
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
   if (g == c.G) { steps_of_request<TI>(a, b); return; }
   const ScanRequest r = scan_request(c, b);
   const int n = scan_upto(c, r), tid = threadIdx.x, e = tid & 127;
-  const bool isC = tid >= 128;
+  const bool isC = tid >= 128, wide = scan_wide(c);
   if (n > a.s.few || (n == 0 && !r.stores())) return;
   const int ch = c.Di + ((isC ? c.G : 0) + g) * 128 + e;
   float w[K], raw[K];
@@ -367,10 +367,13 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
       rows_sm[((isC ? SCAN_FEW : 0) + i0 + i) * CB_PITCH + e] = v;
       const size_t row = a.s.row(b, r.q0, i0 + i);
       if (isC) {
-        const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-        __nv_bfloat16* parts = reinterpret_cast<__nv_bfloat16*>(a.s.c_parts) + (row * c.G + g) * 256 + e;
-        parts[0] = hi;
-        parts[128] = __float2bfloat16_rn(v - __bfloat162float(hi));
+        __nv_bfloat16* parts = reinterpret_cast<__nv_bfloat16*>(a.s.c_parts) + (row * c.G + g) * (SCAN_C_PARTS * 128) + e;
+#pragma unroll
+        for (int p = 0; p < SCAN_C_PARTS; ++p) {
+          if (p == 2 && !wide) break;
+          const __nv_bfloat16 part = parts[p * 128] = __float2bfloat16_rn(v);
+          v -= __bfloat162float(part);
+        }
       } else {
         a.s.xbc[row * a.s.pitch + ch] = v;
       }
@@ -811,7 +814,7 @@ struct Scratch {
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
     step = up(rows * pitch * 4);
     c_parts = step + up(rows * (Di / P) * 16);
-    cb = c_parts + (blocks ? up(rows * G * N * 4) : 0);
+    cb = c_parts + (blocks ? up(rows * G * N * 2 * SCAN_C_PARTS) : 0);
     plan = cb + (blocks ? up(size_t(B) * G * SCAN_FEW * SCAN_FEW * 4) : 0);
     list = plan + 256;
     chunks = list + (tensor ? up(size_t(scan_max_long(T, B)) * 8) : 0);

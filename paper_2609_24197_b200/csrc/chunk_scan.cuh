@@ -36,13 +36,18 @@ inline long long scan_max_long(long long T, int B) { return T / (SCAN_FEW + 1) <
 // (a request's chunks end where its kept rows do: up to two of them are not full)
 inline long long scan_max_chunks(long long T, int B) { return T / SCAN_CHUNK + 2 * scan_max_long(T, B); }
 cudaError_t scan_long_launch(const LongArgs& a, cudaStream_t stream);
+cudaError_t scan_long_wide_launch(const LongArgs& a, cudaStream_t stream);
+
+// Whether products take their operands in three bf16 parts (what they leave is below 2^-24), not two (2^-16): for outputs that are not rounded to 16 bits.
+__host__ __device__ inline bool scan_wide(const ChunkScanCall& c) { return c.y && c.y_dtype == CHUNK_F32; }
+constexpr int SCAN_C_PARTS = 3;
 
 struct ScanScratch {
   float* xbc;                        // [.., pitch] convolved rows
   float4* step;                      // [.., H] dt, and the decay exp(dt A) with what its rounding left out
-  // blocks of rows (scan_block_kernel) have their C apart, split into two bf16 parts, and the products C_t . B_s of a request's rows
+  // blocks of rows (scan_block_kernel) have their C apart, split into bf16 parts, and the products C_t . B_s of a request's rows
   float4* sums;                      // [.., H] dt, e^c, and c, the sum of the log-decays so far, in two parts
-  uint16_t* c_parts;                 // [.., G, 2, N]; null: requests with few rows go through scan_state_kernel
+  uint16_t* c_parts;                 // [.., G, SCAN_C_PARTS, N]; null: requests with few rows go through scan_state_kernel
   float* cb;                         // [B, G, SCAN_FEW, SCAN_FEW]
   int pitch;
   int few;                           // requests with more rows than this go another way
@@ -108,6 +113,17 @@ __device__ __forceinline__ void split2(uint64_t v, uint32_t& hi, uint32_t& lo) {
   hi = pack_bf16(a, b);
   unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), dup2(-1.f), v), a, b);
   lo = pack_bf16(a, b);
+}
+// v in PARTS bf16 parts, each what those in front of it leave
+template <int PARTS>
+__device__ __forceinline__ void split_parts(uint64_t v, uint32_t (&part)[PARTS]) {
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    float a, b;
+    unpack_f32x2(v, a, b);
+    const uint32_t bits = part[p] = pack_bf16(a, b);
+    v = fma_f32x2(pack_f32x2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u)), dup2(-1.f), v);
+  }
 }
 template <typename TI, int N>
 __device__ __forceinline__ void widen(const Word<TI, N>& w, uint64_t (&v)[N / 2]) {

@@ -6,7 +6,7 @@
 // a warp, from its first instruction on.  S C for all rows and what the rows give one another are products of 16 x 8 x 16 on the warp's tensor fragments
 // (32 channels x rows are too few for the other tensor path): S comes from memory in the order of a fragment, four elements of its 128 a thread and step,
 // and C in the same one.  Operands are split into a bf16 head and a bf16 remainder, three products for one (a
-// relative error of some 2^-18 a term, 3 x 2^-16 at most: 32-bit outputs are off by 5e-6 of their size, 16-bit ones round more away).
+// relative error of some 2^-18 a term, 3 x 2^-16 at most, where outputs are rounded to 16 bits), or into three parts and six products for 32-bit outputs.
 // The kept rows are added to the state in 32 bits.  (Row after row through the state, 17 rows of 32 requests of 128 heads take 182 us, three operations an element
 // and row; so they take 80, 2 TB/s: 13 to 18 for the kernel in front, 70 here for 150 MB of states and rows with 2 x 10^9 multiply-adds of the fragments.)
 #include "chunk_scan.cuh"
@@ -20,21 +20,47 @@ namespace {
 
 constexpr int NH = 64, NS = 128, FEW = SCAN_FEW;
 constexpr int X_PITCH = NH + 4, W_PITCH = FEW + 4, C_PITCH = NS + 16;            // of rows in shared memory, in their own elements
+template <int PARTS>
 struct BlockShared {
   float x[FEW][X_PITCH];
   float cb[FEW][W_PITCH];                    // C_t . B_s, up to the diagonal
-  uint16_t c[2][FEW][C_PITCH];               // C's head and remainder
+  uint16_t c[PARTS][FEW][C_PITCH];           // C in bf16 parts
   float b[FEW][NS];
   float4 sums[FEW];                          // dt_t, e^{c_t}, c_t in two parts
 };
 
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = pack_bf16(a, b);
-  lo = pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+// a and b in PARTS bf16 parts, each what those in front of it leave
+template <int PARTS>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[PARTS][4], int i) {
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    const uint32_t v = part[p][i] = pack_bf16(a, b);
+    a -= __uint_as_float(v << 16);
+    b -= __uint_as_float(v & 0xffff0000u);
+  }
+}
+// The products of two operands' parts down to those of the size of what the last part leaves.  The tensor cores cut the bits that do not fit their sums: of three
+// parts the smallest products come first, and what a step gives is added outside, so that a sum is cut once a step and not six times (outputs off by 1.1e-6
+// that way).
+template <int PARTS>
+__device__ __forceinline__ void mma_parts(float (&acc)[4], const uint32_t (&a)[PARTS][4], const uint2 (&b)[PARTS]) {
+  if constexpr (PARTS == 2) {
+    mma_bf16_16816(acc, a[0], b[0].x, b[0].y);
+    mma_bf16_16816(acc, a[0], b[1].x, b[1].y);
+    mma_bf16_16816(acc, a[1], b[0].x, b[0].y);
+  } else {
+    float step[4] = {};
+#pragma unroll
+    for (int size = PARTS - 1; size >= 0; --size)
+#pragma unroll
+      for (int i = 0; i <= size; ++i) mma_bf16_16816(step, a[i], b[size - i].x, b[size - i].y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += step[i];
+  }
 }
 
-template <typename TI, bool Y, bool VEC>
-__global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
+template <typename TI, int PARTS, bool Y, bool VEC>
+__global__ void __launch_bounds__(128, PARTS == 2 ? 4 : 3) scan_block_kernel(StateArgs a) {
   const ChunkScanCall& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gl = lane >> 2, q = lane & 3;
   const int h = blockIdx.x, b = blockIdx.y, g = h / (c.H / c.G);
@@ -52,7 +78,7 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) uint8_t block_sm[];
-  BlockShared& s = *reinterpret_cast<BlockShared*>(block_sm);
+  BlockShared<PARTS>& s = *reinterpret_cast<BlockShared<PARTS>*>(block_sm);
   const size_t at0 = a.s.row(b, r.q0, 0);
   // ---- the rows: steps, x, C, B and their products
   if (tid < n) cp_async16(smem_u32(&s.sums[tid]), a.s.sums + (at0 + tid) * c.H + h, true);
@@ -60,9 +86,10 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
   for (int i = tid; i < r.keep * (NS / 4); i += 128)
     cp_async16(smem_u32(&s.b[i >> 5][(i & 31) * 4]), a.s.xbc + (at0 + (i >> 5)) * a.s.pitch + c.Di + g * NS + (i & 31) * 4, true);
   if (Y) {
-    for (int i = tid; i < n * 32; i += 128) {
-      const int row = i >> 5, part = (i >> 4) & 1, e = (i & 15) * 8;
-      cp_async16(smem_u32(&s.c[part][row][e]), a.s.c_parts + ((at0 + row) * c.G + g) * 2 * NS + part * NS + e, true);
+    for (int i = tid; i < n * 16; i += 128) {
+      const int row = i >> 4, e = (i & 15) * 8;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) cp_async16(smem_u32(&s.c[p][row][e]), a.s.c_parts + (((at0 + row) * c.G + g) * SCAN_C_PARTS + p) * NS + e, true);
     }
     for (int i = tid; i < n * (FEW / 4); i += 128)
       if ((i & 7) * 4 <= i >> 3) cp_async16(smem_u32(&s.cb[i >> 3][(i & 7) * 4]), a.s.cb + ((size_t(b) * c.G + g) * FEW + (i >> 3)) * FEW + (i & 7) * 4, true);
@@ -74,7 +101,8 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
   for (int i = tid; i < padded - n; i += 128) s.sums[n + i] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (Y)
     for (int i = tid; i < (padded - n) * (NS / 8); i += 128)
-      *reinterpret_cast<uint4*>(&s.c[0][n + i / (NS / 8)][i % (NS / 8) * 8]) = *reinterpret_cast<uint4*>(&s.c[1][n + i / (NS / 8)][i % (NS / 8) * 8]) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint4*>(&s.c[p][n + i / (NS / 8)][i % (NS / 8) * 8]) = make_uint4(0, 0, 0, 0);
   // A lane has channels p and p + 8 of rows 8 j + 2 q and + 1; after a swap with the lane four on (or back) two adjacent channels of one of the rows.
   const int odd_lane = gl & 1, out_row = 2 * q + odd_lane, out_ch = warp * 16 + (gl & ~1);
   const TI* gates = reinterpret_cast<const TI*>(c.x) + size_t(r.q0) * c.ld_x + h * NH + out_ch;
@@ -95,18 +123,18 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
     // ---- with the state
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      uint32_t hi[4], lo[4];
-      split_pair(S[0][k].x, S[0][k].y, hi[0], lo[0]);
-      split_pair(S[1][k].x, S[1][k].y, hi[1], lo[1]);
-      split_pair(S[0][k].z, S[0][k].w, hi[2], lo[2]);
-      split_pair(S[1][k].z, S[1][k].w, hi[3], lo[3]);
+      uint32_t sp[PARTS][4];
+      split_pair<PARTS>(S[0][k].x, S[0][k].y, sp, 0);
+      split_pair<PARTS>(S[1][k].x, S[1][k].y, sp, 1);
+      split_pair<PARTS>(S[0][k].z, S[0][k].w, sp, 2);
+      split_pair<PARTS>(S[1][k].z, S[1][k].w, sp, 3);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (j * 8 >= n) break;
-        const uint2 ch = *reinterpret_cast<const uint2*>(&s.c[0][j * 8 + gl][k * 16 + q * 4]), cl = *reinterpret_cast<const uint2*>(&s.c[1][j * 8 + gl][k * 16 + q * 4]);
-        mma_bf16_16816(acc[j], hi, ch.x, ch.y);
-        mma_bf16_16816(acc[j], hi, cl.x, cl.y);
-        mma_bf16_16816(acc[j], lo, ch.x, ch.y);
+        uint2 cp[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) cp[p] = *reinterpret_cast<const uint2*>(&s.c[p][j * 8 + gl][k * 16 + q * 4]);
+        mma_parts<PARTS>(acc[j], sp, cp);
       }
     }
 #pragma unroll
@@ -125,13 +153,13 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       if (k * 16 >= n) break;
-      uint32_t hi[4], lo[4];
+      uint32_t xp[PARTS][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {                          // channel gl (+ 8), rows 16 k + 2 q (+ 8) and the one behind it
         const int p = warp * 16 + gl + (i & 1) * 8, u = k * 16 + 2 * q + (i >> 1) * 8;
         const float x0 = s.x[u][p], x1 = s.x[u + 1][p];
         odd |= fmaf(x0, 0.f, x1 * 0.f) != 0.f;
-        split_pair(x0, x1, hi[i], lo[i]);
+        split_pair<PARTS>(x0, x1, xp, i);
       }
       if (__any_sync(0xffffffffu, odd)) break;
 #pragma unroll
@@ -139,12 +167,13 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
         if (j * 8 >= n) break;
         if (j * 8 + 7 < k * 16) continue;                    // (rows in front of the terms: nothing)
         const int t = j * 8 + gl, u = k * 16 + 2 * q;
-        uint32_t wh[2], wl[2];
-        split_pair(weight(t, u), weight(t, u + 1), wh[0], wl[0]);
-        split_pair(weight(t, u + 8), weight(t, u + 9), wh[1], wl[1]);
-        mma_bf16_16816(acc[j], hi, wh[0], wh[1]);
-        mma_bf16_16816(acc[j], hi, wl[0], wl[1]);
-        mma_bf16_16816(acc[j], lo, wh[0], wh[1]);
+        uint32_t w[PARTS][4];
+        split_pair<PARTS>(weight(t, u), weight(t, u + 1), w, 0);
+        split_pair<PARTS>(weight(t, u + 8), weight(t, u + 9), w, 1);
+        uint2 wp[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) wp[p] = make_uint2(w[p][0], w[p][1]);
+        mma_parts<PARTS>(acc[j], xp, wp);
       }
     }
     if (__any_sync(0xffffffffu, odd)) {
@@ -215,16 +244,17 @@ __global__ void __launch_bounds__(128, 4) scan_block_kernel(StateArgs a) {
     for (int k = 0; k < 8; ++k) __stcs(reinterpret_cast<float4*>(state + i * 8 * NS + k * 16), S[i][k]);
 }
 
-template <typename TI, bool Y, bool VEC>
+template <typename TI, int PARTS, bool Y, bool VEC>
 cudaError_t launch_vec(const StateArgs& a, cudaStream_t stream) {
+  constexpr size_t smem = sizeof(BlockShared<PARTS>);
   static std::atomic<uint32_t> ready{0};                     // devices on which the kernel has been told its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess && (dev >= 32 || !(ready.load() >> dev & 1u)))
-    e = cudaFuncSetAttribute(scan_block_kernel<TI, Y, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockShared)));
+    e = cudaFuncSetAttribute(scan_block_kernel<TI, PARTS, Y, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   if (dev < 32) ready.fetch_or(1u << dev);
-  return launch_pdl(scan_block_kernel<TI, Y, VEC>, dim3(unsigned(a.c.H), unsigned(a.c.B)), dim3(128), sizeof(BlockShared), stream, a);
+  return launch_pdl(scan_block_kernel<TI, PARTS, Y, VEC>, dim3(unsigned(a.c.H), unsigned(a.c.B)), dim3(128), smem, stream, a);
 }
 
 template <typename TI>
@@ -233,8 +263,9 @@ cudaError_t launch_for(StateArgs a, cudaStream_t stream) {
   const int item = c.y_dtype == CHUNK_F32 ? 4 : 2;
   a.y_vec = c.y && reinterpret_cast<uintptr_t>(c.y) % (2 * item) == 0 && c.ld_y % 2 == 0 ? 1 : 0;
   const bool vec = c.ld_x % 2 == 0 && reinterpret_cast<uintptr_t>(c.x) % (2 * sizeof(TI)) == 0;
-  if (!c.y) return vec ? launch_vec<TI, false, true>(a, stream) : launch_vec<TI, false, false>(a, stream);
-  return vec ? launch_vec<TI, true, true>(a, stream) : launch_vec<TI, true, false>(a, stream);
+  if (!c.y) return vec ? launch_vec<TI, 2, false, true>(a, stream) : launch_vec<TI, 2, false, false>(a, stream);
+  if (scan_wide(c)) return vec ? launch_vec<TI, 3, true, true>(a, stream) : launch_vec<TI, 3, true, false>(a, stream);
+  return vec ? launch_vec<TI, 2, true, true>(a, stream) : launch_vec<TI, 2, true, false>(a, stream);
 }
 
 }  // namespace

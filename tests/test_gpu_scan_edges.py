@@ -172,3 +172,37 @@ def test_an_infinite_state_is_no_number_in_its_own_channel_alone(hs, shape, new)
     assert not np.isfinite(got[at]).any() and _near(got, want, size)[~at].all()
     y, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
     assert not np.isfinite(y[:, [3, 5]]).any() and np.delete(_near(y, want, size, HALF[torch.float32]), [3, 5], axis=1).all()
+
+
+# Outputs of 32 bits, in the 2-norm over a call, where signs are any and errors add as squares: in roundings of 32 bits some 4 for each of x, B and C, 6 for the
+# weights (exponential, logarithm, step, C . B), 4 for the gate, 2 each for what three bf16 parts leave and for the sums: below 12.  (Two parts leave 2^-18 of a
+# factor: 4.6e-6, 77 of them.)  What a long request adds to its state by products takes two parts whatever its outputs are: the second one is rounded by half
+# of 2^-8 of itself, which is half of 2^-8 of the value at most, so 2^-18 for either factor, and the product of two seconds that is left out is 2^-18 too.
+DIGITS, TWO_PARTS = 16 * 2.0 ** -24, 3 * 2.0 ** -18
+
+
+@pytest.mark.parametrize("shape", [(4, 64, 128, 2), (2, 64, 128, 1), (2, 40, 24, 1), (4, 64, 16, 1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("new", [[17] * 5, [32, 3, 9], [200], [700, 20, 1, 130], [3000], [1] * 9])
+def test_outputs_of_32_bits_have_their_digits(hs, shape, dtype, new):
+    a = Layer(*shape, new, dtype=dtype, out=torch.float32, pad=1, seed=59)
+    y, _, ssm = a.reference()
+    a.run(hs)
+    torch.cuda.synchronize()
+    off = np.linalg.norm(_wide(a.y)[:a.T] - y) / np.linalg.norm(y)
+    own = a.slots.cpu().numpy()
+    left = np.linalg.norm(_wide(a.ssm)[own] - ssm[own]) / np.linalg.norm(ssm[own])
+    by_products = shape[1:3] == (64, 128) and max(new) > 32
+    assert off <= DIGITS and left <= (TWO_PARTS if by_products else DIGITS), (off, left)
+
+
+@pytest.mark.parametrize("lead,pitch", [(0, 0), (3, 5)])
+@pytest.mark.parametrize("K", [2, 4])
+def test_outputs_of_32_bits_of_rows_at_any_address(hs, lead, pitch, K):
+    for dtype in (torch.bfloat16, torch.float32):
+        a = Layer(2, 64, 128, 1, [3, 200, 20, 129], dtype=dtype, out=torch.float32, K=K, seed=60, lead=lead)
+        buf = torch.full((a.rows_n, a.Di + pitch), 7.0, device="cuda")
+        a.y = buf[:, pitch // 2:pitch // 2 + a.Di]
+        n = torch.tensor([3, 77, 0, 128], dtype=torch.int32, device="cuda")
+        a.check(hs, keep=n)
+        assert (buf[:, :pitch // 2] == 7.0).all() and (buf[:, pitch // 2 + a.Di:] == 7.0).all()
