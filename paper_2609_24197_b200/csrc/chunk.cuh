@@ -33,17 +33,18 @@ __device__ __forceinline__ int chunk_request_of(const int32_t* cu_q, int B, int 
   return n;
 }
 
-// Item `item` of a chunk whose requests are cut into items of `rows` rows (`least` of them at least: 1 where a request without rows has work too):
-// its request (-1: behind the last item), that request's first row and number of rows, and the item's first row among them.  There are at most
+// Item `item` of a chunk whose requests are cut into items of `rows` rows: its request (-1: behind the last item), that request's first row and number of rows,
+// and the item's first row among them.  rows_of(b): {first row, rows} of request b; one without rows has `least` items, one with -1 none.  There are at most
 // T / rows + B items (T / rows + min(B, T) with least = 0).  One warp.
 struct ChunkItem { int b, q0, n, first; };
-__device__ __forceinline__ ChunkItem chunk_item(const int32_t* cu_q, int B, int T, int rows, int least, int item, int lane) {
+struct ChunkRows { int q0, n; };
+template <typename F>
+__device__ __forceinline__ ChunkItem chunk_item(int B, int rows, int least, int item, int lane, F rows_of) {
   int before = 0;
   for (int base = 0; base < B; base += 32) {
-    int c0 = 0, c1 = 0;
-    if (base + lane < B) { c0 = cu_q[base + lane]; c1 = cu_q[base + lane + 1]; }
-    const ChunkRequest r = chunk_request(c0, c1, 0, T, 0);
-    const int items = base + lane < B ? max((r.n + rows - 1) / rows, least) : 0;
+    ChunkRows r{0, 0};
+    if (base + lane < B) r = rows_of(base + lane);
+    const int items = base + lane < B ? (r.n > 0 ? (r.n + rows - 1) / rows : r.n < 0 ? 0 : least) : 0;
     int upto = items;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {

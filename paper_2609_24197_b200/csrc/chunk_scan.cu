@@ -4,10 +4,11 @@
 //   dt_t = softplus(dt_raw_t + bias),  S_t = exp(-dt_t e^A_log) S_{t-1} + dt_t x_t B_t^T,  y_t = (S_t C_t + D x_t) SiLU(z_t)
 //
 // Row after row, any shape, two kernels.  scan_rows_kernel convolves the rows into a scratch of 32-bit rows, with their steps and decays; a thread takes four
-// channels of some rows, the thread of a request's first rows also moves the carried rows on, which nobody else reads.  scan_state_kernel carries the states
-// through the rows: a block has some rows of a head's state in registers, from the first token to the last, and reads the convolved rows from shared
-// memory, a few tokens ahead of their use.  Single tokens are bound by the state, which is read and written once (64 of 160 heads of 64 x 128: 119 us,
-// 5.7 TB/s), long requests with small states by the chain of their rows (100 ns a row; 29 requests of up to 700 rows, 8 heads of 64 x 16: 84 us).
+// channels of some rows, the thread of a request's first rows also moves the carried rows on, which nobody else reads.  scan_state_kernel (scan_few_kernel in
+// calls with hardly more rows than requests) carries the states through the rows: a block has some rows of a head's state in registers, from the first token
+// to the last, and reads the convolved rows from shared memory, a few tokens ahead of their use.  Single tokens are bound by the state, which is read and
+// written once (64 of 160 heads of 64 x 128: 121 us, 5.7 TB/s), long requests with small states by the chain of their rows (100 ns a row; 29 requests of up to
+// 700 rows, 8 heads of 64 x 16: 85 us).
 // By products, heads of 64 channels with 128 state elements: scan_groups_kernel convolves, sums up the steps and multiplies C with B for requests of up to 32
 // rows, which scan_block_kernel finishes; scan_prep_kernel and scan_long_kernel take those with more.  Where these are chosen stands at chunk_scan_launch.
 #include "chunk_scan.cuh"
@@ -39,39 +40,8 @@ __device__ void count_bad(const ChunkScanCall& c) {
   }
 }
 
-// Item `item`: CONV_TILE rows of a request (one item at least, for what its carried rows need).  One warp.
-__device__ __forceinline__ ChunkItem few_item(const ChunkScanCall& c, int item, int lane) {
-  int before = 0;
-  for (int base = 0; base < c.B; base += 32) {
-    int items = 0, q0 = 0, n = 0;
-    if (base + lane < c.B) {
-      const ScanRequest r = scan_request(c, base + lane);
-      q0 = r.q0;
-      n = scan_upto(c, r);
-      items = max((n + CONV_TILE - 1) / CONV_TILE, 1);
-    }
-    int upto = items;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, upto, off);
-      if (lane >= off) upto += up;
-    }
-    const uint32_t mine = __ballot_sync(0xffffffffu, before + upto > item);
-    if (mine) {
-      const int l = __ffs(mine) - 1;
-      return {base + l, __shfl_sync(0xffffffffu, q0, l), __shfl_sync(0xffffffffu, n, l), (item - before - __shfl_sync(0xffffffffu, upto - items, l)) * CONV_TILE};
-    }
-    before += __shfl_sync(0xffffffffu, upto, 31);
-  }
-  return {-1, 0, 0, 0};
-}
-
 // The requests with many rows: a list, longest first, and their chunks in the order of the requests.  One block.
 constexpr int PLAN_SORT = 1024;
-__device__ __forceinline__ int chunks_of(const ChunkScanCall& c, const ScanRequest& r) {
-  const int upto = scan_upto(c, r), k = min(r.keep, upto);
-  return (k + SCAN_CHUNK - 1) / SCAN_CHUNK + (upto - k + SCAN_CHUNK - 1) / SCAN_CHUNK;
-}
 __device__ void plan_long(const ConvArgs& a, int* room) {     // room for 3 PLAN_SORT numbers
   const ChunkScanCall& c = a.c;
   int *key = room, *who = room + PLAN_SORT, *front = room + 2 * PLAN_SORT;
@@ -85,7 +55,7 @@ __device__ void plan_long(const ConvArgs& a, int* room) {     // room for 3 PLAN
     if (b < c.B) {
       const ScanRequest r = scan_request(c, b);
       upto = scan_upto(c, r);
-      if (upto > a.s.few) count = chunks_of(c, r);
+      if (upto > a.s.few) count = chunk_count(r.keep, upto);
     }
     const int one = count > 0 ? 1 : 0;
     int i1 = one, i2 = count;                                // sums up to and with this request
@@ -149,10 +119,17 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_rows_kernel(ConvArgs a) {
   // (the next kernel does not start early: its blocks would take the room of this one's, 29 requests of up to 700 rows 104 us instead of 84)
   const int tid = threadIdx.x, blocks = a.ch_blocks + a.dt_blocks, part = (blockIdx.x - 1) % blocks;
   if (blockIdx.x == 0) {
+    extern __shared__ __align__(16) int plan_room[];
     count_bad(c);
+    if (a.plan) plan_long(a, plan_room);
     return;
   }
-  const ChunkItem item = few_item(c, (blockIdx.x - 1) / blocks, tid & 31);
+  // (a request without rows has an item too, for its carried ones; one with many rows goes another way altogether)
+  const ChunkItem item = chunk_item(c.B, CONV_TILE, 1, (blockIdx.x - 1) / blocks, tid & 31, [&](int b) {
+    const ScanRequest r = scan_request(c, b);
+    const int n = scan_upto(c, r);
+    return ChunkRows{r.q0, n > a.s.few ? -1 : n};
+  });
   if (item.b < 0) return;
   const int rows = min(CONV_TILE, item.n - item.first), t0 = item.q0 + item.first;
   const size_t out0 = a.s.row(item.b, item.q0, item.first);
@@ -400,9 +377,9 @@ __global__ void __launch_bounds__(CONV_THREADS) scan_groups_kernel(ConvArgs a) {
 // The states through the rows.  A group of L lanes has PR rows of a head's state [P, N]: lane l of the group the elements n = 4 (l + L k) .. + 3.
 // Decays are next to one, and there may be thousands of rows.  So a decay comes in two parts, and (CARRY) what a row's rounding leaves out of the state is
 // carried to the next: otherwise both add up, in one direction where rows are alike (8000 equal rows: 4e-4 of the sum of all that entered, so 1e-6).  It
-// costs 2 % where the chain of rows bounds (29 requests of up to 700 rows 84 -> 86 us), and 13 % for blocks (17 rows of 32 requests, 24 heads of 40 x 24: 31 ->
+// costs 1 % where the chain of rows bounds (29 requests of up to 700 rows 84 -> 85 us), and 13 % for blocks (17 rows of 32 requests, 24 heads of 40 x 24: 31 ->
 // 35).  Requests of up to STATE_FEW rows go without in calls with hardly more rows than requests: the registers are those of their loads (64 tokens of 160
-// heads of 64 x 128 124 us; 145 with the rest carried).
+// heads of 64 x 128 121 us; 145 with the rest carried).
 constexpr int STATE_THREADS = 128, STATE_FEW = 8;
 
 __host__ __device__ constexpr int state_tile(int pr, int npt) { return pr * npt <= 8 ? 32 : 8; }
@@ -691,7 +668,9 @@ __global__ void __launch_bounds__(STATE_THREADS) scan_few_kernel(StateArgs a) {
   const int h = blockIdx.x / a.p_blocks, b = blockIdx.y, p0 = blockIdx.x % a.p_blocks * a.p_block;
   const ScanRequest r = scan_request(a.c, b);
   const int upto = scan_upto(a.c, r);
-  if (upto <= STATE_FEW) {
+  if (upto > a.s.few) {
+    pdl_wait();
+  } else if (upto <= STATE_FEW) {
     scan_state<TI, L, PR, NPT, VECN, Y, false>(a, r, upto, h, b, p0, a.p_block);
   } else if constexpr (PR == 1) {
     scan_state<TI, L, PR, NPT, VECN, Y, true>(a, r, upto, h, b, p0, a.p_block);
@@ -742,7 +721,7 @@ cudaError_t launch_states(const StateArgs& a, cudaStream_t stream) {
 
 template <typename TI, int W, int K>
 cudaError_t launch_rows_k(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
-  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), 0, stream, a);
+  return launch_pdl(scan_rows_kernel<TI, W, K>, dim3(blocks), dim3(CONV_THREADS), a.plan ? 3 * PLAN_SORT * sizeof(int) : 0, stream, a);
 }
 template <typename TI, int W>
 cudaError_t launch_rows_w(const ConvArgs& a, unsigned blocks, cudaStream_t stream) {
@@ -806,11 +785,11 @@ struct Scratch {
   size_t step, c_parts, cb, plan, list, chunks, images, total;
   int pitch;
   bool blocks, tensor;               // requests with few rows go through scan_block_kernel, those with many through the tensor cores
-  Scratch(long long T, int B, int Di, int P, int N, int G, bool by_blocks) {
+  Scratch(long long T, int B, int Di, int P, int N, int G, bool by_blocks, bool many) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     blocks = by_blocks;
     pitch = (Di + 2 * G * N + 3) / 4 * 4;
-    tensor = blocks && T > SCAN_FEW;
+    tensor = many && T > SCAN_FEW;
     const size_t rows = tensor && T > (long long)(SCAN_FEW) * B ? size_t(SCAN_FEW) * B : size_t(T);
     step = up(rows * pitch * 4);
     c_parts = step + up(rows * (Di / P) * 16);
@@ -826,13 +805,18 @@ struct Scratch {
 }  // namespace
 
 // (The kernels of this shape need no less with products than without, and what they need grows with T and B.)
-size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) { return Scratch(T, B, Di, P, N, G, scan_has_blocks(P, N)).total; }
-
+size_t chunk_scan_workspace_bytes(long long T, int B, int Di, int P, int N, int G) {
+  return Scratch(T, B, Di, P, N, G, scan_has_blocks(P, N), scan_has_blocks(P, N)).total;
+}
 
 cudaError_t chunk_scan_launch(const ChunkScanCall& c, cudaStream_t stream) {
-  // Row after row where there are hardly more rows than requests: nothing but the state counts then (64 tokens of 64 requests 119 us, with products and the
-  // launches for requests with many rows 184; 17 rows of 32 requests 182 and 82), and a request that has many of the rows all the same takes less than the others' states.
-  const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G, scan_has_blocks(c.P, c.N) && c.T > 2ll * c.B);
+  // Row after row where there are hardly more rows than requests: if all of them have some, nothing but the states counts (64 tokens of 64 requests 121 us, with
+  // products and the launches for requests with many rows 184; 17 rows of 32 requests 182 and 82).  But most of them may be empty places, and the rows one
+  // request's: above LONE rows the kernels for these stand behind (500 rows among 255 empty places 146 us, in one chain of rows 390 to 680; 8 us of 600 where they
+  // find nothing, 300 tokens), below the chain is short.
+  constexpr int LONE = 256;
+  const bool products = scan_has_blocks(c.P, c.N), by_blocks = products && c.T > 2ll * c.B;
+  const Scratch at(c.T, c.B, c.Di, c.P, c.N, c.G, by_blocks, by_blocks || (products && c.T > LONE));
   char* ws = reinterpret_cast<char*>(c.ws);
   ConvArgs a{};
   a.c = c;

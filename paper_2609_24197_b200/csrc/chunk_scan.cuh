@@ -35,6 +35,10 @@ struct LongArgs {
 inline long long scan_max_long(long long T, int B) { return T / (SCAN_FEW + 1) < B ? T / (SCAN_FEW + 1) : B; }
 // (a request's chunks end where its kept rows do: up to two of them are not full)
 inline long long scan_max_chunks(long long T, int B) { return T / SCAN_CHUNK + 2 * scan_max_long(T, B); }
+__device__ __forceinline__ int chunk_count(int keep, int upto) {
+  const int k = min(keep, upto);
+  return (k + SCAN_CHUNK - 1) / SCAN_CHUNK + (upto - k + SCAN_CHUNK - 1) / SCAN_CHUNK;
+}
 cudaError_t scan_long_launch(const LongArgs& a, cudaStream_t stream);
 cudaError_t scan_long_wide_launch(const LongArgs& a, cudaStream_t stream);
 

@@ -6,7 +6,7 @@
 // chunk one after another, the heads of a request side by side.
 //
 // The tensor cores take 16-bit operands, the states want more: every operand is split into a bf16 head and a bf16 remainder (16 bits together, any
-// exponent of 32 bits), and three products, head x head + head x remainder + remainder x head, leave a relative error of some 2^-18 a term, 3 x 2^-18 at
+// exponent of 32 bits), and three products, head x head + head x remainder + remainder x head, leave a relative error of some 2^-18 a term, 3 x 2^-16 at
 // most (outputs would be off by 4.6e-6 of their 2-norm, below what 16 bits round away; states are, by 3e-7 where a few hundred rows count in them, and by up
 // to 5e-6 where some twenty do).  Outputs of 32 bits take three parts and six products (WIDE: off by 4e-7, in 860 us where two parts took 600): shared memory
 // holds them because the scores come from the images, and tensor memory because both products of an output add up in one place.  The next state has two
@@ -53,10 +53,6 @@ __device__ __forceinline__ ChunkRange chunk_range(int keep, int upto, int ci) {
     r.len = min(Q, upto - r.start);
   }
   return r;
-}
-__device__ __forceinline__ int chunk_count(int keep, int upto) {
-  const int k = min(keep, upto);
-  return (k + Q - 1) / Q + (upto - k + Q - 1) / Q;
 }
 
 constexpr int PREP_PITCH = NS + 8;   // bf16 of a staged row: the rows of an ldmatrix spread over the banks

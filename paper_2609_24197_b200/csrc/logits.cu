@@ -77,7 +77,11 @@ __global__ void __launch_bounds__(RULE_THREADS, 4) adjust_logits_kernel(RuleArgs
 
   // ---- the block's request and rows (every warp looks for itself)
   ChunkItem item{int(blockIdx.x) / a.slices, int(blockIdx.x) / a.slices, 1, 0};
-  if (c.cu_q) item = chunk_item(c.cu_q, c.B, c.T, a.rows, 0, item.b, lane);
+  if (c.cu_q)
+    item = chunk_item(c.B, a.rows, 0, item.b, lane, [&](int b) {
+      const ChunkRequest r = chunk_request(c.cu_q[b], c.cu_q[b + 1], 0, c.T, 0);
+      return ChunkRows{r.q0, r.n};
+    });
   if (blockIdx.x == 0 && c.cu_q)
     for (int r = tid; r < c.B; r += RULE_THREADS)
       if (chunk_request_bad(c.cu_q[r], c.cu_q[r + 1], INT_MAX, c.T, INT_MAX)) atomicAdd(c.status + STATUS_WORD_BAD_INPUT, 1u);

@@ -176,8 +176,9 @@ def test_an_infinite_state_is_no_number_in_its_own_channel_alone(hs, shape, new)
 
 # Outputs of 32 bits, in the 2-norm over a call, where signs are any and errors add as squares: in roundings of 32 bits some 4 for each of x, B and C, 6 for the
 # weights (exponential, logarithm, step, C . B), 4 for the gate, 2 each for what three bf16 parts leave and for the sums: below 12.  (Two parts leave 2^-18 of a
-# factor: 4.6e-6, 77 of them.)  What a long request adds to its state by products takes two parts whatever its outputs are: the second one is rounded by half
-# of 2^-8 of itself, which is half of 2^-8 of the value at most, so 2^-18 for either factor, and the product of two seconds that is left out is 2^-18 too.
+# factor: 4.6e-6, 77 of them.)  What a long request adds to its state by products takes two parts whatever its outputs are: the second part is 2^-8 of the value
+# at most and 0.42 x 2^-8 in the mean square, its rounding as much of itself, so 0.18 x 2^-16 for either factor and for the product of two seconds that is left
+# out: 0.31 x 2^-16 together, and 0.75 x 2^-16 is allowed.
 DIGITS, TWO_PARTS = 16 * 2.0 ** -24, 3 * 2.0 ** -18
 
 
@@ -206,3 +207,36 @@ def test_outputs_of_32_bits_of_rows_at_any_address(hs, lead, pitch, K):
         n = torch.tensor([3, 77, 0, 128], dtype=torch.int32, device="cuda")
         a.check(hs, keep=n)
         assert (buf[:, :pitch // 2] == 7.0).all() and (buf[:, pitch // 2 + a.Di:] == 7.0).all()
+
+
+@pytest.mark.parametrize("places,at", [(256, 0), (256, 100), (1000, 999)])
+def test_a_piece_among_empty_places_goes_the_way_of_a_piece_alone(hs, places, at):
+    """By products, to the bit, whatever the number of places without rows beside it; and so do what it commits and the tokens beside it."""
+    alone = Layer(2, 64, 128, 1, [500], seed=61)
+    among = Layer(2, 64, 128, 1, [0] * at + [500] + [0] * (places - 1 - at), seed=62)
+    for name in ("cw", "cb", "bias", "A_log", "D"):
+        setattr(among, name, getattr(alone, name))
+    among.rows.copy_(alone.rows)
+    own, there = int(alone.slots[0]), int(among.slots[at])
+    among.conv[there], among.ssm[there] = alone.conv[own], alone.ssm[own]
+    keep = torch.full((places,), 333, dtype=torch.int32, device="cuda")
+    for y in ("own", None):
+        alone.run(hs, y=y, keep=keep[:1])
+        among.run(hs, y=y, keep=keep)
+        torch.cuda.synchronize()
+        assert torch.equal(alone.y, among.y) and torch.equal(alone.ssm[own], among.ssm[there]) and torch.equal(alone.conv[own], among.conv[there])
+
+
+@pytest.mark.parametrize("new", [[0] * 200 + [300, 33, 32, 31, 9, 8, 1], [1] * 300 + [40] + [0] * 100 + [1] * 5])
+def test_long_requests_among_tokens_and_empty_places(hs, new):
+    for dtype, out in ((torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16)):
+        n = len(new)
+        keep = torch.tensor([max(x - 3, 0) for x in new], dtype=torch.int32, device="cuda")
+        fresh = (torch.arange(n, device="cuda") % 4 == 1).int()
+        Layer(2, 64, 128, 1, new, dtype=dtype, out=out, pad=2, seed=63).check(hs, keep=keep, fresh=fresh)
+        a = Layer(2, 64, 128, 1, new, dtype=dtype, out=out, seed=64)
+        _, conv, ssm = a.reference(keep=keep, fresh=fresh)
+        size = a.reference(sizes=True, keep=keep, fresh=fresh)[2]
+        a.run(hs, y=None, keep=keep, fresh=fresh)
+        np.testing.assert_array_equal(_wide(a.conv), conv)
+        assert _near(_wide(a.ssm), ssm, size).all()
