@@ -29,24 +29,30 @@ WAYS = [((2, 64, 128, 1), [300], 40), ((2, 64, 128, 1), [300], 130), ((2, 64, 12
         ((2, 40, 24, 1), [300], 130), ((4, 64, 16, 1), [300], 40)]
 
 
+# outputs of 16 and of 32 bits take their operands in different numbers of parts
+OUT = [torch.float32, torch.bfloat16]
+
+
+@pytest.mark.parametrize("out", OUT)
 @pytest.mark.parametrize("shape,new,where", WAYS)
-def test_a_row_without_numbers_reaches_no_row_in_front_of_it(hs, shape, new, where):
+def test_a_row_without_numbers_reaches_no_row_in_front_of_it(hs, shape, new, where, out):
     """All of a row NaN: gate, x, B, C and dt.  Every row is kept."""
-    a, b = (Layer(*shape, new, dtype=torch.float32, seed=50) for _ in range(2))
+    a, b = (Layer(*shape, new, dtype=torch.float32, out=out, seed=50) for _ in range(2))
     a.rows[where] = float("nan")
     a.run(hs)
     torch.cuda.synchronize()
     got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
-    assert _near(got, want, size, HALF[torch.float32])[:where].all()
+    assert _near(got, want, size, HALF[out])[:where].all()
     assert not np.isfinite(got[where:]).any()
     assert not torch.isfinite(a.ssm[a.slots.long()]).any()
 
 
+@pytest.mark.parametrize("out", OUT)
 @pytest.mark.parametrize("shape,new,where", WAYS)
 @pytest.mark.parametrize("behind", [1, 20, -2])
 @pytest.mark.parametrize("value,step", [(float("inf"), float("nan")), (float("nan"), float("inf"))])
-def test_x_and_a_step_that_are_no_numbers_in_different_rows(hs, shape, new, where, behind, value, step):
-    a, b = (Layer(*shape, new, dtype=torch.float32, seed=51) for _ in range(2))
+def test_x_and_a_step_that_are_no_numbers_in_different_rows(hs, shape, new, where, behind, value, step, out):
+    a, b = (Layer(*shape, new, dtype=torch.float32, out=out, seed=51) for _ in range(2))
     H, P, N, G = shape
     at = min(where + behind, new[0] - 1)
     a.rows[where, a.Di + 3] = value                            # a channel of x of the first head
@@ -54,7 +60,7 @@ def test_x_and_a_step_that_are_no_numbers_in_different_rows(hs, shape, new, wher
     a.run(hs)
     torch.cuda.synchronize()
     got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
-    near = _near(got, want, size, HALF[torch.float32])
+    near = _near(got, want, size, HALF[out])
     assert near[:min(where, at)].all() and near[:, P:].all()   # rows in front of both, and all other heads
     others = [p for p in range(P) if p != 3]
     assert near[:at, others].all()                             # the head's other channels, up to its step
@@ -102,18 +108,19 @@ def test_an_error_that_another_call_left_does_not_end_the_scan_in_the_middle():
     assert done.returncode == 0, done.stderr[-1500:]
 
 
+@pytest.mark.parametrize("out", OUT)
 @pytest.mark.parametrize("K", [1, 2, 3, 4])
 @pytest.mark.parametrize("shape,new,where", [((2, 64, 128, 1), [300], 130), ((2, 64, 128, 1), [300, 9], 250), ((2, 64, 128, 1), [20], 5), ((2, 40, 24, 1), [40], 9)])
 @pytest.mark.parametrize("place", ["x", "C"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
-def test_a_value_that_is_no_number_reaches_as_far_as_the_convolution(hs, shape, new, where, place, value, K):
-    a, b = (Layer(*shape, new, K=K, dtype=torch.float32, seed=55) for _ in range(2))
+def test_a_value_that_is_no_number_reaches_as_far_as_the_convolution(hs, shape, new, where, place, value, K, out):
+    a, b = (Layer(*shape, new, K=K, dtype=torch.float32, out=out, seed=55) for _ in range(2))
     H, P, N, G = shape
     a.rows[where, a.Di + (3 if place == "x" else a.Di + G * N + 5)] = value
     a.run(hs)
     torch.cuda.synchronize()
     got, want, size = _wide(a.y), b.reference()[0], b.reference(sizes=True)[0]
-    near = _near(got, want, size, HALF[torch.float32])
+    near = _near(got, want, size, HALF[out])
     assert near[:where].all() and near[new[0]:].all()
     if place == "C":                                           # nothing of it stays in the state
         assert near[where + K:].all() and not np.isfinite(got[where]).any()
@@ -240,3 +247,12 @@ def test_long_requests_among_tokens_and_empty_places(hs, new):
         a.run(hs, y=None, keep=keep, fresh=fresh)
         np.testing.assert_array_equal(_wide(a.conv), conv)
         assert _near(_wide(a.ssm), ssm, size).all()
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("K", [4, 2])
+@pytest.mark.parametrize("new", [[31], [32], [33], [127], [128], [129], [256], [257, 0, 3], [1000], [9] * 12, [300, 32, 140, 1, 5]])
+def test_outputs_of_16_bits_at_all_lengths(hs, new, K, out):
+    for dtype, keep in ((torch.float32, None), (out, [x - x // 3 for x in new]), (torch.float32, [x // 2 + 1 for x in new])):
+        a = Layer(2, 64, 128, 1, new, dtype=dtype, out=out, K=K, pad=1, seed=65)
+        a.check(hs, **({} if keep is None else dict(keep=torch.tensor(keep, dtype=torch.int32, device="cuda"))))
