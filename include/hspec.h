@@ -426,12 +426,15 @@ size_t hspec_verify_workspace_bytes(int32_t B, int32_t k);
  *   fresh       device int32 [B] or NULL: nonzero starts the request from zeros, whatever its slot holds
  *   keep        device int32 [B] or NULL: the states behind the request's first keep[b] + keep_more rows are stored (held inside 0 .. its rows); NULL:
  *               behind all of them.  A request of which nothing is kept leaves its states as they are (zeros, if it is fresh)
- *   y           out [T, ld_y] fp32, bf16 or fp16 (y_dtype), all rows of all requests; NULL: the states alone
+ *   y           out [T, ld_y] fp32, bf16 or fp16 (y_dtype), all rows of all requests, apart from zxbcdt; NULL: the states alone
  * Single tokens, draft blocks and pieces of prompts may be mixed.  A verification's pass runs with keep all zero (keep_more 0); once
  * hspec_op_verify has counted the drafts that stand, the same rows with y NULL, keep = n_accept and keep_more = 1 move the states on.
- * States that the call does not store keep their bits.  Accumulation and states are 32-bit.  Where P is 64 and N 128 and there are more than 2 B rows, outputs
- * come from tensor-core products of operands in 16 bits (two bf16 parts): off by some 5e-6 of their size, elsewhere by 2e-7, before they are
- * rounded to y_dtype.  At most 65535 requests.
+ * States that the call does not store keep their bits.  Accumulation and states are 32-bit.  Row after row, whatever the number of rows, outputs are off by
+ * some 1e-7 of their 2-norm before they are rounded to y_dtype, states by as much.  Where P is 64 and N 128, outputs come from tensor-core products if there
+ * are more than 2 B rows, or for requests of more than 32 rows in calls of more than 256: fp32 ones off by up to 4e-7 (operands in three bf16 parts), others by
+ * 5e-6 before they are rounded (two parts), the states behind more than 32 rows (two parts) by 3e-7 where hundreds of rows count in them, by up to 5e-6 where
+ * they fall away within twenty.  So the last digits of a request's results may change with the requests beside it.
+ * Values that are not finite make what they reach infinite or NaN, and nothing in front of their row.  At most 65535 requests.
  * workspace: hspec_chunk_scan_workspace_bytes (it grows with T and B, so that of the largest call does for all), 256-byte aligned, contents undefined
  * between calls; calls that may overlap on the GPU need one each. */
 int hspec_op_chunk_scan(const void* zxbcdt, int32_t in_dtype, int64_t ld_in, const float* dt_raw, const float* conv_w, const float* conv_b,

@@ -16,8 +16,8 @@
 //                      and the scores C_t . B_s below the diagonal (mma.sync: the heads of a group share them, so they are little work)
 //   scan_long_kernel   one block an SM over (request, head) items, longest requests first; all its warps go through a chunk's work together
 //
-// A prompt of 8192 rows, 128 heads: 532 us, of them 505 in the second kernel and 31 in the first (they overlap at their ends).  A chunk and head takes 15 000
-// clocks: 4800 are instructions to issue, some 4000 the products, the rest the latency of one phase after another with 16 warps on the SM.
+// A prompt of 8192 rows, 128 heads: 536 us, of them 505 in the second kernel and 31 in the first (they overlap at their ends).  A chunk and head takes 15 000
+// clocks: 4800 are instructions to issue, the tensor pipe is busy for a sixth, the rest is the latency of one phase after another with 16 warps on the SM.
 #pragma once
 #include "chunk_scan.cuh"
 
